@@ -475,6 +475,105 @@ void sd_plan_destroy(sd_plan_t plan);
  * away as well. */
 void sd_release_memory(void);
 
+/* ------------------------------------------------------ dense operators --- */
+/* What a layer of a graph network does between two sparse products: its node
+ * tables normalised and activated, kept in 8 bits for the backward pass, and
+ * multiplied by weights.  All pointers below are DEVICE pointers of the current
+ * device; tables are row-major, rows `stride` elements apart, columns next to
+ * each other.  Every call enqueues on `stream` (a hipStream_t; NULL: the null
+ * stream), allocates nothing, does not synchronise, and can be captured in a
+ * graph.  Results do not change from run to run.  Outputs must not overlap
+ * inputs or each other; a workspace is 16-byte aligned, belongs to one call at
+ * a time on a stream and needs no initial value.
+ * Errors of them all: SD_ERR_INVALID_VALUE (null or misaligned pointers,
+ * sizes or strides that do not fit together, unknown types or formats, a
+ * workspace too small), SD_ERR_OVERFLOW (2^31 rows or columns or more),
+ * SD_ERR_NO_DEVICE, SD_ERR_HIP. */
+typedef enum { SD_TYPE_F32 = 1, SD_TYPE_F16 = 2, SD_TYPE_BF16 = 3 } sd_type_t;
+
+typedef enum {
+  SD_PACK_E4M3 = 1, /* 4 exponent bits, 3 of mantissa, largest 448; no infinities (they become NaN) */
+  SD_PACK_E5M2 = 2  /* 5 and 2 bits, largest 57344; infinities stay */
+} sd_pack_format_t;
+
+/* A rows x cols table in 8 bits.  Element (r, c) stands for
+ *   f8(codes[r * ld + c]) * 2^(scales[(c / 128) * rows + r] - 127).
+ * Rows are `ld` bytes apart (a multiple of 16, at least cols rounded up to 16);
+ * the bytes from cols to the next multiple of 16 are zero.  A scale byte of 255
+ * is not allowed. */
+typedef struct {
+  int64_t rows, cols, ld;
+  int32_t format;   /* sd_pack_format_t */
+  int32_t reserved; /* 0 */
+  uint8_t *codes;   /* [rows][ld], 16-byte aligned */
+  uint8_t *scales;  /* [ceil(cols / 128)][rows] */
+} sd_packed_t;
+
+/* x (element (r, c) at r * row_stride + c * col_stride; any strides >= 0, so a
+ * transposed or broadcast table too) into out's codes and scales; out gives the
+ * sizes.  For each row and block of 128 columns the scale is the least power of
+ * two with (largest finite magnitude) <= scale * largest of the format (1 for a
+ * block of zeros); codes are x / scale to nearest, ties to even.  NaN stays NaN. */
+int sd_pack(const void *x, int32_t type, int64_t row_stride, int64_t col_stride, const sd_packed_t *out,
+            void *stream);
+/* The values, rounded once to y's type. */
+int sd_unpack(const sd_packed_t *x, void *y, int32_t type, int64_t row_stride, void *stream);
+
+/* Y[m, n] = sum over k of X(m, k) W(n, k), + bias[n] if bias is not null; X and W
+ * have the same cols.  Sums in 32 bits, rounded once to Y's type. */
+int sd_pack_product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void *Y, int32_t type,
+                    int64_t row_stride, void *stream);
+
+/* dW[c, n] (fp32, contiguous) = sum over r of X(r, c) G[r, n]: the weight
+ * gradient from activations kept in 8 bits.  G is used in full (no rounding);
+ * sums in 32 bits.  _size: the workspace in bytes. */
+int sd_pack_gradient_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes);
+int sd_pack_gradient(const sd_packed_t *X, const void *G, int32_t type, int64_t n, int64_t row_stride, float *dW,
+                     void *workspace, size_t bytes, void *stream);
+
+typedef enum { SD_ACT_NONE = 0, SD_ACT_RELU = 1, SD_ACT_SILU = 2, SD_ACT_GELU = 3 /* with erf */ } sd_activation_t;
+
+/* Group norm over segments of rows (the graphs of a batch, or one whole graph),
+ * channels last.  Segment s is rows offsets[s] .. offsets[s + 1] - 1; without
+ * offsets the segments are equally long.  Statistics run over a segment's rows
+ * and a group's channels / groups neighbouring channels. */
+typedef struct {
+  int64_t rows, segments;
+  const int32_t *offsets; /* [segments + 1], from 0 to rows, not decreasing (empty segments are fine); or null:
+                             rows / segments each, which has to come out even */
+  int64_t longest;        /* rows of the longest segment where offsets are given and it is known, else 0; only
+                             speed depends on it */
+  int32_t channels, groups; /* channels a multiple of groups */
+  int32_t type;             /* sd_type_t of x, y, dy, dx */
+  int32_t activation;       /* sd_activation_t */
+  float eps;                /* >= 0 */
+  int32_t reserved;         /* 0 */
+  const float *weight, *bias; /* [channels], or null: 1 and 0 */
+} sd_norm_t;
+
+/* Workspaces in bytes of the two calls below (either pointer may be null). */
+int sd_group_norm_size(const sd_norm_t *d, size_t *forward, size_t *backward);
+
+/* xh = (x - mean) rstd, z = xh weight + bias, y = act(z); mean and rstd =
+ * (variance + eps)^-1/2 are written to [segments][groups] (an empty segment has
+ * mean and variance 0).  Statistics in 32 bits or more, without cancellation.
+ * x_packed, y_packed: 8-bit copies of x (kept for the backward pass) and of y
+ * (the next product's operand), of rows x channels, written in the same pass;
+ * null for none.  y may be null if y_packed is not. */
+int sd_group_norm(const sd_norm_t *d, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                  const sd_packed_t *x_packed, const sd_packed_t *y_packed, float *mean, float *rstd,
+                  void *workspace, size_t bytes, void *stream);
+
+/* From dy, and x either dense or as the 8-bit copy (exactly one of x, x_packed
+ * where there are rows), with the forward pass's mean and rstd:
+ *   dz = dy act'(z), dh = dz weight,
+ *   dx = rstd (dh - mean(dh) - xh mean(dh xh)), dweight = sum dz xh, dbias = sum dz.
+ * dweight and dbias (fp32 [channels]) may be null.  relu has slope 0 at 0. */
+int sd_group_norm_backward(const sd_norm_t *d, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                           const sd_packed_t *x_packed, const float *mean, const float *rstd, void *dx,
+                           int64_t dx_stride, float *dweight, float *dbias, void *workspace, size_t bytes,
+                           void *stream);
+
 /* Static strings; never NULL. */
 const char *sd_status_string(int status);
 /* The last HIP error text seen by this thread ("" if none). */

@@ -121,6 +121,24 @@ class sd_plan_info_t(ctypes.Structure):
     _fields_ = _INFO_FIELDS
 
 
+SD_TYPE_F32, SD_TYPE_F16, SD_TYPE_BF16 = 1, 2, 3
+SD_PACK_E4M3, SD_PACK_E5M2 = 1, 2
+PACK_FORMATS = {"e4m3": SD_PACK_E4M3, "e5m2": SD_PACK_E5M2}
+SD_ACT_NONE, SD_ACT_RELU, SD_ACT_SILU, SD_ACT_GELU = 0, 1, 2, 3
+ACTIVATIONS = {"none": SD_ACT_NONE, "relu": SD_ACT_RELU, "silu": SD_ACT_SILU, "gelu": SD_ACT_GELU}
+
+
+class sd_packed_t(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("ld", _i64), ("format", _i32), ("reserved", _i32), ("codes", _P),
+                ("scales", _P)]
+
+
+class sd_norm_t(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("segments", _i64), ("offsets", _P), ("longest", _i64), ("channels", _i32),
+                ("groups", _i32), ("type", _i32), ("activation", _i32), ("eps", ctypes.c_float), ("reserved", _i32),
+                ("weight", _P), ("bias", _P)]
+
+
 class SparseDittoError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -157,6 +175,19 @@ def _load():
     lib.sd_status_string.restype = ctypes.c_char_p
     lib.sd_last_error.argtypes = []
     lib.sd_last_error.restype = ctypes.c_char_p
+    packed, norm, size = ctypes.POINTER(sd_packed_t), ctypes.POINTER(sd_norm_t), ctypes.POINTER(ctypes.c_size_t)
+    lib.sd_pack.argtypes = [_P, _i32, _i64, _i64, packed, _P]
+    lib.sd_unpack.argtypes = [packed, _P, _i32, _i64, _P]
+    lib.sd_pack_product.argtypes = [packed, packed, _P, _P, _i32, _i64, _P]
+    lib.sd_pack_gradient_size.argtypes = [_i64, _i64, _i64, size]
+    lib.sd_pack_gradient.argtypes = [packed, _P, _i32, _i64, _i64, _P, _P, ctypes.c_size_t, _P]
+    lib.sd_group_norm_size.argtypes = [norm, size, size]
+    lib.sd_group_norm.argtypes = [norm, _P, _i64, _P, _i64, packed, packed, _P, _P, _P, ctypes.c_size_t, _P]
+    lib.sd_group_norm_backward.argtypes = [norm, _P, _i64, _P, _i64, packed, _P, _P, _P, _i64, _P, _P, _P,
+                                           ctypes.c_size_t, _P]
+    for f in ("sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
+              "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward"):
+        getattr(lib, f).restype = ctypes.c_int
     for f in ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_spmm", "sd_plan_info", "sd_plan_export_size",
               "sd_plan_export", "sd_plan_device", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load"):
         getattr(lib, f).restype = ctypes.c_int
@@ -165,7 +196,9 @@ def _load():
 
 _lib = _load()
 EXPORTED = ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_plan_device", "sd_spmm", "sd_spmm_merge_noalloc", "sd_plan_info", "sd_plan_export_size",
-            "sd_plan_export", "sd_plan_destroy", "sd_plan_cache_clear", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load", "sd_release_memory", "sd_status_string", "sd_last_error")
+            "sd_plan_export", "sd_plan_destroy", "sd_plan_cache_clear", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load", "sd_release_memory", "sd_status_string", "sd_last_error",
+            "sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
+            "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward")
 
 
 def _check(status: int, where: str):
@@ -341,6 +374,58 @@ def sd_spmm_merge_noalloc(rowptr, colidx, values, m: int, k: int, nnz: int, n: i
     c = sd_csr_t(int(m), int(k), int(nnz), _devptr(rowptr), _devptr(colidx), _devptr(values))
     _check(_lib.sd_spmm_merge_noalloc(ctypes.byref(c), int(n), int(units), _devptr(B), _devptr(C), stream),
            "sd_spmm_merge_noalloc")
+
+
+def _stream(stream):
+    return stream if stream is None or isinstance(stream, int) else int(stream.cuda_stream)
+
+
+def sd_pack(x, type: int, row_stride: int, col_stride: int, out: sd_packed_t, stream=None) -> None:
+    """Device table x (pointer or tensor) into the codes and scales of `out`."""
+    _check(_lib.sd_pack(_devptr(x), type, row_stride, col_stride, out, _stream(stream)), "sd_pack")
+
+
+def sd_unpack(x: sd_packed_t, y, type: int, row_stride: int, stream=None) -> None:
+    _check(_lib.sd_unpack(x, _devptr(y), type, row_stride, _stream(stream)), "sd_unpack")
+
+
+def sd_pack_product(X: sd_packed_t, W: sd_packed_t, bias, Y, type: int, row_stride: int, stream=None) -> None:
+    """Y = X.W^T (+ bias) of two packed tables."""
+    _check(_lib.sd_pack_product(X, W, _devptr(bias), _devptr(Y), type, row_stride, _stream(stream)),
+           "sd_pack_product")
+
+
+def sd_pack_gradient_size(rows: int, cols: int, n: int) -> int:
+    size = ctypes.c_size_t()
+    _check(_lib.sd_pack_gradient_size(rows, cols, n, size), "sd_pack_gradient_size")
+    return size.value
+
+
+def sd_pack_gradient(X: sd_packed_t, G, type: int, n: int, row_stride: int, dW, workspace, bytes: int,
+                     stream=None) -> None:
+    """dW = X^T.G, X packed, G a device table of n columns."""
+    _check(_lib.sd_pack_gradient(X, _devptr(G), type, n, row_stride, _devptr(dW), _devptr(workspace), bytes,
+                                 _stream(stream)), "sd_pack_gradient")
+
+
+def sd_group_norm_size(d: sd_norm_t):
+    """Workspace bytes of the forward and of the backward call."""
+    forward, backward = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.sd_group_norm_size(d, forward, backward), "sd_group_norm_size")
+    return forward.value, backward.value
+
+
+def sd_group_norm(d: sd_norm_t, x, x_stride: int, y, y_stride: int, x_packed, y_packed, mean, rstd, workspace,
+                  bytes: int, stream=None) -> None:
+    _check(_lib.sd_group_norm(d, _devptr(x), x_stride, _devptr(y), y_stride, x_packed, y_packed, _devptr(mean),
+                              _devptr(rstd), _devptr(workspace), bytes, _stream(stream)), "sd_group_norm")
+
+
+def sd_group_norm_backward(d: sd_norm_t, dy, dy_stride: int, x, x_stride: int, x_packed, mean, rstd, dx,
+                           dx_stride: int, dweight, dbias, workspace, bytes: int, stream=None) -> None:
+    _check(_lib.sd_group_norm_backward(d, _devptr(dy), dy_stride, _devptr(x), x_stride, x_packed, _devptr(mean),
+                                       _devptr(rstd), _devptr(dx), dx_stride, _devptr(dweight), _devptr(dbias),
+                                       _devptr(workspace), bytes, _stream(stream)), "sd_group_norm_backward")
 
 
 def sd_plan_info(plan: Plan) -> dict:

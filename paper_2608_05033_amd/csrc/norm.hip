@@ -1,0 +1,734 @@
+// sd_group_norm / sd_group_norm_backward: group norm with an activation over
+// segments of rows, channels last.
+//
+//   xh = (x - mean) rstd, z = xh w + b, y = act(z), with mean and
+//   rstd = (var + eps)^-1/2 over a segment's rows and a group's channels.
+//   dz = dy act'(z), dh = dz w:
+//   dx = rstd (dh - mean(dh) - xh mean(dh xh)), dw = sum dz xh, db = sum dz.
+//
+// Rows are cut into chunks of equal length whatever the segments are; a chunk's
+// part of a segment is a piece, numbered chunk + segment (both only grow along
+// the rows, so no two pieces share a number).  One kernel leaves sums per piece
+// and channel, one joins them per segment and group in 64 bits, one applies the
+// result, chunks in reverse so that what the first pass read last is still in
+// the Infinity Cache.  Every sum has a fixed order: results do not change from
+// run to run.  Bound by the bytes moved: x is read twice and written once.
+#include "dense.h"
+
+namespace {
+
+using namespace dense;
+
+constexpr int kThreads = 256;
+constexpr int V = 4;         // channels per lane
+constexpr int kBatch = 8;    // rows of a lane in flight
+
+// What every kernel needs of the call.
+struct Shape {
+  int64_t rows, segments, len;  // len: rows of each segment where offsets is null
+  const int32_t *offsets;
+  int32_t channels, groups, per_group;
+  int32_t chunk_rows, chunks, tx, ty;
+  float eps;
+  const float *weight, *bias;
+};
+
+__device__ inline int64_t seg_begin(const Shape &p, int64_t s) { return p.offsets ? p.offsets[s] : s * p.len; }
+// The segment that holds row r: the last one that begins at or before it.
+__device__ inline int64_t seg_of(const Shape &p, int64_t r) {
+  if (!p.offsets) return r / p.len;
+  int64_t lo = 0, hi = p.segments;  // offsets[lo] <= r < offsets[hi]
+  while (hi - lo > 1) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (p.offsets[mid] <= r)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// Rows [lo, hi) of segment s inside rows [r0, r1); calls f(s, lo, hi) for each
+// segment that has some.
+template <typename F>
+__device__ inline void for_pieces(const Shape &p, int64_t r0, int64_t r1, F f) {
+  for (int64_t s = seg_of(p, r0); s < p.segments; ++s) {
+    const int64_t b = seg_begin(p, s), e = seg_begin(p, s + 1);
+    if (b >= r1) break;
+    const int64_t lo = b > r0 ? b : r0, hi = e < r1 ? e : r1;
+    if (lo < hi) f(s, lo, hi);
+  }
+}
+
+// ---- where x comes from: dense rows, or 8-bit codes and their scales ----
+template <typename T>
+struct Dense {
+  const T *p;
+  int64_t stride;
+  __device__ void load(int64_t r, int32_t c, int left, float (&v)[V]) const {
+    const T *q = p + r * stride + c;
+    if (left >= V)
+      load_span(q, v);
+    else
+      load_part(q, left, v);
+  }
+};
+template <int FMT>
+struct Codes {
+  const uint8_t *codes, *scales;
+  int64_t ld, rows;
+  __device__ void load(int64_t r, int32_t c, int left, float (&v)[V]) const {
+    if (left <= 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = 0.0f;
+      return;
+    }
+    const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + r * ld + c);
+    const float s = scale_value(scales[(int64_t)(c / kBlock) * rows + r]);
+    decode4<FMT>(w, v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] *= s;
+  }
+};
+
+// ---- activations; NaN stays NaN ----
+template <int ACT>
+__device__ inline float act(float z) {
+  if constexpr (ACT == SD_ACT_RELU) return z < 0.0f ? 0.0f : z;
+  if constexpr (ACT == SD_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  if constexpr (ACT == SD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  return z;
+}
+template <int ACT>
+__device__ inline float act_slope(float z) {
+  if constexpr (ACT == SD_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
+  if constexpr (ACT == SD_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    return s + z * s * (1.0f - s);
+  }
+  if constexpr (ACT == SD_ACT_GELU)
+    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+  return 1.0f;
+}
+
+// ------------------------------------------------------------- forward -----
+// Per piece and channel: the sums of x and x^2, in 64 bits.  A product of two
+// 24-bit numbers is exact there, so the variance keeps 1e-8 of itself with a
+// mean 10^4 deviations away, and the two 64-bit operations per element still
+// take less time than loading it.
+template <typename X>
+__global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double *__restrict__ part) {
+  __shared__ double s_a[V][kThreads], s_b[V][kThreads];
+  const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
+  const int32_t c = (blockIdx.y * p.tx + tx) * V;
+  const int left = p.channels - c;
+  const int64_t r0 = (int64_t)blockIdx.x * p.chunk_rows;
+  const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
+  for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
+    double a[V] = {}, b[V] = {};
+    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
+      float v[kBatch][V];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = r + (int64_t)u * TY;
+        x.load(row < hi ? row : r, c, left, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const bool live = r + (int64_t)u * TY < hi;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const double d = live ? v[u][i] : 0.0f;
+          a[i] += d;
+          b[i] = fma(d, d, b[i]);
+        }
+      }
+    }
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      s_a[i][t] = a[i];
+      s_b[i][t] = b[i];
+    }
+    __syncthreads();
+    for (int h = TY / 2; h > 0; h /= 2) {
+      if (ty < h) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s_a[i][t] = a[i] += s_a[i][t + h * p.tx];
+          s_b[i][t] = b[i] += s_b[i][t + h * p.tx];
+        }
+      }
+      __syncthreads();
+    }
+    if (ty == 0) {
+      double *o = part + (blockIdx.x + s) * 2 * (int64_t)p.channels + c;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i < left) {
+          o[i] = a[i];
+          o[p.channels + i] = b[i];
+        }
+    }
+  });
+}
+
+// Sum over the workgroup's threads, the same in every thread.
+__device__ inline double wg_sum(double v, double *lds) {
+#pragma unroll
+  for (int d = 32; d > 0; d /= 2) v += __shfl_xor(v, d);
+  if (blockDim.x == 64) return v;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  double t = 0;
+  for (uint32_t w = 0; w < blockDim.x / 64; ++w) t += lds[w];
+  return t;
+}
+
+__device__ inline void write_stats(const Shape &p, double sum, double square, double count, float *mean, float *rstd) {
+  const double mu = sum / count, var = square / count - mu * mu;
+  *mean = (float)mu;
+  *rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)p.eps));
+}
+
+// Of the pieces of a segment's rows [b, e), this thread's share: f(piece's chunk,
+// channel in the group).
+template <typename F>
+__device__ inline void for_items(const Shape &p, int64_t b, int64_t e, F f) {
+  if (e <= b) return;
+  int64_t c0 = b / p.chunk_rows, c1 = (e - 1) / p.chunk_rows;
+  c0 = c0 < 0 ? 0 : c0;
+  c1 = c1 >= p.chunks ? p.chunks - 1 : c1;
+  const int64_t items = (c1 - c0 + 1) * p.per_group;
+  for (int64_t i = threadIdx.x; i < items; i += blockDim.x) {
+    const int64_t k = items < (1ll << 31) ? (uint32_t)i / (uint32_t)p.per_group : i / p.per_group;
+    f(c0 + k, (int32_t)(i - k * p.per_group));
+  }
+}
+
+__global__ void k_norm_join(Shape p, const double *__restrict__ part, float *__restrict__ mean,
+                            float *__restrict__ rstd) {
+  __shared__ double lds[16];
+  for (int64_t at = blockIdx.x; at < p.segments * p.groups; at += gridDim.x) {
+    const int64_t s = at / p.groups;
+    const int32_t g = (int32_t)(at - s * p.groups);
+    const int64_t b = seg_begin(p, s), e = seg_begin(p, s + 1);
+    const double *base = part + s * 2 * (int64_t)p.channels + (int64_t)g * p.per_group;
+    double sum = 0, square = 0;
+    for_items(p, b, e, [&](int64_t k, int32_t i) {
+      sum += base[k * 2 * p.channels + i];
+      square += base[(k * 2 + 1) * p.channels + i];
+    });
+    sum = wg_sum(sum, lds);
+    square = wg_sum(square, lds);
+    if (threadIdx.x == 0) write_stats(p, sum, square, e > b ? (double)(e - b) * p.per_group : 1.0, mean + at, rstd + at);
+    __syncthreads();
+  }
+}
+
+// Where a kernel writes 8-bit copies; codes is null where it does not.
+struct Packs {
+  uint8_t *codes, *scales;
+  int64_t ld;
+};
+template <int FMT>
+__device__ inline void store_packed(const Packs &o, int64_t rows, int64_t r, int32_t c, int32_t channels, int tx,
+                                    int width, const float (&v)[V], bool live) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const uint32_t b = c + i < channels ? finite_bits(v[i]) : 0u;
+    most = most > b ? most : b;
+  }
+  for (int d = 1; d < width; d *= 2) {
+    const uint32_t a = (uint32_t)__shfl_xor((int)most, d);
+    most = most > a ? most : a;
+  }
+  if (!live) return;
+  const uint32_t s = scale_byte<FMT>(most);
+  const float inv = inverse_scale(s);
+  if (c < ((channels + 15) & ~15)) {
+    float u[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) u[i] = c + i < channels ? v[i] * inv : 0.0f;
+    *reinterpret_cast<uint32_t *>(o.codes + r * o.ld + c) = encode4<FMT>(u[0], u[1], u[2], u[3]);
+  }
+  if (tx % (kBlock / V) == 0 && c < channels) o.scales[(int64_t)(c / kBlock) * rows + r] = (uint8_t)s;
+}
+
+// Mean, rstd * weight and bias of a lane's channels.
+struct Coeff {
+  float mean[V], scale[V], shift[V];
+};
+__device__ inline void load_coeff(const Shape &p, const float *mean, const float *rstd, int64_t s, int32_t c, int left,
+                                  Coeff &k, float (&rs)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    if (i < left) {
+      const int64_t g = s * p.groups + (c + i) / p.per_group;
+      rs[i] = rstd[g];
+      k.mean[i] = mean[g];
+      k.scale[i] = rs[i] * (p.weight ? p.weight[c + i] : 1.0f);
+      k.shift[i] = p.bias ? p.bias[c + i] : 0.0f;
+    } else {
+      rs[i] = k.mean[i] = k.scale[i] = k.shift[i] = 0.0f;
+    }
+  }
+}
+
+template <typename T, int ACT, int XF, int YF>
+__global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<T> x, const float *__restrict__ mean,
+                                                         const float *__restrict__ rstd, T *__restrict__ y,
+                                                         int64_t y_stride, Packs xo, Packs yo) {
+  const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
+  const int32_t c = (blockIdx.y * p.tx + tx) * V;
+  const int left = p.channels - c;
+  const int width = p.tx < kBlock / V ? p.tx : kBlock / V;
+  const int64_t r0 = (int64_t)(p.chunks - 1 - blockIdx.x) * p.chunk_rows;
+  const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
+  for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
+    Coeff k;
+    float rs[V];
+    load_coeff(p, mean, rstd, s, c, left, k, rs);
+    for (int64_t base = lo; base < hi; base += (int64_t)TY * kBatch) {
+      float v[kBatch][V];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = base + ty + (int64_t)u * TY;
+        x.load(row < hi ? row : lo, c, left, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = base + ty + (int64_t)u * TY;
+        const bool live = row < hi;
+        if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, v[u], live);
+        float out[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[i] = act<ACT>((v[u][i] - k.mean[i]) * k.scale[i] + k.shift[i]);
+        if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, out, live);
+        if (live && y) {
+          T *q = y + row * y_stride + c;
+          if (left >= V)
+            store_span(q, out);
+          else
+            store_part(q, left, out);
+        }
+      }
+    }
+  });
+}
+
+// ------------------------------------------------------------ backward -----
+// Per piece and channel, and per chunk and channel: sums of dz and dz xh.
+template <typename T, typename X, int ACT>
+__global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
+                                                        const float *__restrict__ rstd, float *__restrict__ part,
+                                                        float *__restrict__ total) {
+  __shared__ float s_a[kThreads][V], s_b[kThreads][V];
+  const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
+  const int32_t c = (blockIdx.y * p.tx + tx) * V;
+  const int left = p.channels - c;
+  const int64_t r0 = (int64_t)blockIdx.x * p.chunk_rows;
+  const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
+  float ta[V] = {}, tb[V] = {};
+  // sums over the workgroup's rows into the threads of ty = 0
+  auto reduce = [&](float (&a)[V], float (&b)[V]) {
+    const int t = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      s_a[t][i] = a[i];
+      s_b[t][i] = b[i];
+    }
+    __syncthreads();
+    for (int h = TY / 2; h > 0; h /= 2) {
+      if (ty < h) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s_a[t][i] = a[i] += s_a[t + h * p.tx][i];
+          s_b[t][i] = b[i] += s_b[t + h * p.tx][i];
+        }
+      }
+      __syncthreads();
+    }
+  };
+  auto write = [&](float *o, const float (&a)[V], const float (&b)[V]) {
+    if (ty != 0 || left <= 0) return;
+    if (left >= V) {
+      store_span(o, a);
+      store_span(o + p.channels, b);
+    } else {
+      store_part(o, left, a);
+      store_part(o + p.channels, left, b);
+    }
+  };
+  for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
+    Coeff k;
+    float rs[V];
+    load_coeff(p, mean, rstd, s, c, left, k, rs);
+    float a[V] = {}, b[V] = {};
+    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
+      float xv[kBatch][V], dv[kBatch][V];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = r + (int64_t)u * TY;
+        x.load(row < hi ? row : r, c, left, xv[u]);
+        dy.load(row < hi ? row : r, c, left, dv[u]);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float sa = 0.0f, sb = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const float d = xv[u][i] - k.mean[i];
+          const float dz = dv[u][i] * act_slope<ACT>(d * k.scale[i] + k.shift[i]);
+          const bool live = r + (int64_t)u * TY < hi;
+          sa += live ? dz : 0.0f;
+          sb += live ? dz * (d * rs[i]) : 0.0f;
+        }
+        a[i] += sa;
+        b[i] += sb;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      ta[i] += a[i];
+      tb[i] += b[i];
+    }
+    reduce(a, b);
+    write(part + (blockIdx.x + s) * 2 * (int64_t)p.channels + c, a, b);
+  });
+  reduce(ta, tb);
+  write(total + (int64_t)blockIdx.x * 2 * p.channels + c, ta, tb);
+}
+
+// Workgroups [0, joins): mean(dh) and mean(dh xh) per segment and group; the
+// others: dweight and dbias of kJoinCols channels over all chunks.
+constexpr int kJoinCols = 16;
+__global__ void k_norm_join_back(Shape p, int32_t joins, const float *__restrict__ part,
+                                 const float *__restrict__ total, float *__restrict__ m1, float *__restrict__ m2,
+                                 float *__restrict__ dweight, float *__restrict__ dbias) {
+  __shared__ double lds[16];
+  __shared__ double s_a[512], s_b[512];
+  if ((int32_t)blockIdx.x >= joins) {
+    const int lane = threadIdx.x % kJoinCols, row = threadIdx.x / kJoinCols, step = blockDim.x / kJoinCols;
+    const int32_t c = (blockIdx.x - joins) * kJoinCols + lane;
+    double a = 0, b = 0;
+    if (c < p.channels)
+      for (int32_t k = row; k < p.chunks; k += step) {
+        a += total[(int64_t)k * 2 * p.channels + c];
+        b += total[((int64_t)k * 2 + 1) * p.channels + c];
+      }
+    s_a[threadIdx.x] = a;
+    s_b[threadIdx.x] = b;
+    __syncthreads();
+    for (int h = step / 2; h > 0; h /= 2) {
+      if (row < h) {
+        s_a[threadIdx.x] += s_a[threadIdx.x + h * kJoinCols];
+        s_b[threadIdx.x] += s_b[threadIdx.x + h * kJoinCols];
+      }
+      __syncthreads();
+    }
+    if (row == 0 && c < p.channels) {
+      if (dbias) dbias[c] = (float)s_a[threadIdx.x];
+      if (dweight) dweight[c] = (float)s_b[threadIdx.x];
+    }
+    return;
+  }
+  for (int64_t at = blockIdx.x; at < p.segments * p.groups; at += joins) {
+    const int64_t s = at / p.groups;
+    const int32_t g = (int32_t)(at - s * p.groups);
+    const int64_t b = seg_begin(p, s), e = seg_begin(p, s + 1);
+    const float *base = part + s * 2 * (int64_t)p.channels + (int64_t)g * p.per_group;
+    const float *w = p.weight ? p.weight + (int64_t)g * p.per_group : nullptr;
+    const double count = e > b ? (double)(e - b) * p.per_group : 1.0;
+    double a = 0, q = 0;
+    for_items(p, b, e, [&](int64_t k, int32_t i) {
+      const double wi = w ? (double)w[i] : 1.0;
+      a += wi * base[k * 2 * p.channels + i];
+      q += wi * base[(k * 2 + 1) * p.channels + i];
+    });
+    a = wg_sum(a, lds);
+    q = wg_sum(q, lds);
+    if (threadIdx.x == 0) {
+      m1[at] = (float)(a / count);
+      m2[at] = (float)(q / count);
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, typename X, int ACT>
+__global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
+                                                        const float *__restrict__ rstd, const float *__restrict__ m1,
+                                                        const float *__restrict__ m2, T *__restrict__ dx,
+                                                        int64_t dx_stride) {
+  const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
+  const int32_t c = (blockIdx.y * p.tx + tx) * V;
+  const int left = p.channels - c;
+  if (left <= 0) return;
+  const int64_t r0 = (int64_t)(p.chunks - 1 - blockIdx.x) * p.chunk_rows;
+  const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
+  for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
+    Coeff k;
+    float rs[V], a1[V], a2[V];
+    load_coeff(p, mean, rstd, s, c, left, k, rs);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int64_t g = s * p.groups + (i < left ? (c + i) / p.per_group : 0);
+      a1[i] = m1[g] * rs[i];
+      a2[i] = m2[g] * rs[i] * rs[i];
+    }
+    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
+      float xv[kBatch][V], dv[kBatch][V];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = r + (int64_t)u * TY;
+        x.load(row < hi ? row : r, c, left, xv[u]);
+        dy.load(row < hi ? row : r, c, left, dv[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int64_t row = r + (int64_t)u * TY;
+        float out[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float d = xv[u][i] - k.mean[i];
+          const float dz = dv[u][i] * act_slope<ACT>(d * k.scale[i] + k.shift[i]);
+          out[i] = dz * k.scale[i] - a1[i] - d * a2[i];
+        }
+        if (row < hi) {
+          T *q = dx + row * dx_stride + c;
+          if (left >= V)
+            store_span(q, out);
+          else
+            store_part(q, left, out);
+        }
+      }
+    }
+  });
+}
+
+// ---------------------------------------------------------------- host -----
+int check(const sd_norm_t *d) {
+  if (!d || d->rows < 0 || d->channels < 1 || d->groups < 1 || d->segments < 0 || d->longest < 0 ||
+      !type_ok(d->type) || d->activation < SD_ACT_NONE || d->activation > SD_ACT_GELU || d->reserved != 0 ||
+      !(d->eps >= 0.0f))
+    return SD_ERR_INVALID_VALUE;
+  if (d->channels % d->groups != 0) return SD_ERR_INVALID_VALUE;
+  if (d->rows > kMaxRows || d->segments > kMaxRows || d->channels > (1 << 24)) return SD_ERR_OVERFLOW;
+  if (!d->offsets && d->rows > 0 && (d->segments < 1 || d->rows % d->segments != 0)) return SD_ERR_INVALID_VALUE;
+  if (d->offsets && d->rows > 0 && d->segments < 1) return SD_ERR_INVALID_VALUE;
+  return SD_OK;
+}
+
+// Lanes for a row, with the 8-bit copies' bytes up to a multiple of 16.
+int64_t lanes_of(int32_t channels) { return ceil_div(channels, 16) * (16 / V); }
+
+// Lanes over channels: a power of two, or whole blocks of 32 lanes, so that a
+// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: eight
+// workgroups per compute unit, each thread a batch of rows at least.
+Shape shape_of(const sd_norm_t *d) {
+  Shape p{};
+  p.rows = d->rows;
+  p.segments = d->segments;
+  p.len = d->segments > 0 ? d->rows / d->segments : 0;
+  p.offsets = d->offsets;
+  p.channels = d->channels;
+  p.groups = d->groups;
+  p.per_group = d->channels / d->groups;
+  p.eps = d->eps;
+  p.weight = d->weight;
+  p.bias = d->bias;
+  const int64_t lanes = lanes_of(d->channels);
+  int32_t tx = 1;
+  while (tx < 32 && tx < lanes) tx *= 2;
+  if (lanes > 32) tx = (int32_t)(lanes > kThreads ? kThreads : ceil_div(lanes, 32) * 32);
+  p.tx = tx;
+  p.ty = 1;
+  while (p.ty * 2 * tx <= kThreads) p.ty *= 2;
+  const int64_t slabs = ceil_div(lanes, tx);
+  const int64_t step = (int64_t)p.ty * kBatch;
+  const int64_t want = 8ll * cu_count() / slabs;
+  int64_t rows = ceil_div(d->rows, want > 0 ? want : 1);
+  rows = ceil_div(rows > 0 ? rows : 1, step) * step;
+  p.chunk_rows = (int32_t)(rows > kMaxRows ? kMaxRows : rows);
+  p.chunks = (int32_t)ceil_div(d->rows, p.chunk_rows);
+  return p;
+}
+uint32_t slabs_of(const Shape &p) { return (uint32_t)ceil_div(lanes_of(p.channels), p.tx); }
+size_t part_bytes(const Shape &p) { return 8 * (size_t)(p.chunks + p.segments) * (size_t)p.channels; }
+size_t stats_bytes(const Shape &p) { return 2 * part_bytes(p); }
+size_t total_bytes(const Shape &p) { return 8 * (size_t)p.chunks * (size_t)p.channels; }
+size_t back_bytes(const Shape &p) {
+  return part_bytes(p) + total_bytes(p) + 8 * (size_t)p.segments * (size_t)p.groups;
+}
+// Workgroups and threads of a joining kernel: one workgroup per segment and
+// group, wide where there are few of them.
+uint32_t join_wgs(const Shape &p) {
+  const int64_t n = p.segments * (int64_t)p.groups;
+  return (uint32_t)(n < (1 << 20) ? n : (1 << 20));
+}
+uint32_t join_threads(const Shape &p) {
+  return p.segments * (int64_t)p.groups >= 1024 || p.chunks < 8 ? 64 : 512;
+}
+
+template <typename T, int ACT, int XF, int YF>
+void apply(const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y, int64_t y_stride, Packs xo,
+           Packs yo, hipStream_t s) {
+  hipLaunchKernelGGL((k_norm_apply<T, ACT, XF, YF>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, x, mean,
+                     rstd, static_cast<T *>(y), y_stride, xo, yo);
+}
+template <typename T, int ACT, int XF>
+void apply_y(int yf, const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y, int64_t y_stride,
+             Packs xo, Packs yo, hipStream_t s) {
+  if (yf == SD_PACK_E4M3)
+    apply<T, ACT, XF, SD_PACK_E4M3>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+  else if (yf == SD_PACK_E5M2)
+    apply<T, ACT, XF, SD_PACK_E5M2>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+  else
+    apply<T, ACT, XF, 0>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+}
+template <typename T, int ACT>
+void apply_x(int xf, int yf, const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y,
+             int64_t y_stride, Packs xo, Packs yo, hipStream_t s) {
+  if (xf == SD_PACK_E4M3)
+    apply_y<T, ACT, SD_PACK_E4M3>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+  else if (xf == SD_PACK_E5M2)
+    apply_y<T, ACT, SD_PACK_E5M2>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+  else
+    apply_y<T, ACT, 0>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+}
+
+template <typename T>
+int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+            const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double *part, hipStream_t s) {
+  const Dense<T> in{static_cast<const T *>(x), x_stride};
+  const Packs none{nullptr, nullptr, 0};
+  const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
+  const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
+  const int xf = xp ? xp->format : 0, yf = yp ? yp->format : 0;
+  if (p.chunks > 0)
+    hipLaunchKernelGGL((k_norm_stats<Dense<T>>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
+  if (join_wgs(p) > 0)
+    hipLaunchKernelGGL(k_norm_join, dim3(join_wgs(p)), dim3(join_threads(p)), 0, s, p, part, mean, rstd);
+  if (p.chunks > 0) {
+    if (activation == SD_ACT_RELU)
+      apply_x<T, SD_ACT_RELU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+    else if (activation == SD_ACT_SILU)
+      apply_x<T, SD_ACT_SILU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+    else if (activation == SD_ACT_GELU)
+      apply_x<T, SD_ACT_GELU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+    else
+      apply_x<T, SD_ACT_NONE>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+  }
+  return launched();
+}
+
+template <typename T, typename X, int ACT>
+int backward_as(const Shape &p, X x, Dense<T> dy, const float *mean, const float *rstd, T *dx, int64_t dx_stride,
+                float *dweight, float *dbias, float *ws, hipStream_t s) {
+  float *part = ws, *total = part + part_bytes(p) / 4, *m1 = total + total_bytes(p) / 4,
+        *m2 = m1 + p.segments * p.groups;
+  const dim3 grid(p.chunks, slabs_of(p)), threads(p.tx * p.ty);
+  if (p.chunks > 0)
+    hipLaunchKernelGGL((k_norm_sums<T, X, ACT>), grid, threads, 0, s, p, x, dy, mean, rstd, part, total);
+  hipLaunchKernelGGL(k_norm_join_back, dim3(join_wgs(p) + (uint32_t)ceil_div(p.channels, kJoinCols)),
+                     dim3(join_threads(p)), 0, s, p, (int32_t)join_wgs(p), part, total, m1, m2, dweight, dbias);
+  if (p.chunks > 0)
+    hipLaunchKernelGGL((k_norm_grad<T, X, ACT>), grid, threads, 0, s, p, x, dy, mean, rstd, m1, m2, dx, dx_stride);
+  return launched();
+}
+template <typename T, typename X>
+int backward_act(int32_t activation, const Shape &p, X x, Dense<T> dy, const float *mean, const float *rstd, T *dx,
+                 int64_t dx_stride, float *dweight, float *dbias, float *ws, hipStream_t s) {
+  if (activation == SD_ACT_RELU)
+    return backward_as<T, X, SD_ACT_RELU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+  if (activation == SD_ACT_SILU)
+    return backward_as<T, X, SD_ACT_SILU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+  if (activation == SD_ACT_GELU)
+    return backward_as<T, X, SD_ACT_GELU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+  return backward_as<T, X, SD_ACT_NONE>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+}
+template <typename T>
+int backward(int32_t activation, const Shape &p, const void *x, int64_t x_stride, const sd_packed_t *xp,
+             const void *dy, int64_t dy_stride, const float *mean, const float *rstd, void *dx, int64_t dx_stride,
+             float *dweight, float *dbias, float *ws, hipStream_t s) {
+  const Dense<T> in{static_cast<const T *>(x), x_stride}, g{static_cast<const T *>(dy), dy_stride};
+  T *out = static_cast<T *>(dx);
+  if (!xp) return backward_act<T>(activation, p, in, g, mean, rstd, out, dx_stride, dweight, dbias, ws, s);
+  if (xp->format == SD_PACK_E4M3)
+    return backward_act<T>(activation, p, Codes<SD_PACK_E4M3>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,
+                           out, dx_stride, dweight, dbias, ws, s);
+  return backward_act<T>(activation, p, Codes<SD_PACK_E5M2>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,
+                         out, dx_stride, dweight, dbias, ws, s);
+}
+
+int check_copy(const sd_norm_t *d, const sd_packed_t *p) {
+  if (!p) return SD_OK;
+  const int st = check_packed(p);
+  if (st != SD_OK) return st;
+  return p->rows == d->rows && p->cols == d->channels ? SD_OK : SD_ERR_INVALID_VALUE;
+}
+
+}  // namespace
+
+extern "C" int sd_group_norm_size(const sd_norm_t *d, size_t *forward, size_t *backward) {
+  const int st = check(d);
+  if (st != SD_OK) return st;
+  if (!forward && !backward) return SD_ERR_INVALID_VALUE;
+  const Shape p = shape_of(d);
+  if (forward) *forward = stats_bytes(p);
+  if (backward) *backward = back_bytes(p);
+  return SD_OK;
+}
+
+extern "C" int sd_group_norm(const sd_norm_t *d, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                             const sd_packed_t *x_packed, const sd_packed_t *y_packed, float *mean, float *rstd,
+                             void *workspace, size_t bytes, void *stream) {
+  int st = check(d);
+  if (st != SD_OK) return st;
+  if ((st = check_table(x, d->type, d->rows, d->channels, x_stride)) != SD_OK) return st;
+  if (y && (st = check_table(y, d->type, d->rows, d->channels, y_stride)) != SD_OK) return st;
+  if ((st = check_copy(d, x_packed)) != SD_OK || (st = check_copy(d, y_packed)) != SD_OK) return st;
+  if (!y && !y_packed && d->rows > 0) return SD_ERR_INVALID_VALUE;
+  if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
+  const Shape p = shape_of(d);
+  if (bytes < stats_bytes(p) || (stats_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
+    return SD_ERR_INVALID_VALUE;
+  if (d->segments == 0) return SD_OK;
+  if ((st = have_device()) != SD_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  double *part = static_cast<double *>(workspace);
+  return d->type == SD_TYPE_F32
+             ? forward<float>(p, d->activation, x, x_stride, y, y_stride, x_packed, y_packed, mean, rstd, part, s)
+         : d->type == SD_TYPE_F16
+             ? forward<f16>(p, d->activation, x, x_stride, y, y_stride, x_packed, y_packed, mean, rstd, part, s)
+             : forward<bf16>(p, d->activation, x, x_stride, y, y_stride, x_packed, y_packed, mean, rstd, part, s);
+}
+
+extern "C" int sd_group_norm_backward(const sd_norm_t *d, const void *dy, int64_t dy_stride, const void *x,
+                                      int64_t x_stride, const sd_packed_t *x_packed, const float *mean,
+                                      const float *rstd, void *dx, int64_t dx_stride, float *dweight, float *dbias,
+                                      void *workspace, size_t bytes, void *stream) {
+  int st = check(d);
+  if (st != SD_OK) return st;
+  if ((st = check_table(dy, d->type, d->rows, d->channels, dy_stride)) != SD_OK) return st;
+  if ((st = check_table(dx, d->type, d->rows, d->channels, dx_stride)) != SD_OK) return st;
+  if ((st = check_copy(d, x_packed)) != SD_OK) return st;
+  if (!x_packed && (st = check_table(x, d->type, d->rows, d->channels, x_stride)) != SD_OK) return st;
+  if (x && x_packed) return SD_ERR_INVALID_VALUE;
+  if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
+  const Shape p = shape_of(d);
+  if (bytes < back_bytes(p) || (back_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
+    return SD_ERR_INVALID_VALUE;
+  if ((st = have_device()) != SD_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  float *ws = static_cast<float *>(workspace);
+  return d->type == SD_TYPE_F32 ? backward<float>(d->activation, p, x, x_stride, x_packed, dy, dy_stride, mean, rstd,
+                                                  dx, dx_stride, dweight, dbias, ws, s)
+         : d->type == SD_TYPE_F16 ? backward<f16>(d->activation, p, x, x_stride, x_packed, dy, dy_stride, mean, rstd,
+                                                  dx, dx_stride, dweight, dbias, ws, s)
+                                  : backward<bf16>(d->activation, p, x, x_stride, x_packed, dy, dy_stride, mean, rstd,
+                                                   dx, dx_stride, dweight, dbias, ws, s);
+}

@@ -1,0 +1,476 @@
+"""The dense operators on the GPU against plain 64-bit forms: 8-bit packing bit
+for bit, products, weight gradients, group norm forward and backward, at the
+sizes, strides and values where they can go wrong."""
+import numpy as np
+import pytest
+
+import dense_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover - CPU container
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from paper_2608_05033_amd import dense  # noqa: E402
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+# half a unit in the last place of a rounding to the type, relative
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def table(x, dtype):
+    """x rounded to dtype on the GPU, and the same numbers in 64 bits."""
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(torch.float64).to(TYPES[dtype])
+    return t.cuda(), t.to(torch.float64).numpy()
+
+
+def to64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def activations(rows, cols, seed):
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((rows, cols)) * np.exp(g.standard_normal((rows, 1)))
+    x[:, ::3] = np.maximum(x[:, ::3], 0)
+    return x
+
+
+def check_packed(p, x64, fmt):
+    """Codes, scales and padding bit for bit."""
+    exps, units = ref.encode(x64, fmt)
+    codes, scales = p.codes.cpu().numpy(), p.scales.cpu().numpy()
+    assert np.array_equal(scales.astype(np.int64) - 127, exps)
+    got = ref.decode_codes(codes[:, :p.cols], fmt)
+    assert np.array_equal(got, units, equal_nan=True)
+    assert not codes[:, p.cols:-(-p.cols // 16) * 16].any()
+
+
+# ---------------------------------------------------------------- packing ---
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 16), (5, 127), (7, 128), (64, 129), (33, 300), (257, 64), (1030, 17)])
+def test_pack_bit_for_bit(rows, cols, dtype, fmt):
+    print(f"case pack {rows}x{cols} {dtype} {fmt}", flush=True)
+    t, x = table(activations(rows, cols, rows * 1000 + cols), dtype)
+    p = dense.pack(t, fmt)
+    check_packed(p, x, fmt)
+    for out in ("f32", "bf16", "f16"):
+        want = torch.from_numpy(ref.values(p.codes.cpu().numpy(), p.scales.cpu().numpy(), cols, fmt))
+        assert torch.equal(dense.unpack(p, TYPES[out]).cpu(), want.to(torch.float32).to(TYPES[out]))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+def test_pack_edges_of_the_range(fmt):
+    """Zeros, ties, subnormal results, infinities and NaN, values at and past a
+    power of two times the largest code, the ends of the fp32 range."""
+    top = ref.FORMATS[fmt][2]
+    x = np.zeros((12, 140))
+    x[1, 3] = top
+    x[2, 5] = np.nextafter(np.float32(top), np.float32(np.inf))
+    x[3, :8] = [np.inf, -np.inf, np.nan, 1.0, -2.0, 3.0, 0.25, -0.0]
+    x[4, :128] = np.arange(128) * 0.0625 + 1  # ties among them
+    x[5, :130] = np.ldexp(1.0, -np.arange(130) % 40)
+    x[6, :4] = [np.finfo(np.float32).max, -1.0, 1e30, 1e-30]
+    x[7, :4] = [1e-38, -2e-38, 3e-39, 1e-44]
+    x[8, 128:] = -5.5
+    x[9, :] = np.nan
+    x[10, :] = -np.inf
+    x[11, :3] = [2.0 ** -126, 2.0 ** -127, 2.0 ** -149]
+    x = x.astype(np.float32).astype(np.float64)
+    p = dense.pack(torch.from_numpy(x).float().cuda(), fmt)
+    check_packed(p, x, fmt)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pack_strides(dtype):
+    """Transposed, strided, broadcast and misaligned tables."""
+    t, x = table(activations(150, 210, 5), dtype)
+    check_packed(dense.pack(t, transpose=True), np.ascontiguousarray(x.T), "e4m3")
+    check_packed(dense.pack(t[3:140, 1:202]), x[3:140, 1:202], "e4m3")
+    check_packed(dense.pack(t[::2, ::3]), x[::2, ::3], "e4m3")
+    check_packed(dense.pack(t[:1].expand(40, 210)), np.repeat(x[:1], 40, 0), "e4m3")
+    check_packed(dense.pack(t[:, 5:6]), x[:, 5:6], "e4m3")
+    flat = torch.zeros(150 * 210 + 1, dtype=t.dtype, device="cuda")
+    flat[1:] = t.reshape(-1)
+    check_packed(dense.pack(flat[1:].view(150, 210)), x, "e4m3")
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (0, 0)])
+def test_empty_tables(rows, cols):
+    p = dense.pack(torch.zeros(rows, cols, device="cuda"))
+    assert tuple(dense.unpack(p).shape) == (rows, cols)
+    w = dense.pack(torch.zeros(3, cols, device="cuda"))
+    bias = torch.arange(3, dtype=torch.float32, device="cuda")
+    assert torch.equal(dense.product(p, w, bias), bias.expand(rows, 3))
+    assert torch.equal(dense.weight_gradient(p, torch.ones(rows, 4, device="cuda")), torch.zeros(cols, 4, device="cuda"))
+
+
+# --------------------------------------------------------------- products ---
+def packed_pair(rows, cols, n, x_fmt="e4m3", w_fmt="e4m3", seed=0):
+    g = np.random.default_rng(rows * 31 + cols * 7 + n + seed)
+    x = g.standard_normal((rows, cols)) * np.exp(0.5 * g.standard_normal((rows, 1)))
+    w = g.standard_normal((n, cols)) / max(cols, 1) ** 0.5
+    X, W = dense.pack(torch.from_numpy(x).float().cuda(), x_fmt), dense.pack(torch.from_numpy(w).float().cuda(), w_fmt)
+    return X, W, of(X), of(W)
+
+
+def of(p):
+    return ref.values(p.codes.cpu().numpy(), p.scales.cpu().numpy(), p.cols, p.format)
+
+
+def check_product(y, x64, w64, bias, dtype):
+    """fp32 sums: each of the cols + 1 additions is off by at most 2^-24 of the
+    magnitudes summed.  16-bit results: the matrix unit's own alignment may drop
+    what is under 2^-12 of the magnitudes, then one rounding."""
+    want = x64 @ w64.T + (0 if bias is None else bias)
+    size = np.abs(x64) @ np.abs(w64).T + (0 if bias is None else np.abs(bias))
+    bound = (x64.shape[1] + 2) * 2.0 ** -24 * size
+    if dtype != "f32":
+        bound = bound + 2.0 ** -12 * size + HALF_ULP[dtype] * np.abs(want) + 2.0 ** -25
+    err = np.abs(to64(y) - want)
+    assert np.all(err <= bound + 1e-37), float((err - bound).max())
+    if dtype == "f32" and want.size > 64:
+        assert np.linalg.norm(to64(y) - want) <= 1e-6 * max(np.linalg.norm(want), 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,n", [(1, 1, 1), (1, 128, 64), (1, 1000, 260), (2, 129, 5), (16, 384, 33), (17, 64, 16),
+                                         (100, 601, 47), (65, 16, 128), (300, 128, 130), (130, 2050, 70), (513, 257, 255),
+                                         (700, 640, 1)])
+def test_product(rows, cols, n, dtype):
+    print(f"case product {rows}x{cols}x{n} {dtype}", flush=True)
+    X, W, x, w = packed_pair(rows, cols, n)
+    check_product(dense.product(X, W, dtype=TYPES[dtype]), x, w, None, dtype)
+    b = np.random.default_rng(n).standard_normal(n).astype(np.float32)
+    check_product(dense.product(X, W, torch.from_numpy(b).cuda(), TYPES[dtype]), x, w, b.astype(np.float64), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("x_fmt,w_fmt", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("rows", [5, 90, 300])
+def test_product_formats(rows, x_fmt, w_fmt, dtype):
+    X, W, x, w = packed_pair(rows, 300, 150, x_fmt, w_fmt)
+    check_product(dense.product(X, W, dtype=TYPES[dtype]), x, w, None, dtype)
+
+
+@pytest.mark.parametrize("rows,n", [(1100, 1030), (2600, 520)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_product_many_tiles(rows, n, dtype):
+    X, W, x, w = packed_pair(rows, 400, n)
+    check_product(dense.product(X, W, dtype=TYPES[dtype]), x, w, None, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [4, 200])
+def test_product_padding_and_strides(rows, dtype):
+    """Rows further apart than their codes need, with codes of other numbers
+    (NaN among them) past the last 16: they take no part."""
+    X, W, x, w = packed_pair(rows, 200, 40)
+    wide = torch.full((rows, 256), 0x7F, dtype=torch.uint8, device="cuda")
+    wide[:, :208] = X.codes
+    check_product(dense.product(dense.Packed(wide, X.scales, 200), W, dtype=TYPES[dtype]), x, w, None, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rows", [3, 150])
+def test_product_keeps_nan_to_its_row(rows, dtype):
+    x = np.random.default_rng(1).standard_normal((rows, 140))
+    x[rows - 1, 130] = np.nan
+    X = dense.pack(torch.from_numpy(x).float().cuda())
+    W = dense.pack(torch.randn(70, 140, generator=torch.Generator().manual_seed(1)).cuda())
+    y = dense.product(X, W, dtype=TYPES[dtype])
+    assert torch.isnan(y[rows - 1]).all() and torch.isfinite(y[:rows - 1]).all()
+
+
+def test_product_scales_at_both_ends():
+    """Tables near the ends of the fp32 range whose products are ordinary numbers."""
+    g = np.random.default_rng(4)
+    x, w = g.standard_normal((40, 200)) * 2.0 ** 100, g.standard_normal((30, 200)) * 2.0 ** -100
+    X, W = dense.pack(torch.from_numpy(x).float().cuda()), dense.pack(torch.from_numpy(w).float().cuda())
+    for dtype in ("f32", "bf16"):
+        check_product(dense.product(X, W, dtype=TYPES[dtype]), of(X), of(W), None, dtype)
+
+
+# ------------------------------------------------------- weight gradients ---
+def check_gradient(dw, x64, g64, rows):
+    """32-bit sums in a tree: at most rows / 16 + 64 additions on any path."""
+    want, size = x64.T @ g64, np.abs(x64).T @ np.abs(g64)
+    err = np.abs(to64(dw) - want)
+    assert np.all(err <= (rows / 16 + 64) * 2.0 ** -24 * size + 1e-37), float(err.max())
+    assert np.linalg.norm(to64(dw) - want) <= 2e-6 * max(np.linalg.norm(want), np.linalg.norm(size) * 1e-2, 1e-30)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,n", [(1, 1, 1), (1, 130, 70), (31, 16, 8), (33, 128, 64), (500, 129, 65),
+                                         (1000, 47, 200), (4099, 300, 33), (9000, 64, 128), (700, 257, 257)])
+def test_gradient(rows, cols, n, dtype, fmt):
+    print(f"case gradient {rows}x{cols}x{n} {dtype} {fmt}", flush=True)
+    g = np.random.default_rng(rows + cols * 3 + n)
+    X = dense.pack(torch.from_numpy(activations(rows, cols, rows + n)).float().cuda(), fmt)
+    G, g64 = table(g.standard_normal((rows, n)) * 0.1, dtype)
+    check_gradient(dense.weight_gradient(X, G), of(X), g64, rows)
+    wide = torch.full((rows, n + 5), float("nan"), dtype=G.dtype, device="cuda")
+    wide[:, 3:3 + n] = G
+    assert torch.equal(dense.weight_gradient(X, wide[:, 3:3 + n]), dense.weight_gradient(X, G))
+
+
+def test_gradient_keeps_infinities_and_large_values():
+    X = dense.pack(torch.ones(40, 20, device="cuda"))
+    G = torch.zeros(40, 6, device="cuda")
+    G[3, 0], G[5, 1], G[6, 2], G[7, 3] = float("inf"), float("nan"), 3.4e38, 1e-38
+    dw = dense.weight_gradient(X, G)
+    assert torch.isposinf(dw[:, 0]).all() and torch.isnan(dw[:, 1]).all()
+    assert torch.allclose(dw[:, 2], torch.full((20,), 3.4e38, device="cuda"), rtol=1e-6)
+    assert torch.allclose(dw[:, 3], torch.full((20,), 1e-38, device="cuda"), rtol=1e-2, atol=0)
+    assert not dw[:, 4:].any()
+
+
+# -------------------------------------------------------------- group norm --
+def offsets_of(rows, segments, seed):
+    """Ragged offsets with empty segments among them, at the ends too."""
+    g = np.random.default_rng(seed)
+    cut = np.sort(g.integers(0, rows + 1, segments - 1)) if segments > 1 else np.zeros(0, np.int64)
+    if segments > 4:
+        cut[0], cut[1], cut[-1] = 0, 0, rows
+    return np.concatenate([[0], cut, [rows]]).astype(np.int64)
+
+
+def norm_inputs(rows, channels, dtype, seed):
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((rows, channels)) * (0.5 + g.random(channels)) + g.standard_normal(channels)
+    t, x64 = table(x, dtype)
+    w, b = (1 + 0.2 * g.standard_normal(channels)).astype(np.float32), (0.2 * g.standard_normal(channels)).astype(np.float32)
+    return t, x64, torch.from_numpy(w).cuda(), torch.from_numpy(b).cuda(), w.astype(np.float64), b.astype(np.float64), g
+
+
+def check_norm(out, x64, groups, w, b, eps, kind, off, dtype):
+    """Values in fp32 are off by some roundings of the numbers that form them:
+    16 of 2^-24 of (|x| + |mean|) rstd |w| + |b|; then the result's rounding."""
+    y, mean, rstd, _, z = ref.norm(x64, groups, w, b, eps, kind, off)
+    per = x64.shape[1] // groups
+    seg = np.repeat(np.arange(len(off) - 1), np.diff(off))
+    spread = lambda v: np.repeat(v[seg], per, axis=1)  # noqa: E731
+    size = (np.abs(x64) + np.abs(spread(mean))) * spread(rstd) * np.abs(w) + np.abs(b) + np.abs(z)
+    assert np.allclose(to64(out.rstd), rstd, rtol=2e-6, atol=0)
+    centre = np.zeros_like(mean)
+    np.maximum.at(centre, seg, np.abs(x64).reshape(len(x64), groups, per).max(2))
+    assert np.all(np.abs(to64(out.mean) - mean) <= 2.0 ** -22 * centre + 1e-37)
+    if out.y is not None:
+        assert np.all(np.abs(to64(out.y) - y) <= 2.0 ** -20 * size + (HALF_ULP[dtype] if dtype != "f32" else 0) *
+                      np.abs(y) * 1.01 + (0 if dtype == "f32" else 2.0 ** -24))
+    return y
+
+
+SHAPES = [  # rows, channels, groups, segments (negative: ragged)
+    (1, 1, 1, 1), (1, 64, 8, 1), (3, 5, 5, 3), (37, 64, 8, 1), (64, 128, 8, 64), (300, 35, 7, -7), (1000, 130, 10, 4),
+    (257, 1028, 4, -3), (5000, 96, 6, -301), (4096, 32, 32, 2), (50, 2052, 1, 1), (6000, 8, 2, -2), (700, 512, 16, -350),
+    (9001, 3, 1, 1), (40000, 16, 4, 1), (2048, 256, 1, 1024)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,channels,groups,segments", SHAPES)
+def test_norm_forward(rows, channels, groups, segments, dtype):
+    kind = ["none", "relu", "silu", "gelu"][(rows + channels) % 4]
+    print(f"case norm {rows}x{channels} groups {groups} segments {segments} {dtype} {kind}", flush=True)
+    t, x64, w, b, w64, b64, _ = norm_inputs(rows, channels, dtype, rows + channels)
+    off = offsets_of(rows, -segments, rows) if segments < 0 else np.arange(segments + 1) * (rows // segments)
+    how = {"offsets": torch.from_numpy(off).int().cuda()} if segments < 0 else {"segments": segments}
+    out = dense.group_norm(t, groups, w, b, 1e-5, kind, **how)
+    y = check_norm(out, x64, groups, w64, b64, 1e-5, kind, off, dtype)
+    # the same through every way of saying it: a known longest segment, wider rows, 8-bit copies
+    if segments < 0:
+        again = dense.group_norm(t, groups, w, b, 1e-5, kind, longest=int(np.diff(off).max()), **how)
+        check_norm(again, x64, groups, w64, b64, 1e-5, kind, off, dtype)
+    wide = torch.full((rows, channels + 3), float("nan"), dtype=t.dtype, device="cuda")
+    wide[:, 1:1 + channels] = t
+    assert torch.equal(dense.group_norm(wide[:, 1:1 + channels], groups, w, b, 1e-5, kind, **how).y, out.y)
+    for fmt in ("e4m3", "e5m2"):
+        both = dense.group_norm(t, groups, w, b, 1e-5, kind, keep=fmt, pack_y=fmt, **how)
+        assert torch.equal(both.y, out.y) and torch.equal(both.mean, out.mean) and torch.equal(both.rstd, out.rstd)
+        check_packed(both.x, x64, fmt)
+        only = dense.group_norm(t, groups, w, b, 1e-5, kind, pack_y=fmt, dense_y=False, **how)
+        assert only.y is None
+        assert torch.equal(only.y_packed.codes, both.y_packed.codes)
+        assert torch.equal(only.y_packed.scales, both.y_packed.scales)
+        # y in 8 bits: half a step of the format, and of its least one
+        step = {"e4m3": 2.0 ** -4, "e5m2": 2.0 ** -3}[fmt]
+        least = np.ldexp({"e4m3": 2.0 ** -10, "e5m2": 2.0 ** -17}[fmt],
+                         both.y_packed.scales.cpu().numpy().astype(int)[np.arange(channels) // 128].T - 127)
+        assert np.all(np.abs(of(both.y_packed) - y) <= 1.001 * step * np.abs(y) + least + 2e-5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("keep", [None, "e4m3", "e5m2"])
+@pytest.mark.parametrize("rows,channels,groups,segments", SHAPES)
+def test_norm_backward(rows, channels, groups, segments, keep, dtype):
+    kind = ["none", "relu", "silu", "gelu"][(rows + channels // 2) % 4]
+    print(f"case norm backward {rows}x{channels} groups {groups} segments {segments} {dtype} {kind} {keep}", flush=True)
+    t, x64, w, b, w64, b64, g = norm_inputs(rows, channels, dtype, rows + channels + 1)
+    off = offsets_of(rows, -segments, rows) if segments < 0 else np.arange(segments + 1) * (rows // segments)
+    how = {"offsets": torch.from_numpy(off).int().cuda()} if segments < 0 else {"segments": segments}
+    out = dense.group_norm(t, groups, w, b, 1e-5, kind, keep=keep, **how)
+    dy, dy64 = table(0.1 * g.standard_normal((rows, channels)), dtype)
+    seen = x64 if keep is None else of(out.x)
+    mean, rstd = to64(out.mean), to64(out.rstd)
+    dx64, dw64, db64, size, size_w, size_b, z = ref.norm_backward(dy64, seen, mean, rstd, groups, w64, b64, kind, off)
+    if kind == "relu":  # the slope jumps at 0: what rounding could carry across is not compared
+        per = channels // groups
+        seg = np.repeat(np.arange(len(off) - 1), np.diff(off))
+        near = np.abs(z) < 1e-5 * (1 + np.abs(seen) * np.repeat(rstd[seg], per, axis=1))
+        if near.any():
+            dy64 = np.where(near, 0.0, dy64)
+            dy = torch.from_numpy(dy64).to(TYPES[dtype]).cuda()
+            dx64, dw64, db64, size, size_w, size_b, z = ref.norm_backward(dy64, seen, mean, rstd, groups, w64, b64,
+                                                                         kind, off)
+    longest = [0, int(np.diff(off).max())] if segments < 0 else [0]
+    for known in longest:
+        dx, dw, db = dense.group_norm_backward(dy, out.x, out.mean, out.rstd, groups, w, b, 1e-5, kind, longest=known,
+                                               **how)
+        if dtype == "f16":  # what f16 cannot hold rounds to an infinity
+            past = np.abs(dx64) >= 65520
+            assert np.array_equal(np.isinf(to64(dx)), past)
+            dx, dx64 = torch.where(torch.isinf(dx), torch.zeros_like(dx), dx), np.where(past, 0.0, dx64)
+        # the slopes' own error grows with |x| rstd: the offset that mean and x share
+        grown = 1 + np.abs(seen).max() * rstd.max()
+        assert np.all(np.abs(to64(dx) - dx64) <= 2.0 ** -19 * grown * size +
+                      (HALF_ULP[dtype] if dtype != "f32" else 0) * np.abs(dx64) * 1.01 +
+                      (0 if dtype == "f32" else 2.0 ** -24))
+        assert np.all(np.abs(to64(dw) - dw64) <= 2.0 ** -19 * grown * (size_w + size_b))
+        assert np.all(np.abs(to64(db) - db64) <= 2.0 ** -19 * grown * size_b)
+
+
+def test_norm_gradient_against_differences():
+    """The gradient of sum(y R) from differences of the 64-bit forward form."""
+    rows, channels, groups, kind = 9, 12, 3, "gelu"
+    t, x64, w, b, w64, b64, g = norm_inputs(rows, channels, "f32", 3)
+    off = np.array([0, 4, 4, 9])
+    r = g.standard_normal((rows, channels)).astype(np.float32).astype(np.float64)
+    how = {"offsets": torch.from_numpy(off).int().cuda()}
+    out = dense.group_norm(t, groups, w, b, 1e-5, kind, **how)
+    dx, dw, db = dense.group_norm_backward(torch.from_numpy(r).float().cuda(), out.x, out.mean, out.rstd, groups, w, b,
+                                           1e-5, kind, **how)
+    loss = lambda x, ww, bb: float((ref.norm(x, groups, ww, bb, 1e-5, kind, off)[0] * r).sum())  # noqa: E731
+    h = 1e-5
+
+    def differences(v, f):
+        out = np.zeros_like(v)
+        for i in np.ndindex(*v.shape):
+            up, down = v.copy(), v.copy()
+            up[i] += h
+            down[i] -= h
+            out[i] = (f(up) - f(down)) / (2 * h)
+        return out
+
+    # differences: h^2 times third derivatives, and 2^-52 of the loss over h
+    assert np.allclose(to64(dx), differences(x64, lambda v: loss(v, w64, b64)), rtol=1e-4, atol=2e-5)
+    assert np.allclose(to64(dw), differences(w64, lambda v: loss(x64, v, b64)), rtol=1e-4, atol=2e-5)
+    assert np.allclose(to64(db), differences(b64, lambda v: loss(x64, w64, v)), rtol=1e-4, atol=2e-5)
+
+
+def test_norm_large_mean_and_constant_rows():
+    """Statistics without cancellation: a mean 10^4 standard deviations away; a
+    constant table has variance 0 exactly; an outlier in the first row."""
+    g = np.random.default_rng(8)
+    x = (g.standard_normal((5000, 16)) + 1e4).astype(np.float32).astype(np.float64)
+    x[0, :4] = 3e4
+    out = dense.group_norm(torch.from_numpy(x).float().cuda(), 4)
+    _, mean, rstd, _, _ = ref.norm(x, 4, None, None, 1e-5, "none", [0, 5000])
+    assert np.allclose(to64(out.rstd), rstd, rtol=1e-5, atol=0)
+    assert np.allclose(to64(out.mean), mean, rtol=2.0 ** -23, atol=0)
+    flat = dense.group_norm(torch.full((700, 24), 0.1, device="cuda"), 2, eps=1e-3)
+    assert not flat.y.abs().gt(1e-5).any()
+    assert torch.allclose(flat.rstd, torch.full_like(flat.rstd, 1e-3 ** -0.5), rtol=1e-6)
+
+
+def test_norm_nan_and_infinity_stay_in_their_group():
+    x = torch.randn(90, 32, generator=torch.Generator().manual_seed(2))
+    x[40, 3], x[70, 30] = float("nan"), float("inf")
+    y = dense.group_norm(x.cuda(), 4, segments=3, activation="relu").y.view(3, 30, 4, 8)
+    bad = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+    bad[1, 0] = bad[2, 3] = True
+    assert torch.isfinite(y).all(3).all(1)[~bad].all() and torch.isnan(y[1, :, 0]).all()
+    assert not torch.isfinite(y[2, :, 3]).all()
+
+
+def test_norm_no_rows_and_empty_segments():
+    for segments in (0, 3):
+        off = torch.zeros(segments + 1, dtype=torch.int32, device="cuda")
+        out = dense.group_norm(torch.zeros(0, 8, device="cuda"), 2, offsets=off, eps=0.25)
+        assert out.y.shape == (0, 8) and (out.mean == 0).all() and (out.rstd == 2).all()
+        dx, dw, db = dense.group_norm_backward(torch.zeros(0, 8, device="cuda"), out.x, out.mean, out.rstd, 2, offsets=off)
+        assert dx.shape == (0, 8) and not dw.any() and not db.any()
+
+
+# ------------------------------------------------ streams, graphs, ranges ---
+def layer(x, w8, gamma, beta, dz):
+    x8 = dense.pack(x)
+    z = dense.product(x8, w8)
+    out = dense.group_norm(z, 4, gamma, beta, activation="silu", keep="e4m3", pack_y="e4m3")
+    dh = dense.product(dense.pack(dz, "e5m2"), w8)
+    dx, dg, db = dense.group_norm_backward(dh, out.x, out.mean, out.rstd, 4, gamma, beta, activation="silu")
+    dw = dense.weight_gradient(out.y_packed, dz)
+    return [z, out.y, dx, dg, db, dw, dense.unpack(out.y_packed)]
+
+
+def layer_inputs(rows=777, width=64):
+    g = torch.Generator().manual_seed(6)
+    r = lambda *s: torch.randn(*s, generator=g).cuda()  # noqa: E731
+    return r(rows, width), dense.pack(r(width, width) / 8), 1 + 0.1 * r(width), 0.1 * r(width), 0.1 * r(rows, width)
+
+
+def test_same_bits_each_time_and_on_another_stream():
+    args = layer_inputs(3000)
+    first = layer(*args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        junk = torch.randn(2000, 2000, device="cuda")
+        for _ in range(5):
+            junk = junk @ junk * 1e-3
+        other = layer(*args)
+    side.synchronize()
+    for a, b, c in zip(first, other, layer(*args)):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_graph_replays_equal_eager_calls():
+    x, w8, gamma, beta, dz = layer_inputs()
+    layer(x, w8, gamma, beta, dz)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = layer(x, w8, gamma, beta, dz)
+    for k in range(4):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator().manual_seed(k)))
+        want = [v.clone() for v in layer(x, w8, gamma, beta, dz)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.slow
+def test_offsets_past_two_to_the_31():
+    """Tables of more than 2^31 elements: their last rows."""
+    rows, channels = (1 << 24) + 37, 130
+    x = torch.zeros(rows, channels, dtype=torch.float16, device="cuda")
+    tail = torch.randn(37, channels, generator=torch.Generator().manual_seed(1)).half()
+    x[-37:] = tail.cuda()
+    off = torch.tensor([0, rows - 37, rows], dtype=torch.int32, device="cuda")
+    want = dense.group_norm(tail.cuda(), 10, activation="silu", keep="e4m3")
+    out = dense.group_norm(x, 10, activation="silu", offsets=off, keep="e4m3")
+    assert torch.allclose(out.y[-37:].float(), want.y.float(), rtol=2e-3, atol=1e-5) and not out.y[:1000].any()
+    assert torch.equal(out.x.codes[-37:], want.x.codes) and torch.equal(out.x.scales[:, -37:], want.x.scales)
+    dx, _, _ = dense.group_norm_backward(x, out.x, out.mean, out.rstd, 10, activation="silu", offsets=off)
+    dt, _, _ = dense.group_norm_backward(tail.cuda(), want.x, want.mean, want.rstd, 10, activation="silu")
+    assert torch.allclose(dx[-37:].float(), dt.float(), rtol=2e-3, atol=1e-4)
+    del out.y, dx, x
+    got = dense.weight_gradient(out.x, torch.ones(rows, 8, dtype=torch.bfloat16, device="cuda"))
+    assert torch.allclose(got, dense.unpack(want.x).sum(0)[:, None].expand(-1, 8), rtol=1e-5, atol=1e-4)
+    w = dense.pack(torch.randn(140, channels, generator=torch.Generator().manual_seed(3)).cuda())
+    y = dense.product(out.x, w, dtype=torch.bfloat16)
+    assert torch.equal(y[-37:], dense.product(want.x, w, dtype=torch.bfloat16)) and not y[:1000].any()
+    assert torch.equal(dense.unpack(out.x, torch.float16)[-37:], dense.unpack(want.x, torch.float16))
