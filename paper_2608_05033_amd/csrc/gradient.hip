@@ -19,10 +19,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256;
-constexpr int kRows = 32;   // rows of a step
+constexpr int kRows = 64;   // rows of a step
 constexpr int kTileC = 128; // columns of X per tile: one block, so one scale a row
-constexpr int kTileN = 64;  // columns of G per tile
-constexpr int kPad = 8;     // 16-bit values between the columns in shared memory beyond kRows
 
 template <typename T>
 constexpr int terms() {
@@ -49,110 +47,168 @@ __device__ inline uint32_t cut(float &v) {
   return top;
 }
 
-// Rows [r0, r1) of one tile by one workgroup: out[kTileC][kTileN] sums.
-template <typename T, int FMT>
+// Shared memory holds columns of kRows 16-bit values, in units of 8 rows.  The
+// unit's place is mixed with the column's, so that 16 neighbouring columns read
+// at one unit, and every fourth column written at one, touch different banks.
+__device__ inline int place(int col, int unit) {
+  return (col * (kRows / 8) + (unit ^ ((col >> 1) & 7) ^ ((col >> 4) & 1))) * 8;
+}
+
+// Rows [r0, r1) of one kTileC x TN tile by one workgroup.  The next step's rows
+// are read into registers while this step's products run.
+template <typename T, int FMT, int TN>
 __global__ __launch_bounds__(kThreads) void k_gradient(const uint8_t *__restrict__ codes,
                                                        const uint8_t *__restrict__ scales, int64_t ld, int64_t rows,
                                                        int32_t cols, const T *__restrict__ G, int64_t stride,
                                                        int32_t n, int32_t nt, int32_t splits, int64_t split_rows,
                                                        float *__restrict__ out, int64_t out_split) {
   constexpr int TERMS = terms<T>();
-  constexpr int LD = kRows + kPad;
-  __shared__ __align__(16) bf16 sx[kTileC * LD];
-  __shared__ __align__(16) bf16 sg[TERMS][kTileN * LD];
+  constexpr int NJ = TN / 32, GU = TN / 32;  // 16-column products per wave; row units per thread
+  __shared__ __align__(16) bf16 sx[kTileC * kRows];
+  __shared__ __align__(16) bf16 sg[TERMS][TN * kRows];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g4 = lane >> 4;
   const int32_t split = blockIdx.x % (uint32_t)splits, tile = blockIdx.x / (uint32_t)splits;
-  const int32_t ct = tile / nt, c0 = ct * kTileC, n0 = (tile % nt) * kTileN;
+  const int32_t ct = tile / nt, c0 = ct * kTileC, n0 = (tile % nt) * TN;
   const int64_t r0 = (int64_t)split * split_rows;
   const int64_t r1 = r0 + split_rows < rows ? r0 + split_rows : rows;
-  // wave w: columns [64 (w / 2), +64) of X, [32 (w % 2), +32) of G
-  f32x4 acc[4][2] = {};
-  // X: 32 threads over the tile's columns (4 codes each), 8 groups of 4 rows; G: 64 threads over columns, 4 of 8 rows
-  const int xc = (t & 31) * 4, xr = (t >> 5) * 4;
-  const int gc = t & 63, gr = (t >> 6) * 8;
+  // wave w: columns [64 (w / 2), +64) of X, [TN / 2 (w % 2), +TN / 2) of G
+  f32x4 acc[4][NJ] = {};
+  // X: 4 codes of 8 rows per thread; G: one column, GU units of 8 rows
+  const int xc = (t & 31) * 4, xu = t >> 5;
+  const int gc = t % TN, gu = t / TN * GU;
   const int32_t k16 = (cols + 15) & ~15;
   const bool x_in = c0 + xc < k16, g_in = n0 + gc < n;
-  for (int64_t r = r0; r < r1; r += kRows) {
-    bf16x2 lo[4], hi[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int64_t row = r + xr + u;
-      uint32_t w = 0;
-      float s = 0.0f;
-      if (row < r1 && x_in) {
-        w = *reinterpret_cast<const uint32_t *>(codes + row * ld + c0 + xc);
-        s = scale_value(scales[(int64_t)ct * rows + row]);
-      }
-      lo[u] = to_bf16<FMT>(w, s, false);
-      hi[u] = to_bf16<FMT>(w, s, true);
-    }
-    float gv[8];
+  const uint8_t *xp = codes + c0 + xc, *sp = scales + (int64_t)ct * rows;
+  const T *gp = G + n0 + gc;
+  uint32_t xw[8], xs[8];
+  T gw[GU][8];
+  auto fetch = [&](int64_t r) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int64_t row = r + gr + u;
-      gv[u] = row < r1 && g_in ? (float)G[row * stride + n0 + gc] : 0.0f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      sx[(xc + 0) * LD + xr + u] = lo[u][0];
-      sx[(xc + 1) * LD + xr + u] = lo[u][1];
-      sx[(xc + 2) * LD + xr + u] = hi[u][0];
-      sx[(xc + 3) * LD + xr + u] = hi[u][1];
+      const int64_t row = r + xu * 8 + u;
+      const bool in = row < r1 && x_in;
+      xw[u] = in ? *reinterpret_cast<const uint32_t *>(xp + row * ld) : 0u;
+      xs[u] = in ? sp[row] : 127u;
     }
 #pragma unroll
-    for (int k = 0; k < TERMS; ++k) {
-      u32x4 o;
+    for (int k = 0; k < GU; ++k)
 #pragma unroll
-      for (int u = 0; u < 8; u += 2) o[u / 2] = (cut(gv[u]) >> 16) | cut(gv[u + 1]);
-      *reinterpret_cast<u32x4 *>(&sg[k][gc * LD + gr]) = o;
-    }
-    __syncthreads();
-    bf16x8 a[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      a[i] = *reinterpret_cast<const bf16x8 *>(&sx[((wave >> 1) * 64 + i * 16 + r16) * LD + g4 * 8]);
-#pragma unroll
-    for (int k = TERMS - 1; k >= 0; --k)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const bf16x8 b = *reinterpret_cast<const bf16x8 *>(&sg[k][((wave & 1) * 32 + j * 16 + r16) * LD + g4 * 8]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i][j], 0, 0, 0);
+      for (int u = 0; u < 8; ++u) {
+        const int64_t row = r + (gu + k) * 8 + u;
+        gw[k][u] = row < r1 && g_in ? gp[row * stride] : (T)0.0f;
       }
+  };
+  if (r0 < r1) fetch(r0);
+  for (int64_t r = r0; r < r1; r += kRows) {
+    __syncthreads();
+    {
+      // four columns of eight rows: pairs of rows side by side
+      bf16x2 lo[8], hi[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float s = scale_value(xs[u]);
+        lo[u] = to_bf16<FMT>(xw[u], s, false);
+        hi[u] = to_bf16<FMT>(xw[u], s, true);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 o;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[u] = j < 2 ? lo[u][j & 1] : hi[u][j & 1];
+        *reinterpret_cast<bf16x8 *>(&sx[place(xc + j, xu)]) = o;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < GU; ++k) {
+      if constexpr (TERMS == 1) {
+        bf16x8 o;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) o[u] = gw[k][u];
+        *reinterpret_cast<bf16x8 *>(&sg[0][place(gc, gu + k)]) = o;
+      } else {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = (float)gw[k][u];
+#pragma unroll
+        for (int q = 0; q < TERMS; ++q) {
+          u32x4 o;
+#pragma unroll
+          for (int u = 0; u < 8; u += 2) {
+            const uint32_t a = cut(v[u]), b = cut(v[u + 1]);
+            o[u / 2] = (a >> 16) | b;
+          }
+          *reinterpret_cast<u32x4 *>(&sg[q][place(gc, gu + k)]) = o;
+        }
+      }
+    }
+    __syncthreads();
+    if (r + kRows < r1) fetch(r + kRows);
+#pragma unroll
+    for (int h = 0; h < kRows / 32; ++h) {
+      bf16x8 a[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        a[i] = *reinterpret_cast<const bf16x8 *>(&sx[place((wave >> 1) * 64 + i * 16 + r16, h * 4 + g4)]);
+#pragma unroll
+      for (int q = TERMS - 1; q >= 0; --q)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const bf16x8 b =
+              *reinterpret_cast<const bf16x8 *>(&sg[q][place((wave & 1) * (TN / 2) + j * 16 + r16, h * 4 + g4)]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b, acc[i][j], 0, 0, 0);
+        }
+    }
   }
   float *o = out + split * out_split;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int32_t c = c0 + (wave >> 1) * 64 + i * 16 + g4 * 4 + u, q = n0 + (wave & 1) * 32 + j * 16 + r16;
+        const int32_t c = c0 + (wave >> 1) * 64 + i * 16 + g4 * 4 + u, q = n0 + (wave & 1) * (TN / 2) + j * 16 + r16;
         if (c < cols && q < n) o[(int64_t)c * n + q] = acc[i][j][u];
       }
 }
 
-__global__ __launch_bounds__(kThreads) void k_gradient_join(const float *__restrict__ part, int64_t size,
-                                                            int32_t splits, float *__restrict__ dw) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < size; i += (int64_t)gridDim.x * kThreads) {
+// Sixteen threads share an output, each adding every sixteenth part.
+constexpr int kJoinOut = 64, kJoinWays = 16;
+__global__ __launch_bounds__(kJoinOut *kJoinWays) void k_gradient_join(const float *__restrict__ part, int64_t size,
+                                                                       int32_t splits, float *__restrict__ dw) {
+  __shared__ float sums[kJoinWays][kJoinOut];
+  const int o = threadIdx.x % kJoinOut, way = threadIdx.x / kJoinOut;
+  for (int64_t base = (int64_t)blockIdx.x * kJoinOut; base < size; base += (int64_t)gridDim.x * kJoinOut) {
     float sum = 0.0f;
-    for (int32_t s = 0; s < splits; ++s) sum += part[s * size + i];
-    dw[i] = sum;
+    if (base + o < size) {
+#pragma unroll 8
+      for (int32_t s = way; s < splits; s += kJoinWays) sum += part[s * size + base + o];
+    }
+    sums[way][o] = sum;
+    __syncthreads();
+    if (way == 0 && base + o < size) {
+#pragma unroll
+      for (int w = 1; w < kJoinWays; ++w) sum += sums[w][o];
+      dw[base + o] = sum;
+    }
+    __syncthreads();
   }
 }
 
 struct Split {
   int64_t tiles, split_rows;
-  int32_t nt, splits;
+  int32_t nt, splits, tn;
 };
-// Two workgroups per compute unit over all tiles; a part of at least 8 steps.
+// Two workgroups per compute unit over all tiles; a part of at least 4 steps.
+// Tiles of 128 columns of G where more than 64 are left to fill: X is then read
+// half as often.
 Split split_of(int64_t rows, int64_t cols, int64_t n) {
   Split p{};
-  p.nt = (int32_t)ceil_div(n, kTileN);
+  p.tn = n > 64 ? 128 : 64;
+  p.nt = (int32_t)ceil_div(n, p.tn);
   p.tiles = blocks_of(cols) * p.nt;
-  int64_t want = ceil_div(2ll * cu_count(), p.tiles > 0 ? p.tiles : 1);
-  const int64_t most = ceil_div(rows, 8 * kRows);
+  int64_t want = 2ll * cu_count() / (p.tiles > 0 ? p.tiles : 1);
+  const int64_t most = ceil_div(rows, 4 * kRows);
   if (want > most) want = most;
   if (want < 1) want = 1;
   p.split_rows = ceil_div(ceil_div(rows, want), kRows) * kRows;
@@ -168,13 +224,14 @@ int gradient(const sd_packed_t *X, const void *G, int64_t n, int64_t stride, flo
   const int64_t wgs = p.tiles * p.splits, size = X->cols * n;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   float *out = p.splits > 1 ? ws : dW;
-  hipLaunchKernelGGL((k_gradient<T, FMT>), dim3((uint32_t)wgs), dim3(kThreads), 0, s, X->codes, X->scales, X->ld,
+  auto *kernel = p.tn == 128 ? k_gradient<T, FMT, 128> : k_gradient<T, FMT, 64>;
+  hipLaunchKernelGGL(kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, s, X->codes, X->scales, X->ld,
                      X->rows, (int32_t)X->cols, static_cast<const T *>(G), stride, (int32_t)n, p.nt, p.splits,
                      p.split_rows, out, size);
   if (p.splits > 1) {
-    const int64_t join = ceil_div(size, kThreads);
-    hipLaunchKernelGGL(k_gradient_join, dim3((uint32_t)(join < 65536 ? join : 65536)), dim3(kThreads), 0, s, ws, size,
-                       p.splits, dW);
+    const int64_t join = ceil_div(size, kJoinOut);
+    hipLaunchKernelGGL(k_gradient_join, dim3((uint32_t)(join < 65536 ? join : 65536)), dim3(kJoinOut * kJoinWays), 0,
+                       s, ws, size, p.splits, dW);
   }
   return launched();
 }
