@@ -27,8 +27,8 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // N elements of T at any address that T's own alignment allows: gfx950 takes
 // wide loads and stores at element alignment.
-template <typename T, int N>
-struct __attribute__((packed, aligned(sizeof(T)))) Span {
+template <typename T, int N, int ALIGN = sizeof(T)>
+struct __attribute__((packed, aligned(ALIGN))) Span {
   T v[N];
 };
 
@@ -117,6 +117,14 @@ __device__ inline uint32_t group_max(uint32_t v) {
     v = v > o ? v : o;
   }
   return v;
+}
+
+// Workgroup b of n as a place in a list of which each of the eight XCDs takes a
+// contiguous run: workgroups go to the XCDs in turn, and neighbours in the list
+// then share an L2.
+__device__ inline uint32_t xcd_place(uint32_t b, uint32_t n) {
+  const uint32_t x = b & 7, j = b >> 3, whole = n >> 3, more = n & 7;
+  return x * whole + (x < more ? x : more) + j;
 }
 
 // ------------------------------------------------------------ host side ---

@@ -37,14 +37,17 @@ __device__ inline bf16x2 to_bf16(uint32_t w, float s, bool hi) {
               : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
 }
 
-// The leading 8 significant bits of v (the upper half of its 32), and v without
-// them, which is exact.  Cutting never overflows as rounding up could; infinities
-// and NaN go whole into the first term.
-__device__ inline uint32_t cut(float &v) {
-  const uint32_t b = __float_as_uint(v);
-  const uint32_t top = v == v ? b & 0xffff0000u : 0x7fc00000u;
-  v = (b & 0x7f800000u) == 0x7f800000u ? 0.0f : v - __uint_as_float(top);
-  return top;
+// v without its leading 8 significant bits (the upper half of its 32), which is
+// exact: the next term.  Cutting never overflows as rounding up could.
+// Infinities and NaN are whole in the first term (the quiet bit is in the upper
+// half), nothing is left of them.
+__device__ inline float rest_of(float v) {
+  const float r = v - __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+  return r == r ? r : 0.0f;
+}
+// The upper halves of a and b side by side.
+__device__ inline uint32_t upper_halves(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
 // Shared memory holds columns of kRows 16-bit values, in units of 8 rows.  The
@@ -63,40 +66,67 @@ __global__ __launch_bounds__(kThreads) void k_gradient(const uint8_t *__restrict
                                                        int32_t n, int32_t nt, int32_t splits, int64_t split_rows,
                                                        float *__restrict__ out, int64_t out_split) {
   constexpr int TERMS = terms<T>();
-  constexpr int NJ = TN / 32, GU = TN / 32;  // 16-column products per wave; row units per thread
+  constexpr int NJ = TN / 32;                              // 16-column products per wave
+  constexpr int GC = 4 / sizeof(T), GU = TN / (32 * GC);  // G: columns (one word) and units of 8 rows per thread
   __shared__ __align__(16) bf16 sx[kTileC * kRows];
   __shared__ __align__(16) bf16 sg[TERMS][TN * kRows];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g4 = lane >> 4;
-  const int32_t split = blockIdx.x % (uint32_t)splits, tile = blockIdx.x / (uint32_t)splits;
+  // a split's tiles, which read the same rows, run on one XCD
+  const uint32_t tiles = gridDim.x / (uint32_t)splits, at = xcd_place(blockIdx.x, gridDim.x);
+  const int32_t split = at / tiles, tile = at % tiles;
   const int32_t ct = tile / nt, c0 = ct * kTileC, n0 = (tile % nt) * TN;
   const int64_t r0 = (int64_t)split * split_rows;
   const int64_t r1 = r0 + split_rows < rows ? r0 + split_rows : rows;
   // wave w: columns [64 (w / 2), +64) of X, [TN / 2 (w % 2), +TN / 2) of G
   f32x4 acc[4][NJ] = {};
-  // X: 4 codes of 8 rows per thread; G: one column, GU units of 8 rows
+  // X: 4 codes (one word) of 8 rows per thread
   const int xc = (t & 31) * 4, xu = t >> 5;
-  const int gc = t % TN, gu = t / TN * GU;
+  const int gc = t % (TN / GC) * GC, gu = t / (TN / GC) * GU;
   const int32_t k16 = (cols + 15) & ~15;
-  const bool x_in = c0 + xc < k16, g_in = n0 + gc < n;
-  const uint8_t *xp = codes + c0 + xc, *sp = scales + (int64_t)ct * rows;
-  const T *gp = G + n0 + gc;
-  uint32_t xw[8], xs[8];
-  T gw[GU][8];
+  // Columns past the last read the last ones' place: their sums go nowhere.  A
+  // word that holds the last column as its first is read one column earlier and
+  // shifted when it is used.
+  const int32_t xcol = c0 + xc < k16 ? c0 + xc : k16 - 4;
+  const int32_t gcol = n0 + gc, gword = gcol + GC <= n ? gcol : n - GC;
+  const int gshift = gword < gcol ? 16 : 0;
+  const uint8_t *xp = codes + xcol + xu * 8 * ld, *sp = scales + (int64_t)ct * rows + xu * 8;
+  const T *gp = G + gword + gu * 8 * stride;
+  uint32_t xw[8], gw[GU][8], shift = 0;
+  Span<uint8_t, 8> xs;
   auto fetch = [&](int64_t r) {
+    const uint8_t *xr = xp + r * ld, *sr = sp + r;
+    const T *gr = gp + r * stride;
+    if (r + kRows <= r1 && n >= GC) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int64_t row = r + xu * 8 + u;
-      const bool in = row < r1 && x_in;
-      xw[u] = in ? *reinterpret_cast<const uint32_t *>(xp + row * ld) : 0u;
-      xs[u] = in ? sp[row] : 127u;
-    }
+      for (int u = 0; u < 8; ++u) xw[u] = *reinterpret_cast<const uint32_t *>(xr + u * ld);
+      xs = *reinterpret_cast<const Span<uint8_t, 8> *>(sr);
 #pragma unroll
-    for (int k = 0; k < GU; ++k)
+      for (int u = 0; u < GU * 8; ++u)
+        gw[u / 8][u % 8] = reinterpret_cast<const Span<uint32_t, 1, sizeof(T)> *>(gr + u * stride)->v[0];
+      shift = gshift;
+    } else {
+      const int xl = (int)(r1 - r) - xu * 8, gl = (int)(r1 - r) - gu * 8;  // rows left for this thread
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int64_t row = r + (gu + k) * 8 + u;
-        gw[k][u] = row < r1 && g_in ? gp[row * stride] : (T)0.0f;
+        xw[u] = u < xl ? *reinterpret_cast<const uint32_t *>(xr + u * ld) : 0u;
+        xs.v[u] = u < xl ? sr[u] : (uint8_t)127;
       }
+#pragma unroll
+      for (int u = 0; u < GU * 8; ++u) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int j = 0; j < GC; ++j)
+          if (u < gl && gcol + j < n) {
+            const T *p = G + gcol + j + (r + gu * 8 + u) * stride;
+            if constexpr (GC == 1)
+              w = *reinterpret_cast<const uint32_t *>(p);
+            else
+              w |= (uint32_t)*reinterpret_cast<const uint16_t *>(p) << (16 * j);
+          }
+        gw[u / 8][u % 8] = w;
+      }
+      shift = 0;
+    }
   };
   if (r0 < r1) fetch(r0);
   for (int64_t r = r0; r < r1; r += kRows) {
@@ -106,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void k_gradient(const uint8_t *__restrict
       bf16x2 lo[8], hi[8];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const float s = scale_value(xs[u]);
+        const float s = scale_value(xs.v[u]);
         lo[u] = to_bf16<FMT>(xw[u], s, false);
         hi[u] = to_bf16<FMT>(xw[u], s, true);
       }
@@ -118,26 +148,43 @@ __global__ __launch_bounds__(kThreads) void k_gradient(const uint8_t *__restrict
         *reinterpret_cast<bf16x8 *>(&sx[place(xc + j, xu)]) = o;
       }
     }
+    if constexpr (GC > 1) {
+#pragma unroll
+      for (int u = 0; u < GU * 8; ++u) gw[u / 8][u % 8] >>= shift;
+    }
 #pragma unroll
     for (int k = 0; k < GU; ++k) {
       if constexpr (TERMS == 1) {
-        bf16x8 o;
+        u32x4 even, odd;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) o[u] = gw[k][u];
-        *reinterpret_cast<bf16x8 *>(&sg[0][place(gc, gu + k)]) = o;
+        for (int u = 0; u < 8; u += 2) {
+          even[u / 2] = __builtin_amdgcn_perm(gw[k][u + 1], gw[k][u], 0x05040100u);
+          odd[u / 2] = __builtin_amdgcn_perm(gw[k][u + 1], gw[k][u], 0x07060302u);
+        }
+        *reinterpret_cast<u32x4 *>(&sg[0][place(gc, gu + k)]) = even;
+        *reinterpret_cast<u32x4 *>(&sg[0][place(gc + 1, gu + k)]) = odd;
       } else {
-        float v[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = (float)gw[k][u];
+        for (int j = 0; j < GC; ++j) {
+          float v[8];
 #pragma unroll
-        for (int q = 0; q < TERMS; ++q) {
-          u32x4 o;
-#pragma unroll
-          for (int u = 0; u < 8; u += 2) {
-            const uint32_t a = cut(v[u]), b = cut(v[u + 1]);
-            o[u / 2] = (a >> 16) | b;
+          for (int u = 0; u < 8; ++u) {
+            if constexpr (GC == 1)
+              v[u] = __builtin_canonicalizef(__uint_as_float(gw[k][u]));
+            else
+              v[u] = (float)__builtin_bit_cast(f16, (uint16_t)(gw[k][u] >> (16 * j)));
           }
-          *reinterpret_cast<u32x4 *>(&sg[q][place(gc, gu + k)]) = o;
+#pragma unroll
+          for (int q = 0; q < TERMS; ++q) {
+            u32x4 o;
+#pragma unroll
+            for (int u = 0; u < 8; u += 2) o[u / 2] = upper_halves(v[u], v[u + 1]);
+            *reinterpret_cast<u32x4 *>(&sg[q][place(gc + j, gu + k)]) = o;
+            if (q + 1 < TERMS)
+#pragma unroll
+              for (int u = 0; u < 8; ++u)
+                v[u] = q == 0 ? rest_of(v[u]) : v[u] - __uint_as_float(__float_as_uint(v[u]) & 0xffff0000u);
+          }
         }
       }
     }
