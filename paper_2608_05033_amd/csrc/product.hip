@@ -81,6 +81,25 @@ __device__ inline void load_frag(const Operand &p, int64_t row, int32_t kb, int 
   f.s = p.scales[kb * p.rows + row];
 }
 
+// Four neighbouring n of row m, with the bias, where they are inside Y.
+template <typename T>
+__device__ inline void store_tile(const f32x4 &sum, int64_t m, int64_t n, int64_t rows, int64_t cols,
+                                  const float *__restrict__ bias, T *__restrict__ Y, int64_t stride) {
+  if (m >= rows || n >= cols) return;
+  const int left = cols - n < 4 ? (int)(cols - n) : 4;
+  float out[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) out[t] = sum[t] + (bias && t < left ? bias[n + t] : 0.0f);
+  T *q = Y + m * stride + n;
+  if (left == 4)
+    store_span(q, out);
+  else
+    store_part(q, left, out);
+}
+
+// What stands in for the codes past a row's end.
+__device__ __align__(16) uint8_t kZeros[16];
+
 // MF x NF tiles of 16 x 16 per wave, operands straight from memory.  KW waves
 // share a tile, each taking every KW-th block of k, and join their sums in
 // shared memory; with KW = 1 the four waves of a workgroup take four tiles.
@@ -145,18 +164,141 @@ __global__ __launch_bounds__(KW > 4 ? KW * 64 : 256) void k_product_rows(Operand
         sum = part[0][i * NF + j][lane];
         for (int t = 1; t < KW; ++t) sum += part[t][i * NF + j][lane];
       }
-      const int64_t m = m0 + i * 16 + r, n = n0 + j * 16 + g * 4;
-      if (m >= X.rows || n >= W.rows) continue;
-      float out[4];
-      const int left = W.rows - n < 4 ? (int)(W.rows - n) : 4;
-#pragma unroll
-      for (int t = 0; t < 4; ++t) out[t] = sum[t] + (bias && t < left ? bias[n + t] : 0.0f);
-      T *q = Y + m * stride + n;
-      if (left == 4)
-        store_span(q, out);
-      else
-        store_part(q, left, out);
+      store_tile(sum, m0 + i * 16 + r, n0 + j * 16 + g * 4, X.rows, W.rows, bias, Y, stride);
     }
+}
+
+// BM x BN tiles (rows of X by rows of W), operands through shared memory: WM x WN
+// waves, each (BM / WM) x (BN / WN).  Two buffers hold a block of 128 k each; the
+// next block's codes go from memory straight to shared memory (16 bytes a lane)
+// while this block's products run.  Rows lie 128 bytes apart, their eight 16-byte
+// chunks mixed with the row so that 16 rows read at one chunk touch all banks;
+// the mixing is done on the memory side, since a wave's 64 lanes write 1 KiB in
+// order.  Scale bytes lie by lane, the tile's 16-row groups side by side, so one
+// read serves all of a lane's products.
+template <typename T, int XF, int WF, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand W, const float *__restrict__ bias,
+                                                              T *__restrict__ Y, int64_t stride, int32_t k16,
+                                                              int32_t nb, int32_t mt, int32_t nt) {
+  constexpr int THREADS = WM * WN * 64, MF = BM / WM / 16, NF = BN / WN / 16;
+  constexpr int ROWS = BM + BN, CHUNKS = ROWS * 8 / THREADS;  // 16-byte chunks per thread and block
+  static_assert(MF % 4 == 0 && NF % 4 == 0 && ROWS * 8 % THREADS == 0, "scales are read four at a time");
+  __shared__ __align__(16) uint8_t codes[2][ROWS * kBlock];
+  __shared__ __align__(16) uint8_t scales[2][16][ROWS / 16];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, g = lane >> 4;
+  const int wm = wave / WN, wn = wave % WN;
+  const uint32_t at = xcd_place(blockIdx.x, gridDim.x);
+  // tiles in bands of 8 along m: neighbours in the list share X's and W's rows
+  const uint32_t band = at / (8u * nt), left = mt - band * 8u < 8u ? mt - band * 8u : 8u;
+  const uint32_t in_band = at - band * 8u * nt;
+  const int64_t m0 = (int64_t)(band * 8u + in_band % left) * BM, n0 = (int64_t)(in_band / left) * BN;
+
+  // Chunk i of thread t: row i * THREADS / 8 + t / 8 of the tile (X's rows first),
+  // place t % 8.  Rows past the last read the last one.
+  static_assert(THREADS % 128 == 0 && BM % (THREADS / 8) == 0, "one operand and one mixing for a thread's chunks");
+  constexpr int XC = BM / (THREADS / 8);  // of them, chunks of X
+  const int chunk = ((t & 7) ^ ((t >> 4) & 7)) * 16;
+  const uint8_t *xbase = X.codes + m0 * X.ld, *wbase = W.codes + n0 * W.ld;
+  uint32_t off[CHUNKS];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int row = (i < XC ? i : i - XC) * (THREADS / 8) + t / 8;
+    const int64_t most = i < XC ? X.rows - 1 - m0 : W.rows - 1 - n0;
+    off[i] = (uint32_t)(row < most ? row : most) * (uint32_t)(i < XC ? X.ld : W.ld) + chunk;
+  }
+  const uint8_t *ssrc[(ROWS + THREADS - 1) / THREADS];
+  int64_t sstep[(ROWS + THREADS - 1) / THREADS];
+#pragma unroll
+  for (int i = 0; i * THREADS < ROWS; ++i) {
+    const int row = i * THREADS + t;
+    const Operand &p = row < BM ? X : W;
+    const int64_t want = row < BM ? m0 + row : n0 + row - BM, have = want < p.rows ? want : p.rows - 1;
+    ssrc[i] = p.scales + have;
+    sstep[i] = p.rows;
+  }
+  uint8_t sv[(ROWS + THREADS - 1) / THREADS];
+  auto fetch = [&](int32_t kb, int buf) {
+    const int32_t room = k16 - kb * kBlock;  // bytes of the rows from this block on
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const uint8_t *p = (i < XC ? xbase : wbase) + (int64_t)kb * kBlock + off[i];
+      if (chunk >= room) p = kZeros;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void *)(p),
+          (__attribute__((address_space(3))) void *)(&codes[buf][(i * THREADS + wave * 64) * 16]), 16, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i * THREADS < ROWS; ++i)
+      if (ROWS % THREADS == 0 || i * THREADS + t < ROWS) sv[i] = ssrc[i][kb * sstep[i]];
+  };
+  auto store_scales = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i * THREADS < ROWS; ++i) {
+      const int row = i * THREADS + t;
+      if (ROWS % THREADS == 0 || row < ROWS) scales[buf][row & 15][row >> 4] = sv[i];
+    }
+  };
+  auto frag = [&](int buf, int row) {
+    const uint8_t *base = &codes[buf][row * kBlock];
+    const int mix = (row >> 1) & 7;
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(base + ((2 * g) ^ mix) * 16);
+    const u32x4 b = *reinterpret_cast<const u32x4 *>(base + ((2 * g + 1) ^ mix) * 16);
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f.v[i] = (int)a[i];
+      f.v[4 + i] = (int)b[i];
+    }
+    return f;
+  };
+
+  f32x4 acc[MF][NF] = {};
+  if (nb > 0) {
+    fetch(0, 0);
+    store_scales(0);
+  }
+  for (int32_t kb = 0; kb < nb; ++kb) {
+    const int buf = kb & 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what this wave asked for is in shared memory
+    __syncthreads();                     // every wave's part of this block is there, the other buffer is free
+    if (kb + 1 < nb) fetch(kb + 1, buf ^ 1);
+    uint32_t sx[MF / 4], sw[NF / 4];
+#pragma unroll
+    for (int i = 0; i < MF / 4; ++i)
+      sx[i] = *reinterpret_cast<const uint32_t *>(&scales[buf][r][wm * MF + 4 * i]);
+#pragma unroll
+    for (int i = 0; i < NF / 4; ++i)
+      sw[i] = *reinterpret_cast<const uint32_t *>(&scales[buf][r][BM / 16 + wn * NF + 4 * i]);
+    Frag w[NF];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      w[j] = frag(buf, BM + (wn * NF + j) * 16 + r);
+      w[j].s = (sw[j / 4] >> (8 * (j % 4))) & 255;
+    }
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      Frag x = frag(buf, (wm * MF + i) * 16 + r);
+      x.s = (sx[i / 4] >> (8 * (i % 4))) & 255;
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = mfma_scaled<WF, XF>(w[j], x, acc[i][j]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bf16x8 xb = bf16_of<XF>(x, q);
+#pragma unroll
+          for (int j = 0; j < NF; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w[j], q), xb, acc[i][j], 0, 0, 0);
+        }
+      }
+    }
+    if (kb + 1 < nb) store_scales(buf ^ 1);
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+      store_tile(acc[i][j], m0 + (wm * MF + i) * 16 + r, n0 + (wn * NF + j) * 16 + g * 4, X.rows, W.rows, bias, Y, stride);
 }
 
 template <typename T, int XF, int WF, int MF, int NF, int KW>
@@ -170,13 +312,28 @@ int rows_launch(const Operand &x, const Operand &w, const float *bias, T *y, int
   return launched();
 }
 
+template <typename T, int XF, int WF, int BM, int BN, int WM, int WN>
+int tile_launch(const Operand &x, const Operand &w, const float *bias, T *y, int64_t stride, int32_t k16, int32_t nb,
+                hipStream_t s) {
+  const int64_t mt = ceil_div(x.rows, BM), nt = ceil_div(w.rows, BN);
+  if (mt * nt > INT32_MAX) return SD_ERR_OVERFLOW;
+  hipLaunchKernelGGL((k_product_tile<T, XF, WF, BM, BN, WM, WN>), dim3((uint32_t)(mt * nt)), dim3(WM * WN * 64), 0, s,
+                     x, w, bias, y, stride, k16, nb, (int32_t)mt, (int32_t)nt);
+  return launched();
+}
+
 template <typename T, int XF, int WF>
 int product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void *Y, int64_t stride, hipStream_t s) {
   const Operand x{X->codes, X->scales, X->ld, X->rows}, w{W->codes, W->scales, W->ld, W->rows};
   const int32_t k16 = (int32_t)(ceil_div(X->cols, 16) * 16), nb = (int32_t)blocks_of(X->cols);
   T *y = static_cast<T *>(Y);
+  // the tiles' row offsets are kept in 32 bits
+  const bool near = x.ld <= (1 << 23) && w.ld <= (1 << 23);
   if (x.rows <= 16) return rows_launch<T, XF, WF, 1, 1, 8>(x, w, bias, y, stride, k16, nb, s);
-  return rows_launch<T, XF, WF, 4, 4, 1>(x, w, bias, y, stride, k16, nb, s);
+  if (!near) return rows_launch<T, XF, WF, 4, 4, 1>(x, w, bias, y, stride, k16, nb, s);
+  if (ceil_div(x.rows, 256) * ceil_div(w.rows, 256) >= 128)
+    return tile_launch<T, XF, WF, 256, 256, 2, 4>(x, w, bias, y, stride, k16, nb, s);
+  return tile_launch<T, XF, WF, 128, 128, 2, 2>(x, w, bias, y, stride, k16, nb, s);
 }
 template <typename T>
 int product_as(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void *Y, int64_t stride, hipStream_t s) {
