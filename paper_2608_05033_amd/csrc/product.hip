@@ -183,8 +183,9 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   constexpr int THREADS = WM * WN * 64, MF = BM / WM / 16, NF = BN / WN / 16;
   constexpr int ROWS = BM + BN, CHUNKS = ROWS * 8 / THREADS;  // 16-byte chunks per thread and block
   static_assert(MF % 4 == 0 && NF % 4 == 0 && ROWS * 8 % THREADS == 0, "scales are read four at a time");
-  __shared__ __align__(16) uint8_t codes[2][ROWS * kBlock];
-  __shared__ __align__(16) uint8_t scales[2][16][ROWS / 16];
+  // two objects and not an array of two: reads of one then need not wait for what is on its way to the other
+  __shared__ __align__(16) uint8_t codes_a[ROWS * kBlock], codes_b[ROWS * kBlock];
+  __shared__ __align__(16) uint8_t scales_a[16][ROWS / 16], scales_b[16][ROWS / 16];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, g = lane >> 4;
   const int wm = wave / WN, wn = wave % WN;
   const uint32_t at = xcd_place(blockIdx.x, gridDim.x);
@@ -217,32 +218,32 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
     sstep[i] = p.rows;
   }
   uint8_t sv[(ROWS + THREADS - 1) / THREADS];
-  auto fetch = [&](int32_t kb, int buf) {
+  auto fetch = [&](int32_t kb, uint8_t *codes) {
     const int32_t room = k16 - kb * kBlock;  // bytes of the rows from this block on
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const uint8_t *p = (i < XC ? xbase : wbase) + (int64_t)kb * kBlock + off[i];
       if (chunk >= room) p = kZeros;
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void *)(p),
-          (__attribute__((address_space(3))) void *)(&codes[buf][(i * THREADS + wave * 64) * 16]), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p),
+                                       (__attribute__((address_space(3))) void *)(&codes[(i * THREADS + wave * 64) * 16]),
+                                       16, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i * THREADS < ROWS; ++i)
       if (ROWS % THREADS == 0 || i * THREADS + t < ROWS) sv[i] = ssrc[i][kb * sstep[i]];
   };
-  auto store_scales = [&](int buf) {
+  auto store_scales = [&](uint8_t (*scales)[ROWS / 16]) {
 #pragma unroll
     for (int i = 0; i * THREADS < ROWS; ++i) {
       const int row = i * THREADS + t;
-      if (ROWS % THREADS == 0 || row < ROWS) scales[buf][row & 15][row >> 4] = sv[i];
+      if (ROWS % THREADS == 0 || row < ROWS) scales[row & 15][row >> 4] = sv[i];
     }
   };
-  auto frag = [&](int buf, int row) {
-    const uint8_t *base = &codes[buf][row * kBlock];
+  auto frag = [&](const uint8_t *codes, int row) {
+    const uint8_t *base = &codes[row * kBlock];
     const int mix = (row >> 1) & 7;
-    const u32x4 a = *reinterpret_cast<const u32x4 *>(base + ((2 * g) ^ mix) * 16);
-    const u32x4 b = *reinterpret_cast<const u32x4 *>(base + ((2 * g + 1) ^ mix) * 16);
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(base + (g ^ mix) * 16);
+    const u32x4 b = *reinterpret_cast<const u32x4 *>(base + ((g + 4) ^ mix) * 16);
     Frag f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -253,31 +254,26 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   };
 
   f32x4 acc[MF][NF] = {};
-  if (nb > 0) {
-    fetch(0, 0);
-    store_scales(0);
-  }
-  for (int32_t kb = 0; kb < nb; ++kb) {
-    const int buf = kb & 1;
+  // One block's products from (codes, scales), the next one on its way to (codes_next, scales_next).
+  auto step = [&](int32_t kb, const uint8_t *codes, const uint8_t (*scales)[ROWS / 16], uint8_t *codes_next,
+                  uint8_t (*scales_next)[ROWS / 16]) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what this wave asked for is in shared memory
     __syncthreads();                     // every wave's part of this block is there, the other buffer is free
-    if (kb + 1 < nb) fetch(kb + 1, buf ^ 1);
+    if (kb + 1 < nb) fetch(kb + 1, codes_next);
     uint32_t sx[MF / 4], sw[NF / 4];
 #pragma unroll
-    for (int i = 0; i < MF / 4; ++i)
-      sx[i] = *reinterpret_cast<const uint32_t *>(&scales[buf][r][wm * MF + 4 * i]);
+    for (int i = 0; i < MF / 4; ++i) sx[i] = *reinterpret_cast<const uint32_t *>(&scales[r][wm * MF + 4 * i]);
 #pragma unroll
-    for (int i = 0; i < NF / 4; ++i)
-      sw[i] = *reinterpret_cast<const uint32_t *>(&scales[buf][r][BM / 16 + wn * NF + 4 * i]);
+    for (int i = 0; i < NF / 4; ++i) sw[i] = *reinterpret_cast<const uint32_t *>(&scales[r][BM / 16 + wn * NF + 4 * i]);
     Frag w[NF];
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
-      w[j] = frag(buf, BM + (wn * NF + j) * 16 + r);
+      w[j] = frag(codes, BM + (wn * NF + j) * 16 + r);
       w[j].s = (sw[j / 4] >> (8 * (j % 4))) & 255;
     }
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      Frag x = frag(buf, (wm * MF + i) * 16 + r);
+      Frag x = frag(codes, (wm * MF + i) * 16 + r);
       x.s = (sx[i / 4] >> (8 * (i % 4))) & 255;
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -292,7 +288,15 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
         }
       }
     }
-    if (kb + 1 < nb) store_scales(buf ^ 1);
+    if (kb + 1 < nb) store_scales(scales_next);
+  };
+  if (nb > 0) {
+    fetch(0, codes_a);
+    store_scales(scales_a);
+  }
+  for (int32_t kb = 0; kb < nb; kb += 2) {
+    step(kb, codes_a, scales_a, codes_b, scales_b);
+    if (kb + 1 < nb) step(kb + 1, codes_b, scales_b, codes_a, scales_a);
   }
 #pragma unroll
   for (int i = 0; i < MF; ++i)
