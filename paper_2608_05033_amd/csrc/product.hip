@@ -81,20 +81,46 @@ __device__ inline void load_frag(const Operand &p, int64_t row, int32_t kb, int 
   f.s = p.scales[kb * p.rows + row];
 }
 
-// Four neighbouring n of row m, with the bias, where they are inside Y.
-template <typename T>
-__device__ inline void store_tile(const f32x4 &sum, int64_t m, int64_t n, int64_t rows, int64_t cols,
-                                  const float *__restrict__ bias, T *__restrict__ Y, int64_t stride) {
-  if (m >= rows || n >= cols) return;
-  const int left = cols - n < 4 ? (int)(cols - n) : 4;
-  float out[4];
+// A wave's MF x NF tiles from (m0, n0) on, with the bias, as far as they are inside Y: lane (r, g) holds
+// four neighbouring n from 4 g on of row r of each.
+template <int MF, int NF, typename T>
+__device__ inline void store_tiles(const f32x4 (&acc)[MF][NF], int64_t m0, int64_t n0, int64_t rows, int64_t cols,
+                                   const float *__restrict__ bias, T *__restrict__ Y, int64_t stride) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  float b[NF][4] = {};
+  if (bias) {
 #pragma unroll
-  for (int t = 0; t < 4; ++t) out[t] = sum[t] + (bias && t < left ? bias[n + t] : 0.0f);
-  T *q = Y + m * stride + n;
-  if (left == 4)
-    store_span(q, out);
-  else
-    store_part(q, left, out);
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int64_t n = n0 + j * 16 + g * 4 + t;
+        b[j][t] = n < cols ? bias[n] : 0.0f;
+      }
+  }
+  T *y = Y + (m0 + r) * stride + n0 + g * 4;
+  if (n0 + NF * 16 <= cols) {  // the same for the wave
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      if (m0 + i * 16 + r < rows) {
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+          float out[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) out[t] = acc[i][j][t] + b[j][t];
+          store_span(y + i * 16 * stride + j * 16, out);
+        }
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (m0 + i * 16 + r < rows && n0 + j * 16 + g * 4 + t < cols)
+          y[i * 16 * stride + j * 16 + t] = (T)(acc[i][j][t] + b[j][t]);
 }
 
 // What stands in for the codes past a row's end.
@@ -154,18 +180,13 @@ __global__ __launch_bounds__(KW > 4 ? KW * 64 : 256) void k_product_rows(Operand
       for (int j = 0; j < NF; ++j) part[wave][i * NF + j][lane] = acc[i][j];
     __syncthreads();
   }
+  if constexpr (KW > 1) {
+    static_assert(MF * NF == 1, "the first wave of a tile adds its parts");
+    if (wave % KW != 0) return;
 #pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      f32x4 sum = acc[i][j];
-      if constexpr (KW > 1) {
-        if ((i * NF + j) % KW != wave) continue;
-        sum = part[0][i * NF + j][lane];
-        for (int t = 1; t < KW; ++t) sum += part[t][i * NF + j][lane];
-      }
-      store_tile(sum, m0 + i * 16 + r, n0 + j * 16 + g * 4, X.rows, W.rows, bias, Y, stride);
-    }
+    for (int t = 1; t < KW; ++t) acc[0][0] += part[wave + t][0][lane];
+  }
+  store_tiles<MF, NF>(acc, m0, n0, X.rows, W.rows, bias, Y, stride);
 }
 
 // BM x BN tiles (rows of X by rows of W), operands through shared memory: WM x WN
@@ -218,16 +239,15 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
     sstep[i] = p.rows;
   }
   uint8_t sv[(ROWS + THREADS - 1) / THREADS];
-  auto fetch = [&](int32_t kb, uint8_t *codes) {
-    const int32_t room = k16 - kb * kBlock;  // bytes of the rows from this block on
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) {
-      const uint8_t *p = (i < XC ? xbase : wbase) + (int64_t)kb * kBlock + off[i];
-      if (chunk >= room) p = kZeros;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p),
-                                       (__attribute__((address_space(3))) void *)(&codes[(i * THREADS + wave * 64) * 16]),
-                                       16, 0, 0);
-    }
+  // 16 bytes a lane of block kb; past the rows' last 16 bytes, zeros.
+  auto fetch_chunk = [&](int32_t kb, int i, uint8_t *codes) {
+    const uint8_t *p = (i < XC ? xbase : wbase) + (int64_t)kb * kBlock + off[i];
+    if (chunk >= k16 - kb * kBlock) p = kZeros;
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p),
+                                     (__attribute__((address_space(3))) void *)(&codes[(i * THREADS + wave * 64) * 16]),
+                                     16, 0, 0);
+  };
+  auto fetch_scales = [&](int32_t kb) {
 #pragma unroll
     for (int i = 0; i * THREADS < ROWS; ++i)
       if (ROWS % THREADS == 0 || i * THREADS + t < ROWS) sv[i] = ssrc[i][kb * sstep[i]];
@@ -239,11 +259,12 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
       if (ROWS % THREADS == 0 || row < ROWS) scales[row & 15][row >> 4] = sv[i];
     }
   };
-  auto frag = [&](const uint8_t *codes, int row) {
-    const uint8_t *base = &codes[row * kBlock];
-    const int mix = (row >> 1) & 7;
-    const u32x4 a = *reinterpret_cast<const u32x4 *>(base + (g ^ mix) * 16);
-    const u32x4 b = *reinterpret_cast<const u32x4 *>(base + ((g + 4) ^ mix) * 16);
+  // A lane's two chunks of its row in a group of 16 rows: places g and g + 4, mixed.
+  const int lo = r * kBlock + (g ^ ((r >> 1) & 7)) * 16;
+  const int xlo = lo + wm * MF * 16 * kBlock, wlo = lo + (BM + wn * NF * 16) * kBlock;
+  auto frag = [&](const uint8_t *codes, int at, int group) {
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(codes + at + group * 16 * kBlock);
+    const u32x4 b = *reinterpret_cast<const u32x4 *>(codes + (at ^ 64) + group * 16 * kBlock);
     Frag f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -254,12 +275,16 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   };
 
   f32x4 acc[MF][NF] = {};
-  // One block's products from (codes, scales), the next one on its way to (codes_next, scales_next).
+  // One block's products from (codes, scales).  The next one is asked for a part at a time between
+  // the products: a wave that asks for all of it at once waits until the last request is taken.
   auto step = [&](int32_t kb, const uint8_t *codes, const uint8_t (*scales)[ROWS / 16], uint8_t *codes_next,
                   uint8_t (*scales_next)[ROWS / 16]) {
+    constexpr int PARTS = CHUNKS / (MF / 2);
+    static_assert(CHUNKS % (MF / 2) == 0, "the first half of the products asks for the next block");
+    const int32_t next = kb + 1 < nb ? kb + 1 : kb;  // after the last block: that one again, for nothing
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what this wave asked for is in shared memory
     __syncthreads();                     // every wave's part of this block is there, the other buffer is free
-    if (kb + 1 < nb) fetch(kb + 1, codes_next);
+    fetch_scales(next);
     uint32_t sx[MF / 4], sw[NF / 4];
 #pragma unroll
     for (int i = 0; i < MF / 4; ++i) sx[i] = *reinterpret_cast<const uint32_t *>(&scales[r][wm * MF + 4 * i]);
@@ -268,12 +293,12 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
     Frag w[NF];
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
-      w[j] = frag(codes, BM + (wn * NF + j) * 16 + r);
+      w[j] = frag(codes, wlo, j);
       w[j].s = (sw[j / 4] >> (8 * (j % 4))) & 255;
     }
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      Frag x = frag(codes, (wm * MF + i) * 16 + r);
+      Frag x = frag(codes, xlo, i);
       x.s = (sx[i / 4] >> (8 * (i % 4))) & 255;
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -287,22 +312,26 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w[j], q), xb, acc[i][j], 0, 0, 0);
         }
       }
+      if (i < MF / 2) {
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) fetch_chunk(next, i * PARTS + q, codes_next);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (kb + 1 < nb) store_scales(scales_next);
+    store_scales(scales_next);
   };
   if (nb > 0) {
-    fetch(0, codes_a);
+    fetch_scales(0);
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) fetch_chunk(0, i, codes_a);
     store_scales(scales_a);
   }
   for (int32_t kb = 0; kb < nb; kb += 2) {
     step(kb, codes_a, scales_a, codes_b, scales_b);
     if (kb + 1 < nb) step(kb + 1, codes_b, scales_b, codes_a, scales_a);
   }
-#pragma unroll
-  for (int i = 0; i < MF; ++i)
-#pragma unroll
-    for (int j = 0; j < NF; ++j)
-      store_tile(acc[i][j], m0 + (wm * MF + i) * 16 + r, n0 + (wn * NF + j) * 16 + g * 4, X.rows, W.rows, bias, Y, stride);
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // nothing is on its way to shared memory when the workgroup ends
+  store_tiles<MF, NF>(acc, m0 + wm * MF * 16, n0 + wn * NF * 16, X.rows, W.rows, bias, Y, stride);
 }
 
 template <typename T, int XF, int WF, int MF, int NF, int KW>
