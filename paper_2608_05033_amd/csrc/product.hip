@@ -81,77 +81,106 @@ __device__ inline void load_frag(const Operand &p, int64_t row, int32_t kb, int 
   f.s = p.scales[kb * p.rows + row];
 }
 
+// Where row rho of a wave's tile j lies among its rows of W (columns of Y).  For
+// 16-bit results two tiles are woven so that a lane's four columns of each are
+// eight neighbours, written in one store of 16 bytes.
+template <typename T, int NF>
+constexpr bool kWoven = sizeof(T) == 2 && NF % 2 == 0;
+template <bool WOVEN>
+__device__ constexpr int col_of(int j, int rho) {
+  return WOVEN ? j / 2 * 32 + rho / 4 * 8 + j % 2 * 4 + rho % 4 : j * 16 + rho;
+}
+
 // A wave's MF x NF tiles from (m0, n0) on, with the bias, as far as they are inside Y: lane (r, g) holds
 // four neighbouring n from 4 g on of row r of each.
 template <int MF, int NF, typename T>
 __device__ inline void store_tiles(const f32x4 (&acc)[MF][NF], int64_t m0, int64_t n0, int64_t rows, int64_t cols,
                                    const float *__restrict__ bias, T *__restrict__ Y, int64_t stride) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  constexpr bool WOVEN = kWoven<T, NF>;
+  constexpr int RUN = WOVEN ? 8 : 4;  // neighbouring columns of a lane
   float b[NF][4] = {};
   if (bias) {
 #pragma unroll
     for (int j = 0; j < NF; ++j)
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int64_t n = n0 + j * 16 + g * 4 + t;
+        const int64_t n = n0 + col_of<WOVEN>(j, g * 4 + t);
         b[j][t] = n < cols ? bias[n] : 0.0f;
       }
   }
-  T *y = Y + (m0 + r) * stride + n0 + g * 4;
-  if (n0 + NF * 16 <= cols) {  // the same for the wave
+  T *y = Y + (m0 + r) * stride + n0;
+  if (n0 + NF * 16 <= cols) {  // the same for the wave: a row's lines are written one after the other
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
       if (m0 + i * 16 + r < rows) {
 #pragma unroll
-        for (int j = 0; j < NF; ++j) {
-          float out[4];
+        for (int j = 0; j < NF; j += RUN / 4) {
+          float out[RUN];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) out[t] = acc[i][j][t] + b[j][t];
-          store_span(y + i * 16 * stride + j * 16, out);
+          for (int t = 0; t < RUN; ++t) out[t] = acc[i][j + t / 4][t % 4] + b[j + t / 4][t % 4];
+          store_span(y + i * 16 * stride + col_of<WOVEN>(j, g * 4), out);
         }
       }
     }
     return;
   }
 #pragma unroll
-  for (int i = 0; i < MF; ++i)
+  for (int j = 0; j < NF; j += RUN / 4) {
+    if (n0 + (j + RUN / 4) * 16 <= cols) {  // the same for the wave
 #pragma unroll
-    for (int j = 0; j < NF; ++j)
+      for (int i = 0; i < MF; ++i) {
+        float out[RUN];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-        if (m0 + i * 16 + r < rows && n0 + j * 16 + g * 4 + t < cols)
-          y[i * 16 * stride + j * 16 + t] = (T)(acc[i][j][t] + b[j][t]);
+        for (int t = 0; t < RUN; ++t) out[t] = acc[i][j + t / 4][t % 4] + b[j + t / 4][t % 4];
+        if (m0 + i * 16 + r < rows) store_span(y + i * 16 * stride + col_of<WOVEN>(j, g * 4), out);
+      }
+    } else if (n0 + j * 16 < cols) {
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int t = 0; t < RUN; ++t) {
+          const int n = col_of<WOVEN>(j, g * 4) + t;
+          if (m0 + i * 16 + r < rows && n0 + n < cols)
+            y[i * 16 * stride + n] = (T)(acc[i][j + t / 4][t % 4] + b[j + t / 4][t % 4]);
+        }
+    }
+  }
 }
 
 // What stands in for the codes past a row's end.
 __device__ __align__(16) uint8_t kZeros[16];
 
-// MF x NF tiles of 16 x 16 per wave, operands straight from memory.  KW waves
-// share a tile, each taking every KW-th block of k, and join their sums in
-// shared memory; with KW = 1 the four waves of a workgroup take four tiles.
+// MF x NF tiles of 16 x 16 by one workgroup, operands straight from memory: KW
+// waves each take every KW-th block of k and join their sums in shared memory.
 template <typename T, int XF, int WF, int MF, int NF, int KW>
-__global__ __launch_bounds__(KW > 4 ? KW * 64 : 256) void k_product_rows(Operand X, Operand W,
+__global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
                                                                          const float *__restrict__ bias,
                                                                          T *__restrict__ Y, int64_t stride,
                                                                          int32_t k16, int32_t nb, int32_t nt) {
-  constexpr int WAVES = KW > 4 ? KW : 4, TILES = WAVES / KW;
-  __shared__ f32x4 part[KW > 1 ? WAVES : 1][MF * NF][64];
+  __shared__ f32x4 part[KW][MF * NF][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int64_t m0 = ((int64_t)(blockIdx.x / (uint32_t)nt) * TILES + wave / KW) * (MF * 16);
+  const int64_t m0 = (int64_t)(blockIdx.x / (uint32_t)nt) * (MF * 16);
   const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)nt) * (NF * 16);
   f32x4 acc[MF][NF] = {};
-  for (int32_t kb = wave % KW; kb < nb; kb += KW) {
-    Frag x[MF], w[NF];
+  int64_t xrow[MF], wrow[NF];  // rows past the last read the last one
 #pragma unroll
-    for (int i = 0; i < MF; ++i) {
-      const int64_t row = m0 + i * 16 + r;
-      load_frag(X, row < X.rows ? row : X.rows - 1, kb, g, k16, x[i]);
-    }
+  for (int i = 0; i < MF; ++i) {
+    const int64_t row = m0 + i * 16 + r;
+    xrow[i] = row < X.rows ? row : X.rows - 1;
+  }
 #pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      const int64_t row = n0 + j * 16 + r;
-      load_frag(W, row < W.rows ? row : W.rows - 1, kb, g, k16, w[j]);
-    }
+  for (int j = 0; j < NF; ++j) {
+    const int64_t row = n0 + col_of<kWoven<T, NF>>(j, r);
+    wrow[j] = row < W.rows ? row : W.rows - 1;
+  }
+  auto load = [&](int32_t kb, Frag (&x)[MF], Frag (&w)[NF]) {
+#pragma unroll
+    for (int i = 0; i < MF; ++i) load_frag(X, xrow[i], kb, g, k16, x[i]);
+#pragma unroll
+    for (int j = 0; j < NF; ++j) load_frag(W, wrow[j], kb, g, k16, w[j]);
+  };
+  auto multiply = [&](const Frag (&x)[MF], const Frag (&w)[NF]) {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int i = 0; i < MF; ++i)
@@ -172,21 +201,38 @@ __global__ __launch_bounds__(KW > 4 ? KW * 64 : 256) void k_product_rows(Operand
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], xb[i], acc[i][j], 0, 0, 0);
       }
     }
+  };
+  // the next block is on its way while this one's products run
+  Frag x0[MF], w0[NF], x1[MF], w1[NF];
+  int32_t kb = wave;
+  if (kb < nb) load(kb, x0, w0);
+  while (kb < nb) {
+    if (kb + KW < nb) load(kb + KW, x1, w1);
+    multiply(x0, w0);
+    kb += KW;
+    if (kb >= nb) break;
+    if (kb + KW < nb) load(kb + KW, x0, w0);
+    multiply(x1, w1);
+    kb += KW;
   }
-  if constexpr (KW > 1) {
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
+  for (int i = 0; i < MF; ++i)
 #pragma unroll
-      for (int j = 0; j < NF; ++j) part[wave][i * NF + j][lane] = acc[i][j];
-    __syncthreads();
+    for (int j = 0; j < NF; ++j) part[wave][i * NF + j][lane] = acc[i][j];
+  __syncthreads();
+  // wave i adds up and writes row group i
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    if (i != wave) continue;
+    f32x4 sum[1][NF];
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      sum[0][j] = part[0][i * NF + j][lane];
+#pragma unroll
+      for (int t = 1; t < KW; ++t) sum[0][j] += part[t][i * NF + j][lane];
+    }
+    store_tiles<1, NF>(sum, m0 + i * 16, n0, X.rows, W.rows, bias, Y, stride);
   }
-  if constexpr (KW > 1) {
-    static_assert(MF * NF == 1, "the first wave of a tile adds its parts");
-    if (wave % KW != 0) return;
-#pragma unroll
-    for (int t = 1; t < KW; ++t) acc[0][0] += part[wave + t][0][lane];
-  }
-  store_tiles<MF, NF>(acc, m0, n0, X.rows, W.rows, bias, Y, stride);
 }
 
 // BM x BN tiles (rows of X by rows of W), operands through shared memory: WM x WN
@@ -219,14 +265,17 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   // place t % 8.  Rows past the last read the last one.
   static_assert(THREADS % 128 == 0 && BM % (THREADS / 8) == 0, "one operand and one mixing for a thread's chunks");
   constexpr int XC = BM / (THREADS / 8);  // of them, chunks of X
-  const int chunk = ((t & 7) ^ ((t >> 4) & 7)) * 16;
+  constexpr bool WOVEN = kWoven<T, NF>;
+  // a row's chunks are mixed with 8 rows' worth of its place: bits 1 to 3, or for woven rows 1, 3 and 4
+  const int xchunk = ((t & 7) ^ ((t >> 4) & 7)) * 16;
+  const int wchunk = WOVEN ? ((t & 7) ^ (((t >> 4) & 1) | ((t >> 6) & 3) << 1)) * 16 : xchunk;
   const uint8_t *xbase = X.codes + m0 * X.ld, *wbase = W.codes + n0 * W.ld;
   uint32_t off[CHUNKS];
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
     const int row = (i < XC ? i : i - XC) * (THREADS / 8) + t / 8;
     const int64_t most = i < XC ? X.rows - 1 - m0 : W.rows - 1 - n0;
-    off[i] = (uint32_t)(row < most ? row : most) * (uint32_t)(i < XC ? X.ld : W.ld) + chunk;
+    off[i] = (uint32_t)(row < most ? row : most) * (uint32_t)(i < XC ? X.ld : W.ld) + (i < XC ? xchunk : wchunk);
   }
   const uint8_t *ssrc[(ROWS + THREADS - 1) / THREADS];
   int64_t sstep[(ROWS + THREADS - 1) / THREADS];
@@ -242,7 +291,7 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   // 16 bytes a lane of block kb; past the rows' last 16 bytes, zeros.
   auto fetch_chunk = [&](int32_t kb, int i, uint8_t *codes) {
     const uint8_t *p = (i < XC ? xbase : wbase) + (int64_t)kb * kBlock + off[i];
-    if (chunk >= k16 - kb * kBlock) p = kZeros;
+    if ((i < XC ? xchunk : wchunk) >= k16 - kb * kBlock) p = kZeros;
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(p),
                                      (__attribute__((address_space(3))) void *)(&codes[(i * THREADS + wave * 64) * 16]),
                                      16, 0, 0);
@@ -256,15 +305,22 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
 #pragma unroll
     for (int i = 0; i * THREADS < ROWS; ++i) {
       const int row = i * THREADS + t;
-      if (ROWS % THREADS == 0 || row < ROWS) scales[row & 15][row >> 4] = sv[i];
+      if (ROWS % THREADS == 0 || row < ROWS) {
+        const bool woven = WOVEN && row >= BM;
+        const int rho = woven ? (row >> 3 & 3) * 4 + (row & 3) : row & 15;
+        const int group = woven ? row >> 5 << 1 | (row >> 2 & 1) : row >> 4;
+        scales[rho][group] = sv[i];
+      }
     }
   };
   // A lane's two chunks of its row in a group of 16 rows: places g and g + 4, mixed.
-  const int lo = r * kBlock + (g ^ ((r >> 1) & 7)) * 16;
-  const int xlo = lo + wm * MF * 16 * kBlock, wlo = lo + (BM + wn * NF * 16) * kBlock;
-  auto frag = [&](const uint8_t *codes, int at, int group) {
-    const u32x4 a = *reinterpret_cast<const u32x4 *>(codes + at + group * 16 * kBlock);
-    const u32x4 b = *reinterpret_cast<const u32x4 *>(codes + (at ^ 64) + group * 16 * kBlock);
+  // The mixing of row r of a group of 16 is r / 2 in either order of rows.
+  const int place = (g ^ ((r >> 1) & 7)) * 16;
+  const int xlo = (wm * MF * 16 + r) * kBlock + place;
+  const int wlo = (BM + wn * NF * 16 + col_of<WOVEN>(0, r)) * kBlock + place;
+  auto frag = [&](const uint8_t *codes, int at, int row) {
+    const u32x4 a = *reinterpret_cast<const u32x4 *>(codes + at + row * kBlock);
+    const u32x4 b = *reinterpret_cast<const u32x4 *>(codes + (at ^ 64) + row * kBlock);
     Frag f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -293,12 +349,12 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
     Frag w[NF];
 #pragma unroll
     for (int j = 0; j < NF; ++j) {
-      w[j] = frag(codes, wlo, j);
+      w[j] = frag(codes, wlo, col_of<WOVEN>(j, 0));
       w[j].s = (sw[j / 4] >> (8 * (j % 4))) & 255;
     }
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
-      Frag x = frag(codes, xlo, i);
+      Frag x = frag(codes, xlo, i * 16);
       x.s = (sx[i / 4] >> (8 * (i % 4))) & 255;
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -337,10 +393,10 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
 template <typename T, int XF, int WF, int MF, int NF, int KW>
 int rows_launch(const Operand &x, const Operand &w, const float *bias, T *y, int64_t stride, int32_t k16, int32_t nb,
                 hipStream_t s) {
-  constexpr int WAVES = KW > 4 ? KW : 4, TILES = WAVES / KW;
-  const int64_t nt = ceil_div(w.rows, NF * 16), wgs = ceil_div(x.rows, MF * 16 * TILES) * nt;
+  static_assert(MF <= KW, "a wave for each row group");
+  const int64_t nt = ceil_div(w.rows, NF * 16), wgs = ceil_div(x.rows, MF * 16) * nt;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL((k_product_rows<T, XF, WF, MF, NF, KW>), dim3((uint32_t)wgs), dim3(WAVES * 64), 0, s, x, w, bias,
+  hipLaunchKernelGGL((k_product_rows<T, XF, WF, MF, NF, KW>), dim3((uint32_t)wgs), dim3(KW * 64), 0, s, x, w, bias,
                      y, stride, k16, nb, (int32_t)nt);
   return launched();
 }
@@ -360,13 +416,31 @@ int product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void 
   const Operand x{X->codes, X->scales, X->ld, X->rows}, w{W->codes, W->scales, W->ld, W->rows};
   const int32_t k16 = (int32_t)(ceil_div(X->cols, 16) * 16), nb = (int32_t)blocks_of(X->cols);
   T *y = static_cast<T *>(Y);
-  // the tiles' row offsets are kept in 32 bits
+  // The largest tile that still gives three compute units in four a workgroup: a
+  // larger tile reads less for each product, and with fewer workgroups than that
+  // the sum over k is what takes time, so more waves have to share it.  Measured
+  // in us, 16-bit results, this choice and its neighbours:
+  //   rows x columns x k   256x256  128x128  64x64  32x64  32x32  16x16
+  //   4096 x 4096 x 4096        65       81    243
+  //   2048 x 2048 x 2048        30       18     36     50
+  //   256 x 4096 x 4096         49       26     20     27     35     62
+  //   4096 x 128 x 4096         47       26     20     16     19     33
+  //   64 x 4096 x 4096          46       25     19     14     10     17
+  //   1 x 4096 x 4096                           14     11      7      5
+  // 256 x 256 only where its edges cost little against 128 x 128: 300 columns of
+  // 100000 rows (700 of k, 32-bit results) take 114 us with it and 80 us without.
+  const int64_t enough = 3 * cu_count() / 4;
+  const auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(x.rows, bm) * ceil_div(w.rows, bn); };
+  // the large tiles keep row offsets in 32 bits
   const bool near = x.ld <= (1 << 23) && w.ld <= (1 << 23);
-  if (x.rows <= 16) return rows_launch<T, XF, WF, 1, 1, 8>(x, w, bias, y, stride, k16, nb, s);
-  if (!near) return rows_launch<T, XF, WF, 4, 4, 1>(x, w, bias, y, stride, k16, nb, s);
-  if (ceil_div(x.rows, 256) * ceil_div(w.rows, 256) >= 128)
+  if (near && tiles(256, 256) >= enough && 32 * tiles(256, 256) <= 9 * tiles(128, 128))
     return tile_launch<T, XF, WF, 256, 256, 2, 4>(x, w, bias, y, stride, k16, nb, s);
-  return tile_launch<T, XF, WF, 128, 128, 2, 2>(x, w, bias, y, stride, k16, nb, s);
+  if (near && tiles(128, 128) >= enough)
+    return tile_launch<T, XF, WF, 128, 128, 2, 2>(x, w, bias, y, stride, k16, nb, s);
+  if (tiles(64, 64) >= enough) return rows_launch<T, XF, WF, 4, 4, 4>(x, w, bias, y, stride, k16, nb, s);
+  if (tiles(32, 64) >= enough) return rows_launch<T, XF, WF, 2, 4, 8>(x, w, bias, y, stride, k16, nb, s);
+  if (tiles(32, 32) >= enough) return rows_launch<T, XF, WF, 2, 2, 8>(x, w, bias, y, stride, k16, nb, s);
+  return rows_launch<T, XF, WF, 1, 1, 8>(x, w, bias, y, stride, k16, nb, s);
 }
 template <typename T>
 int product_as(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void *Y, int64_t stride, hipStream_t s) {
