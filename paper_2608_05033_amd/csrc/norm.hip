@@ -29,6 +29,10 @@ struct Shape {
   const int32_t *offsets;
   int32_t channels, groups, per_group;
   int32_t chunk_rows, chunks, tx, ty;
+  int32_t share;  // lanes that add up one group's channels
+  // A slab of tx * V channels leaves sums for the groups that it has a part of, at
+  // group + slab of a piece's slots: both only grow along the channels.
+  int32_t slots;
   float eps;
   const float *weight, *bias;
 };
@@ -112,13 +116,13 @@ __device__ inline float act_slope(float z) {
 }
 
 // ------------------------------------------------------------- forward -----
-// Per piece and channel: the sums of x and x^2, in 64 bits.  A product of two
+// Per piece and group: the sums of x and x^2, in 64 bits.  A product of two
 // 24-bit numbers is exact there, so the variance keeps 1e-8 of itself with a
 // mean 10^4 deviations away, and the two 64-bit operations per element still
 // take less time than loading it.
 template <typename X>
-__global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double *__restrict__ part) {
-  __shared__ double s_a[V][kThreads], s_b[V][kThreads];
+__global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *__restrict__ part) {
+  __shared__ double2 s_sum[kThreads][V];
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
   const int left = p.channels - c;
@@ -146,30 +150,38 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double *_
     }
     const int t = threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      s_a[i][t] = a[i];
-      s_b[i][t] = b[i];
-    }
+    for (int i = 0; i < V; ++i) s_sum[t][i] = double2{a[i], b[i]};
     __syncthreads();
     for (int h = TY / 2; h > 0; h /= 2) {
       if (ty < h) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          s_a[i][t] = a[i] += s_a[i][t + h * p.tx];
-          s_b[i][t] = b[i] += s_b[i][t + h * p.tx];
+          const double2 o = s_sum[t + h * p.tx][i];
+          s_sum[t][i] = double2{a[i] += o.x, b[i] += o.y};
         }
       }
       __syncthreads();
     }
-    if (ty == 0) {
-      double *o = part + (blockIdx.x + s) * 2 * (int64_t)p.channels + c;
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (i < left) {
-          o[i] = a[i];
-          o[p.channels + i] = b[i];
-        }
+    // s_sum[0 .. tx) holds the slab's channels in order; a few lanes per group add them up
+    double2 *out = part + (blockIdx.x + s) * p.slots;
+    const double2 *in = &s_sum[0][0];
+    const int32_t first = blockIdx.y * p.tx * V, last = p.channels - first < p.tx * V ? p.channels : first + p.tx * V;
+    const int32_t g0 = first / p.per_group, g1 = (last - 1) / p.per_group;
+    for (int32_t k = t / p.share; k <= g1 - g0; k += blockDim.x / p.share) {
+      const int32_t lo_c = (g0 + k) * p.per_group, hi_c = lo_c + p.per_group;
+      const int32_t from = lo_c > first ? lo_c : first, to = hi_c < last ? hi_c : last;
+      double sum = 0, square = 0;
+      for (int32_t q = from + t % p.share; q < to; q += p.share) {
+        sum += in[q - first].x;
+        square += in[q - first].y;
+      }
+      for (int d = 1; d < p.share; d *= 2) {
+        sum += __shfl_xor(sum, d);
+        square += __shfl_xor(square, d);
+      }
+      if (t % p.share == 0) out[g0 + k + blockIdx.y] = double2{sum, square};
     }
+    __syncthreads();
   });
 }
 
@@ -192,34 +204,36 @@ __device__ inline void write_stats(const Shape &p, double sum, double square, do
   *rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)p.eps));
 }
 
-// Of the pieces of a segment's rows [b, e), this thread's share: f(piece's chunk,
-// channel in the group).
-template <typename F>
-__device__ inline void for_items(const Shape &p, int64_t b, int64_t e, F f) {
-  if (e <= b) return;
-  int64_t c0 = b / p.chunk_rows, c1 = (e - 1) / p.chunk_rows;
-  c0 = c0 < 0 ? 0 : c0;
-  c1 = c1 >= p.chunks ? p.chunks - 1 : c1;
-  const int64_t items = (c1 - c0 + 1) * p.per_group;
-  for (int64_t i = threadIdx.x; i < items; i += blockDim.x) {
-    const int64_t k = items < (1ll << 31) ? (uint32_t)i / (uint32_t)p.per_group : i / p.per_group;
-    f(c0 + k, (int32_t)(i - k * p.per_group));
-  }
+// The chunks that hold rows [b, e).
+__device__ inline bool chunks_of(const Shape &p, int64_t b, int64_t e, int64_t *c0, int64_t *c1) {
+  if (e <= b) return false;
+  *c0 = b / p.chunk_rows;
+  *c1 = (e - 1) / p.chunk_rows;
+  *c0 = *c0 < 0 ? 0 : *c0;
+  *c1 = *c1 >= p.chunks ? p.chunks - 1 : *c1;
+  return *c0 <= *c1;
 }
 
-__global__ void k_norm_join(Shape p, const double *__restrict__ part, float *__restrict__ mean,
+__global__ void k_norm_join(Shape p, const double2 *__restrict__ part, float *__restrict__ mean,
                             float *__restrict__ rstd) {
   __shared__ double lds[16];
+  const int32_t slab = p.tx * V;
   for (int64_t at = blockIdx.x; at < p.segments * p.groups; at += gridDim.x) {
     const int64_t s = at / p.groups;
     const int32_t g = (int32_t)(at - s * p.groups);
     const int64_t b = seg_begin(p, s), e = seg_begin(p, s + 1);
-    const double *base = part + s * 2 * (int64_t)p.channels + (int64_t)g * p.per_group;
+    const int32_t k0 = g + g * p.per_group / slab, k1 = g + ((g + 1) * p.per_group - 1) / slab;
     double sum = 0, square = 0;
-    for_items(p, b, e, [&](int64_t k, int32_t i) {
-      sum += base[k * 2 * p.channels + i];
-      square += base[(k * 2 + 1) * p.channels + i];
-    });
+    int64_t c0, c1;
+    if (chunks_of(p, b, e, &c0, &c1)) {
+#pragma unroll 4
+      for (int64_t c = c0 + threadIdx.x; c <= c1; c += blockDim.x)
+        for (int32_t k = k0; k <= k1; ++k) {
+          const double2 v = part[(c + s) * p.slots + k];
+          sum += v.x;
+          square += v.y;
+        }
+    }
     sum = wg_sum(sum, lds);
     square = wg_sum(square, lds);
     if (threadIdx.x == 0) write_stats(p, sum, square, e > b ? (double)(e - b) * p.per_group : 1.0, mean + at, rstd + at);
@@ -404,21 +418,23 @@ __global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<T> d
 
 // Workgroups [0, joins): mean(dh) and mean(dh xh) per segment and group; the
 // others: dweight and dbias of kJoinCols channels over all chunks.
-constexpr int kJoinCols = 16;
+constexpr int kJoinCols = 8;
 __global__ void k_norm_join_back(Shape p, int32_t joins, const float *__restrict__ part,
                                  const float *__restrict__ total, float *__restrict__ m1, float *__restrict__ m2,
                                  float *__restrict__ dweight, float *__restrict__ dbias) {
   __shared__ double lds[16];
-  __shared__ double s_a[512], s_b[512];
+  __shared__ double s_a[1024], s_b[1024];
   if ((int32_t)blockIdx.x >= joins) {
     const int lane = threadIdx.x % kJoinCols, row = threadIdx.x / kJoinCols, step = blockDim.x / kJoinCols;
     const int32_t c = (blockIdx.x - joins) * kJoinCols + lane;
     double a = 0, b = 0;
-    if (c < p.channels)
+    if (c < p.channels) {
+#pragma unroll 8
       for (int32_t k = row; k < p.chunks; k += step) {
         a += total[(int64_t)k * 2 * p.channels + c];
         b += total[((int64_t)k * 2 + 1) * p.channels + c];
       }
+    }
     s_a[threadIdx.x] = a;
     s_b[threadIdx.x] = b;
     __syncthreads();
@@ -443,11 +459,22 @@ __global__ void k_norm_join_back(Shape p, int32_t joins, const float *__restrict
     const float *w = p.weight ? p.weight + (int64_t)g * p.per_group : nullptr;
     const double count = e > b ? (double)(e - b) * p.per_group : 1.0;
     double a = 0, q = 0;
-    for_items(p, b, e, [&](int64_t k, int32_t i) {
-      const double wi = w ? (double)w[i] : 1.0;
-      a += wi * base[k * 2 * p.channels + i];
-      q += wi * base[(k * 2 + 1) * p.channels + i];
-    });
+    int64_t c0, c1;
+    if (chunks_of(p, b, e, &c0, &c1)) {
+      // lanes over the group's channels, the rest of the workgroup over chunks
+      const int lane = threadIdx.x % p.share, row = threadIdx.x / p.share, step = blockDim.x / p.share;
+      for (int32_t i = lane; i < p.per_group; i += p.share) {
+        const double wi = w ? (double)w[i] : 1.0;
+        double ai = 0, qi = 0;
+#pragma unroll 4
+        for (int64_t k = c0 + row; k <= c1; k += step) {
+          ai += base[k * 2 * p.channels + i];
+          qi += base[(k * 2 + 1) * p.channels + i];
+        }
+        a += wi * ai;
+        q += wi * qi;
+      }
+    }
     a = wg_sum(a, lds);
     q = wg_sum(q, lds);
     if (threadIdx.x == 0) {
@@ -526,8 +553,9 @@ int check(const sd_norm_t *d) {
 int64_t lanes_of(int32_t channels) { return ceil_div(channels, 16) * (16 / V); }
 
 // Lanes over channels: a power of two, or whole blocks of 32 lanes, so that a
-// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: eight
-// workgroups per compute unit, each thread a batch of rows at least.
+// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: four
+// workgroups per compute unit, all resident at once, each thread a batch of rows
+// at least.
 Shape shape_of(const sd_norm_t *d) {
   Shape p{};
   p.rows = d->rows;
@@ -548,8 +576,11 @@ Shape shape_of(const sd_norm_t *d) {
   p.ty = 1;
   while (p.ty * 2 * tx <= kThreads) p.ty *= 2;
   const int64_t slabs = ceil_div(lanes, tx);
+  p.slots = p.groups + (int32_t)slabs - 1;
+  p.share = 1;
+  while (p.share < 64 && p.share * 4 <= p.per_group) p.share *= 2;
   const int64_t step = (int64_t)p.ty * kBatch;
-  const int64_t want = 8ll * cu_count() / slabs;
+  const int64_t want = 4ll * cu_count() / slabs;
   int64_t rows = ceil_div(d->rows, want > 0 ? want : 1);
   rows = ceil_div(rows > 0 ? rows : 1, step) * step;
   p.chunk_rows = (int32_t)(rows > kMaxRows ? kMaxRows : rows);
@@ -558,7 +589,7 @@ Shape shape_of(const sd_norm_t *d) {
 }
 uint32_t slabs_of(const Shape &p) { return (uint32_t)ceil_div(lanes_of(p.channels), p.tx); }
 size_t part_bytes(const Shape &p) { return 8 * (size_t)(p.chunks + p.segments) * (size_t)p.channels; }
-size_t stats_bytes(const Shape &p) { return 2 * part_bytes(p); }
+size_t stats_bytes(const Shape &p) { return 16 * (size_t)(p.chunks + p.segments) * (size_t)p.slots; }
 size_t total_bytes(const Shape &p) { return 8 * (size_t)p.chunks * (size_t)p.channels; }
 size_t back_bytes(const Shape &p) {
   return part_bytes(p) + total_bytes(p) + 8 * (size_t)p.segments * (size_t)p.groups;
@@ -570,7 +601,7 @@ uint32_t join_wgs(const Shape &p) {
   return (uint32_t)(n < (1 << 20) ? n : (1 << 20));
 }
 uint32_t join_threads(const Shape &p) {
-  return p.segments * (int64_t)p.groups >= 1024 || p.chunks < 8 ? 64 : 512;
+  return p.segments * (int64_t)p.groups >= 1024 || p.chunks < 8 ? 64 : 1024;
 }
 
 template <typename T, int ACT, int XF, int YF>
@@ -602,7 +633,7 @@ void apply_x(int xf, int yf, const Shape &p, Dense<T> x, const float *mean, cons
 
 template <typename T>
 int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride, void *y, int64_t y_stride,
-            const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double *part, hipStream_t s) {
+            const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double2 *part, hipStream_t s) {
   const Dense<T> in{static_cast<const T *>(x), x_stride};
   const Packs none{nullptr, nullptr, 0};
   const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
@@ -699,7 +730,7 @@ extern "C" int sd_group_norm(const sd_norm_t *d, const void *x, int64_t x_stride
   if (d->segments == 0) return SD_OK;
   if ((st = have_device()) != SD_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  double *part = static_cast<double *>(workspace);
+  double2 *part = static_cast<double2 *>(workspace);
   return d->type == SD_TYPE_F32
              ? forward<float>(p, d->activation, x, x_stride, y, y_stride, x_packed, y_packed, mean, rstd, part, s)
          : d->type == SD_TYPE_F16
