@@ -62,12 +62,6 @@ __device__ inline void store_part(T *p, int count, const float (&in)[N]) {
 // power of two that brings the largest finite magnitude to at most 1.75 * 2^8
 // (e4m3) or 1.75 * 2^15 (e5m2).  Powers of two multiply exactly, so the codes
 // follow from the values alone. ----
-// Magnitude bits of one value for the block's maximum: infinities and NaN
-// count as 0.
-__device__ inline uint32_t finite_bits(float x) {
-  const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-  return b < 0x7f800000u ? b : 0u;
-}
 template <int FMT>
 __device__ inline uint32_t scale_byte(uint32_t max_bits) {
   if (max_bits == 0) return 127;
@@ -108,15 +102,43 @@ __device__ inline void decode4(uint32_t w, float (&out)[4]) {
   out[3] = hi[1];
 }
 
-// Largest value over aligned groups of `width` lanes (a power of two up to 32).
-template <int WIDTH>
-__device__ inline uint32_t group_max(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < WIDTH; d *= 2) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
-    v = v > o ? v : o;
+// v of another lane: quad_perm and mirror forms of the data-parallel primitives.
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// Largest value over aligned groups of `width` lanes (a power of two up to 32);
+// NaN counts as nothing.  Each step takes the largest of another half that
+// already agrees within itself: pairs, quads, mirrored halves of 8 and 16, and
+// 16 lanes swapped against their neighbours.
+__device__ inline float group_max(float v, int width) {
+  if (width >= 2) v = fmaxf(v, dpp<0xb1>(v));
+  if (width >= 4) v = fmaxf(v, dpp<0x4e>(v));
+  if (width >= 8) v = fmaxf(v, dpp<0x141>(v));
+  if (width >= 16) v = fmaxf(v, dpp<0x140>(v));
+  if (width >= 32) {
+    const uint32_t b = __float_as_uint(v);
+    const u32x2 p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
   }
   return v;
+}
+// The largest finite magnitude of the first `count` of N values in each lane of
+// groups of `width` lanes, as its bits.
+template <int N>
+__device__ inline uint32_t largest_finite(const float (&v)[N], int count, int width) {
+  float most = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = fmaxf(most, i < count ? fabsf(v[i]) : 0.0f);
+  most = group_max(most, width);
+  if (__any(__float_as_uint(most) >= 0x7f800000u)) {  // an infinity somewhere in the wave: once more without them
+    most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      most = fmaxf(most, i < count && (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u ? fabsf(v[i]) : 0.0f);
+    most = group_max(most, width);
+  }
+  return __float_as_uint(most);
 }
 
 // Workgroup b of n as a place in a list of which each of the eight XCDs takes a

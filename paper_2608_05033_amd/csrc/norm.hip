@@ -21,7 +21,7 @@ using namespace dense;
 
 constexpr int kThreads = 256;
 constexpr int V = 4;         // channels per lane
-constexpr int kBatch = 8;    // rows of a lane in flight
+constexpr int kBatch = 4;    // rows of a lane in flight: eight waves per SIMD fit the registers
 
 // What every kernel needs of the call.
 struct Shape {
@@ -62,6 +62,20 @@ __device__ inline void for_pieces(const Shape &p, int64_t r0, int64_t r1, F f) {
     const int64_t lo = b > r0 ? b : r0, hi = e < r1 ? e : r1;
     if (lo < hi) f(s, lo, hi);
   }
+}
+
+// This thread's rows of [lo, hi), every ty_count-th: f(row, count) for kBatch of
+// them at a time (row, row + ty_count, ...) while all threads have that many, then
+// one by one.
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+template <typename F>
+__device__ inline void for_rows(int64_t lo, int64_t hi, int ty, int ty_count, F f) {
+  int64_t r = lo;
+  for (; r + ty_count * kBatch <= hi; r += ty_count * kBatch) f(r + ty, Count<kBatch>());
+  for (r += ty; r < hi; r += ty_count) f(r, Count<1>());
 }
 
 // ---- where x comes from: dense rows, or 8-bit codes and their scales ----
@@ -108,7 +122,7 @@ __device__ inline float act_slope(float z) {
   if constexpr (ACT == SD_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
   if constexpr (ACT == SD_ACT_SILU) {
     const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-    return s + z * s * (1.0f - s);
+    return s * (1.0f + z * (1.0f - s));
   }
   if constexpr (ACT == SD_ACT_GELU)
     return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
@@ -130,24 +144,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
   for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
     double a[V] = {}, b[V] = {};
-    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
-      float v[kBatch][V];
+    for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
+      constexpr int N = decltype(count)::value;
+      float v[N][V];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = r + (int64_t)u * TY;
-        x.load(row < hi ? row : r, c, left, v[u]);
-      }
+      for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, v[u]);
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const bool live = r + (int64_t)u * TY < hi;
+      for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const double d = live ? v[u][i] : 0.0f;
+          const double d = v[u][i];
           a[i] += d;
           b[i] = fma(d, d, b[i]);
         }
-      }
-    }
+    });
     const int t = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < V; ++i) s_sum[t][i] = double2{a[i], b[i]};
@@ -248,18 +258,8 @@ struct Packs {
 };
 template <int FMT>
 __device__ inline void store_packed(const Packs &o, int64_t rows, int64_t r, int32_t c, int32_t channels, int tx,
-                                    int width, const float (&v)[V], bool live) {
-  uint32_t most = 0;
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const uint32_t b = c + i < channels ? finite_bits(v[i]) : 0u;
-    most = most > b ? most : b;
-  }
-  for (int d = 1; d < width; d *= 2) {
-    const uint32_t a = (uint32_t)__shfl_xor((int)most, d);
-    most = most > a ? most : a;
-  }
-  if (!live) return;
+                                    int width, const float (&v)[V]) {
+  const uint32_t most = largest_finite(v, channels - c, width);
   const uint32_t s = scale_byte<FMT>(most);
   const float inv = inverse_scale(s);
   if (c < ((channels + 15) & ~15)) {
@@ -305,31 +305,29 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<T> x, co
     Coeff k;
     float rs[V];
     load_coeff(p, mean, rstd, s, c, left, k, rs);
-    for (int64_t base = lo; base < hi; base += (int64_t)TY * kBatch) {
-      float v[kBatch][V];
+    // the lanes of a row take its last rows together: they share its 8-bit scale
+    for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
+      constexpr int N = decltype(count)::value;
+      float v[N][V];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = base + ty + (int64_t)u * TY;
-        x.load(row < hi ? row : lo, c, left, v[u]);
-      }
+      for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, v[u]);
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = base + ty + (int64_t)u * TY;
-        const bool live = row < hi;
-        if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, v[u], live);
+      for (int u = 0; u < N; ++u) {
+        const int64_t at = row + u * TY;
+        if constexpr (XF != 0) store_packed<XF>(xo, p.rows, at, c, p.channels, tx, width, v[u]);
         float out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) out[i] = act<ACT>((v[u][i] - k.mean[i]) * k.scale[i] + k.shift[i]);
-        if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, out, live);
-        if (live && y) {
-          T *q = y + row * y_stride + c;
+        if constexpr (YF != 0) store_packed<YF>(yo, p.rows, at, c, p.channels, tx, width, out);
+        if (y) {
+          T *q = y + at * y_stride + c;
           if (left >= V)
             store_span(q, out);
           else
             store_part(q, left, out);
         }
       }
-    }
+    });
   });
 }
 
@@ -381,29 +379,30 @@ __global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<T> d
     float rs[V];
     load_coeff(p, mean, rstd, s, c, left, k, rs);
     float a[V] = {}, b[V] = {};
-    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
-      float xv[kBatch][V], dv[kBatch][V];
+    for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
+      constexpr int N = decltype(count)::value;
+      float xv[N][V], dv[N][V];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = r + (int64_t)u * TY;
-        x.load(row < hi ? row : r, c, left, xv[u]);
-        dy.load(row < hi ? row : r, c, left, dv[u]);
+      for (int u = 0; u < N; ++u) {
+        x.load(row + u * TY, c, left, xv[u]);
+        dy.load(row + u * TY, c, left, dv[u]);
       }
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        float sa = 0.0f, sb = 0.0f;
+        float sa = 0.0f, sb = 0.0f;  // a batch by itself: fewer additions on the way to the sum
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
+        for (int u = 0; u < N; ++u) {
           const float d = xv[u][i] - k.mean[i];
           const float dz = dv[u][i] * act_slope<ACT>(d * k.scale[i] + k.shift[i]);
-          const bool live = r + (int64_t)u * TY < hi;
-          sa += live ? dz : 0.0f;
-          sb += live ? dz * (d * rs[i]) : 0.0f;
+          sa += dz;
+          sb += dz * d;
         }
         a[i] += sa;
         b[i] += sb;
       }
-    }
+    });
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] *= rs[i];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       ta[i] += a[i];
@@ -506,17 +505,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> d
       a1[i] = m1[g] * rs[i];
       a2[i] = m2[g] * rs[i] * rs[i];
     }
-    for (int64_t r = lo + ty; r < hi; r += (int64_t)TY * kBatch) {
-      float xv[kBatch][V], dv[kBatch][V];
+    for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
+      constexpr int N = decltype(count)::value;
+      float xv[N][V], dv[N][V];
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = r + (int64_t)u * TY;
-        x.load(row < hi ? row : r, c, left, xv[u]);
-        dy.load(row < hi ? row : r, c, left, dv[u]);
+      for (int u = 0; u < N; ++u) {
+        x.load(row + u * TY, c, left, xv[u]);
+        dy.load(row + u * TY, c, left, dv[u]);
       }
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int64_t row = r + (int64_t)u * TY;
+      for (int u = 0; u < N; ++u) {
         float out[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
@@ -524,15 +522,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> d
           const float dz = dv[u][i] * act_slope<ACT>(d * k.scale[i] + k.shift[i]);
           out[i] = dz * k.scale[i] - a1[i] - d * a2[i];
         }
-        if (row < hi) {
-          T *q = dx + row * dx_stride + c;
-          if (left >= V)
-            store_span(q, out);
-          else
-            store_part(q, left, out);
-        }
+        T *q = dx + (row + u * TY) * dx_stride + c;
+        if (left >= V)
+          store_span(q, out);
+        else
+          store_part(q, left, out);
       }
-    }
+    });
   });
 }
 
@@ -553,7 +549,7 @@ int check(const sd_norm_t *d) {
 int64_t lanes_of(int32_t channels) { return ceil_div(channels, 16) * (16 / V); }
 
 // Lanes over channels: a power of two, or whole blocks of 32 lanes, so that a
-// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: four
+// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: eight
 // workgroups per compute unit, all resident at once, each thread a batch of rows
 // at least.
 Shape shape_of(const sd_norm_t *d) {

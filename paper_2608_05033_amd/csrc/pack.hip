@@ -76,13 +76,7 @@ __global__ __launch_bounds__(kThreads) void k_pack(const T *__restrict__ x, int6
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const uint32_t b = finite_bits(v[u][i]);
-      most = most > b ? most : b;
-    }
-    const uint32_t s = scale_byte<FMT>(group_max<LANES>(most));
+    const uint32_t s = scale_byte<FMT>(largest_finite(v[u], V, LANES));
     const float inv = inverse_scale(s);
     uint32_t w[V / 4];
 #pragma unroll
