@@ -11,8 +11,12 @@
 // the rows, so no two pieces share a number).  One kernel leaves sums per piece
 // and channel, one joins them per segment and group in 64 bits, one applies the
 // result, chunks in reverse so that what the first pass read last is still in
-// the Infinity Cache.  Every sum has a fixed order: results do not change from
-// run to run.  Bound by the bytes moved: x is read twice and written once.
+// the Infinity Cache.  Bound by the bytes moved: x is read twice and written once.
+//
+// Short segments take one launch instead: a team of threads holds a segment's
+// rows in registers, adds them up in shared memory and applies the result.
+//
+// Every sum has a fixed order: results do not change from run to run.
 #include "dense.h"
 
 namespace {
@@ -33,6 +37,8 @@ struct Shape {
   // A slab of tx * V channels leaves sums for the groups that it has a part of, at
   // group + slab of a piece's slots: both only grow along the channels.
   int32_t slots;
+  // Short segments: teams of tx * ty threads, wgs workgroups; 0: chunks are used.
+  int32_t wgs;
   float eps;
   const float *weight, *bias;
 };
@@ -532,6 +538,279 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> d
   });
 }
 
+
+// ------------------------------------------------------ short segments -----
+constexpr int kHeld = 8;  // rows of a lane that stay in registers
+
+// Adds a team's values, `count` per group and lane row: rows ty of items[ty][tx * V],
+// for each group, share lanes each a part; f(group, sums) in one lane per group.
+template <typename S, typename A, typename F>
+__device__ inline void team_sums(const Shape &p, const S *items, int t, F f) {
+  const int team = p.tx * p.ty, row = p.tx * V;
+  for (int32_t g = t / p.share; g < p.groups; g += team / p.share) {
+    A a = 0, b = 0;
+    for (int32_t q = t % p.share; q < p.per_group * p.ty; q += p.share) {
+      const int32_t y = q / p.per_group;
+      const S v = items[y * row + g * p.per_group + (q - y * p.per_group)];
+      a += v.x;
+      b += v.y;
+    }
+    for (int d = 1; d < p.share; d *= 2) {
+      a += __shfl_xor(a, d);
+      b += __shfl_xor(b, d);
+    }
+    if (t % p.share == 0) f(g, a, b);
+  }
+}
+
+// A team per segment.  Its first kHeld rows a lane are read once and kept; what a
+// longer segment has beyond them is read again, from L2.
+template <typename T, int ACT, int XF, int YF>
+__global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<T> x, float *__restrict__ mean,
+                                                        float *__restrict__ rstd, T *__restrict__ y, int64_t y_stride,
+                                                        Packs xo, Packs yo) {
+  __shared__ double2 s_sum[kThreads][V];
+  __shared__ float2 s_stat[kThreads * V];
+  const int team = p.tx * p.ty, which = threadIdx.x / team, teams = blockDim.x / team, t = threadIdx.x % team;
+  const int tx = t % p.tx, ty = t / p.tx, TY = p.ty;
+  const int32_t c = tx * V, left = p.channels - c, width = p.tx < kBlock / V ? p.tx : kBlock / V;
+  float2 *stat = s_stat + which * p.groups;
+  for (int64_t s0 = (int64_t)blockIdx.x * teams; s0 < p.segments; s0 += (int64_t)gridDim.x * teams) {
+    const int64_t s = s0 + which;
+    const bool here = s < p.segments;
+    int64_t lo = here ? seg_begin(p, s) : 0, hi = here ? seg_begin(p, s + 1) : 0;
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > p.rows ? p.rows : hi;
+    const int64_t mid = lo + TY * kHeld < hi ? lo + TY * kHeld : hi;
+    float v[kHeld][V];
+    double a[V] = {}, b[V] = {};
+    auto add = [&](const float (&u)[V]) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const double d = u[i];
+        a[i] += d;
+        b[i] = fma(d, d, b[i]);
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      const int64_t row = lo + ty + u * TY;
+      x.load(row < mid ? row : lo, c, row < mid ? left : 0, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) add(v[u]);
+    if (mid < hi)
+      for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
+        constexpr int N = decltype(count)::value;
+        float w[N][V];
+#pragma unroll
+        for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, w[u]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) add(w[u]);
+      });
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_sum[threadIdx.x][i] = double2{a[i], b[i]};
+    __syncthreads();
+    if (here)
+      team_sums<double2, double>(p, &s_sum[which * team][0], t, [&](int32_t g, double sum, double square) {
+        float m, r;
+        write_stats(p, sum, square, hi > lo ? (double)(hi - lo) * p.per_group : 1.0, &m, &r);
+        stat[g] = float2{m, r};
+        mean[s * p.groups + g] = m;
+        rstd[s * p.groups + g] = r;
+      });
+    __syncthreads();
+    if (lo >= hi) continue;
+    Coeff k;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float2 st = i < left ? stat[(c + i) / p.per_group] : float2{0, 0};
+      k.mean[i] = st.x;
+      k.scale[i] = st.y * (p.weight && i < left ? p.weight[c + i] : 1.0f);
+      k.shift[i] = p.bias && i < left ? p.bias[c + i] : 0.0f;
+    }
+    auto finish = [&](int64_t row, const float (&u)[V]) {
+      if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, u);
+      float out[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) out[i] = act<ACT>((u[i] - k.mean[i]) * k.scale[i] + k.shift[i]);
+      if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, out);
+      if (y) {
+        T *q = y + row * y_stride + c;
+        if (left >= V)
+          store_span(q, out);
+        else
+          store_part(q, left, out);
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+      const int64_t row = lo + ty + u * TY;
+      if (row < mid) finish(row, v[u]);
+    }
+    if (mid < hi)
+      for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
+        constexpr int N = decltype(count)::value;
+        float w[N][V];
+#pragma unroll
+        for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, w[u]);
+#pragma unroll
+        for (int u = 0; u < N; ++u) finish(row + u * TY, w[u]);
+      });
+  }
+}
+
+// The gradients the same way; a workgroup leaves its segments' sums of dz and
+// dz xh per channel in total.
+template <typename T, typename X, int ACT>
+__global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
+                                                             const float *__restrict__ rstd, T *__restrict__ dx,
+                                                             int64_t dx_stride, float *__restrict__ total) {
+  constexpr int kHeldBack = kHeld / 2;
+  __shared__ float2 s_sum[kThreads][V];
+  __shared__ float2 s_stat[kThreads * V];
+  const int team = p.tx * p.ty, which = threadIdx.x / team, teams = blockDim.x / team, t = threadIdx.x % team;
+  const int tx = t % p.tx, ty = t / p.tx, TY = p.ty;
+  const int32_t c = tx * V, left = p.channels - c;
+  float2 *stat = s_stat + which * p.groups;
+  float w[V], ta[V] = {}, tb[V] = {};
+#pragma unroll
+  for (int i = 0; i < V; ++i) w[i] = i >= left ? 0.0f : p.weight ? p.weight[c + i] : 1.0f;
+  for (int64_t s0 = (int64_t)blockIdx.x * teams; s0 < p.segments; s0 += (int64_t)gridDim.x * teams) {
+    const int64_t s = s0 + which;
+    const bool here = s < p.segments;
+    int64_t lo = here ? seg_begin(p, s) : 0, hi = here ? seg_begin(p, s + 1) : 0;
+    lo = lo < 0 ? 0 : lo;
+    hi = hi > p.rows ? p.rows : hi;
+    const int64_t mid = lo + TY * kHeldBack < hi ? lo + TY * kHeldBack : hi;
+    Coeff k;
+    float rs[V];
+    load_coeff(p, mean, rstd, here ? s : 0, c, left, k, rs);
+    float d[kHeldBack][V], dz[kHeldBack][V], a[V] = {}, b[V] = {};
+    // x - mean and dz of one row in place of x and dy
+    auto shape = [&](float (&xv)[V], float (&dv)[V]) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        xv[i] -= k.mean[i];
+        dv[i] *= act_slope<ACT>(xv[i] * k.scale[i] + k.shift[i]);
+      }
+    };
+#pragma unroll
+    for (int u = 0; u < kHeldBack; ++u) {
+      const int64_t row = lo + ty + u * TY;
+      x.load(row < mid ? row : lo, c, row < mid ? left : 0, d[u]);
+      dy.load(row < mid ? row : lo, c, row < mid ? left : 0, dz[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kHeldBack; ++u) {
+      shape(d[u], dz[u]);  // rows that are not there have dz = 0
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const bool in = lo + ty + u * TY < mid;
+        a[i] += in ? dz[u][i] : 0.0f;
+        b[i] += in ? dz[u][i] * d[u][i] : 0.0f;
+      }
+    }
+    if (mid < hi)
+      for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
+        constexpr int N = decltype(count)::value;
+        float xv[N][V], dv[N][V], sa[V] = {}, sb[V] = {};
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          x.load(row + u * TY, c, left, xv[u]);
+          dy.load(row + u * TY, c, left, dv[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          shape(xv[u], dv[u]);
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            sa[i] += dv[u][i];
+            sb[i] += dv[u][i] * xv[u][i];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          a[i] += sa[i];
+          b[i] += sb[i];
+        }
+      });
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      b[i] *= rs[i];
+      ta[i] += a[i];
+      tb[i] += b[i];
+      s_sum[threadIdx.x][i] = float2{w[i] * a[i], w[i] * b[i]};
+    }
+    __syncthreads();
+    if (here)
+      team_sums<float2, double>(p, &s_sum[which * team][0], t, [&](int32_t g, double sa, double sb) {
+        const double count = hi > lo ? (double)(hi - lo) * p.per_group : 1.0;
+        stat[g] = float2{(float)(sa / count), (float)(sb / count)};
+      });
+    __syncthreads();
+    if (lo >= hi || left <= 0) continue;
+    float a1[V], a2[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float2 st = i < left ? stat[(c + i) / p.per_group] : float2{0, 0};
+      a1[i] = st.x * rs[i];
+      a2[i] = st.y * rs[i] * rs[i];
+    }
+    auto finish = [&](int64_t row, const float (&xv)[V], const float (&dv)[V]) {
+      float out[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) out[i] = dv[i] * k.scale[i] - a1[i] - xv[i] * a2[i];
+      T *q = dx + row * dx_stride + c;
+      if (left >= V)
+        store_span(q, out);
+      else
+        store_part(q, left, out);
+    };
+#pragma unroll
+    for (int u = 0; u < kHeldBack; ++u) {
+      const int64_t row = lo + ty + u * TY;
+      if (row < mid) finish(row, d[u], dz[u]);
+    }
+    if (mid < hi)
+      for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
+        constexpr int N = decltype(count)::value;
+        float xv[N][V], dv[N][V];
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          x.load(row + u * TY, c, left, xv[u]);
+          dy.load(row + u * TY, c, left, dv[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+          shape(xv[u], dv[u]);
+          finish(row + u * TY, xv[u], dv[u]);
+        }
+      });
+  }
+  // the workgroup's sums over its lane rows
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < V; ++i) s_sum[threadIdx.x][i] = float2{ta[i], tb[i]};
+  __syncthreads();
+  for (int h = blockDim.x / p.tx / 2; h > 0; h /= 2) {
+    if ((int)threadIdx.x < h * p.tx) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float2 o = s_sum[threadIdx.x + h * p.tx][i];
+        s_sum[threadIdx.x][i].x += o.x;
+        s_sum[threadIdx.x][i].y += o.y;
+      }
+    }
+    __syncthreads();
+  }
+  for (int32_t i = threadIdx.x; i < p.channels; i += blockDim.x) {
+    const float2 o = (&s_sum[0][0])[i];
+    total[(int64_t)blockIdx.x * 2 * p.channels + i] = o.x;
+    total[((int64_t)blockIdx.x * 2 + 1) * p.channels + i] = o.y;
+  }
+}
+
 // ---------------------------------------------------------------- host -----
 int check(const sd_norm_t *d) {
   if (!d || d->rows < 0 || d->channels < 1 || d->groups < 1 || d->segments < 0 || d->longest < 0 ||
@@ -548,11 +827,20 @@ int check(const sd_norm_t *d) {
 // Lanes for a row, with the 8-bit copies' bytes up to a multiple of 16.
 int64_t lanes_of(int32_t channels) { return ceil_div(channels, 16) * (16 / V); }
 
+// Rows of the longest segment as far as the caller says; all of them else.
+int64_t longest_of(const sd_norm_t *d) {
+  if (!d->offsets) return d->segments > 0 ? d->rows / d->segments : 0;
+  return d->longest > 0 && d->longest < d->rows ? d->longest : d->rows;
+}
+
 // Lanes over channels: a power of two, or whole blocks of 32 lanes, so that a
-// row's block of 128 columns lies in aligned lanes of one wave.  Chunks: eight
-// workgroups per compute unit, all resident at once, each thread a batch of rows
-// at least.
-Shape shape_of(const sd_norm_t *d) {
+// row's block of 128 columns lies in aligned lanes of one wave.
+// Short segments, of at most kTeamBytes, go to teams: a power of two of threads,
+// with as many lane rows as a segment of the mean length keeps busy.  Else chunks:
+// four workgroups per compute unit, all resident at once, each thread a batch of
+// rows at least.
+constexpr int64_t kTeamBytes = 128 << 10;
+Shape shape_of(const sd_norm_t *d, bool back) {
   Shape p{};
   p.rows = d->rows;
   p.segments = d->segments;
@@ -568,6 +856,21 @@ Shape shape_of(const sd_norm_t *d) {
   int32_t tx = 1;
   while (tx < 32 && tx < lanes) tx *= 2;
   if (lanes > 32) tx = (int32_t)(lanes > kThreads ? kThreads : ceil_div(lanes, 32) * 32);
+  if (lanes <= kThreads && longest_of(d) * d->channels * type_bytes(d->type) <= kTeamBytes && d->segments > 0) {
+    while (tx & (tx - 1)) tx += 32;
+    const int64_t held = back ? kHeld / 2 : kHeld, mean = ceil_div(d->rows, d->segments);
+    p.tx = tx;
+    p.ty = 1;
+    while (p.ty * 2 * tx <= kThreads && p.ty * held < mean) p.ty *= 2;
+    const int32_t team = p.tx * p.ty;
+    p.share = 1;
+    while (p.share < 64 && p.share * 2 <= team && p.share * 2 * p.groups <= team) p.share *= 2;
+    // the gradients' sums over all segments are kept per workgroup
+    const int64_t wgs = ceil_div(d->segments, kThreads / team), most = back ? 4ll * cu_count() : 1 << 24;
+    p.wgs = (int32_t)(wgs < most ? wgs : most);
+    p.chunks = p.wgs;
+    return p;
+  }
   p.tx = tx;
   p.ty = 1;
   while (p.ty * 2 * tx <= kThreads) p.ty *= 2;
@@ -585,9 +888,10 @@ Shape shape_of(const sd_norm_t *d) {
 }
 uint32_t slabs_of(const Shape &p) { return (uint32_t)ceil_div(lanes_of(p.channels), p.tx); }
 size_t part_bytes(const Shape &p) { return 8 * (size_t)(p.chunks + p.segments) * (size_t)p.channels; }
-size_t stats_bytes(const Shape &p) { return 16 * (size_t)(p.chunks + p.segments) * (size_t)p.slots; }
+size_t stats_bytes(const Shape &p) { return p.wgs ? 0 : 16 * (size_t)(p.chunks + p.segments) * (size_t)p.slots; }
 size_t total_bytes(const Shape &p) { return 8 * (size_t)p.chunks * (size_t)p.channels; }
 size_t back_bytes(const Shape &p) {
+  if (p.wgs) return total_bytes(p);
   return part_bytes(p) + total_bytes(p) + 8 * (size_t)p.segments * (size_t)p.groups;
 }
 // Workgroups and threads of a joining kernel: one workgroup per segment and
@@ -597,17 +901,22 @@ uint32_t join_wgs(const Shape &p) {
   return (uint32_t)(n < (1 << 20) ? n : (1 << 20));
 }
 uint32_t join_threads(const Shape &p) {
-  return p.segments * (int64_t)p.groups >= 1024 || p.chunks < 8 ? 64 : 1024;
+  return (!p.wgs && p.segments * (int64_t)p.groups >= 1024) || p.chunks < 8 ? 64 : 1024;
 }
 
 template <typename T, int ACT, int XF, int YF>
-void apply(const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y, int64_t y_stride, Packs xo,
-           Packs yo, hipStream_t s) {
+void apply(const Shape &p, Dense<T> x, float *mean, float *rstd, void *y, int64_t y_stride, Packs xo, Packs yo,
+           hipStream_t s) {
+  if (p.wgs) {
+    hipLaunchKernelGGL((k_norm_team<T, ACT, XF, YF>), dim3(p.wgs), dim3(kThreads), 0, s, p, x, mean, rstd,
+                       static_cast<T *>(y), y_stride, xo, yo);
+    return;
+  }
   hipLaunchKernelGGL((k_norm_apply<T, ACT, XF, YF>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, x, mean,
                      rstd, static_cast<T *>(y), y_stride, xo, yo);
 }
 template <typename T, int ACT, int XF>
-void apply_y(int yf, const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y, int64_t y_stride,
+void apply_y(int yf, const Shape &p, Dense<T> x, float *mean, float *rstd, void *y, int64_t y_stride,
              Packs xo, Packs yo, hipStream_t s) {
   if (yf == SD_PACK_E4M3)
     apply<T, ACT, XF, SD_PACK_E4M3>(p, x, mean, rstd, y, y_stride, xo, yo, s);
@@ -617,7 +926,7 @@ void apply_y(int yf, const Shape &p, Dense<T> x, const float *mean, const float 
     apply<T, ACT, XF, 0>(p, x, mean, rstd, y, y_stride, xo, yo, s);
 }
 template <typename T, int ACT>
-void apply_x(int xf, int yf, const Shape &p, Dense<T> x, const float *mean, const float *rstd, void *y,
+void apply_x(int xf, int yf, const Shape &p, Dense<T> x, float *mean, float *rstd, void *y,
              int64_t y_stride, Packs xo, Packs yo, hipStream_t s) {
   if (xf == SD_PACK_E4M3)
     apply_y<T, ACT, SD_PACK_E4M3>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
@@ -635,9 +944,9 @@ int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride,
   const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
   const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
   const int xf = xp ? xp->format : 0, yf = yp ? yp->format : 0;
-  if (p.chunks > 0)
+  if (!p.wgs && p.chunks > 0)
     hipLaunchKernelGGL((k_norm_stats<Dense<T>>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
-  if (join_wgs(p) > 0)
+  if (!p.wgs && join_wgs(p) > 0)
     hipLaunchKernelGGL(k_norm_join, dim3(join_wgs(p)), dim3(join_threads(p)), 0, s, p, part, mean, rstd);
   if (p.chunks > 0) {
     if (activation == SD_ACT_RELU)
@@ -655,6 +964,14 @@ int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride,
 template <typename T, typename X, int ACT>
 int backward_as(const Shape &p, X x, Dense<T> dy, const float *mean, const float *rstd, T *dx, int64_t dx_stride,
                 float *dweight, float *dbias, float *ws, hipStream_t s) {
+  if (p.wgs) {
+    hipLaunchKernelGGL((k_norm_team_grad<T, X, ACT>), dim3(p.wgs), dim3(kThreads), 0, s, p, x, dy, mean, rstd, dx,
+                       dx_stride, ws);
+    if (dweight || dbias)
+      hipLaunchKernelGGL(k_norm_join_back, dim3((uint32_t)ceil_div(p.channels, kJoinCols)), dim3(join_threads(p)), 0, s,
+                         p, 0, nullptr, ws, nullptr, nullptr, dweight, dbias);
+    return launched();
+  }
   float *part = ws, *total = part + part_bytes(p) / 4, *m1 = total + total_bytes(p) / 4,
         *m2 = m1 + p.segments * p.groups;
   const dim3 grid(p.chunks, slabs_of(p)), threads(p.tx * p.ty);
@@ -704,9 +1021,8 @@ extern "C" int sd_group_norm_size(const sd_norm_t *d, size_t *forward, size_t *b
   const int st = check(d);
   if (st != SD_OK) return st;
   if (!forward && !backward) return SD_ERR_INVALID_VALUE;
-  const Shape p = shape_of(d);
-  if (forward) *forward = stats_bytes(p);
-  if (backward) *backward = back_bytes(p);
+  if (forward) *forward = stats_bytes(shape_of(d, false));
+  if (backward) *backward = back_bytes(shape_of(d, true));
   return SD_OK;
 }
 
@@ -720,7 +1036,7 @@ extern "C" int sd_group_norm(const sd_norm_t *d, const void *x, int64_t x_stride
   if ((st = check_copy(d, x_packed)) != SD_OK || (st = check_copy(d, y_packed)) != SD_OK) return st;
   if (!y && !y_packed && d->rows > 0) return SD_ERR_INVALID_VALUE;
   if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
-  const Shape p = shape_of(d);
+  const Shape p = shape_of(d, false);
   if (bytes < stats_bytes(p) || (stats_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
     return SD_ERR_INVALID_VALUE;
   if (d->segments == 0) return SD_OK;
@@ -746,7 +1062,7 @@ extern "C" int sd_group_norm_backward(const sd_norm_t *d, const void *dy, int64_
   if (!x_packed && (st = check_table(x, d->type, d->rows, d->channels, x_stride)) != SD_OK) return st;
   if (x && x_packed) return SD_ERR_INVALID_VALUE;
   if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
-  const Shape p = shape_of(d);
+  const Shape p = shape_of(d, true);
   if (bytes < back_bytes(p) || (back_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
     return SD_ERR_INVALID_VALUE;
   if ((st = have_device()) != SD_OK) return st;
