@@ -44,18 +44,26 @@ __device__ inline void load_part(const T *p, int count, float (&out)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) out[i] = i < count ? (float)p[i] : 0.0f;
 }
+// v rounded to T from its 32 bits.  Without the barrier the compiler may fuse the
+// operation that makes v with an f16 rounding in some places and not in others,
+// and one value would round differently from call to call.
+template <typename T>
+__device__ inline T rounded(float v) {
+  if constexpr (__is_same(T, f16)) asm("" : "+v"(v));
+  return (T)v;
+}
 template <int N, typename T>
 __device__ inline void store_span(T *p, const float (&in)[N]) {
   Span<T, N> s;
 #pragma unroll
-  for (int i = 0; i < N; ++i) s.v[i] = (T)in[i];
+  for (int i = 0; i < N; ++i) s.v[i] = rounded<T>(in[i]);
   *reinterpret_cast<Span<T, N> *>(p) = s;
 }
 template <int N, typename T>
 __device__ inline void store_part(T *p, int count, const float (&in)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    if (i < count) p[i] = (T)in[i];
+    if (i < count) p[i] = rounded<T>(in[i]);
 }
 
 // ---- 8-bit formats.  A block's scale is 2^(s - 127), s its byte: the least

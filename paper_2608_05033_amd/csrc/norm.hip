@@ -84,34 +84,78 @@ __device__ inline void for_rows(int64_t lo, int64_t hi, int ty, int ty_count, F 
   for (r += ty; r < hi; r += ty_count) f(r, Count<1>());
 }
 
-// ---- where x comes from: dense rows, or 8-bit codes and their scales ----
+// ---- where x comes from: dense rows, or 8-bit codes and their scales.  N rows
+// from r on, `step` apart, V channels from c on; all of them are there.  Where
+// channels come in whole vectors (`whole`, the same for all threads) the loads
+// stand together without conditions; a lane past the last channel reads the
+// first, for nothing. ----
 template <typename T>
 struct Dense {
-  const T *p;
+  T *p;
   int64_t stride;
-  __device__ void load(int64_t r, int32_t c, int left, float (&v)[V]) const {
-    const T *q = p + r * stride + c;
-    if (left >= V)
-      load_span(q, v);
-    else
-      load_part(q, left, v);
+  template <int N>
+  __device__ void load(int64_t r, int64_t step, int32_t c, int left, bool whole, float (&v)[N][V]) const {
+    if (whole) {
+      const T *q = p + r * stride + (left > 0 ? c : 0);
+#pragma unroll
+      for (int u = 0; u < N; ++u) load_span(q + u * step * stride, v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < N; ++u) load_part(p + (r + u * step) * stride + c, left, v[u]);
+    }
+  }
+  // Rows past `last` read that one, for nothing.
+  template <int N>
+  __device__ void load_to(int64_t last, int64_t r, int64_t step, int32_t c, int left, bool whole,
+                          float (&v)[N][V]) const {
+    if (whole) {
+      const T *q = p + (left > 0 ? c : 0);
+#pragma unroll
+      for (int u = 0; u < N; ++u) load_span(q + (r + u * step < last ? r + u * step : last) * stride, v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < N; ++u) load_part(p + (r + u * step < last ? r + u * step : last) * stride + c, left, v[u]);
+    }
+  }
+  template <int N>
+  __device__ void store(int64_t r, int64_t step, int32_t c, int left, bool whole, const float (&v)[N][V]) const {
+    T *q = p + r * stride + c;
+    if (whole) {
+      if (left > 0)
+#pragma unroll
+        for (int u = 0; u < N; ++u) store_span(q + u * step * stride, v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < N; ++u) store_part(q + u * step * stride, left, v[u]);
+    }
   }
 };
 template <int FMT>
 struct Codes {
   const uint8_t *codes, *scales;
   int64_t ld, rows;
-  __device__ void load(int64_t r, int32_t c, int left, float (&v)[V]) const {
-    if (left <= 0) {
+  template <int N>
+  __device__ void load_to(int64_t last, int64_t r, int64_t step, int32_t c, int left, bool, float (&v)[N][V]) const {
+    const int32_t at = left > 0 ? c : 0;  // codes are there up to a multiple of 16
+    const uint8_t *q = codes + at, *sq = scales + (int64_t)(at / kBlock) * rows;
+    uint32_t w[N], s[N];
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = 0.0f;
-      return;
+    for (int u = 0; u < N; ++u) {
+      const int64_t row = r + u * step < last ? r + u * step : last;
+      w[u] = *reinterpret_cast<const uint32_t *>(q + row * ld);
+      s[u] = sq[row];
     }
-    const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + r * ld + c);
-    const float s = scale_value(scales[(int64_t)(c / kBlock) * rows + r]);
-    decode4<FMT>(w, v);
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] *= s;
+    for (int u = 0; u < N; ++u) {
+      const float f = scale_value(s[u]);
+      decode4<FMT>(w[u], v[u]);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[u][i] *= f;
+    }
+  }
+  template <int N>
+  __device__ void load(int64_t r, int64_t step, int32_t c, int left, bool whole, float (&v)[N][V]) const {
+    load_to(INT64_MAX, r, step, c, left, whole, v);
   }
 };
 
@@ -146,6 +190,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
   const int left = p.channels - c;
+  const bool whole = p.channels % V == 0;
   const int64_t r0 = (int64_t)blockIdx.x * p.chunk_rows;
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
   for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
@@ -153,8 +198,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *
     for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
       constexpr int N = decltype(count)::value;
       float v[N][V];
-#pragma unroll
-      for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, v[u]);
+      x.load(row, TY, c, left, whole, v);
 #pragma unroll
       for (int u = 0; u < N; ++u)
 #pragma unroll
@@ -298,12 +342,13 @@ __device__ inline void load_coeff(const Shape &p, const float *mean, const float
 }
 
 template <typename T, int ACT, int XF, int YF>
-__global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<T> x, const float *__restrict__ mean,
-                                                         const float *__restrict__ rstd, T *__restrict__ y,
-                                                         int64_t y_stride, Packs xo, Packs yo) {
+__global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<const T> x, const float *__restrict__ mean,
+                                                         const float *__restrict__ rstd, Dense<T> y, Packs xo,
+                                                         Packs yo) {
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
   const int left = p.channels - c;
+  const bool whole = p.channels % V == 0;
   const int width = p.tx < kBlock / V ? p.tx : kBlock / V;
   const int64_t r0 = (int64_t)(p.chunks - 1 - blockIdx.x) * p.chunk_rows;
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
@@ -315,24 +360,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<T> x, co
     for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
       constexpr int N = decltype(count)::value;
       float v[N][V];
-#pragma unroll
-      for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, v[u]);
+      x.load(row, TY, c, left, whole, v);
 #pragma unroll
       for (int u = 0; u < N; ++u) {
         const int64_t at = row + u * TY;
         if constexpr (XF != 0) store_packed<XF>(xo, p.rows, at, c, p.channels, tx, width, v[u]);
-        float out[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = act<ACT>((v[u][i] - k.mean[i]) * k.scale[i] + k.shift[i]);
-        if constexpr (YF != 0) store_packed<YF>(yo, p.rows, at, c, p.channels, tx, width, out);
-        if (y) {
-          T *q = y + at * y_stride + c;
-          if (left >= V)
-            store_span(q, out);
-          else
-            store_part(q, left, out);
-        }
+        for (int i = 0; i < V; ++i) v[u][i] = act<ACT>((v[u][i] - k.mean[i]) * k.scale[i] + k.shift[i]);
+        if constexpr (YF != 0) store_packed<YF>(yo, p.rows, at, c, p.channels, tx, width, v[u]);
       }
+      if (y.p) y.store(row, TY, c, left, whole, v);
     });
   });
 }
@@ -340,13 +377,14 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(Shape p, Dense<T> x, co
 // ------------------------------------------------------------ backward -----
 // Per piece and channel, and per chunk and channel: sums of dz and dz xh.
 template <typename T, typename X, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
+__global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<const T> dy, const float *__restrict__ mean,
                                                         const float *__restrict__ rstd, float *__restrict__ part,
                                                         float *__restrict__ total) {
   __shared__ float s_a[kThreads][V], s_b[kThreads][V];
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
   const int left = p.channels - c;
+  const bool whole = p.channels % V == 0;
   const int64_t r0 = (int64_t)blockIdx.x * p.chunk_rows;
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
   float ta[V] = {}, tb[V] = {};
@@ -388,11 +426,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_sums(Shape p, X x, Dense<T> d
     for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
       constexpr int N = decltype(count)::value;
       float xv[N][V], dv[N][V];
-#pragma unroll
-      for (int u = 0; u < N; ++u) {
-        x.load(row + u * TY, c, left, xv[u]);
-        dy.load(row + u * TY, c, left, dv[u]);
-      }
+      x.load(row, TY, c, left, whole, xv);
+      dy.load(row, TY, c, left, whole, dv);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float sa = 0.0f, sb = 0.0f;  // a batch by itself: fewer additions on the way to the sum
@@ -491,13 +526,13 @@ __global__ void k_norm_join_back(Shape p, int32_t joins, const float *__restrict
 }
 
 template <typename T, typename X, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
+__global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<const T> dy, const float *__restrict__ mean,
                                                         const float *__restrict__ rstd, const float *__restrict__ m1,
-                                                        const float *__restrict__ m2, T *__restrict__ dx,
-                                                        int64_t dx_stride) {
+                                                        const float *__restrict__ m2, Dense<T> dx) {
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
   const int left = p.channels - c;
+  const bool whole = p.channels % V == 0;
   if (left <= 0) return;
   const int64_t r0 = (int64_t)(p.chunks - 1 - blockIdx.x) * p.chunk_rows;
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
@@ -514,30 +549,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<T> d
     for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
       constexpr int N = decltype(count)::value;
       float xv[N][V], dv[N][V];
+      x.load(row, TY, c, left, whole, xv);
+      dy.load(row, TY, c, left, whole, dv);
 #pragma unroll
-      for (int u = 0; u < N; ++u) {
-        x.load(row + u * TY, c, left, xv[u]);
-        dy.load(row + u * TY, c, left, dv[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < N; ++u) {
-        float out[V];
+      for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float d = xv[u][i] - k.mean[i];
           const float dz = dv[u][i] * act_slope<ACT>(d * k.scale[i] + k.shift[i]);
-          out[i] = dz * k.scale[i] - a1[i] - d * a2[i];
+          dv[u][i] = dz * k.scale[i] - a1[i] - d * a2[i];
         }
-        T *q = dx + (row + u * TY) * dx_stride + c;
-        if (left >= V)
-          store_span(q, out);
-        else
-          store_part(q, left, out);
-      }
+      dx.store(row, TY, c, left, whole, dv);
     });
   });
 }
-
 
 // ------------------------------------------------------ short segments -----
 constexpr int kHeld = 8;  // rows of a lane that stay in registers
@@ -566,14 +591,14 @@ __device__ inline void team_sums(const Shape &p, const S *items, int t, F f) {
 // A team per segment.  Its first kHeld rows a lane are read once and kept; what a
 // longer segment has beyond them is read again, from L2.
 template <typename T, int ACT, int XF, int YF>
-__global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<T> x, float *__restrict__ mean,
-                                                        float *__restrict__ rstd, T *__restrict__ y, int64_t y_stride,
-                                                        Packs xo, Packs yo) {
+__global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> x, float *__restrict__ mean,
+                                                        float *__restrict__ rstd, Dense<T> y, Packs xo, Packs yo) {
   __shared__ double2 s_sum[kThreads][V];
   __shared__ float2 s_stat[kThreads * V];
   const int team = p.tx * p.ty, which = threadIdx.x / team, teams = blockDim.x / team, t = threadIdx.x % team;
   const int tx = t % p.tx, ty = t / p.tx, TY = p.ty;
   const int32_t c = tx * V, left = p.channels - c, width = p.tx < kBlock / V ? p.tx : kBlock / V;
+  const bool whole = p.channels % V == 0;
   float2 *stat = s_stat + which * p.groups;
   for (int64_t s0 = (int64_t)blockIdx.x * teams; s0 < p.segments; s0 += (int64_t)gridDim.x * teams) {
     const int64_t s = s0 + which;
@@ -592,19 +617,15 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<T> x, flo
         b[i] = fma(d, d, b[i]);
       }
     };
+    if (p.rows > 0) x.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, v);
 #pragma unroll
-    for (int u = 0; u < kHeld; ++u) {
-      const int64_t row = lo + ty + u * TY;
-      x.load(row < mid ? row : lo, c, row < mid ? left : 0, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < kHeld; ++u) add(v[u]);
+    for (int u = 0; u < kHeld; ++u)
+      if (lo + ty + u * TY < mid) add(v[u]);
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
         constexpr int N = decltype(count)::value;
         float w[N][V];
-#pragma unroll
-        for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, w[u]);
+        x.load(row, TY, c, left, whole, w);
 #pragma unroll
         for (int u = 0; u < N; ++u) add(w[u]);
       });
@@ -629,33 +650,25 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<T> x, flo
       k.scale[i] = st.y * (p.weight && i < left ? p.weight[c + i] : 1.0f);
       k.shift[i] = p.bias && i < left ? p.bias[c + i] : 0.0f;
     }
-    auto finish = [&](int64_t row, const float (&u)[V]) {
-      if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, u);
-      float out[V];
+    auto finish = [&](int64_t row, float (&u)[1][V]) {
+      if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, u[0]);
 #pragma unroll
-      for (int i = 0; i < V; ++i) out[i] = act<ACT>((u[i] - k.mean[i]) * k.scale[i] + k.shift[i]);
-      if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, out);
-      if (y) {
-        T *q = y + row * y_stride + c;
-        if (left >= V)
-          store_span(q, out);
-        else
-          store_part(q, left, out);
-      }
+      for (int i = 0; i < V; ++i) u[0][i] = act<ACT>((u[0][i] - k.mean[i]) * k.scale[i] + k.shift[i]);
+      if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, u[0]);
+      if (y.p) y.store(row, 0, c, left, whole, u);
     };
 #pragma unroll
     for (int u = 0; u < kHeld; ++u) {
       const int64_t row = lo + ty + u * TY;
-      if (row < mid) finish(row, v[u]);
+      if (row < mid) finish(row, *reinterpret_cast<float(*)[1][V]>(&v[u]));
     }
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
         constexpr int N = decltype(count)::value;
         float w[N][V];
+        x.load(row, TY, c, left, whole, w);
 #pragma unroll
-        for (int u = 0; u < N; ++u) x.load(row + u * TY, c, left, w[u]);
-#pragma unroll
-        for (int u = 0; u < N; ++u) finish(row + u * TY, w[u]);
+        for (int u = 0; u < N; ++u) finish(row + u * TY, *reinterpret_cast<float(*)[1][V]>(&w[u]));
       });
   }
 }
@@ -663,15 +676,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<T> x, flo
 // The gradients the same way; a workgroup leaves its segments' sums of dz and
 // dz xh per channel in total.
 template <typename T, typename X, int ACT>
-__global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense<T> dy, const float *__restrict__ mean,
-                                                             const float *__restrict__ rstd, T *__restrict__ dx,
-                                                             int64_t dx_stride, float *__restrict__ total) {
+__global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense<const T> dy, const float *__restrict__ mean,
+                                                             const float *__restrict__ rstd, Dense<T> dx,
+                                                             float *__restrict__ total) {
   constexpr int kHeldBack = kHeld / 2;
   __shared__ float2 s_sum[kThreads][V];
   __shared__ float2 s_stat[kThreads * V];
   const int team = p.tx * p.ty, which = threadIdx.x / team, teams = blockDim.x / team, t = threadIdx.x % team;
   const int tx = t % p.tx, ty = t / p.tx, TY = p.ty;
   const int32_t c = tx * V, left = p.channels - c;
+  const bool whole = p.channels % V == 0;
   float2 *stat = s_stat + which * p.groups;
   float w[V], ta[V] = {}, tb[V] = {};
 #pragma unroll
@@ -695,15 +709,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
         dv[i] *= act_slope<ACT>(xv[i] * k.scale[i] + k.shift[i]);
       }
     };
-#pragma unroll
-    for (int u = 0; u < kHeldBack; ++u) {
-      const int64_t row = lo + ty + u * TY;
-      x.load(row < mid ? row : lo, c, row < mid ? left : 0, d[u]);
-      dy.load(row < mid ? row : lo, c, row < mid ? left : 0, dz[u]);
+    if (p.rows > 0) {
+      x.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, d);
+      dy.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, dz);
     }
 #pragma unroll
     for (int u = 0; u < kHeldBack; ++u) {
-      shape(d[u], dz[u]);  // rows that are not there have dz = 0
+      shape(d[u], dz[u]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const bool in = lo + ty + u * TY < mid;
@@ -715,11 +727,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
         constexpr int N = decltype(count)::value;
         float xv[N][V], dv[N][V], sa[V] = {}, sb[V] = {};
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-          x.load(row + u * TY, c, left, xv[u]);
-          dy.load(row + u * TY, c, left, dv[u]);
-        }
+        x.load(row, TY, c, left, whole, xv);
+        dy.load(row, TY, c, left, whole, dv);
 #pragma unroll
         for (int u = 0; u < N; ++u) {
           shape(xv[u], dv[u]);
@@ -758,14 +767,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       a2[i] = st.y * rs[i] * rs[i];
     }
     auto finish = [&](int64_t row, const float (&xv)[V], const float (&dv)[V]) {
-      float out[V];
+      float out[1][V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) out[i] = dv[i] * k.scale[i] - a1[i] - xv[i] * a2[i];
-      T *q = dx + row * dx_stride + c;
-      if (left >= V)
-        store_span(q, out);
-      else
-        store_part(q, left, out);
+      for (int i = 0; i < V; ++i) out[0][i] = dv[i] * k.scale[i] - a1[i] - xv[i] * a2[i];
+      dx.store(row, 0, c, left, whole, out);
     };
 #pragma unroll
     for (int u = 0; u < kHeldBack; ++u) {
@@ -776,11 +781,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
         constexpr int N = decltype(count)::value;
         float xv[N][V], dv[N][V];
-#pragma unroll
-        for (int u = 0; u < N; ++u) {
-          x.load(row + u * TY, c, left, xv[u]);
-          dy.load(row + u * TY, c, left, dv[u]);
-        }
+        x.load(row, TY, c, left, whole, xv);
+        dy.load(row, TY, c, left, whole, dv);
 #pragma unroll
         for (int u = 0; u < N; ++u) {
           shape(xv[u], dv[u]);
@@ -905,68 +907,68 @@ uint32_t join_threads(const Shape &p) {
 }
 
 template <typename T, int ACT, int XF, int YF>
-void apply(const Shape &p, Dense<T> x, float *mean, float *rstd, void *y, int64_t y_stride, Packs xo, Packs yo,
-           hipStream_t s) {
+void apply(const Shape &p, Dense<const T> x, float *mean, float *rstd, Dense<T> y, Packs xo, Packs yo, hipStream_t s) {
   if (p.wgs) {
-    hipLaunchKernelGGL((k_norm_team<T, ACT, XF, YF>), dim3(p.wgs), dim3(kThreads), 0, s, p, x, mean, rstd,
-                       static_cast<T *>(y), y_stride, xo, yo);
+    hipLaunchKernelGGL((k_norm_team<T, ACT, XF, YF>), dim3(p.wgs), dim3(kThreads), 0, s, p, x, mean, rstd, y,
+                       xo, yo);
     return;
   }
   hipLaunchKernelGGL((k_norm_apply<T, ACT, XF, YF>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, x, mean,
-                     rstd, static_cast<T *>(y), y_stride, xo, yo);
+                     rstd, y, xo, yo);
 }
 template <typename T, int ACT, int XF>
-void apply_y(int yf, const Shape &p, Dense<T> x, float *mean, float *rstd, void *y, int64_t y_stride,
-             Packs xo, Packs yo, hipStream_t s) {
+void apply_y(int yf, const Shape &p, Dense<const T> x, float *mean, float *rstd, Dense<T> y, Packs xo, Packs yo,
+             hipStream_t s) {
   if (yf == SD_PACK_E4M3)
-    apply<T, ACT, XF, SD_PACK_E4M3>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply<T, ACT, XF, SD_PACK_E4M3>(p, x, mean, rstd, y, xo, yo, s);
   else if (yf == SD_PACK_E5M2)
-    apply<T, ACT, XF, SD_PACK_E5M2>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply<T, ACT, XF, SD_PACK_E5M2>(p, x, mean, rstd, y, xo, yo, s);
   else
-    apply<T, ACT, XF, 0>(p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply<T, ACT, XF, 0>(p, x, mean, rstd, y, xo, yo, s);
 }
 template <typename T, int ACT>
-void apply_x(int xf, int yf, const Shape &p, Dense<T> x, float *mean, float *rstd, void *y,
-             int64_t y_stride, Packs xo, Packs yo, hipStream_t s) {
+void apply_x(int xf, int yf, const Shape &p, Dense<const T> x, float *mean, float *rstd, Dense<T> y, Packs xo,
+             Packs yo, hipStream_t s) {
   if (xf == SD_PACK_E4M3)
-    apply_y<T, ACT, SD_PACK_E4M3>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply_y<T, ACT, SD_PACK_E4M3>(yf, p, x, mean, rstd, y, xo, yo, s);
   else if (xf == SD_PACK_E5M2)
-    apply_y<T, ACT, SD_PACK_E5M2>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply_y<T, ACT, SD_PACK_E5M2>(yf, p, x, mean, rstd, y, xo, yo, s);
   else
-    apply_y<T, ACT, 0>(yf, p, x, mean, rstd, y, y_stride, xo, yo, s);
+    apply_y<T, ACT, 0>(yf, p, x, mean, rstd, y, xo, yo, s);
 }
 
 template <typename T>
 int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride, void *y, int64_t y_stride,
             const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double2 *part, hipStream_t s) {
-  const Dense<T> in{static_cast<const T *>(x), x_stride};
+  const Dense<const T> in{static_cast<const T *>(x), x_stride};
+  const Dense<T> out{static_cast<T *>(y), y_stride};
   const Packs none{nullptr, nullptr, 0};
   const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
   const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
   const int xf = xp ? xp->format : 0, yf = yp ? yp->format : 0;
   if (!p.wgs && p.chunks > 0)
-    hipLaunchKernelGGL((k_norm_stats<Dense<T>>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
+    hipLaunchKernelGGL((k_norm_stats<Dense<const T>>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
   if (!p.wgs && join_wgs(p) > 0)
     hipLaunchKernelGGL(k_norm_join, dim3(join_wgs(p)), dim3(join_threads(p)), 0, s, p, part, mean, rstd);
   if (p.chunks > 0) {
     if (activation == SD_ACT_RELU)
-      apply_x<T, SD_ACT_RELU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+      apply_x<T, SD_ACT_RELU>(xf, yf, p, in, mean, rstd, out, xo, yo, s);
     else if (activation == SD_ACT_SILU)
-      apply_x<T, SD_ACT_SILU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+      apply_x<T, SD_ACT_SILU>(xf, yf, p, in, mean, rstd, out, xo, yo, s);
     else if (activation == SD_ACT_GELU)
-      apply_x<T, SD_ACT_GELU>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+      apply_x<T, SD_ACT_GELU>(xf, yf, p, in, mean, rstd, out, xo, yo, s);
     else
-      apply_x<T, SD_ACT_NONE>(xf, yf, p, in, mean, rstd, y, y_stride, xo, yo, s);
+      apply_x<T, SD_ACT_NONE>(xf, yf, p, in, mean, rstd, out, xo, yo, s);
   }
   return launched();
 }
 
 template <typename T, typename X, int ACT>
-int backward_as(const Shape &p, X x, Dense<T> dy, const float *mean, const float *rstd, T *dx, int64_t dx_stride,
+int backward_as(const Shape &p, X x, Dense<const T> dy, const float *mean, const float *rstd, Dense<T> dx,
                 float *dweight, float *dbias, float *ws, hipStream_t s) {
   if (p.wgs) {
     hipLaunchKernelGGL((k_norm_team_grad<T, X, ACT>), dim3(p.wgs), dim3(kThreads), 0, s, p, x, dy, mean, rstd, dx,
-                       dx_stride, ws);
+                       ws);
     if (dweight || dbias)
       hipLaunchKernelGGL(k_norm_join_back, dim3((uint32_t)ceil_div(p.channels, kJoinCols)), dim3(join_threads(p)), 0, s,
                          p, 0, nullptr, ws, nullptr, nullptr, dweight, dbias);
@@ -980,32 +982,32 @@ int backward_as(const Shape &p, X x, Dense<T> dy, const float *mean, const float
   hipLaunchKernelGGL(k_norm_join_back, dim3(join_wgs(p) + (uint32_t)ceil_div(p.channels, kJoinCols)),
                      dim3(join_threads(p)), 0, s, p, (int32_t)join_wgs(p), part, total, m1, m2, dweight, dbias);
   if (p.chunks > 0)
-    hipLaunchKernelGGL((k_norm_grad<T, X, ACT>), grid, threads, 0, s, p, x, dy, mean, rstd, m1, m2, dx, dx_stride);
+    hipLaunchKernelGGL((k_norm_grad<T, X, ACT>), grid, threads, 0, s, p, x, dy, mean, rstd, m1, m2, dx);
   return launched();
 }
 template <typename T, typename X>
-int backward_act(int32_t activation, const Shape &p, X x, Dense<T> dy, const float *mean, const float *rstd, T *dx,
-                 int64_t dx_stride, float *dweight, float *dbias, float *ws, hipStream_t s) {
+int backward_act(int32_t activation, const Shape &p, X x, Dense<const T> dy, const float *mean, const float *rstd,
+                 Dense<T> dx, float *dweight, float *dbias, float *ws, hipStream_t s) {
   if (activation == SD_ACT_RELU)
-    return backward_as<T, X, SD_ACT_RELU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+    return backward_as<T, X, SD_ACT_RELU>(p, x, dy, mean, rstd, dx, dweight, dbias, ws, s);
   if (activation == SD_ACT_SILU)
-    return backward_as<T, X, SD_ACT_SILU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+    return backward_as<T, X, SD_ACT_SILU>(p, x, dy, mean, rstd, dx, dweight, dbias, ws, s);
   if (activation == SD_ACT_GELU)
-    return backward_as<T, X, SD_ACT_GELU>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
-  return backward_as<T, X, SD_ACT_NONE>(p, x, dy, mean, rstd, dx, dx_stride, dweight, dbias, ws, s);
+    return backward_as<T, X, SD_ACT_GELU>(p, x, dy, mean, rstd, dx, dweight, dbias, ws, s);
+  return backward_as<T, X, SD_ACT_NONE>(p, x, dy, mean, rstd, dx, dweight, dbias, ws, s);
 }
 template <typename T>
 int backward(int32_t activation, const Shape &p, const void *x, int64_t x_stride, const sd_packed_t *xp,
              const void *dy, int64_t dy_stride, const float *mean, const float *rstd, void *dx, int64_t dx_stride,
              float *dweight, float *dbias, float *ws, hipStream_t s) {
-  const Dense<T> in{static_cast<const T *>(x), x_stride}, g{static_cast<const T *>(dy), dy_stride};
-  T *out = static_cast<T *>(dx);
-  if (!xp) return backward_act<T>(activation, p, in, g, mean, rstd, out, dx_stride, dweight, dbias, ws, s);
+  const Dense<const T> in{static_cast<const T *>(x), x_stride}, g{static_cast<const T *>(dy), dy_stride};
+  const Dense<T> out{static_cast<T *>(dx), dx_stride};
+  if (!xp) return backward_act<T>(activation, p, in, g, mean, rstd, out, dweight, dbias, ws, s);
   if (xp->format == SD_PACK_E4M3)
     return backward_act<T>(activation, p, Codes<SD_PACK_E4M3>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,
-                           out, dx_stride, dweight, dbias, ws, s);
+                           out, dweight, dbias, ws, s);
   return backward_act<T>(activation, p, Codes<SD_PACK_E5M2>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,
-                         out, dx_stride, dweight, dbias, ws, s);
+                         out, dweight, dbias, ws, s);
 }
 
 int check_copy(const sd_norm_t *d, const sd_packed_t *p) {

@@ -142,7 +142,7 @@ __device__ inline void store_tiles(const f32x4 (&acc)[MF][NF], int64_t m0, int64
         for (int t = 0; t < RUN; ++t) {
           const int n = col_of<WOVEN>(j, g * 4) + t;
           if (m0 + i * 16 + r < rows && n0 + n < cols)
-            y[i * 16 * stride + n] = (T)(acc[i][j + t / 4][t % 4] + b[j + t / 4][t % 4]);
+            y[i * 16 * stride + n] = rounded<T>(acc[i][j + t / 4][t % 4] + b[j + t / 4][t % 4]);
         }
     }
   }
