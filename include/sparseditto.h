@@ -487,7 +487,7 @@ void sd_release_memory(void);
  * a time on a stream and needs no initial value.
  * Errors of them all: SD_ERR_INVALID_VALUE (null or misaligned pointers,
  * sizes or strides that do not fit together, unknown types or formats, a
- * workspace too small), SD_ERR_OVERFLOW (2^31 rows or columns or more),
+ * workspace too small), SD_ERR_OVERFLOW (2^31 rows, columns or a stride of that or more),
  * SD_ERR_NO_DEVICE, SD_ERR_HIP. */
 typedef enum { SD_TYPE_F32 = 1, SD_TYPE_F16 = 2, SD_TYPE_BF16 = 3 } sd_type_t;
 

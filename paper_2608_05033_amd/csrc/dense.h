@@ -179,7 +179,7 @@ inline int check_table(const void *p, int32_t type, int64_t rows, int64_t cols, 
   if (!type_ok(type)) return SD_ERR_INVALID_VALUE;
   if (rows == 0 || cols == 0) return SD_OK;
   if (!p || !aligned_to(p, type_bytes(type)) || (rows > 1 && stride < cols)) return SD_ERR_INVALID_VALUE;
-  if (stride > (1ll << 40)) return SD_ERR_OVERFLOW;
+  if (stride > INT32_MAX) return SD_ERR_OVERFLOW;
   return SD_OK;
 }
 // SD_ERR_NO_DEVICE without a GPU, SD_OK else.

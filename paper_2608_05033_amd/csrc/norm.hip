@@ -92,34 +92,35 @@ __device__ inline void for_rows(int64_t lo, int64_t hi, int ty, int ty_count, F 
 template <typename T>
 struct Dense {
   T *p;
-  int64_t stride;
+  uint32_t stride;  // below 2^31, as rows are: one 32-bit product a row
+  __device__ T *at(int64_t r) const { return p + (uint64_t)(uint32_t)r * stride; }
   template <int N>
   __device__ void load(int64_t r, int64_t step, int32_t c, int left, bool whole, float (&v)[N][V]) const {
     if (whole) {
-      const T *q = p + r * stride + (left > 0 ? c : 0);
+      const T *q = at(r) + (left > 0 ? c : 0);
 #pragma unroll
       for (int u = 0; u < N; ++u) load_span(q + u * step * stride, v[u]);
     } else {
 #pragma unroll
-      for (int u = 0; u < N; ++u) load_part(p + (r + u * step) * stride + c, left, v[u]);
+      for (int u = 0; u < N; ++u) load_part(at(r + u * step) + c, left, v[u]);
     }
   }
-  // Rows past `last` read that one, for nothing.
+  // Rows past `last` read one before, for nothing.
   template <int N>
   __device__ void load_to(int64_t last, int64_t r, int64_t step, int32_t c, int left, bool whole,
                           float (&v)[N][V]) const {
     if (whole) {
-      const T *q = p + (left > 0 ? c : 0);
+      const T *q = at(r < last ? r : last) + (left > 0 ? c : 0);
 #pragma unroll
-      for (int u = 0; u < N; ++u) load_span(q + (r + u * step < last ? r + u * step : last) * stride, v[u]);
+      for (int u = 0; u < N; ++u) load_span(r + u * step <= last ? q + u * step * stride : q, v[u]);
     } else {
 #pragma unroll
-      for (int u = 0; u < N; ++u) load_part(p + (r + u * step < last ? r + u * step : last) * stride + c, left, v[u]);
+      for (int u = 0; u < N; ++u) load_part(at(r + u * step < last ? r + u * step : last) + c, left, v[u]);
     }
   }
   template <int N>
   __device__ void store(int64_t r, int64_t step, int32_t c, int left, bool whole, const float (&v)[N][V]) const {
-    T *q = p + r * stride + c;
+    T *q = at(r) + c;
     if (whole) {
       if (left > 0)
 #pragma unroll
@@ -160,22 +161,37 @@ struct Codes {
 };
 
 // ---- activations; NaN stays NaN ----
+__device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// The normal distribution's tail beyond |z|, 0.5 erfc(|z| / sqrt 2), from its
+// density e = exp(-z^2 / 2): Abramowitz and Stegun, Handbook of Mathematical
+// Functions, 7.1.26, absolute error 1.5e-7 in erf.  A quarter of the operations
+// of the library's erf, whose two ranges both run in a wave.
+__device__ inline float normal_tail(float z, float e) {
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.70710678f * fabsf(z));
+  const float q = 0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)));
+  return 0.5f * t * q * e;
+}
 template <int ACT>
 __device__ inline float act(float z) {
   if constexpr (ACT == SD_ACT_RELU) return z < 0.0f ? 0.0f : z;
-  if constexpr (ACT == SD_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
-  if constexpr (ACT == SD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  if constexpr (ACT == SD_ACT_SILU) return z * sigmoid(z);
+  if constexpr (ACT == SD_ACT_GELU) {
+    const float tail = normal_tail(z, __expf(-0.5f * z * z));
+    return z * (z < 0.0f ? tail : 1.0f - tail);
+  }
   return z;
 }
 template <int ACT>
 __device__ inline float act_slope(float z) {
   if constexpr (ACT == SD_ACT_RELU) return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
   if constexpr (ACT == SD_ACT_SILU) {
-    const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+    const float s = sigmoid(z);
     return s * (1.0f + z * (1.0f - s));
   }
-  if constexpr (ACT == SD_ACT_GELU)
-    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+  if constexpr (ACT == SD_ACT_GELU) {
+    const float e = __expf(-0.5f * z * z), tail = normal_tail(z, e);
+    return (z < 0.0f ? tail : 1.0f - tail) + z * e * 0.39894228f;
+  }
   return 1.0f;
 }
 
@@ -940,8 +956,8 @@ void apply_x(int xf, int yf, const Shape &p, Dense<const T> x, float *mean, floa
 template <typename T>
 int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride, void *y, int64_t y_stride,
             const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double2 *part, hipStream_t s) {
-  const Dense<const T> in{static_cast<const T *>(x), x_stride};
-  const Dense<T> out{static_cast<T *>(y), y_stride};
+  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride};
+  const Dense<T> out{static_cast<T *>(y), (uint32_t)y_stride};
   const Packs none{nullptr, nullptr, 0};
   const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
   const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
@@ -1000,8 +1016,8 @@ template <typename T>
 int backward(int32_t activation, const Shape &p, const void *x, int64_t x_stride, const sd_packed_t *xp,
              const void *dy, int64_t dy_stride, const float *mean, const float *rstd, void *dx, int64_t dx_stride,
              float *dweight, float *dbias, float *ws, hipStream_t s) {
-  const Dense<const T> in{static_cast<const T *>(x), x_stride}, g{static_cast<const T *>(dy), dy_stride};
-  const Dense<T> out{static_cast<T *>(dx), dx_stride};
+  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride}, g{static_cast<const T *>(dy), (uint32_t)dy_stride};
+  const Dense<T> out{static_cast<T *>(dx), (uint32_t)dx_stride};
   if (!xp) return backward_act<T>(activation, p, in, g, mean, rstd, out, dweight, dbias, ws, s);
   if (xp->format == SD_PACK_E4M3)
     return backward_act<T>(activation, p, Codes<SD_PACK_E4M3>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,
