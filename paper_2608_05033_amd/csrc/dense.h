@@ -182,13 +182,16 @@ inline int check_table(const void *p, int32_t type, int64_t rows, int64_t cols, 
   if (stride > INT32_MAX) return SD_ERR_OVERFLOW;
   return SD_OK;
 }
-// SD_ERR_NO_DEVICE without a GPU, SD_OK else.
+// SD_ERR_NO_DEVICE without a GPU, SD_OK else.  Asked until there is one.
 inline int have_device() {
+  static bool found = false;
+  if (__atomic_load_n(&found, __ATOMIC_RELAXED)) return SD_OK;
   int count = 0;
   if (hipGetDeviceCount(&count) != hipSuccess || count <= 0) {
     (void)hipGetLastError();
     return SD_ERR_NO_DEVICE;
   }
+  __atomic_store_n(&found, true, __ATOMIC_RELAXED);
   return SD_OK;
 }
 inline int launched() {

@@ -13,14 +13,21 @@ functions of a whole layer from these calls.
 """
 from __future__ import annotations
 
+import ctypes
+import functools
+
 import torch
 
-from . import (ACTIVATIONS, PACK_FORMATS, SD_TYPE_BF16, SD_TYPE_F16, SD_TYPE_F32, sd_group_norm,
-               sd_group_norm_backward, sd_group_norm_size, sd_norm_t, sd_pack, sd_pack_gradient,
-               sd_pack_gradient_size, sd_pack_product, sd_packed_t, sd_unpack)
+from . import (ACTIVATIONS, PACK_FORMATS, SD_TYPE_BF16, SD_TYPE_F16, SD_TYPE_F32, _check, _lib, sd_norm_t, sd_packed_t)
 
 BLOCK = 128  # columns that share a scale
 TYPES = {torch.float32: SD_TYPE_F32, torch.float16: SD_TYPE_F16, torch.bfloat16: SD_TYPE_BF16}
+# Small calls take a few microseconds on the GPU, so the way there is kept short:
+# the library is called with plain addresses, and the raw handle of the current
+# stream is asked for where torch gives it without making a stream object.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_empty, _uint8, _float32 = torch.empty, torch.uint8, torch.float32
 
 
 def _table(x, what):
@@ -35,30 +42,27 @@ def _table(x, what):
     return x.stride(0) if rows > 1 else cols
 
 
-def _vector(v, n, like, what):
-    if v is not None and (v.shape != (n,) or v.dtype != torch.float32 or v.device != like.device or
-                          not v.is_contiguous()):
-        raise ValueError(f"{what} must be a contiguous float32 vector of {n} on {like.device}")
-    return v
+def _vector(v, n, device, what):
+    """The address of a float32 vector of n, or None."""
+    if v is None:
+        return None
+    if v.shape != (n,) or v.dtype != _float32 or v.device != device or not v.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 vector of {n} on {device}")
+    return v.data_ptr()
 
 
-class _On:
-    """Makes a tensor's device current where it is not, and names its current stream."""
+def _on_its_device(call):
+    """Runs call(first, ...) with the first argument's device as the current one."""
 
-    def __init__(self, x):
-        self.device = x.device
-        self.other = None
+    @functools.wraps(call)
+    def wrapped(first, *args, **kw):
+        index = first.get_device()
+        if index < 0 or index == torch.cuda.current_device():
+            return call(first, *args, **kw)
+        with torch.cuda.device(index):
+            return call(first, *args, **kw)
 
-    def __enter__(self):
-        index = self.device.index
-        if index != torch.cuda.current_device():
-            self.other = torch.cuda.device(index)
-            self.other.__enter__()
-        return torch.cuda.current_stream(index).cuda_stream
-
-    def __exit__(self, *e):
-        if self.other is not None:
-            self.other.__exit__(*e)
+    return wrapped
 
 
 class Packed:
@@ -69,82 +73,105 @@ class Packed:
     __slots__ = ("codes", "scales", "rows", "cols", "format", "c")
 
     def __init__(self, codes, scales, cols: int, format: str = "e4m3"):
-        rows = codes.shape[0]
-        if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_cuda or \
-                codes.device != scales.device:
+        if codes.dtype != _uint8 or scales.dtype != _uint8 or codes.dim() != 2 or not codes.is_cuda or \
+                codes.get_device() != scales.get_device():
             raise ValueError("codes and scales must be uint8 tensors on one GPU")
         if format not in PACK_FORMATS:
             raise ValueError(f"format must be one of {sorted(PACK_FORMATS)}, got {format!r}")
-        ld = codes.stride(0) if rows > 1 and cols else -(-cols // 16) * 16
-        if cols < 0 or codes.shape[1] < -(-cols // 16) * 16 or codes.shape[1] > 1 and codes.stride(1) != 1:
+        rows, width = codes.shape
+        ld, step = codes.stride()
+        need = -(-cols // 16) * 16
+        if cols < 0 or width < need or width > 1 and step != 1:
             raise ValueError(f"codes must hold {cols} columns, rounded up to 16, next to each other")
         if scales.shape != (-(-cols // BLOCK), rows) or not scales.is_contiguous():
             raise ValueError(f"scales must be contiguous [{-(-cols // BLOCK)}, {rows}], got {tuple(scales.shape)}")
+        self._set(codes, scales, rows, cols, ld if rows > 1 and cols else need, format, codes.data_ptr(),
+                  scales.data_ptr())
+
+    def _set(self, codes, scales, rows, cols, ld, format, codes_at, scales_at):
         self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, rows, cols, format
-        self.c = sd_packed_t(rows, cols, ld, PACK_FORMATS[format], 0, codes.data_ptr(), scales.data_ptr())
+        self.c = sd_packed_t(rows, cols, ld, PACK_FORMATS[format], 0, codes_at, scales_at)
 
     @property
     def device(self):
         return self.codes.device
 
+    def get_device(self) -> int:
+        return self.codes.get_device()
+
     @classmethod
     def empty(cls, rows: int, cols: int, format: str, device):
         """One allocation for codes and scales."""
+        if format not in PACK_FORMATS:
+            raise ValueError(f"format must be one of {sorted(PACK_FORMATS)}, got {format!r}")
         ld = -(-cols // 16) * 16
         blocks = -(-cols // BLOCK)
-        store = torch.empty(rows * ld + blocks * rows, dtype=torch.uint8, device=device)
-        return cls(store[:rows * ld].view(rows, ld), store[rows * ld:].view(blocks, rows), cols, format)
+        size = rows * ld
+        store = _empty(size + blocks * rows, dtype=_uint8, device=device)
+        at = store.data_ptr()
+        p = cls.__new__(cls)
+        p._set(store.as_strided((rows, ld), (ld, 1)), store.as_strided((blocks, rows), (rows, 1), size), rows, cols, ld,
+               format, at, at + size)
+        return p
 
 
+@_on_its_device
 def pack(x, format: str = "e4m3", transpose: bool = False) -> Packed:
     """x in 8 bits (of x^T with transpose=True: a weight [k, n] as product's
     second operand).  Any strides."""
     if x.dim() != 2 or x.dtype not in TYPES or not x.is_cuda:
         raise ValueError(f"x must be a float32, float16 or bfloat16 matrix on the GPU, got {x.dtype} "
                          f"{tuple(x.shape)} on {x.device}")
+    (rows, cols), (down, right) = x.shape, x.stride()
     if transpose:
-        x = x.t()
-    rows, cols = x.shape
-    with _On(x) as stream:
-        out = Packed.empty(rows, cols, format, x.device)
-        sd_pack(x, TYPES[x.dtype], x.stride(0), 1 if cols == 1 else x.stride(1), out.c, stream)
+        rows, cols, down, right = cols, rows, right, down
+    out = Packed.empty(rows, cols, format, x.device)
+    _check(_lib.sd_pack(x.data_ptr(), TYPES[x.dtype], down, 1 if cols == 1 else right, out.c,
+                        _raw_stream(x.get_device())), "sd_pack")
     return out
 
 
+@_on_its_device
 def unpack(x: Packed, dtype=torch.float32) -> torch.Tensor:
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
-    with _On(x) as stream:
-        y = torch.empty((x.rows, x.cols), dtype=dtype, device=x.device)
-        sd_unpack(x.c, y, TYPES[dtype], x.cols, stream)
+    y = _empty((x.rows, x.cols), dtype=dtype, device=x.device)
+    _check(_lib.sd_unpack(x.c, y.data_ptr(), TYPES[dtype], x.cols, _raw_stream(x.get_device())), "sd_unpack")
     return y
 
 
+@_on_its_device
 def product(x: Packed, w: Packed, bias=None, dtype=torch.float32) -> torch.Tensor:
     """x.w^T (+ bias), [x.rows, w.rows], summed in 32 bits and rounded once to dtype."""
-    if x.cols != w.cols or x.device != w.device:
-        raise ValueError(f"operands must have the same columns on one device, got {x.cols} on {x.device} and "
+    device = x.device
+    if x.cols != w.cols or device != w.device:
+        raise ValueError(f"operands must have the same columns on one device, got {x.cols} on {device} and "
                          f"{w.cols} on {w.device}")
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
-    _vector(bias, w.rows, x, "bias")
-    with _On(x) as stream:
-        y = torch.empty((x.rows, w.rows), dtype=dtype, device=x.device)
-        sd_pack_product(x.c, w.c, bias, y, TYPES[dtype], w.rows, stream)
+    n = w.rows
+    bias = _vector(bias, n, device, "bias")
+    y = _empty((x.rows, n), dtype=dtype, device=device)
+    _check(_lib.sd_pack_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, _raw_stream(x.get_device())),
+           "sd_pack_product")
     return y
 
 
+@_on_its_device
 def weight_gradient(x: Packed, g) -> torch.Tensor:
     """x^T.g in float32, [x.cols, g.shape[1]]."""
     stride = _table(g, "g")
-    if g.shape[0] != x.rows or g.device != x.device:
-        raise ValueError(f"g must have {x.rows} rows on {x.device}, got {tuple(g.shape)} on {g.device}")
-    n = g.shape[1]
-    with _On(x) as stream:
-        dw = torch.empty((x.cols, n), dtype=torch.float32, device=x.device)
-        size = sd_pack_gradient_size(x.rows, x.cols, n)
-        work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-        sd_pack_gradient(x.c, g, TYPES[g.dtype], n, stride, dw, work, size, stream)
+    rows, n = g.shape
+    device = x.device
+    if rows != x.rows or g.device != device:
+        raise ValueError(f"g must have {x.rows} rows on {device}, got {tuple(g.shape)} on {g.device}")
+    dw = _empty((x.cols, n), dtype=_float32, device=device)
+    size = ctypes.c_size_t()
+    _check(_lib.sd_pack_gradient_size(rows, x.cols, n, size), "sd_pack_gradient_size")
+    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    _check(_lib.sd_pack_gradient(x.c, g.data_ptr(), TYPES[g.dtype], n, stride, dw.data_ptr(),
+                                 None if work is None else work.data_ptr(), size, _raw_stream(x.get_device())),
+           "sd_pack_gradient")
     return dw
 
 
@@ -158,29 +185,28 @@ class NormOut:
         self.y, self.y_packed, self.x, self.mean, self.rstd = y, y_packed, x, mean, rstd
 
 
-def _norm_of(like, rows, channels, dtype, groups, weight, bias, eps, activation, segments, offsets, longest):
+def _norm_of(device, rows, channels, dtype, groups, weight, bias, eps, activation, segments, offsets, longest):
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
     if groups < 1 or channels < 1 or channels % groups:
         raise ValueError(f"{channels} channels cannot be cut into {groups} equal groups")
-    _vector(weight, channels, like, "weight")
-    _vector(bias, channels, like, "bias")
+    at = None
     if offsets is not None:
-        if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.device != like.device or \
+        if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.device != device or \
                 not offsets.is_contiguous() or offsets.numel() < 1:
-            raise ValueError(f"offsets must be a contiguous int32 vector on {like.device}")
+            raise ValueError(f"offsets must be a contiguous int32 vector on {device}")
         if segments not in (None, offsets.numel() - 1):
             raise ValueError(f"{segments} segments need {segments + 1} offsets, got {offsets.numel()}")
-        segments = offsets.numel() - 1
-    else:
-        segments = 1 if segments is None else segments
-    if segments < 0 or rows and (segments < 1 or offsets is None and rows % segments):
+        segments, at = offsets.numel() - 1, offsets.data_ptr()
+    elif segments is None:
+        segments = 1
+    if segments < 0 or rows and (segments < 1 or at is None and rows % segments):
         raise ValueError(f"{rows} rows cannot be cut into {segments} equal segments")
-    return sd_norm_t(rows, segments, offsets.data_ptr() if offsets is not None else None, longest, channels, groups,
-                     TYPES[dtype], ACTIVATIONS[activation], eps, 0, weight.data_ptr() if weight is not None else None,
-                     bias.data_ptr() if bias is not None else None)
+    return sd_norm_t(rows, segments, at, longest, channels, groups, TYPES[dtype], ACTIVATIONS[activation], eps, 0,
+                     _vector(weight, channels, device, "weight"), _vector(bias, channels, device, "bias"))
 
 
+@_on_its_device
 def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, activation: str = "none", segments=None,
                offsets=None, longest: int = 0, keep=None, pack_y=None, dense_y: bool = True) -> NormOut:
     """act(group norm(x) * weight + bias) over segments of x's rows.
@@ -192,22 +218,25 @@ def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, activa
     dense_y=False leaves out y itself."""
     stride = _table(x, "x")
     rows, channels = x.shape
-    d = _norm_of(x, rows, channels, x.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
+    device = x.device
+    d = _norm_of(device, rows, channels, x.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
     if not dense_y and pack_y is None:
         raise ValueError("dense_y=False needs pack_y")
-    with _On(x) as stream:
-        y = torch.empty((rows, channels), dtype=x.dtype, device=x.device) if dense_y else None
-        xp = Packed.empty(rows, channels, keep, x.device) if keep is not None else None
-        yp = Packed.empty(rows, channels, pack_y, x.device) if pack_y is not None else None
-        stats = torch.empty((2, d.segments, groups), dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        size = sd_group_norm_size(d)[0]
-        work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
-        sd_group_norm(d, x, stride, y, channels, xp.c if xp else None, yp.c if yp else None, mean, rstd, work, size,
-                      stream)
+    y = _empty((rows, channels), dtype=x.dtype, device=device) if dense_y else None
+    xp = Packed.empty(rows, channels, keep, device) if keep is not None else None
+    yp = Packed.empty(rows, channels, pack_y, device) if pack_y is not None else None
+    mean, rstd = _empty((2, d.segments, groups), dtype=_float32, device=device).unbind(0)
+    size = ctypes.c_size_t()
+    _check(_lib.sd_group_norm_size(d, size, None), "sd_group_norm_size")
+    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    _check(_lib.sd_group_norm(d, x.data_ptr(), stride, y.data_ptr() if dense_y else None, channels,
+                              xp.c if xp else None, yp.c if yp else None, mean.data_ptr(), rstd.data_ptr(),
+                              None if work is None else work.data_ptr(), size, _raw_stream(x.get_device())),
+           "sd_group_norm")
     return NormOut(y, yp, x if xp is None else xp, mean, rstd)
 
 
+@_on_its_device
 def group_norm_backward(dy, x, mean, rstd, groups: int, weight=None, bias=None, eps: float = 1e-5,
                         activation: str = "none", segments=None, offsets=None, longest: int = 0):
     """(dx, dweight, dbias) from dy and what group_norm left: x (dense or
@@ -223,17 +252,19 @@ def group_norm_backward(dy, x, mean, rstd, groups: int, weight=None, bias=None, 
         if x.shape != dy.shape or x.dtype != dy.dtype or x.device != dy.device:
             raise ValueError(f"x must be {dy.dtype} {tuple(dy.shape)} on {dy.device}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
-    d = _norm_of(dy, rows, channels, dy.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
+    device = dy.device
+    d = _norm_of(device, rows, channels, dy.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
     for v, what in ((mean, "mean"), (rstd, "rstd")):
-        if v.shape != (d.segments, groups) or v.dtype != torch.float32 or v.device != dy.device or \
-                not v.is_contiguous():
-            raise ValueError(f"{what} must be contiguous float32 [{d.segments}, {groups}] on {dy.device}")
-    with _On(dy) as stream:
-        dx = torch.empty((rows, channels), dtype=dy.dtype, device=dy.device)
-        dparam = torch.empty((2, channels), dtype=torch.float32, device=dy.device)
-        size = sd_group_norm_size(d)[1]
-        work = torch.empty(size, dtype=torch.uint8, device=dy.device) if size else None
-        sd_group_norm_backward(d, dy, stride, None if packed else x, 0 if packed else x_stride,
-                               x.c if packed else None, mean, rstd, dx, channels, dparam[0], dparam[1], work, size,
-                               stream)
-    return dx, dparam[0], dparam[1]
+        if v.shape != (d.segments, groups) or v.dtype != _float32 or v.device != device or not v.is_contiguous():
+            raise ValueError(f"{what} must be contiguous float32 [{d.segments}, {groups}] on {device}")
+    dx = _empty((rows, channels), dtype=dy.dtype, device=device)
+    dweight, dbias = _empty((2, channels), dtype=_float32, device=device).unbind(0)
+    size = ctypes.c_size_t()
+    _check(_lib.sd_group_norm_size(d, None, size), "sd_group_norm_size")
+    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    _check(_lib.sd_group_norm_backward(d, dy.data_ptr(), stride, None if packed else x.data_ptr(),
+                                       0 if packed else x_stride, x.c if packed else None, mean.data_ptr(),
+                                       rstd.data_ptr(), dx.data_ptr(), channels, dweight.data_ptr(), dbias.data_ptr(),
+                                       None if work is None else work.data_ptr(), size,
+                                       _raw_stream(dy.get_device())), "sd_group_norm_backward")
+    return dx, dweight, dbias

@@ -6,6 +6,12 @@ epoch: Â·(X W1) and Â·(H1 W2) forward, Âᵀ·G at both widths backward. Onl
 aggregation is replaced; the dense transforms, activation, loss and optimiser
 are ordinary torch operations.
 
+GCN2Packed is the same network with a group norm before the activation and its
+node tables in 8 bits: the dense transforms multiply 8-bit operands, and what the
+backward pass needs of each layer (the features, the normalisation's input, the
+activation) is kept at one byte an element instead of four, through the operators
+of dense.py.  The aggregations stay in fp32.
+
 Each aggregation is `spmm(B, fwd, bwd)`: C = Â·B with plan `fwd`, and in the
 backward pass dB = Âᵀ·dC with the transpose plan `bwd` (A is not assumed
 symmetric).  Plans are built once per (graph, width) and reused every epoch.
@@ -14,7 +20,7 @@ from __future__ import annotations
 
 import torch
 
-from . import Plan, sd_plan_device, sd_plan_ex, sd_spmm
+from . import Plan, dense, sd_plan_device, sd_plan_ex, sd_spmm
 
 
 class _SpMM(torch.autograd.Function):
@@ -102,7 +108,70 @@ class GCN2(torch.nn.Module):
         return self.agg(H1 @ self.W2)
 
 
-def train_epoch(model: GCN2, X, labels, opt) -> torch.Tensor:
+class _PackedTransform(torch.autograd.Function):
+    """X.W from X in 8 bits; the gradient with respect to W alone."""
+
+    @staticmethod
+    def forward(ctx, X8: dense.Packed, W):
+        ctx.X8 = X8
+        return dense.product(X8, dense.pack(W, X8.format, transpose=True))
+
+    @staticmethod
+    def backward(ctx, dZ):
+        return None, dense.weight_gradient(ctx.X8, dZ.contiguous())
+
+
+class _NormTransform(torch.autograd.Function):
+    """act(group norm(A)).W.  A and the activation are kept in 8 bits, and the
+    output gradient is multiplied in 8 bits for dA, in full for dW."""
+
+    @staticmethod
+    def forward(ctx, A, gamma, beta, W, groups, eps, activation, fmt, grad_fmt):
+        out = dense.group_norm(A, groups, gamma, beta, eps, activation, keep=fmt, pack_y=fmt, dense_y=False)
+        ctx.kept, ctx.args, ctx.grad_fmt = out, (groups, eps, activation), grad_fmt
+        ctx.save_for_backward(W, gamma, beta)
+        return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True))
+
+    @staticmethod
+    def backward(ctx, dZ):
+        out, dZ = ctx.kept, dZ.contiguous()
+        W, gamma, beta = ctx.saved_tensors
+        groups, eps, activation = ctx.args
+        dW = dense.weight_gradient(out.y_packed, dZ)
+        dH = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, out.y_packed.format))
+        dA, dgamma, dbeta = dense.group_norm_backward(dH, out.x, out.mean, out.rstd, groups, gamma, beta, eps,
+                                                       activation)
+        return dA, dgamma, dbeta, dW, None, None, None, None, None
+
+
+class GCN2Packed(torch.nn.Module):
+    """H1 = act(group norm(Â X W1)), logits = Â H1 W2 with the node tables in 8 bits.
+
+    X is given as a float tensor or, since it does not change between epochs,
+    once packed by `dense.pack(X, model.format)`.  format: of features,
+    activations and weights; grad_format: of the output gradient where it is
+    multiplied by the weights."""
+
+    def __init__(self, A, in_feats: int, hidden: int, classes: int, device, seed: int = 0, groups: int = 8,
+                 activation: str = "relu", eps: float = 1e-5, format: str = "e4m3", grad_format: str = "e4m3",
+                 **plan_opts):
+        super().__init__()
+        plain = GCN2(A, in_feats, hidden, classes, device, seed, **plan_opts)
+        self.W1, self.W2, self.agg = plain.W1, plain.W2, plain.agg
+        self.gamma = torch.nn.Parameter(torch.ones(hidden, device=device))
+        self.beta = torch.nn.Parameter(torch.zeros(hidden, device=device))
+        self.groups, self.activation, self.eps = groups, activation, eps
+        self.format, self.grad_format = format, grad_format
+
+    def forward(self, X) -> torch.Tensor:
+        X8 = X if isinstance(X, dense.Packed) else dense.pack(X, self.format)
+        A1 = self.agg(_PackedTransform.apply(X8, self.W1))
+        Z2 = _NormTransform.apply(A1, self.gamma, self.beta, self.W2, self.groups, self.eps, self.activation,
+                                  self.format, self.grad_format)
+        return self.agg(Z2)
+
+
+def train_epoch(model, X, labels, opt) -> torch.Tensor:
     """One full-batch epoch: forward, cross-entropy, backward, optimiser step."""
     opt.zero_grad(set_to_none=True)
     loss = torch.nn.functional.cross_entropy(model(X), labels)
