@@ -59,6 +59,19 @@ __device__ inline void store_span(T *p, const float (&in)[N]) {
   for (int i = 0; i < N; ++i) s.v[i] = rounded<T>(in[i]);
   *reinterpret_cast<Span<T, N> *>(p) = s;
 }
+// The same past the caches, for tables that are larger than them: what is read
+// next then stays where it is.
+template <int N, typename T>
+__device__ inline void stream_span(T *p, const float (&in)[N]) {
+  constexpr int WORDS = N * sizeof(T) / 4;
+  typedef uint32_t words __attribute__((ext_vector_type(WORDS), aligned(sizeof(T))));
+  Span<T, N> s;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s.v[i] = rounded<T>(in[i]);
+  words w;
+  __builtin_memcpy(&w, &s, sizeof(w));
+  __builtin_nontemporal_store(w, reinterpret_cast<words *>(p));
+}
 template <int N, typename T>
 __device__ inline void store_part(T *p, int count, const float (&in)[N]) {
 #pragma unroll

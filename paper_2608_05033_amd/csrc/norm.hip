@@ -93,6 +93,7 @@ template <typename T>
 struct Dense {
   T *p;
   uint32_t stride;  // below 2^31, as rows are: one 32-bit product a row
+  bool stream;      // written past the caches
   __device__ T *at(int64_t r) const { return p + (uint64_t)(uint32_t)r * stride; }
   template <int N>
   __device__ void load(int64_t r, int64_t step, int32_t c, int left, bool whole, float (&v)[N][V]) const {
@@ -121,7 +122,11 @@ struct Dense {
   template <int N>
   __device__ void store(int64_t r, int64_t step, int32_t c, int left, bool whole, const float (&v)[N][V]) const {
     T *q = at(r) + c;
-    if (whole) {
+    if (whole && stream) {
+      if (left > 0)
+#pragma unroll
+        for (int u = 0; u < N; ++u) stream_span(q + u * step * stride, v[u]);
+    } else if (whole) {
       if (left > 0)
 #pragma unroll
         for (int u = 0; u < N; ++u) store_span(q + u * step * stride, v[u]);
@@ -922,6 +927,14 @@ uint32_t join_threads(const Shape &p) {
   return (!p.wgs && p.segments * (int64_t)p.groups >= 1024) || p.chunks < 8 ? 64 : 1024;
 }
 
+// A result of 64 MB or more leaves the Infinity Cache to the table that the second
+// pass reads again: a training step of 262144 x 128 fp32 takes 190 us, and 219 us
+// with ordinary stores.
+template <typename T>
+bool streamed(const Shape &p) {
+  return p.rows * p.channels * (int64_t)sizeof(T) >= 64 << 20;
+}
+
 template <typename T, int ACT, int XF, int YF>
 void apply(const Shape &p, Dense<const T> x, float *mean, float *rstd, Dense<T> y, Packs xo, Packs yo, hipStream_t s) {
   if (p.wgs) {
@@ -956,8 +969,8 @@ void apply_x(int xf, int yf, const Shape &p, Dense<const T> x, float *mean, floa
 template <typename T>
 int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride, void *y, int64_t y_stride,
             const sd_packed_t *xp, const sd_packed_t *yp, float *mean, float *rstd, double2 *part, hipStream_t s) {
-  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride};
-  const Dense<T> out{static_cast<T *>(y), (uint32_t)y_stride};
+  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride, false};
+  const Dense<T> out{static_cast<T *>(y), (uint32_t)y_stride, streamed<T>(p)};
   const Packs none{nullptr, nullptr, 0};
   const Packs xo = xp ? Packs{xp->codes, xp->scales, xp->ld} : none;
   const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
@@ -1016,8 +1029,8 @@ template <typename T>
 int backward(int32_t activation, const Shape &p, const void *x, int64_t x_stride, const sd_packed_t *xp,
              const void *dy, int64_t dy_stride, const float *mean, const float *rstd, void *dx, int64_t dx_stride,
              float *dweight, float *dbias, float *ws, hipStream_t s) {
-  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride}, g{static_cast<const T *>(dy), (uint32_t)dy_stride};
-  const Dense<T> out{static_cast<T *>(dx), (uint32_t)dx_stride};
+  const Dense<const T> in{static_cast<const T *>(x), (uint32_t)x_stride, false}, g{static_cast<const T *>(dy), (uint32_t)dy_stride, false};
+  const Dense<T> out{static_cast<T *>(dx), (uint32_t)dx_stride, streamed<T>(p)};
   if (!xp) return backward_act<T>(activation, p, in, g, mean, rstd, out, dweight, dbias, ws, s);
   if (xp->format == SD_PACK_E4M3)
     return backward_act<T>(activation, p, Codes<SD_PACK_E4M3>{xp->codes, xp->scales, xp->ld, xp->rows}, g, mean, rstd,

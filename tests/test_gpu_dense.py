@@ -161,6 +161,15 @@ def test_product_many_tiles(rows, n, dtype):
     check_product(dense.product(X, W, dtype=TYPES[dtype]), x, w, None, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rows,cols,n", [(15001, 48, 47), (20000, 200, 64), (30011, 128, 128), (14003, 512, 100),
+                                         (16001, 513, 33)])
+def test_product_long_and_narrow(rows, cols, n, dtype):
+    X, W, x, w = packed_pair(rows, cols, n)
+    b = np.random.default_rng(n).standard_normal(n).astype(np.float32)
+    check_product(dense.product(X, W, torch.from_numpy(b).cuda(), TYPES[dtype]), x, w, b.astype(np.float64), dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [4, 200])
 def test_product_padding_and_strides(rows, dtype):
