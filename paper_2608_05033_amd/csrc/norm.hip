@@ -33,12 +33,14 @@ struct Shape {
   const int32_t *offsets;
   int32_t channels, groups, per_group;
   int32_t chunk_rows, chunks, tx, ty;
-  int32_t share;  // lanes that add up one group's channels
+  int32_t share;   // lanes that add up one group's channels
+  int32_t across;  // of a team's, those side by side on channels
   // A slab of tx * V channels leaves sums for the groups that it has a part of, at
   // group + slab of a piece's slots: both only grow along the channels.
   int32_t slots;
   // Short segments: teams of tx * ty threads, wgs workgroups; 0: chunks are used.
   int32_t wgs;
+  bool one_row;  // each thread keeps one row of a segment, as many as the caller says there are
   float eps;
   const float *weight, *bias;
 };
@@ -279,10 +281,11 @@ __device__ inline double wg_sum(double v, double *lds) {
   return t;
 }
 
-__device__ inline void write_stats(const Shape &p, double sum, double square, double count, float *mean, float *rstd) {
-  const double mu = sum / count, var = square / count - mu * mu;
+// one: 1 over the count.  The variance is rounded to 32 bits once its difference is taken.
+__device__ inline void write_stats(const Shape &p, double sum, double square, double one, float *mean, float *rstd) {
+  const double mu = sum * one, var = square * one - mu * mu;
   *mean = (float)mu;
-  *rstd = (float)(1.0 / sqrt((var < 0.0 ? 0.0 : var) + (double)p.eps));
+  *rstd = 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + p.eps);
 }
 
 // The chunks that hold rows [b, e).
@@ -317,7 +320,7 @@ __global__ void k_norm_join(Shape p, const double2 *__restrict__ part, float *__
     }
     sum = wg_sum(sum, lds);
     square = wg_sum(square, lds);
-    if (threadIdx.x == 0) write_stats(p, sum, square, e > b ? (double)(e - b) * p.per_group : 1.0, mean + at, rstd + at);
+    if (threadIdx.x == 0) write_stats(p, sum, square, 1.0 / (e > b ? (double)(e - b) * p.per_group : 1.0), mean + at, rstd + at);
     __syncthreads();
   }
 }
@@ -588,24 +591,30 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<cons
 // ------------------------------------------------------ short segments -----
 constexpr int kHeld = 8;  // rows of a lane that stay in registers
 
-// Adds a team's values, `count` per group and lane row: rows ty of items[ty][tx * V],
-// for each group, share lanes each a part; f(group, sums) in one lane per group.
-template <typename S, typename A, typename F>
+template <int N>
+__device__ inline float (&first_of(float (&v)[N][V]))[1][V] {
+  return *reinterpret_cast<float(*)[1][V]>(&v[0]);
+}
+
+// Adds a team's values, items[ty][tx * V], group by group: `share` lanes to a
+// group, `across` of them over its channels; f(group, sums) in one lane of them.
+template <typename S, typename F>
 __device__ inline void team_sums(const Shape &p, const S *items, int t, F f) {
   const int team = p.tx * p.ty, row = p.tx * V;
+  const int down = p.share / p.across, lane = t & (p.share - 1);
   for (int32_t g = t / p.share; g < p.groups; g += team / p.share) {
-    A a = 0, b = 0;
-    for (int32_t q = t % p.share; q < p.per_group * p.ty; q += p.share) {
-      const int32_t y = q / p.per_group;
-      const S v = items[y * row + g * p.per_group + (q - y * p.per_group)];
-      a += v.x;
-      b += v.y;
-    }
+    double a = 0, b = 0;
+    for (int32_t y = lane / p.across; y < p.ty; y += down)
+      for (int32_t q = lane & (p.across - 1); q < p.per_group; q += p.across) {
+        const S v = items[y * row + g * p.per_group + q];
+        a += v.x;
+        b += v.y;
+      }
     for (int d = 1; d < p.share; d *= 2) {
       a += __shfl_xor(a, d);
       b += __shfl_xor(b, d);
     }
-    if (t % p.share == 0) f(g, a, b);
+    if (lane == 0) f(g, a, b);
   }
 }
 
@@ -621,13 +630,23 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
   const int32_t c = tx * V, left = p.channels - c, width = p.tx < kBlock / V ? p.tx : kBlock / V;
   const bool whole = p.channels % V == 0;
   float2 *stat = s_stat + which * p.groups;
+  const int most = p.one_row ? TY : TY * kHeld;  // rows that are kept
+  float weight[V], shift[V];
+  int32_t group[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    weight[i] = p.weight && i < left ? p.weight[c + i] : 1.0f;
+    shift[i] = p.bias && i < left ? p.bias[c + i] : 0.0f;
+    group[i] = i < left ? (c + i) / p.per_group : 0;
+  }
   for (int64_t s0 = (int64_t)blockIdx.x * teams; s0 < p.segments; s0 += (int64_t)gridDim.x * teams) {
     const int64_t s = s0 + which;
     const bool here = s < p.segments;
     int64_t lo = here ? seg_begin(p, s) : 0, hi = here ? seg_begin(p, s + 1) : 0;
     lo = lo < 0 ? 0 : lo;
     hi = hi > p.rows ? p.rows : hi;
-    const int64_t mid = lo + TY * kHeld < hi ? lo + TY * kHeld : hi;
+    const int64_t mid = lo + most < hi ? lo + most : hi;
+    const double one = 1.0 / (hi > lo ? (double)(hi - lo) * p.per_group : 1.0);
     float v[kHeld][V];
     double a[V] = {}, b[V] = {};
     auto add = [&](const float (&u)[V]) {
@@ -638,10 +657,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
         b[i] = fma(d, d, b[i]);
       }
     };
-    if (p.rows > 0) x.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, v);
+    const int64_t last = mid > 0 ? mid - 1 : 0;
+    if (p.one_row) {  // the same for all threads
+      if (p.rows > 0) x.load_to(last, lo + ty, TY, c, left, whole, first_of(v));
+      if (lo + ty < mid) add(v[0]);
+    } else {
+      if (p.rows > 0) x.load_to(last, lo + ty, TY, c, left, whole, v);
 #pragma unroll
-    for (int u = 0; u < kHeld; ++u)
-      if (lo + ty + u * TY < mid) add(v[u]);
+      for (int u = 0; u < kHeld; ++u)
+        if (lo + ty + u * TY < mid) add(v[u]);
+    }
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
         constexpr int N = decltype(count)::value;
@@ -654,9 +679,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
     for (int i = 0; i < V; ++i) s_sum[threadIdx.x][i] = double2{a[i], b[i]};
     __syncthreads();
     if (here)
-      team_sums<double2, double>(p, &s_sum[which * team][0], t, [&](int32_t g, double sum, double square) {
+      team_sums(p, &s_sum[which * team][0], t, [&](int32_t g, double sum, double square) {
         float m, r;
-        write_stats(p, sum, square, hi > lo ? (double)(hi - lo) * p.per_group : 1.0, &m, &r);
+        write_stats(p, sum, square, one, &m, &r);
         stat[g] = float2{m, r};
         mean[s * p.groups + g] = m;
         rstd[s * p.groups + g] = r;
@@ -666,10 +691,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
     Coeff k;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float2 st = i < left ? stat[(c + i) / p.per_group] : float2{0, 0};
+      const float2 st = stat[group[i]];
       k.mean[i] = st.x;
-      k.scale[i] = st.y * (p.weight && i < left ? p.weight[c + i] : 1.0f);
-      k.shift[i] = p.bias && i < left ? p.bias[c + i] : 0.0f;
+      k.scale[i] = st.y * weight[i];
+      k.shift[i] = shift[i];
     }
     auto finish = [&](int64_t row, float (&u)[1][V]) {
       if constexpr (XF != 0) store_packed<XF>(xo, p.rows, row, c, p.channels, tx, width, u[0]);
@@ -678,8 +703,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
       if constexpr (YF != 0) store_packed<YF>(yo, p.rows, row, c, p.channels, tx, width, u[0]);
       if (y.p) y.store(row, 0, c, left, whole, u);
     };
+    if (lo + ty < mid) finish(lo + ty, first_of(v));
+    if (p.one_row) continue;
 #pragma unroll
-    for (int u = 0; u < kHeld; ++u) {
+    for (int u = 1; u < kHeld; ++u) {
       const int64_t row = lo + ty + u * TY;
       if (row < mid) finish(row, *reinterpret_cast<float(*)[1][V]>(&v[u]));
     }
@@ -708,6 +735,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
   const int32_t c = tx * V, left = p.channels - c;
   const bool whole = p.channels % V == 0;
   float2 *stat = s_stat + which * p.groups;
+  const int most = p.one_row ? TY : TY * kHeldBack;  // rows that are kept
   float w[V], ta[V] = {}, tb[V] = {};
 #pragma unroll
   for (int i = 0; i < V; ++i) w[i] = i >= left ? 0.0f : p.weight ? p.weight[c + i] : 1.0f;
@@ -717,7 +745,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
     int64_t lo = here ? seg_begin(p, s) : 0, hi = here ? seg_begin(p, s + 1) : 0;
     lo = lo < 0 ? 0 : lo;
     hi = hi > p.rows ? p.rows : hi;
-    const int64_t mid = lo + TY * kHeldBack < hi ? lo + TY * kHeldBack : hi;
+    const int64_t mid = lo + most < hi ? lo + most : hi;
     Coeff k;
     float rs[V];
     load_coeff(p, mean, rstd, here ? s : 0, c, left, k, rs);
@@ -730,19 +758,27 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
         dv[i] *= act_slope<ACT>(xv[i] * k.scale[i] + k.shift[i]);
       }
     };
-    if (p.rows > 0) {
-      x.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, d);
-      dy.load_to(mid > 0 ? mid - 1 : 0, lo + ty, TY, c, left, whole, dz);
+    const int64_t last = mid > 0 ? mid - 1 : 0;
+    if (p.one_row && p.rows > 0) {  // the same for all threads
+      x.load_to(last, lo + ty, TY, c, left, whole, first_of(d));
+      dy.load_to(last, lo + ty, TY, c, left, whole, first_of(dz));
+    } else if (p.rows > 0) {
+      x.load_to(last, lo + ty, TY, c, left, whole, d);
+      dy.load_to(last, lo + ty, TY, c, left, whole, dz);
     }
-#pragma unroll
-    for (int u = 0; u < kHeldBack; ++u) {
+    auto add = [&](int u) {
       shape(d[u], dz[u]);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const bool in = lo + ty + u * TY < mid;
-        a[i] += in ? dz[u][i] : 0.0f;
-        b[i] += in ? dz[u][i] * d[u][i] : 0.0f;
+        a[i] += dz[u][i];
+        b[i] += dz[u][i] * d[u][i];
       }
+    };
+    if (lo + ty < mid) add(0);
+    if (!p.one_row) {
+#pragma unroll
+      for (int u = 1; u < kHeldBack; ++u)
+        if (lo + ty + u * TY < mid) add(u);
     }
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
@@ -774,7 +810,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
     }
     __syncthreads();
     if (here)
-      team_sums<float2, double>(p, &s_sum[which * team][0], t, [&](int32_t g, double sa, double sb) {
+      team_sums(p, &s_sum[which * team][0], t, [&](int32_t g, double sa, double sb) {
         const double count = hi > lo ? (double)(hi - lo) * p.per_group : 1.0;
         stat[g] = float2{(float)(sa / count), (float)(sb / count)};
       });
@@ -793,8 +829,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       for (int i = 0; i < V; ++i) out[0][i] = dv[i] * k.scale[i] - a1[i] - xv[i] * a2[i];
       dx.store(row, 0, c, left, whole, out);
     };
+    if (lo + ty < mid) finish(lo + ty, d[0], dz[0]);
+    if (p.one_row) continue;
 #pragma unroll
-    for (int u = 0; u < kHeldBack; ++u) {
+    for (int u = 1; u < kHeldBack; ++u) {
       const int64_t row = lo + ty + u * TY;
       if (row < mid) finish(row, d[u], dz[u]);
     }
@@ -888,8 +926,12 @@ Shape shape_of(const sd_norm_t *d, bool back) {
     const int32_t team = p.tx * p.ty;
     p.share = 1;
     while (p.share < 64 && p.share * 2 <= team && p.share * 2 * p.groups <= team) p.share *= 2;
-    // the gradients' sums over all segments are kept per workgroup
-    const int64_t wgs = ceil_div(d->segments, kThreads / team), most = back ? 4ll * cu_count() : 1 << 24;
+    p.across = 1;
+    while (p.across * 2 <= p.share && p.across * 2 <= p.per_group) p.across *= 2;
+    p.one_row = longest_of(d) <= p.ty;
+    // what a thread needs of its channels is read once for all its segments; the
+    // gradients' sums over all segments are kept per workgroup
+    const int64_t wgs = ceil_div(d->segments, kThreads / team), most = (back ? 4ll : 6ll) * cu_count();
     p.wgs = (int32_t)(wgs < most ? wgs : most);
     p.chunks = p.wgs;
     return p;

@@ -350,6 +350,24 @@ def test_norm_backward(rows, channels, groups, segments, keep, dtype):
         assert np.all(np.abs(to64(db) - db64) <= 2.0 ** -19 * grown * size_b)
 
 
+@pytest.mark.parametrize("channels", [16, 130])
+@pytest.mark.parametrize("longest", [1, 7, 10 ** 6])
+def test_norm_does_not_depend_on_the_stated_longest(channels, longest):
+    """A wrong longest segment costs time, not results."""
+    rows, groups, kind = 3000, 2, "silu"
+    t, x64, w, b, w64, b64, g = norm_inputs(rows, channels, "f32", 9)
+    off = offsets_of(rows, 40, 2)
+    how = {"offsets": torch.from_numpy(off).int().cuda(), "longest": longest}
+    out = dense.group_norm(t, groups, w, b, 1e-5, kind, keep="e4m3", **how)
+    check_norm(out, x64, groups, w64, b64, 1e-5, kind, off, "f32")
+    dy, dy64 = table(0.1 * g.standard_normal((rows, channels)), "f32")
+    dx, dw, db = dense.group_norm_backward(dy, out.x, out.mean, out.rstd, groups, w, b, 1e-5, kind, **how)
+    dx64, dw64, db64 = ref.norm_backward(dy64, of(out.x), to64(out.mean), to64(out.rstd), groups, w64, b64, kind,
+                                         off)[:3]
+    for got, want in ((dx, dx64), (dw, dw64), (db, db64)):
+        assert np.linalg.norm(to64(got) - want) <= 1e-5 * np.linalg.norm(want)
+
+
 def test_norm_gradient_against_differences():
     """The gradient of sum(y R) from differences of the 64-bit forward form."""
     rows, channels, groups, kind = 9, 12, 3, "gelu"
