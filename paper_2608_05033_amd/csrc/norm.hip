@@ -704,11 +704,12 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
       if (y.p) y.store(row, 0, c, left, whole, u);
     };
     if (lo + ty < mid) finish(lo + ty, first_of(v));
-    if (p.one_row) continue;
+    if (!p.one_row) {
 #pragma unroll
-    for (int u = 1; u < kHeld; ++u) {
-      const int64_t row = lo + ty + u * TY;
-      if (row < mid) finish(row, *reinterpret_cast<float(*)[1][V]>(&v[u]));
+      for (int u = 1; u < kHeld; ++u) {
+        const int64_t row = lo + ty + u * TY;
+        if (row < mid) finish(row, *reinterpret_cast<float(*)[1][V]>(&v[u]));
+      }
     }
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
@@ -830,11 +831,12 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       dx.store(row, 0, c, left, whole, out);
     };
     if (lo + ty < mid) finish(lo + ty, d[0], dz[0]);
-    if (p.one_row) continue;
+    if (!p.one_row) {
 #pragma unroll
-    for (int u = 1; u < kHeldBack; ++u) {
-      const int64_t row = lo + ty + u * TY;
-      if (row < mid) finish(row, d[u], dz[u]);
+      for (int u = 1; u < kHeldBack; ++u) {
+        const int64_t row = lo + ty + u * TY;
+        if (row < mid) finish(row, d[u], dz[u]);
+      }
     }
     if (mid < hi)
       for_rows(mid, hi, ty, TY, [&](int64_t row, auto count) {
