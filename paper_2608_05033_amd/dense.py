@@ -27,7 +27,7 @@ TYPES = {torch.float32: SD_TYPE_F32, torch.float16: SD_TYPE_F16, torch.bfloat16:
 # stream is asked for where torch gives it without making a stream object.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
-_empty, _uint8, _float32 = torch.empty, torch.uint8, torch.float32
+_uint8, _float32 = torch.uint8, torch.float32
 
 
 def _table(x, what):
@@ -42,13 +42,16 @@ def _table(x, what):
     return x.stride(0) if rows > 1 else cols
 
 
-def _vector(v, n, device, what):
-    """The address of a float32 vector of n, or None."""
+def _vector(v, n, index, what):
+    """The address of a float32 vector of n on GPU `index`, or None."""
     if v is None:
         return None
-    if v.shape != (n,) or v.dtype != _float32 or v.device != device or not v.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous float32 vector of {n} on {device}")
+    if v.shape != (n,) or v.dtype != _float32 or v.get_device() != index or not v.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 vector of {n} on cuda:{index}")
     return v.data_ptr()
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _on_its_device(call):
@@ -57,7 +60,7 @@ def _on_its_device(call):
     @functools.wraps(call)
     def wrapped(first, *args, **kw):
         index = first.get_device()
-        if index < 0 or index == torch.cuda.current_device():
+        if index < 0 or index == _current_device():
             return call(first, *args, **kw)
         with torch.cuda.device(index):
             return call(first, *args, **kw)
@@ -70,48 +73,45 @@ class Packed:
     16, zeros from cols to the next multiple of 16) and scales uint8
     [ceil(cols / 128), rows], a code's value times 2^(scale - 127)."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "format", "c")
+    __slots__ = ("codes", "scales", "rows", "cols", "format", "index", "c")
 
     def __init__(self, codes, scales, cols: int, format: str = "e4m3"):
-        if codes.dtype != _uint8 or scales.dtype != _uint8 or codes.dim() != 2 or not codes.is_cuda or \
-                codes.get_device() != scales.get_device():
+        index = codes.get_device()
+        if codes.dtype != _uint8 or scales.dtype != _uint8 or codes.dim() != 2 or index < 0 or \
+                index != scales.get_device():
             raise ValueError("codes and scales must be uint8 tensors on one GPU")
         if format not in PACK_FORMATS:
             raise ValueError(f"format must be one of {sorted(PACK_FORMATS)}, got {format!r}")
         rows, width = codes.shape
         ld, step = codes.stride()
-        need = -(-cols // 16) * 16
+        need = (cols + 15) // 16 * 16
         if cols < 0 or width < need or width > 1 and step != 1:
             raise ValueError(f"codes must hold {cols} columns, rounded up to 16, next to each other")
-        if scales.shape != (-(-cols // BLOCK), rows) or not scales.is_contiguous():
+        if scales.shape != ((cols + 127) // BLOCK, rows) or not scales.is_contiguous():
             raise ValueError(f"scales must be contiguous [{-(-cols // BLOCK)}, {rows}], got {tuple(scales.shape)}")
-        self._set(codes, scales, rows, cols, ld if rows > 1 and cols else need, format, codes.data_ptr(),
-                  scales.data_ptr())
-
-    def _set(self, codes, scales, rows, cols, ld, format, codes_at, scales_at):
-        self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, rows, cols, format
-        self.c = sd_packed_t(rows, cols, ld, PACK_FORMATS[format], 0, codes_at, scales_at)
+        self.codes, self.scales, self.rows, self.cols, self.format, self.index = codes, scales, rows, cols, format, index
+        self.c = sd_packed_t(rows, cols, ld if rows > 1 and cols else need, PACK_FORMATS[format], 0, codes.data_ptr(),
+                             scales.data_ptr())
 
     @property
     def device(self):
         return self.codes.device
 
     def get_device(self) -> int:
-        return self.codes.get_device()
+        return self.index
 
     @classmethod
-    def empty(cls, rows: int, cols: int, format: str, device):
-        """One allocation for codes and scales."""
+    def empty(cls, rows: int, cols: int, format: str, like):
+        """A new one on the device of the tensor `like`: one allocation for codes and scales."""
         if format not in PACK_FORMATS:
             raise ValueError(f"format must be one of {sorted(PACK_FORMATS)}, got {format!r}")
-        ld = -(-cols // 16) * 16
-        blocks = -(-cols // BLOCK)
+        ld, blocks = (cols + 15) // 16 * 16, (cols + 127) // BLOCK
         size = rows * ld
-        store = _empty(size + blocks * rows, dtype=_uint8, device=device)
-        at = store.data_ptr()
-        p = cls.__new__(cls)
-        p._set(store.as_strided((rows, ld), (ld, 1)), store.as_strided((blocks, rows), (rows, 1), size), rows, cols, ld,
-               format, at, at + size)
+        store = like.new_empty(size + blocks * rows, dtype=_uint8)
+        p, at = cls.__new__(cls), store.data_ptr()
+        p.codes, p.scales = store.as_strided((rows, ld), (ld, 1)), store.as_strided((blocks, rows), (rows, 1), size)
+        p.rows, p.cols, p.format, p.index = rows, cols, format, store.get_device()
+        p.c = sd_packed_t(rows, cols, ld, PACK_FORMATS[format], 0, at, at + size)
         return p
 
 
@@ -125,7 +125,7 @@ def pack(x, format: str = "e4m3", transpose: bool = False) -> Packed:
     (rows, cols), (down, right) = x.shape, x.stride()
     if transpose:
         rows, cols, down, right = cols, rows, right, down
-    out = Packed.empty(rows, cols, format, x.device)
+    out = Packed.empty(rows, cols, format, x)
     _check(_lib.sd_pack(x.data_ptr(), TYPES[x.dtype], down, 1 if cols == 1 else right, out.c,
                         _raw_stream(x.get_device())), "sd_pack")
     return out
@@ -135,24 +135,23 @@ def pack(x, format: str = "e4m3", transpose: bool = False) -> Packed:
 def unpack(x: Packed, dtype=torch.float32) -> torch.Tensor:
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
-    y = _empty((x.rows, x.cols), dtype=dtype, device=x.device)
-    _check(_lib.sd_unpack(x.c, y.data_ptr(), TYPES[dtype], x.cols, _raw_stream(x.get_device())), "sd_unpack")
+    y = x.codes.new_empty((x.rows, x.cols), dtype=dtype)
+    _check(_lib.sd_unpack(x.c, y.data_ptr(), TYPES[dtype], x.cols, _raw_stream(x.index)), "sd_unpack")
     return y
 
 
 @_on_its_device
 def product(x: Packed, w: Packed, bias=None, dtype=torch.float32) -> torch.Tensor:
     """x.w^T (+ bias), [x.rows, w.rows], summed in 32 bits and rounded once to dtype."""
-    device = x.device
-    if x.cols != w.cols or device != w.device:
-        raise ValueError(f"operands must have the same columns on one device, got {x.cols} on {device} and "
+    if x.cols != w.cols or x.index != w.index:
+        raise ValueError(f"operands must have the same columns on one device, got {x.cols} on {x.device} and "
                          f"{w.cols} on {w.device}")
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
     n = w.rows
-    bias = _vector(bias, n, device, "bias")
-    y = _empty((x.rows, n), dtype=dtype, device=device)
-    _check(_lib.sd_pack_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, _raw_stream(x.get_device())),
+    bias = _vector(bias, n, x.index, "bias")
+    y = x.codes.new_empty((x.rows, n), dtype=dtype)
+    _check(_lib.sd_pack_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, _raw_stream(x.index)),
            "sd_pack_product")
     return y
 
@@ -162,15 +161,14 @@ def weight_gradient(x: Packed, g) -> torch.Tensor:
     """x^T.g in float32, [x.cols, g.shape[1]]."""
     stride = _table(g, "g")
     rows, n = g.shape
-    device = x.device
-    if rows != x.rows or g.device != device:
-        raise ValueError(f"g must have {x.rows} rows on {device}, got {tuple(g.shape)} on {g.device}")
-    dw = _empty((x.cols, n), dtype=_float32, device=device)
+    if rows != x.rows or g.get_device() != x.index:
+        raise ValueError(f"g must have {x.rows} rows on {x.device}, got {tuple(g.shape)} on {g.device}")
+    dw = g.new_empty((x.cols, n), dtype=_float32)
     size = ctypes.c_size_t()
     _check(_lib.sd_pack_gradient_size(rows, x.cols, n, size), "sd_pack_gradient_size")
-    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    work = g.new_empty(size.value, dtype=_uint8) if size.value else None
     _check(_lib.sd_pack_gradient(x.c, g.data_ptr(), TYPES[g.dtype], n, stride, dw.data_ptr(),
-                                 None if work is None else work.data_ptr(), size, _raw_stream(x.get_device())),
+                                 None if work is None else work.data_ptr(), size, _raw_stream(x.index)),
            "sd_pack_gradient")
     return dw
 
@@ -185,16 +183,16 @@ class NormOut:
         self.y, self.y_packed, self.x, self.mean, self.rstd = y, y_packed, x, mean, rstd
 
 
-def _norm_of(device, rows, channels, dtype, groups, weight, bias, eps, activation, segments, offsets, longest):
+def _norm_of(index, rows, channels, dtype, groups, weight, bias, eps, activation, segments, offsets, longest):
     if activation not in ACTIVATIONS:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
     if groups < 1 or channels < 1 or channels % groups:
         raise ValueError(f"{channels} channels cannot be cut into {groups} equal groups")
     at = None
     if offsets is not None:
-        if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.device != device or \
+        if offsets.dim() != 1 or offsets.dtype != torch.int32 or offsets.get_device() != index or \
                 not offsets.is_contiguous() or offsets.numel() < 1:
-            raise ValueError(f"offsets must be a contiguous int32 vector on {device}")
+            raise ValueError(f"offsets must be a contiguous int32 vector on cuda:{index}")
         if segments not in (None, offsets.numel() - 1):
             raise ValueError(f"{segments} segments need {segments + 1} offsets, got {offsets.numel()}")
         segments, at = offsets.numel() - 1, offsets.data_ptr()
@@ -203,7 +201,7 @@ def _norm_of(device, rows, channels, dtype, groups, weight, bias, eps, activatio
     if segments < 0 or rows and (segments < 1 or at is None and rows % segments):
         raise ValueError(f"{rows} rows cannot be cut into {segments} equal segments")
     return sd_norm_t(rows, segments, at, longest, channels, groups, TYPES[dtype], ACTIVATIONS[activation], eps, 0,
-                     _vector(weight, channels, device, "weight"), _vector(bias, channels, device, "bias"))
+                     _vector(weight, channels, index, "weight"), _vector(bias, channels, index, "bias"))
 
 
 @_on_its_device
@@ -218,20 +216,20 @@ def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, activa
     dense_y=False leaves out y itself."""
     stride = _table(x, "x")
     rows, channels = x.shape
-    device = x.device
-    d = _norm_of(device, rows, channels, x.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
+    index = x.get_device()
+    d = _norm_of(index, rows, channels, x.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
     if not dense_y and pack_y is None:
         raise ValueError("dense_y=False needs pack_y")
-    y = _empty((rows, channels), dtype=x.dtype, device=device) if dense_y else None
-    xp = Packed.empty(rows, channels, keep, device) if keep is not None else None
-    yp = Packed.empty(rows, channels, pack_y, device) if pack_y is not None else None
-    mean, rstd = _empty((2, d.segments, groups), dtype=_float32, device=device).unbind(0)
+    y = x.new_empty((rows, channels)) if dense_y else None
+    xp = Packed.empty(rows, channels, keep, x) if keep is not None else None
+    yp = Packed.empty(rows, channels, pack_y, x) if pack_y is not None else None
+    mean, rstd = x.new_empty((2, d.segments, groups), dtype=_float32).unbind(0)
     size = ctypes.c_size_t()
     _check(_lib.sd_group_norm_size(d, size, None), "sd_group_norm_size")
-    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    work = x.new_empty(size.value, dtype=_uint8) if size.value else None
     _check(_lib.sd_group_norm(d, x.data_ptr(), stride, y.data_ptr() if dense_y else None, channels,
                               xp.c if xp else None, yp.c if yp else None, mean.data_ptr(), rstd.data_ptr(),
-                              None if work is None else work.data_ptr(), size, _raw_stream(x.get_device())),
+                              None if work is None else work.data_ptr(), size, _raw_stream(index)),
            "sd_group_norm")
     return NormOut(y, yp, x if xp is None else xp, mean, rstd)
 
@@ -252,19 +250,19 @@ def group_norm_backward(dy, x, mean, rstd, groups: int, weight=None, bias=None, 
         if x.shape != dy.shape or x.dtype != dy.dtype or x.device != dy.device:
             raise ValueError(f"x must be {dy.dtype} {tuple(dy.shape)} on {dy.device}, got {x.dtype} "
                              f"{tuple(x.shape)} on {x.device}")
-    device = dy.device
-    d = _norm_of(device, rows, channels, dy.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
+    index = dy.get_device()
+    d = _norm_of(index, rows, channels, dy.dtype, groups, weight, bias, eps, activation, segments, offsets, longest)
     for v, what in ((mean, "mean"), (rstd, "rstd")):
-        if v.shape != (d.segments, groups) or v.dtype != _float32 or v.device != device or not v.is_contiguous():
-            raise ValueError(f"{what} must be contiguous float32 [{d.segments}, {groups}] on {device}")
-    dx = _empty((rows, channels), dtype=dy.dtype, device=device)
-    dweight, dbias = _empty((2, channels), dtype=_float32, device=device).unbind(0)
+        if v.shape != (d.segments, groups) or v.dtype != _float32 or v.get_device() != index or not v.is_contiguous():
+            raise ValueError(f"{what} must be contiguous float32 [{d.segments}, {groups}] on cuda:{index}")
+    dx = dy.new_empty((rows, channels))
+    dweight, dbias = dy.new_empty((2, channels), dtype=_float32).unbind(0)
     size = ctypes.c_size_t()
     _check(_lib.sd_group_norm_size(d, None, size), "sd_group_norm_size")
-    work = _empty(size.value, dtype=_uint8, device=device) if size.value else None
+    work = dy.new_empty(size.value, dtype=_uint8) if size.value else None
     _check(_lib.sd_group_norm_backward(d, dy.data_ptr(), stride, None if packed else x.data_ptr(),
                                        0 if packed else x_stride, x.c if packed else None, mean.data_ptr(),
                                        rstd.data_ptr(), dx.data_ptr(), channels, dweight.data_ptr(), dbias.data_ptr(),
                                        None if work is None else work.data_ptr(), size,
-                                       _raw_stream(dy.get_device())), "sd_group_norm_backward")
+                                       _raw_stream(index)), "sd_group_norm_backward")
     return dx, dweight, dbias
