@@ -350,6 +350,19 @@ def test_norm_backward(rows, channels, groups, segments, keep, dtype):
         assert np.all(np.abs(to64(db) - db64) <= 2.0 ** -19 * grown * size_b)
 
 
+@pytest.mark.parametrize("rows,channels,groups,segments", [(300, 640, 5, 1), (200, 896, 4, 2), (257, 636, 3, -2), (300, 884, 2, 1),
+                                                           (400, 384, 3, 1)])
+def test_norm_wide_groups_where_threads_leave_half_a_wave(rows, channels, groups, segments):
+    """Rows of 160 and 224 threads and groups of 128 channels or more, in chunks:
+    a group's sums may not be shared by more lanes than come out even."""
+    print(f"case norm wide groups {rows}x{channels} groups {groups} segments {segments}", flush=True)
+    t, x64, w, b, w64, b64, _ = norm_inputs(rows, channels, "f32", rows + channels)
+    off = offsets_of(rows, -segments, rows) if segments < 0 else np.arange(segments + 1) * (rows // segments)
+    how = {"offsets": torch.from_numpy(off).int().cuda()} if segments < 0 else {"segments": segments}
+    for _ in range(3):
+        check_norm(dense.group_norm(t, groups, w, b, 1e-5, "silu", **how), x64, groups, w64, b64, 1e-5, "silu", off, "f32")
+
+
 @pytest.mark.parametrize("channels", [16, 130])
 @pytest.mark.parametrize("longest", [1, 7, 10 ** 6])
 def test_norm_does_not_depend_on_the_stated_longest(channels, longest):
