@@ -250,11 +250,17 @@ struct Split {
   int32_t nt, splits, tn;
 };
 // Two workgroups per compute unit over all tiles; a part of at least 4 steps.
-// Tiles of 128 columns of G where more than 64 are left to fill: X is then read
-// half as often.
-Split split_of(int64_t rows, int64_t cols, int64_t n) {
+// Columns of G a tile: 128 of 16-bit G where more than 64 are there, so that X is
+// read half as often; 64 of fp32, whose three terms fill the registers and shared
+// memory.  Measured in us, 64 and 128 columns:
+//   rows x columns x n         fp32        f16         bf16
+//   262144 x 128 x 128       47   63     36   38     30   30
+//   50021 x 601 x 129        58  101     48   52     39   39
+//   20000 x 1024 x 256       54   76     47   44     39   36
+//   8000 x 2048 x 1024      176  230    152  134    127  106
+Split split_of(int64_t rows, int64_t cols, int64_t n, bool wide_type) {
   Split p{};
-  p.tn = n > 64 ? 128 : 64;
+  p.tn = n > 64 && !wide_type ? 128 : 64;
   p.nt = (int32_t)ceil_div(n, p.tn);
   p.tiles = blocks_of(cols) * p.nt;
   int64_t want = 2ll * cu_count() / (p.tiles > 0 ? p.tiles : 1);
@@ -274,7 +280,9 @@ int gradient(const sd_packed_t *X, const void *G, int64_t n, int64_t stride, flo
   const int64_t wgs = p.tiles * p.splits, size = X->cols * n;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   float *out = p.splits > 1 ? ws : dW;
-  auto *kernel = p.tn == 128 ? k_gradient<T, FMT, 128> : k_gradient<T, FMT, 64>;
+  auto *kernel = k_gradient<T, FMT, 64>;
+  if constexpr (sizeof(T) == 2)
+    if (p.tn == 128) kernel = k_gradient<T, FMT, 128>;
   hipLaunchKernelGGL(kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, s, X->codes, X->scales, X->ld,
                      X->rows, (int32_t)X->cols, static_cast<const T *>(G), stride, (int32_t)n, p.nt, p.splits,
                      p.split_rows, out, size);
@@ -292,8 +300,10 @@ int gradient_as(const sd_packed_t *X, const void *G, int64_t n, int64_t stride, 
                                    : gradient<T, SD_PACK_E5M2>(X, G, n, stride, dW, ws, p, s);
 }
 
-size_t workspace_of(const Split &p, int64_t cols, int64_t n) {
-  return p.splits > 1 ? 4 * (size_t)p.splits * (size_t)cols * (size_t)n : 0;
+// Enough for any type of G.
+size_t workspace_of(int64_t rows, int64_t cols, int64_t n) {
+  const int32_t a = split_of(rows, cols, n, true).splits, b = split_of(rows, cols, n, false).splits, most = a > b ? a : b;
+  return most > 1 ? 4 * (size_t)most * (size_t)cols * (size_t)n : 0;
 }
 
 }  // namespace
@@ -301,7 +311,7 @@ size_t workspace_of(const Split &p, int64_t cols, int64_t n) {
 extern "C" int sd_pack_gradient_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes) {
   if (!bytes || rows < 0 || cols < 0 || n < 0) return SD_ERR_INVALID_VALUE;
   if (rows > kMaxRows || cols > kMaxRows - 1024 || n > kMaxRows - 1024) return SD_ERR_OVERFLOW;
-  *bytes = workspace_of(split_of(rows, cols, n), cols, n);
+  *bytes = workspace_of(rows, cols, n);
   return SD_OK;
 }
 
@@ -313,8 +323,8 @@ extern "C" int sd_pack_gradient(const sd_packed_t *X, const void *G, int32_t typ
   if (n > kMaxRows - 1024) return SD_ERR_OVERFLOW;
   if ((st = check_table(G, type, X->rows, n, row_stride)) != SD_OK) return st;
   if (X->cols == 0 || n == 0) return SD_OK;
-  const Split p = split_of(X->rows, X->cols, n);
-  const size_t need = workspace_of(p, X->cols, n);
+  const Split p = split_of(X->rows, X->cols, n, type == SD_TYPE_F32);
+  const size_t need = workspace_of(X->rows, X->cols, n);
   if (!dW || !aligned_to(dW, 4) || bytes < need || (need > 0 && (!workspace || !aligned_to(workspace, 16))))
     return SD_ERR_INVALID_VALUE;
   if ((st = have_device()) != SD_OK) return st;
