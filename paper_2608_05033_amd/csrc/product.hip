@@ -7,12 +7,15 @@
 // agree, since one scale covers them all.  W is the first operand, so a lane
 // ends with four neighbouring n of one row m and writes them in one store.
 //
-// Two instruction forms (measured on this card against 64 bits, normal values):
-//  * 16-bit results: v_mfma_scale_f32_16x16x128_f8f6f4, codes and scales as they
-//    are.  It aligns the 128 products of a step to the largest and drops what
-//    is below, 1.6e-5 of the result in 2-norm: under a tenth of an f16 rounding.
-//  * 32-bit results: the codes become bf16, exactly (4 or 3 significant bits and
-//    a power of two), and v_mfma_f32_16x16x32_bf16 sums in 32 bits (1.2e-7).
+// The codes become bf16 with their scale (4 or 3 significant bits and a power of
+// two: exact as far as bf16 reaches, to multiples of 2^-133), and
+// v_mfma_f32_16x16x32_bf16 sums in 32 bits: 1.2e-7 of the result in 2-norm on
+// normal values.  The matrix units' 8-bit forms, scaled or not, run at twice the
+// rate but are not used: in each run of 8 neighbouring k they drop what lies under
+// 2^-13 of the run's largest product, taken by the codes' stored exponents.
+// Measured, that is 1.5e-5 of the result on normal values, 2e-3 of the magnitudes
+// summed where a run's codes differ widely, and all of a result that is left when
+// larger terms cancel.
 #include "dense.h"
 
 namespace {
@@ -58,12 +61,6 @@ __device__ inline bf16x8 bf16_of(const Frag &f, int q) {
     o[4 * j + 3] = hi[1];
   }
   return o;
-}
-
-template <int WF, int XF>
-__device__ inline f32x4 mfma_scaled(const Frag &w, const Frag &x, f32x4 c) {
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.v, x.v, c, WF == SD_PACK_E5M2, XF == SD_PACK_E5M2, 0,
-                                                          (int)w.s, 0, (int)x.s);
 }
 
 // Chunks of 16 codes g and g + 4 of block kb of one row; zero past the row's last.
@@ -153,8 +150,8 @@ __device__ __align__(16) uint8_t kZeros[16];
 
 // MF x NF tiles of 16 x 16 by one workgroup, operands straight from memory: KW
 // waves each take every KW-th block of k and join their sums in shared memory.
-// Bound by the latency of the loads: one row of 4096 by 4096 x 4096 takes 5.6 us,
-// 3 TB/s of W.
+// Bound by the latency of the loads: one row of 4096 by 4096 x 4096 takes 6 us,
+// 2.8 TB/s of W.
 template <typename T, int XF, int WF, int MF, int NF, int KW>
 __global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
                                                                          const float *__restrict__ bias,
@@ -183,25 +180,18 @@ __global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
     for (int j = 0; j < NF; ++j) load_frag(W, wrow[j], kb, g, k16, w[j]);
   };
   auto multiply = [&](const Frag (&x)[MF], const Frag (&w)[NF]) {
-    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      bf16x8 xb[MF], wb[NF];
+#pragma unroll
+      for (int i = 0; i < MF; ++i) xb[i] = bf16_of<XF>(x[i], q);
+#pragma unroll
+      for (int j = 0; j < NF; ++j) wb[j] = bf16_of<WF>(w[j], q);
 #pragma unroll
       for (int i = 0; i < MF; ++i)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = mfma_scaled<WF, XF>(w[j], x[i], acc[i][j]);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        bf16x8 xb[MF], wb[NF];
-#pragma unroll
-        for (int i = 0; i < MF; ++i) xb[i] = bf16_of<XF>(x[i], q);
-#pragma unroll
-        for (int j = 0; j < NF; ++j) wb[j] = bf16_of<WF>(w[j], q);
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-          for (int j = 0; j < NF; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], xb[i], acc[i][j], 0, 0, 0);
-      }
+        for (int j = 0; j < NF; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], xb[i], acc[i][j], 0, 0, 0);
     }
   };
   // the next block is on its way while this one's products run
@@ -244,8 +234,8 @@ __global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
 // chunks mixed with the row so that 16 rows read at one chunk touch all banks;
 // the mixing is done on the memory side, since a wave's 64 lanes write 1 KiB in
 // order.  Scale bytes lie by lane, the tile's 16-row groups side by side, so one
-// read serves all of a lane's products.  Bound by the matrix units: 8192 cubed in
-// 450 us, 2.44 PFLOP/s.
+// read serves all of a lane's products.  Bound by the matrix units and the
+// conversions to bf16: 8192 cubed in 800 to 890 us, 1.3 PFLOP/s.
 template <typename T, int XF, int WF, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand W, const float *__restrict__ bias,
                                                               T *__restrict__ Y, int64_t stride, int32_t k16,
@@ -359,17 +349,12 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
     for (int i = 0; i < MF; ++i) {
       Frag x = frag(codes, xlo, i * 16);
       x.s = (sx[i / 4] >> (8 * (i % 4))) & 255;
-      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int j = 0; j < NF; ++j) acc[i][j] = mfma_scaled<WF, XF>(w[j], x, acc[i][j]);
-      } else {
+      for (int q = 0; q < 4; ++q) {
+        const bf16x8 xb = bf16_of<XF>(x, q);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bf16x8 xb = bf16_of<XF>(x, q);
-#pragma unroll
-          for (int j = 0; j < NF; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w[j], q), xb, acc[i][j], 0, 0, 0);
-        }
+        for (int j = 0; j < NF; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w[j], q), xb, acc[i][j], 0, 0, 0);
       }
       if (i < MF / 2) {
 #pragma unroll
@@ -455,13 +440,9 @@ __global__ __launch_bounds__(256) void k_product_narrow(Operand X, Operand W, co
           w.v[4 + i] = (int)b[i];
         }
         w.s = (sw[j / 4] >> (8 * (j % 4))) & 255;
-        if constexpr (sizeof(T) == 2) {
-          acc[0][j] = mfma_scaled<WF, XF>(w, x, acc[0][j]);
-        } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w, q), bf16_of<XF>(x, q), acc[0][j], 0, 0, 0);
-        }
+        for (int q = 0; q < 4; ++q)
+          acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of<WF>(w, q), bf16_of<XF>(x, q), acc[0][j], 0, 0, 0);
       }
     }
     store_tiles<1, NF>(acc, strip * 16, 0, X.rows, W.rows, bias, Y, stride);
@@ -510,14 +491,14 @@ int product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void 
   // the sum over k is what takes time, so more waves have to share it.  Measured
   // in us, 16-bit results, this choice and its neighbours:
   //   rows x columns x k   256x256  128x128  64x64  32x64  32x32  16x16
-  //   4096 x 4096 x 4096        65       81    243
-  //   2048 x 2048 x 2048        30       18     36     50
-  //   256 x 4096 x 4096         49       26     20     27     35     62
-  //   4096 x 128 x 4096         47       26     20     16     19     33
-  //   64 x 4096 x 4096          46       25     19     14     10     17
-  //   1 x 4096 x 4096                           14     11      7      5
+  //   4096 x 4096 x 4096       104      156    308    417
+  //   2048 x 2048 x 2048        49       24     52     64     79    120
+  //   256 x 4096 x 4096         88       39     22     28     36     61
+  //   4096 x 128 x 4096         87       38     23     16     20     33
+  //   64 x 4096 x 4096          86       38     21     15     11     18
+  //   1 x 4096 x 4096           86       38     18     12      8      7
   // 256 x 256 only where its edges cost little against 128 x 128: 300 columns of
-  // 100000 rows (700 of k, 32-bit results) take 114 us with it and 80 us without.
+  // 100000 rows (700 of k, 32-bit results) take 120 us with it and 76 us without.
   const int64_t enough = 3 * cu_count() / 4;
   const auto tiles = [&](int64_t bm, int64_t bn) { return ceil_div(x.rows, bm) * ceil_div(w.rows, bn); };
   // the large tiles keep row offsets in 32 bits
@@ -525,7 +506,7 @@ int product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void 
   if (near && tiles(256, 256) >= enough && 32 * tiles(256, 256) <= 9 * tiles(128, 128))
     return tile_launch<T, XF, WF, 256, 256, 2, 4>(x, w, bias, y, stride, k16, nb, s);
   // W in shared memory for long tables of few columns: 1000000 x 47 of 64 k, 32-bit
-  // results, take 65 us so and 92 us with 128 x 128 tiles
+  // results, take 63 us so and 88 us with 128 x 128 tiles
   if (nb <= kNarrowBlocks && w.rows <= 128 && x.rows >= 64 * enough)
     return w.rows <= 64 ? narrow_launch<T, XF, WF, 4>(x, w, bias, y, stride, k16, nb, s)
                         : narrow_launch<T, XF, WF, 8>(x, w, bias, y, stride, k16, nb, s);
