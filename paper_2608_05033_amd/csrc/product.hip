@@ -506,8 +506,9 @@ int product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void 
   if (near && tiles(256, 256) >= enough && 32 * tiles(256, 256) <= 9 * tiles(128, 128))
     return tile_launch<T, XF, WF, 256, 256, 2, 4>(x, w, bias, y, stride, k16, nb, s);
   // W in shared memory for long tables of few columns: 1000000 x 47 of 64 k, 32-bit
-  // results, take 63 us so and 88 us with 128 x 128 tiles
-  if (nb <= kNarrowBlocks && w.rows <= 128 && x.rows >= 64 * enough)
+  // results, take 63 us so and 88 us with 128 x 128 tiles.  That kernel reads a block
+  // ahead, so there has to be one.
+  if (nb > 0 && nb <= kNarrowBlocks && w.rows <= 128 && x.rows >= 64 * enough)
     return w.rows <= 64 ? narrow_launch<T, XF, WF, 4>(x, w, bias, y, stride, k16, nb, s)
                         : narrow_launch<T, XF, WF, 8>(x, w, bias, y, stride, k16, nb, s);
   if (near && tiles(128, 128) >= enough)
