@@ -808,7 +808,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_team_grad(Shape p, X x, Dense
       });
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      b[i] *= rs[i];
+      b[i] = lo < hi ? b[i] * rs[i] : 0.0f;  // with eps 0 an empty segment's rstd is infinite
       ta[i] += a[i];
       tb[i] += b[i];
       s_sum[threadIdx.x][i] = float2{w[i] * a[i], w[i] * b[i]};
