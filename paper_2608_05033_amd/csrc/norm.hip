@@ -207,12 +207,35 @@ __device__ inline float act_slope(float z) {
 }
 
 // ------------------------------------------------------------- forward -----
-// Per piece and group: the sums of x and x^2, in 64 bits.  A product of two
-// 24-bit numbers is exact there, so the variance keeps 1e-8 of itself with a
-// mean 10^4 deviations away, and the two 64-bit operations per element still
-// take less time than loading it.
-template <typename X>
-__global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *__restrict__ part) {
+// What the numbers of a segment and group are counted from: the first of them
+// (0 where that is not finite).  Its distance from the mean is no more than
+// sqrt(n) deviations, so the variance, a difference of sums counted from here,
+// keeps n 2^-53 of itself however large the mean is, and is 0 where all n
+// numbers are the same.
+template <typename T>
+__device__ inline float origin_of(const Shape &p, const Dense<const T> &x, int64_t first_row, int32_t first_channel) {
+  const int64_t row = first_row < 0 ? 0 : first_row < p.rows ? first_row : p.rows - 1;
+  const float v = (float)x.at(row)[first_channel];
+  return fabsf(v) < __builtin_inff() ? v : 0.0f;
+}
+// Of a lane's channels, whose groups begin at `first`; one where they share a group.
+template <typename T>
+__device__ inline void origins_of(const Shape &p, const Dense<const T> &x, int64_t first_row, const int32_t (&first)[V],
+                                  float (&k)[V]) {
+  if (p.per_group % V == 0) {  // the same for all threads
+    const float v = origin_of(p, x, first_row, first[0]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) k[i] = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) k[i] = origin_of(p, x, first_row, first[i]);
+  }
+}
+
+// Per piece and group: the sums of x and x^2, counted from the segment's origin, in
+// 64 bits.  The three 64-bit operations per element take less time than loading it.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, Dense<const T> x, double2 *__restrict__ part) {
   __shared__ double2 s_sum[kThreads][V];
   const int tx = threadIdx.x % p.tx, ty = threadIdx.x / p.tx, TY = p.ty;
   const int32_t c = (blockIdx.y * p.tx + tx) * V;
@@ -220,8 +243,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *
   const bool whole = p.channels % V == 0;
   const int64_t r0 = (int64_t)blockIdx.x * p.chunk_rows;
   const int64_t r1 = r0 + p.chunk_rows < p.rows ? r0 + p.chunk_rows : p.rows;
+  int32_t group_first[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) group_first[i] = i < left ? (c + i) / p.per_group * p.per_group : 0;
   for_pieces(p, r0, r1, [&](int64_t s, int64_t lo, int64_t hi) {
     double a[V] = {}, b[V] = {};
+    float origin[V];
+    origins_of(p, x, seg_begin(p, s), group_first, origin);
     for_rows(lo, hi, ty, TY, [&](int64_t row, auto count) {
       constexpr int N = decltype(count)::value;
       float v[N][V];
@@ -230,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_stats(Shape p, X x, double2 *
       for (int u = 0; u < N; ++u)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const double d = v[u][i];
+          const double d = (double)v[u][i] - (double)origin[i];
           a[i] += d;
           b[i] = fma(d, d, b[i]);
         }
@@ -285,10 +313,12 @@ __device__ inline double wg_sum(double v, double *lds) {
   return t;
 }
 
-// one: 1 over the count.  The variance is rounded to 32 bits once its difference is taken.
-__device__ inline void write_stats(const Shape &p, double sum, double square, double one, float *mean, float *rstd) {
+// From sums counted from `origin`; one: 1 over the count.  The variance is rounded
+// to 32 bits once its difference is taken.
+__device__ inline void write_stats(const Shape &p, double sum, double square, double one, float origin, float *mean,
+                                   float *rstd) {
   const double mu = sum * one, var = square * one - mu * mu;
-  *mean = (float)mu;
+  *mean = (float)((double)origin + mu);
   *rstd = 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + p.eps);
 }
 
@@ -302,7 +332,8 @@ __device__ inline bool chunks_of(const Shape &p, int64_t b, int64_t e, int64_t *
   return *c0 <= *c1;
 }
 
-__global__ void k_norm_join(Shape p, const double2 *__restrict__ part, float *__restrict__ mean,
+template <typename T>
+__global__ void k_norm_join(Shape p, Dense<const T> x, const double2 *__restrict__ part, float *__restrict__ mean,
                             float *__restrict__ rstd) {
   __shared__ double lds[16];
   const int32_t slab = p.tx * V;
@@ -312,8 +343,10 @@ __global__ void k_norm_join(Shape p, const double2 *__restrict__ part, float *__
     const int64_t b = seg_begin(p, s), e = seg_begin(p, s + 1);
     const int32_t k0 = g + g * p.per_group / slab, k1 = g + ((g + 1) * p.per_group - 1) / slab;
     double sum = 0, square = 0;
+    float origin = 0.0f;
     int64_t c0, c1;
     if (chunks_of(p, b, e, &c0, &c1)) {
+      origin = origin_of(p, x, b, g * p.per_group);
 #pragma unroll 4
       for (int64_t c = c0 + threadIdx.x; c <= c1; c += blockDim.x)
         for (int32_t k = k0; k <= k1; ++k) {
@@ -324,7 +357,8 @@ __global__ void k_norm_join(Shape p, const double2 *__restrict__ part, float *__
     }
     sum = wg_sum(sum, lds);
     square = wg_sum(square, lds);
-    if (threadIdx.x == 0) write_stats(p, sum, square, 1.0 / (e > b ? (double)(e - b) * p.per_group : 1.0), mean + at, rstd + at);
+    if (threadIdx.x == 0)
+      write_stats(p, sum, square, 1.0 / (e > b ? (double)(e - b) * p.per_group : 1.0), origin, mean + at, rstd + at);
     __syncthreads();
   }
 }
@@ -629,6 +663,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
                                                         float *__restrict__ rstd, Dense<T> y, Packs xo, Packs yo) {
   __shared__ double2 s_sum[kThreads][V];
   __shared__ float2 s_stat[kThreads * V];
+  __shared__ float s_origin[kThreads * V];
   const int team = p.tx * p.ty, which = threadIdx.x / team, teams = blockDim.x / team, t = threadIdx.x % team;
   const int tx = t % p.tx, ty = t / p.tx, TY = p.ty;
   const int32_t c = tx * V, left = p.channels - c, width = p.tx < kBlock / V ? p.tx : kBlock / V;
@@ -636,12 +671,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
   float2 *stat = s_stat + which * p.groups;
   const int most = p.one_row ? TY : TY * kHeld;  // rows that are kept
   float weight[V], shift[V];
-  int32_t group[V];
+  int32_t group[V], group_first[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     weight[i] = p.weight && i < left ? p.weight[c + i] : 1.0f;
     shift[i] = p.bias && i < left ? p.bias[c + i] : 0.0f;
     group[i] = i < left ? (c + i) / p.per_group : 0;
+    group_first[i] = group[i] * p.per_group;
   }
   for (int64_t s0 = (int64_t)blockIdx.x * teams; s0 < p.segments; s0 += (int64_t)gridDim.x * teams) {
     const int64_t s = s0 + which;
@@ -651,12 +687,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
     hi = hi > p.rows ? p.rows : hi;
     const int64_t mid = lo + most < hi ? lo + most : hi;
     const double one = 1.0 / (hi > lo ? (double)(hi - lo) * p.per_group : 1.0);
-    float v[kHeld][V];
+    float v[kHeld][V], origin[V] = {};
     double a[V] = {}, b[V] = {};
+    if (lo < hi) origins_of(p, x, lo, group_first, origin);
     auto add = [&](const float (&u)[V]) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const double d = u[i];
+        const double d = (double)u[i] - (double)origin[i];
         a[i] += d;
         b[i] = fma(d, d, b[i]);
       }
@@ -681,11 +718,16 @@ __global__ __launch_bounds__(kThreads) void k_norm_team(Shape p, Dense<const T> 
       });
 #pragma unroll
     for (int i = 0; i < V; ++i) s_sum[threadIdx.x][i] = double2{a[i], b[i]};
+    if (ty == 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)  // one lane has a group's first channel
+        if (i < left && c + i == group_first[i]) s_origin[which * p.groups + group[i]] = origin[i];
+    }
     __syncthreads();
     if (here)
       team_sums(p, &s_sum[which * team][0], t, [&](int32_t g, double sum, double square) {
         float m, r;
-        write_stats(p, sum, square, one, &m, &r);
+        write_stats(p, sum, square, one, s_origin[which * p.groups + g], &m, &r);
         stat[g] = float2{m, r};
         mean[s * p.groups + g] = m;
         rstd[s * p.groups + g] = r;
@@ -1026,9 +1068,9 @@ int forward(const Shape &p, int32_t activation, const void *x, int64_t x_stride,
   const Packs yo = yp ? Packs{yp->codes, yp->scales, yp->ld} : none;
   const int xf = xp ? xp->format : 0, yf = yp ? yp->format : 0;
   if (!p.wgs && p.chunks > 0)
-    hipLaunchKernelGGL((k_norm_stats<Dense<const T>>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
+    hipLaunchKernelGGL((k_norm_stats<T>), dim3(p.chunks, slabs_of(p)), dim3(p.tx * p.ty), 0, s, p, in, part);
   if (!p.wgs && join_wgs(p) > 0)
-    hipLaunchKernelGGL(k_norm_join, dim3(join_wgs(p)), dim3(join_threads(p)), 0, s, p, part, mean, rstd);
+    hipLaunchKernelGGL((k_norm_join<T>), dim3(join_wgs(p)), dim3(join_threads(p)), 0, s, p, in, part, mean, rstd);
   if (p.chunks > 0) {
     if (activation == SD_ACT_RELU)
       apply_x<T, SD_ACT_RELU>(xf, yf, p, in, mean, rstd, out, xo, yo, s);

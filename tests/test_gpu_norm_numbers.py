@@ -49,3 +49,54 @@ def test_gradients_beside_empty_segments_without_eps(cuts, channels, groups, kee
     assert np.all(np.abs(to64(got[0]) - dx) <= 2.0 ** -19 * grown * size)
     assert np.all(np.abs(to64(got[1]) - dw) <= 2.0 ** -19 * grown * (size_w + size_b))
     assert np.all(np.abs(to64(got[2]) - db) <= 2.0 ** -19 * grown * size_b)
+
+
+# ------------------------------------------- little spread, a large mean ---
+WAYS = [  # rows, channels, groups, cuts: teams, chunks, pieces of both
+    (33, 24, 2, [0, 33]), (700, 35, 7, [0, 3, 3, 500, 700]), (5000, 24, 2, [0, 5000]), (100000, 32, 4, [0, 100000]),
+    (9000, 130, 10, [0, 1, 4097, 4097, 9000]), (300, 1028, 4, [0, 120, 300])]
+
+
+def cut(cuts):
+    return {"offsets": gpu(np.array(cuts), torch.int32)}
+
+
+@pytest.mark.parametrize("dtype,value", [(torch.float32, 1234567.0), (torch.float32, -3.3333334e7), (torch.float32, 0.1),
+                                         (torch.bfloat16, 999424.0), (torch.float16, 60032.0), (torch.float32, 3e-7)])
+@pytest.mark.parametrize("rows,channels,groups,cuts", WAYS)
+def test_constant_groups_have_no_variance(rows, channels, groups, cuts, value, dtype):
+    """All numbers of a group alike: mean is the number, rstd is eps^-1/2 to a
+    rounding of its operations, y is 0 and dx is rstd (dh - mean(dh))."""
+    print(f"case constant {value} {rows}x{channels} {dtype}", flush=True)
+    x = torch.full((rows, channels), value, device="cuda").to(dtype)
+    out = dense.group_norm(x, groups, **cut(cuts))
+    full = np.diff(cuts) > 0
+    assert (out.y == 0).all()
+    assert (out.mean[gpu(full, torch.bool)] == x[0, 0].float()).all() and (out.mean[gpu(~full, torch.bool)] == 0).all()
+    assert np.allclose(to64(out.rstd), 1e-5 ** -0.5, rtol=2.0 ** -21, atol=0)
+    dy = np.random.default_rng(rows).standard_normal((rows, channels)).astype(np.float32).astype(np.float64)
+    dy = to64(gpu(dy, dtype))
+    dx, dw, db = dense.group_norm_backward(gpu(dy, dtype), x, out.mean, out.rstd, groups, **cut(cuts))
+    want, _, want_b, size, _, size_b, _ = ref.norm_backward(dy, to64(x), to64(out.mean), to64(out.rstd), groups, None, None,
+                                                           "none", np.array(cuts))
+    half_ulp = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}[dtype]
+    assert np.all(np.abs(to64(dx) - want) <= 2.0 ** -19 * size + half_ulp * 1.01 * np.abs(want) + 2.0 ** -25)
+    assert not dw.any() and np.all(np.abs(to64(db) - want_b) <= 2.0 ** -19 * size_b)
+
+
+@pytest.mark.parametrize("first", [None, 0.0, 3e7])
+@pytest.mark.parametrize("mean,spread", [(1e6, 0.5), (1e7, 3.0), (-12345.0, 0.01)])
+@pytest.mark.parametrize("rows,channels,groups,cuts", WAYS)
+def test_little_spread_around_a_large_mean(rows, channels, groups, cuts, mean, spread, first):
+    """Spreads of a few units in the last place of the numbers, at the usual eps;
+    with a first number of each segment that is far from the others too.  rstd is
+    right to some roundings of 2^-24, the mean to one of its own."""
+    print(f"case spread {spread} around {mean}, first {first}, {rows}x{channels}", flush=True)
+    g = np.random.default_rng(rows + channels)
+    x = (mean + spread * g.standard_normal((rows, channels))).astype(np.float32)
+    if first is not None:
+        x[[c for c in cuts[:-1] if c < rows]] = first
+    out = dense.group_norm(gpu(x), groups, **cut(cuts))
+    _, want_mean, want_rstd, _, _ = ref.norm(x.astype(np.float64), groups, None, None, 1e-5, "none", cuts)
+    assert np.allclose(to64(out.rstd), want_rstd, rtol=2e-6, atol=0)
+    assert np.allclose(to64(out.mean), want_mean, rtol=2.0 ** -23, atol=0)
