@@ -100,3 +100,35 @@ def test_little_spread_around_a_large_mean(rows, channels, groups, cuts, mean, s
     _, want_mean, want_rstd, _, _ = ref.norm(x.astype(np.float64), groups, None, None, 1e-5, "none", cuts)
     assert np.allclose(to64(out.rstd), want_rstd, rtol=2e-6, atol=0)
     assert np.allclose(to64(out.mean), want_mean, rtol=2.0 ** -23, atol=0)
+
+
+# --------------------------------------------------- magnitudes far from 1 ---
+@pytest.mark.parametrize("power", [-100, -80, -63, 0, 66, 90, 100])
+@pytest.mark.parametrize("rows,channels,groups,cuts", WAYS)
+def test_magnitudes_far_from_one(rows, channels, groups, cuts, power):
+    """Without eps, numbers times a power of two have the same xh, y, dweight and
+    dbias, and dx over that power, whatever becomes of their squares in 32 bits.
+    The bounds are those of ordinary numbers."""
+    print(f"case 2^{power} {rows}x{channels}", flush=True)
+    g, off, kind = np.random.default_rng(channels), np.array(cuts), "silu"
+    x = np.ldexp((g.standard_normal((rows, channels)) + 0.5).astype(np.float32).astype(np.float64), power)
+    w = (1 + 0.2 * g.standard_normal(channels)).astype(np.float32).astype(np.float64)
+    b = (0.2 * g.standard_normal(channels)).astype(np.float32).astype(np.float64)
+    dy = g.standard_normal((rows, channels)).astype(np.float32).astype(np.float64)
+    how = {"offsets": gpu(off, torch.int32), "eps": 0.0, "activation": kind}
+    t = gpu(x)
+    assert np.array_equal(to64(t), x)
+    out = dense.group_norm(t, groups, gpu(w), gpu(b), **how)
+    y, mean, rstd, xh, z = ref.norm(x, groups, w, b, 0.0, kind, off)
+    full = np.diff(off) > 0
+    assert np.allclose(to64(out.rstd)[full], rstd[full], rtol=2e-6, atol=0)
+    per, seg = channels // groups, np.repeat(np.arange(len(off) - 1), np.diff(off))
+    spread = lambda v: np.repeat(v[seg], per, axis=1)  # noqa: E731
+    size = (np.abs(x) + np.abs(spread(mean))) * spread(rstd) * np.abs(w) + np.abs(b) + np.abs(z)
+    assert np.all(np.abs(to64(out.y) - y) <= 2.0 ** -20 * size)
+    got = dense.group_norm_backward(gpu(dy), t, out.mean, out.rstd, groups, gpu(w), gpu(b), **how)
+    dx, dw, db, size, size_w, size_b, _ = ref.norm_backward(dy, x, to64(out.mean), to64(out.rstd), groups, w, b, kind, off)
+    grown = 1 + np.abs(x).max() * rstd[full].max()
+    assert np.all(np.abs(to64(got[0]) - dx) <= 2.0 ** -19 * grown * size)
+    assert np.all(np.abs(to64(got[1]) - dw) <= 2.0 ** -19 * grown * (size_w + size_b))
+    assert np.all(np.abs(to64(got[2]) - db) <= 2.0 ** -19 * grown * size_b)
