@@ -170,7 +170,17 @@ __device__ inline uint32_t xcd_place(uint32_t b, uint32_t n) {
   return x * whole + (x < more ? x : more) + j;
 }
 
+// This workgroup's number in a grid of grid_of().
+__device__ inline uint32_t workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ------------------------------------------------------------ host side ---
+// A launch holds fewer than 2^32 threads along a dimension: workgroups (of at most
+// 1024 threads, fewer than 2^31 of them) past 2^21 go along a second one.  The last
+// row of such a grid has some too many, which find no work.
+inline dim3 grid_of(int64_t wgs) {
+  constexpr int64_t kAlong = 1 << 21;
+  return wgs <= kAlong ? dim3((uint32_t)wgs) : dim3((uint32_t)kAlong, (uint32_t)ceil_div(wgs, kAlong));
+}
 inline bool type_ok(int32_t t) { return t == SD_TYPE_F32 || t == SD_TYPE_F16 || t == SD_TYPE_BF16; }
 inline int64_t type_bytes(int32_t t) { return t == SD_TYPE_F32 ? 4 : 2; }
 inline bool aligned_to(const void *p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }

@@ -66,16 +66,18 @@ template <typename T, int FMT, int TN>
 __global__ __launch_bounds__(kThreads) void k_gradient(const uint8_t *__restrict__ codes,
                                                        const uint8_t *__restrict__ scales, int64_t ld, int64_t rows,
                                                        int32_t cols, const T *__restrict__ G, int64_t stride,
-                                                       int32_t n, int32_t nt, int32_t splits, int64_t split_rows,
-                                                       float *__restrict__ out, int64_t out_split) {
+                                                       int32_t n, int32_t nt, uint32_t tiles, uint32_t wgs,
+                                                       int64_t split_rows, float *__restrict__ out,
+                                                       int64_t out_split) {
   constexpr int TERMS = terms<T>();
   constexpr int NJ = TN / 32;                              // 16-column products per wave
   constexpr int GC = 4 / sizeof(T), GU = TN / (32 * GC);  // G: columns (one word) and units of 8 rows per thread
   __shared__ __align__(16) bf16 sx[kTileC * kRows];
   __shared__ __align__(16) bf16 sg[TERMS][TN * kRows];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r16 = lane & 15, g4 = lane >> 4;
+  if (workgroup() >= wgs) return;
   // a split's tiles, which read the same rows, run on one XCD
-  const uint32_t tiles = gridDim.x / (uint32_t)splits, at = xcd_place(blockIdx.x, gridDim.x);
+  const uint32_t at = xcd_place(workgroup(), wgs);
   const int32_t split = at / tiles, tile = at % tiles;
   const int32_t ct = tile / nt, c0 = ct * kTileC, n0 = (tile % nt) * TN;
   const int64_t r0 = (int64_t)split * split_rows;
@@ -283,9 +285,9 @@ int gradient(const sd_packed_t *X, const void *G, int64_t n, int64_t stride, flo
   auto *kernel = k_gradient<T, FMT, 64>;
   if constexpr (sizeof(T) == 2)
     if (p.tn == 128) kernel = k_gradient<T, FMT, 128>;
-  hipLaunchKernelGGL(kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, s, X->codes, X->scales, X->ld,
-                     X->rows, (int32_t)X->cols, static_cast<const T *>(G), stride, (int32_t)n, p.nt, p.splits,
-                     p.split_rows, out, size);
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, X->codes, X->scales, X->ld,
+                     X->rows, (int32_t)X->cols, static_cast<const T *>(G), stride, (int32_t)n, p.nt,
+                     (uint32_t)p.tiles, (uint32_t)wgs, p.split_rows, out, size);
   if (p.splits > 1) {
     const int64_t join = ceil_div(size, kJoinOut);
     hipLaunchKernelGGL(k_gradient_join, dim3((uint32_t)(join < 65536 ? join : 65536)), dim3(kJoinOut * kJoinWays), 0,

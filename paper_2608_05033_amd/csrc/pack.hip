@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kThreads) void k_pack(const T *__restrict__ x, int6
                                                    int64_t ld, uint8_t *__restrict__ scales) {
   constexpr int V = 16 / sizeof(T), LANES = kBlock / V, GROUPS = kThreads / LANES;
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
-  const int64_t first = (int64_t)blockIdx.x * (GROUPS * kUnroll);
+  const int64_t first = (int64_t)workgroup() * (GROUPS * kUnroll);
   const int64_t r0 = first / nb;
   const uint32_t b0 = (uint32_t)(first - r0 * nb);
   float v[kUnroll][V];
@@ -102,7 +102,7 @@ template <typename T, int FMT>
 __global__ __launch_bounds__(kThreads) void k_unpack(const uint8_t *__restrict__ codes, int64_t ld,
                                                      const uint8_t *__restrict__ scales, int64_t rows, int32_t cols,
                                                      int32_t quads, T *__restrict__ y, int64_t row_stride) {
-  const int64_t first = (int64_t)blockIdx.x * (kThreads * kUnroll);
+  const int64_t first = (int64_t)workgroup() * (kThreads * kUnroll);
   const int64_t r0 = first / quads;
   const uint32_t q0 = (uint32_t)(first - r0 * quads);
   uint32_t w[kUnroll];
@@ -143,7 +143,7 @@ int pack_as(const T *x, int64_t row_stride, int64_t col_stride, const sd_packed_
   const int64_t nb = blocks_of(out->cols), wgs = ceil_div(out->rows * nb, per_wg);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   auto *kernel = col_stride == 1 ? k_pack<T, FMT, true> : k_pack<T, FMT, false>;
-  hipLaunchKernelGGL(kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, s, x, row_stride, col_stride, out->rows,
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, x, row_stride, col_stride, out->rows,
                      (int32_t)out->cols, (int32_t)nb, out->codes, out->ld, out->scales);
   return launched();
 }
@@ -159,7 +159,7 @@ int unpack_as(const sd_packed_t *x, void *y, int64_t row_stride, hipStream_t s) 
   const int64_t quads = ceil_div(x->cols, 4), wgs = ceil_div(x->rows * quads, kThreads * kUnroll);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   auto *kernel = x->format == SD_PACK_E4M3 ? k_unpack<T, SD_PACK_E4M3> : k_unpack<T, SD_PACK_E5M2>;
-  hipLaunchKernelGGL(kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, s, x->codes, x->ld, x->scales, x->rows,
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, x->codes, x->ld, x->scales, x->rows,
                      (int32_t)x->cols, (int32_t)quads, static_cast<T *>(y), row_stride);
   return launched();
 }

@@ -159,8 +159,9 @@ __global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
                                                                          int32_t k16, int32_t nb, int32_t nt) {
   __shared__ f32x4 part[KW][MF * NF][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int64_t m0 = (int64_t)(blockIdx.x / (uint32_t)nt) * (MF * 16);
-  const int64_t n0 = (int64_t)(blockIdx.x % (uint32_t)nt) * (NF * 16);
+  const int64_t m0 = (int64_t)(workgroup() / (uint32_t)nt) * (MF * 16);
+  const int64_t n0 = (int64_t)(workgroup() % (uint32_t)nt) * (NF * 16);
+  if (m0 >= X.rows) return;
   f32x4 acc[MF][NF] = {};
   int64_t xrow[MF], wrow[NF];  // rows past the last read the last one
 #pragma unroll
@@ -248,7 +249,9 @@ __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand
   __shared__ __align__(16) uint8_t scales_a[16][ROWS / 16], scales_b[16][ROWS / 16];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = lane & 15, g = lane >> 4;
   const int wm = wave / WN, wn = wave % WN;
-  const uint32_t at = xcd_place(blockIdx.x, gridDim.x);
+  const uint32_t tiles = (uint32_t)mt * (uint32_t)nt;
+  if (workgroup() >= tiles) return;
+  const uint32_t at = xcd_place(workgroup(), tiles);
   // tiles in bands of 8 along m: neighbours in the list share X's and W's rows
   const uint32_t band = at / (8u * nt), left = mt - band * 8u < 8u ? mt - band * 8u : 8u;
   const uint32_t in_band = at - band * 8u * nt;
@@ -466,7 +469,7 @@ int rows_launch(const Operand &x, const Operand &w, const float *bias, T *y, int
   static_assert(MF <= KW, "a wave for each row group");
   const int64_t nt = ceil_div(w.rows, NF * 16), wgs = ceil_div(x.rows, MF * 16) * nt;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL((k_product_rows<T, XF, WF, MF, NF, KW>), dim3((uint32_t)wgs), dim3(KW * 64), 0, s, x, w, bias,
+  hipLaunchKernelGGL((k_product_rows<T, XF, WF, MF, NF, KW>), grid_of(wgs), dim3(KW * 64), 0, s, x, w, bias,
                      y, stride, k16, nb, (int32_t)nt);
   return launched();
 }
@@ -476,7 +479,7 @@ int tile_launch(const Operand &x, const Operand &w, const float *bias, T *y, int
                 hipStream_t s) {
   const int64_t mt = ceil_div(x.rows, BM), nt = ceil_div(w.rows, BN);
   if (mt * nt > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL((k_product_tile<T, XF, WF, BM, BN, WM, WN>), dim3((uint32_t)(mt * nt)), dim3(WM * WN * 64), 0, s,
+  hipLaunchKernelGGL((k_product_tile<T, XF, WF, BM, BN, WM, WN>), grid_of(mt * nt), dim3(WM * WN * 64), 0, s,
                      x, w, bias, y, stride, k16, nb, (int32_t)mt, (int32_t)nt);
   return launched();
 }
