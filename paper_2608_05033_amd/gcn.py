@@ -109,16 +109,25 @@ class GCN2(torch.nn.Module):
 
 
 class _PackedTransform(torch.autograd.Function):
-    """X.W from X in 8 bits; the gradient with respect to W alone."""
+    """X.W from X in 8 bits, packed here where it is a float tensor.  That one has a
+    gradient too, as if the packing did not round: the output gradient, multiplied
+    in 8 bits."""
 
     @staticmethod
-    def forward(ctx, X8: dense.Packed, W):
-        ctx.X8 = X8
-        return dense.product(X8, dense.pack(W, X8.format, transpose=True))
+    def forward(ctx, X, W, fmt, grad_fmt):
+        ctx.X8 = X if isinstance(X, dense.Packed) else dense.pack(X, fmt)
+        if ctx.needs_input_grad[0]:
+            ctx.dtype, ctx.grad_fmt = X.dtype, grad_fmt
+            ctx.save_for_backward(W)
+        return dense.product(ctx.X8, dense.pack(W, ctx.X8.format, transpose=True))
 
     @staticmethod
     def backward(ctx, dZ):
-        return None, dense.weight_gradient(ctx.X8, dZ.contiguous())
+        dX, dZ = None, dZ.contiguous()
+        if ctx.needs_input_grad[0]:
+            W, = ctx.saved_tensors
+            dX = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, ctx.X8.format), dtype=ctx.dtype)
+        return dX, dense.weight_gradient(ctx.X8, dZ), None, None
 
 
 class _NormTransform(torch.autograd.Function):
@@ -147,8 +156,9 @@ class _NormTransform(torch.autograd.Function):
 class GCN2Packed(torch.nn.Module):
     """H1 = act(group norm(Â X W1)), logits = Â H1 W2 with the node tables in 8 bits.
 
-    X is given as a float tensor or, since it does not change between epochs,
-    once packed by `dense.pack(X, model.format)`.  format: of features,
+    X is given as a float tensor, which has a gradient if it requires one, or,
+    since it does not change between epochs, once packed by
+    `dense.pack(X, model.format)`.  format: of features,
     activations and weights; grad_format: of the output gradient where it is
     multiplied by the weights."""
 
@@ -164,8 +174,7 @@ class GCN2Packed(torch.nn.Module):
         self.format, self.grad_format = format, grad_format
 
     def forward(self, X) -> torch.Tensor:
-        X8 = X if isinstance(X, dense.Packed) else dense.pack(X, self.format)
-        A1 = self.agg(_PackedTransform.apply(X8, self.W1))
+        A1 = self.agg(_PackedTransform.apply(X, self.W1, self.format, self.grad_format))
         Z2 = _NormTransform.apply(A1, self.gamma, self.beta, self.W2, self.groups, self.eps, self.activation,
                                   self.format, self.grad_format)
         return self.agg(Z2)

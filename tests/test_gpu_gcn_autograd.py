@@ -1,0 +1,71 @@
+"""What autograd makes of the GCN with 8-bit node tables: the features' gradient,
+second derivatives, tables changed under way, parameters that stand still."""
+import pytest
+
+import gen
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover - CPU container
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import scipy.sparse  # noqa: E402
+
+from paper_2608_05033_amd import dense, gcn  # noqa: E402
+
+IN, HIDDEN, CLASSES, GROUPS = 48, 32, 8, 4
+
+
+@pytest.fixture(scope="module")
+def case():
+    A = gen.rmat(10, 12000, nmax=1000, seed=3)
+    X = torch.from_numpy(gen.dense_normal(A.m, IN, seed=1)).cuda()
+    R = torch.from_numpy(gen.dense_normal(A.m, CLASSES, seed=2)).cuda()
+    model = gcn.GCN2Packed(A, IN, HIDDEN, CLASSES, device="cuda", seed=5, groups=GROUPS, activation="silu")
+    yield A, X, R, model
+    model.agg.destroy()
+
+
+def grads(model, X, R):
+    """Gradients of sum(logits R): the parameters', by name, and the features'."""
+    for p in model.parameters():
+        p.grad = None
+    (model(X) * R).sum().backward()
+    out = {name: None if p.grad is None else p.grad.clone() for name, p in model.named_parameters()}
+    out["X"] = X.grad if isinstance(X, torch.Tensor) else None
+    return out
+
+
+# ------------------------------------------------------ features' gradient ---
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_features_have_a_gradient(case, dtype):
+    """Against the 64-bit network without roundings: a value rounded to 4 significant
+    bits moves by 2.6 % rms at most, and this gradient goes through six such tables
+    (X, A1, H1, two output gradients, two weights), so it stays within 0.15 in
+    2-norm, as the parameters' do."""
+    A, X, R, model = case
+    X = X.to(dtype, copy=True).requires_grad_()
+    got = grads(model, X, R)["X"]
+    assert got.dtype == dtype and got.shape == X.shape
+
+    dense_A = torch.from_numpy(scipy.sparse.csr_matrix((A.values, A.colidx, A.rowptr), shape=(A.m, A.k)).toarray()).double()
+    x = X.detach().double().cpu().requires_grad_()
+    p = {k: v.detach().double().cpu() for k, v in model.named_parameters()}
+    v = (dense_A @ (x @ p["W1"])).view(A.m, GROUPS, -1)
+    mean = v.mean((0, 2), keepdim=True)
+    xh = (v - mean) / torch.sqrt(((v - mean) ** 2).mean((0, 2), keepdim=True) + model.eps)
+    z = xh.reshape(A.m, HIDDEN) * p["gamma"] + p["beta"]
+    ((dense_A @ ((z * torch.sigmoid(z)) @ p["W2"])) * R.double().cpu()).sum().backward()
+    assert (got.double().cpu() - x.grad).norm() <= 0.15 * x.grad.norm()
+
+
+def test_parameters_gradients_do_not_depend_on_the_features(case):
+    """The same bits with features that require a gradient, that do not, and packed."""
+    _, X, R, model = case
+    first = grads(model, X.clone().requires_grad_(), R)
+    for other in (X, dense.pack(X, model.format)):
+        again = grads(model, other, R)
+        assert again["X"] is None
+        for name, _ in model.named_parameters():
+            assert torch.equal(again[name], first[name]), name
