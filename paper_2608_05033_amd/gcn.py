@@ -18,6 +18,8 @@ symmetric).  Plans are built once per (graph, width) and reused every epoch.
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import Plan, dense, sd_plan_device, sd_plan_ex, sd_spmm
@@ -108,10 +110,38 @@ class GCN2(torch.nn.Module):
         return self.agg(H1 @ self.W2)
 
 
+class _FirstOnly(torch.autograd.Function):
+    """A gradient as it is; asking for its derivative is an error."""
+
+    @staticmethod
+    def forward(ctx, g, anchor):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, dg):
+        raise RuntimeError("GCN2Packed has no second derivatives: its kernels' gradients are not recorded")
+
+
+def _first_derivatives_only(backward):
+    """A backward pass through kernels: where a graph of it is asked for
+    (create_graph), its results lead to an error and not to a part that is missing."""
+
+    @functools.wraps(backward)
+    def wrapped(ctx, dZ):
+        with torch.no_grad():
+            grads = backward(ctx, dZ)
+        if not torch.is_grad_enabled():
+            return grads
+        anchor = dZ.new_empty(0).requires_grad_()
+        return tuple(g if g is None else _FirstOnly.apply(g, anchor) for g in grads)
+
+    return wrapped
+
+
 class _PackedTransform(torch.autograd.Function):
     """X.W from X in 8 bits, packed here where it is a float tensor.  That one has a
     gradient too, as if the packing did not round: the output gradient, multiplied
-    in 8 bits."""
+    in 8 bits.  There are no second derivatives."""
 
     @staticmethod
     def forward(ctx, X, W, fmt, grad_fmt):
@@ -122,6 +152,7 @@ class _PackedTransform(torch.autograd.Function):
         return dense.product(ctx.X8, dense.pack(W, ctx.X8.format, transpose=True))
 
     @staticmethod
+    @_first_derivatives_only
     def backward(ctx, dZ):
         dX, dZ = None, dZ.contiguous()
         if ctx.needs_input_grad[0]:
@@ -132,7 +163,8 @@ class _PackedTransform(torch.autograd.Function):
 
 class _NormTransform(torch.autograd.Function):
     """act(group norm(A)).W.  A and the activation are kept in 8 bits, and the
-    output gradient is multiplied in 8 bits for dA, in full for dW."""
+    output gradient is multiplied in 8 bits for dA, in full for dW.  There are no second
+    derivatives."""
 
     @staticmethod
     def forward(ctx, A, gamma, beta, W, groups, eps, activation, fmt, grad_fmt):
@@ -142,6 +174,7 @@ class _NormTransform(torch.autograd.Function):
         return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True))
 
     @staticmethod
+    @_first_derivatives_only
     def backward(ctx, dZ):
         out, dZ = ctx.kept, dZ.contiguous()
         W, gamma, beta = ctx.saved_tensors

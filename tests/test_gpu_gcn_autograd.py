@@ -69,3 +69,19 @@ def test_parameters_gradients_do_not_depend_on_the_features(case):
         assert again["X"] is None
         for name, _ in model.named_parameters():
             assert torch.equal(again[name], first[name]), name
+
+
+# ----------------------------------------------------- second derivatives ---
+@pytest.mark.parametrize("loss", [lambda y, R: (y * R).sum(), lambda y, R: y.square().sum()], ids=["linear", "square"])
+@pytest.mark.parametrize("of", ["W1", "gamma", "W2", "X"])
+def test_second_derivatives_are_refused(case, of, loss):
+    """The kernels' gradients have no derivatives of their own: asking for them
+    beside others that are there is an error, not a sum without those terms."""
+    _, X, R, model = case
+    X = X.clone().requires_grad_()
+    v = X if of == "X" else getattr(model, of)
+    g, = torch.autograd.grad(loss(model(X), R), v, create_graph=True)
+    plain, = torch.autograd.grad(loss(model(X), R), v)
+    assert torch.equal(g, plain)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        (g.square().sum() + v.square().sum()).backward()
