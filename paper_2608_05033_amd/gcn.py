@@ -145,20 +145,24 @@ class _PackedTransform(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, X, W, fmt, grad_fmt):
-        ctx.X8 = X if isinstance(X, dense.Packed) else dense.pack(X, fmt)
+        X8 = X if isinstance(X, dense.Packed) else dense.pack(X, fmt)
+        ctx.of_table = X8.cols, X8.format
+        kept = [X8.codes, X8.scales]
         if ctx.needs_input_grad[0]:
             ctx.dtype, ctx.grad_fmt = X.dtype, grad_fmt
-            ctx.save_for_backward(W)
-        return dense.product(ctx.X8, dense.pack(W, ctx.X8.format, transpose=True))
+            kept.append(W)
+        ctx.save_for_backward(*kept)
+        return dense.product(X8, dense.pack(W, X8.format, transpose=True))
 
     @staticmethod
     @_first_derivatives_only
     def backward(ctx, dZ):
         dX, dZ = None, dZ.contiguous()
+        codes, scales, *rest = ctx.saved_tensors
+        X8 = dense.Packed(codes, scales, *ctx.of_table)
         if ctx.needs_input_grad[0]:
-            W, = ctx.saved_tensors
-            dX = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, ctx.X8.format), dtype=ctx.dtype)
-        return dX, dense.weight_gradient(ctx.X8, dZ), None, None
+            dX = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(rest[0], X8.format), dtype=ctx.dtype)
+        return dX, dense.weight_gradient(X8, dZ), None, None
 
 
 class _NormTransform(torch.autograd.Function):
@@ -169,20 +173,21 @@ class _NormTransform(torch.autograd.Function):
     @staticmethod
     def forward(ctx, A, gamma, beta, W, groups, eps, activation, fmt, grad_fmt):
         out = dense.group_norm(A, groups, gamma, beta, eps, activation, keep=fmt, pack_y=fmt, dense_y=False)
-        ctx.kept, ctx.args, ctx.grad_fmt = out, (groups, eps, activation), grad_fmt
-        ctx.save_for_backward(W, gamma, beta)
+        ctx.of_table, ctx.args, ctx.grad_fmt = (out.x.cols, fmt), (groups, eps, activation), grad_fmt
+        ctx.save_for_backward(W, gamma, beta, out.x.codes, out.x.scales, out.y_packed.codes, out.y_packed.scales,
+                              out.mean, out.rstd)
         return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True))
 
     @staticmethod
     @_first_derivatives_only
     def backward(ctx, dZ):
-        out, dZ = ctx.kept, dZ.contiguous()
-        W, gamma, beta = ctx.saved_tensors
+        dZ = dZ.contiguous()
+        W, gamma, beta, *A8, codes, scales, mean, rstd = ctx.saved_tensors
+        A8, H8 = dense.Packed(*A8, *ctx.of_table), dense.Packed(codes, scales, *ctx.of_table)
         groups, eps, activation = ctx.args
-        dW = dense.weight_gradient(out.y_packed, dZ)
-        dH = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, out.y_packed.format))
-        dA, dgamma, dbeta = dense.group_norm_backward(dH, out.x, out.mean, out.rstd, groups, gamma, beta, eps,
-                                                       activation)
+        dW = dense.weight_gradient(H8, dZ)
+        dH = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, H8.format))
+        dA, dgamma, dbeta = dense.group_norm_backward(dH, A8, mean, rstd, groups, gamma, beta, eps, activation)
         return dA, dgamma, dbeta, dW, None, None, None, None, None
 
 

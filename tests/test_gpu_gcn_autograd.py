@@ -85,3 +85,34 @@ def test_second_derivatives_are_refused(case, of, loss):
     assert torch.equal(g, plain)
     with pytest.raises(RuntimeError, match="second derivatives"):
         (g.square().sum() + v.square().sum()).backward()
+
+
+# ------------------------------------------------- tables changed under way ---
+@pytest.mark.parametrize("part", ["codes", "scales"])
+def test_a_packed_table_written_between_the_passes_is_noticed(case, part):
+    """The backward pass reads the features once more; written in between, they are
+    not what the forward pass read, and autograd says so as for any tensor."""
+    _, X, R, model = case
+    X8 = dense.pack(X, model.format)
+    loss = (model(X8) * R).sum()
+    getattr(X8, part).zero_()
+    with pytest.raises(RuntimeError, match="inplace operation"):
+        loss.backward()
+
+
+def test_kept_tables_go_through_autograds_hooks(case):
+    """Kept tables moved to the host between the passes, as torch's own hook does it,
+    give the same gradients."""
+    _, X, R, model = case
+    want = grads(model, X.clone().requires_grad_(), R)
+    seen = []
+
+    def away(t):
+        seen.append(t.dtype)
+        return t.device, t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(away, lambda kept: kept[1].to(kept[0])):
+        got = grads(model, X.clone().requires_grad_(), R)
+    assert seen.count(torch.uint8) == 6
+    for name, g in want.items():
+        assert torch.equal(got[name], g), name
