@@ -157,12 +157,14 @@ class _PackedTransform(torch.autograd.Function):
     @staticmethod
     @_first_derivatives_only
     def backward(ctx, dZ):
-        dX, dZ = None, dZ.contiguous()
+        dX, dW, dZ = None, None, dZ.contiguous()
         codes, scales, *rest = ctx.saved_tensors
         X8 = dense.Packed(codes, scales, *ctx.of_table)
         if ctx.needs_input_grad[0]:
             dX = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(rest[0], X8.format), dtype=ctx.dtype)
-        return dX, dense.weight_gradient(X8, dZ), None, None
+        if ctx.needs_input_grad[1]:
+            dW = dense.weight_gradient(X8, dZ)
+        return dX, dW, None, None
 
 
 class _NormTransform(torch.autograd.Function):
@@ -185,9 +187,12 @@ class _NormTransform(torch.autograd.Function):
         W, gamma, beta, *A8, codes, scales, mean, rstd = ctx.saved_tensors
         A8, H8 = dense.Packed(*A8, *ctx.of_table), dense.Packed(codes, scales, *ctx.of_table)
         groups, eps, activation = ctx.args
-        dW = dense.weight_gradient(H8, dZ)
-        dH = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, H8.format))
-        dA, dgamma, dbeta = dense.group_norm_backward(dH, A8, mean, rstd, groups, gamma, beta, eps, activation)
+        dA = dgamma = dbeta = dW = None
+        if ctx.needs_input_grad[3]:
+            dW = dense.weight_gradient(H8, dZ)
+        if any(ctx.needs_input_grad[:3]):
+            dH = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(W, H8.format))
+            dA, dgamma, dbeta = dense.group_norm_backward(dH, A8, mean, rstd, groups, gamma, beta, eps, activation)
         return dA, dgamma, dbeta, dW, None, None, None, None, None
 
 

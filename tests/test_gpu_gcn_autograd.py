@@ -116,3 +116,34 @@ def test_kept_tables_go_through_autograds_hooks(case):
     assert seen.count(torch.uint8) == 6
     for name, g in want.items():
         assert torch.equal(got[name], g), name
+
+
+# --------------------------------------------- parameters that stand still ---
+@pytest.mark.parametrize("still,calls", [(["W1"], {"weight_gradient": 1, "group_norm_backward": 1}),
+                                         (["W2"], {"weight_gradient": 1, "group_norm_backward": 1}),
+                                         (["W1", "gamma", "beta"], {"weight_gradient": 1, "group_norm_backward": 0}),
+                                         (["W1", "W2", "beta"], {"weight_gradient": 0, "group_norm_backward": 1})])
+def test_gradients_that_nobody_needs_are_not_computed(case, still, calls, monkeypatch):
+    """The others keep their bits."""
+    _, X, R, model = case
+    want = grads(model, X, R)
+    counted = dict.fromkeys(calls, 0)
+
+    def counting(name, call):
+        def counted_call(*args, **kw):
+            counted[name] += 1
+            return call(*args, **kw)
+        return counted_call
+
+    for name in calls:
+        monkeypatch.setattr(dense, name, counting(name, getattr(dense, name)))
+    try:
+        for name in still:
+            getattr(model, name).requires_grad_(False)
+        got = grads(model, X, R)
+    finally:
+        for p in model.parameters():
+            p.requires_grad_(True)
+    assert counted == calls
+    for name, _ in model.named_parameters():
+        assert got[name] is None if name in still else torch.equal(got[name], want[name]), name
