@@ -934,6 +934,7 @@ int check(const sd_norm_t *d) {
       !(d->eps >= 0.0f))
     return SD_ERR_INVALID_VALUE;
   if (d->channels % d->groups != 0) return SD_ERR_INVALID_VALUE;
+  if (!aligned_to(d->offsets, 4) || !aligned_to(d->weight, 4) || !aligned_to(d->bias, 4)) return SD_ERR_INVALID_VALUE;
   if (d->rows > kMaxRows || d->segments > kMaxRows || d->channels > (1 << 24)) return SD_ERR_OVERFLOW;
   if (!d->offsets && d->rows > 0 && (d->segments < 1 || d->rows % d->segments != 0)) return SD_ERR_INVALID_VALUE;
   if (d->offsets && d->rows > 0 && d->segments < 1) return SD_ERR_INVALID_VALUE;
@@ -1166,6 +1167,7 @@ extern "C" int sd_group_norm(const sd_norm_t *d, const void *x, int64_t x_stride
   if ((st = check_copy(d, x_packed)) != SD_OK || (st = check_copy(d, y_packed)) != SD_OK) return st;
   if (!y && !y_packed && d->rows > 0) return SD_ERR_INVALID_VALUE;
   if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
+  if (!aligned_to(mean, 4) || !aligned_to(rstd, 4)) return SD_ERR_INVALID_VALUE;
   const Shape p = shape_of(d, false);
   if (bytes < stats_bytes(p) || (stats_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
     return SD_ERR_INVALID_VALUE;
@@ -1192,6 +1194,8 @@ extern "C" int sd_group_norm_backward(const sd_norm_t *d, const void *dy, int64_
   if (!x_packed && (st = check_table(x, d->type, d->rows, d->channels, x_stride)) != SD_OK) return st;
   if (x && x_packed) return SD_ERR_INVALID_VALUE;
   if (d->segments > 0 && (!mean || !rstd)) return SD_ERR_INVALID_VALUE;
+  if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned_to(dweight, 4) || !aligned_to(dbias, 4))
+    return SD_ERR_INVALID_VALUE;
   const Shape p = shape_of(d, true);
   if (bytes < back_bytes(p) || (back_bytes(p) > 0 && (!workspace || !aligned_to(workspace, 16))))
     return SD_ERR_INVALID_VALUE;
