@@ -520,13 +520,15 @@ int sd_pack(const void *x, int32_t type, int64_t row_stride, int64_t col_stride,
 int sd_unpack(const sd_packed_t *x, void *y, int32_t type, int64_t row_stride, void *stream);
 
 /* Y[m, n] = sum over k of X(m, k) W(n, k), + bias[n] if bias is not null; X and W
- * have the same cols.  Sums in 32 bits, rounded once to Y's type. */
+ * have the same cols.  Sums in 32 bits, rounded once to Y's type.  The tables'
+ * numbers are multiplied as bf16, which holds them down to multiples of 2^-133:
+ * all of a block whose scale is 2^-124 (e4m3), 2^-117 (e5m2) or more. */
 int sd_pack_product(const sd_packed_t *X, const sd_packed_t *W, const float *bias, void *Y, int32_t type,
                     int64_t row_stride, void *stream);
 
 /* dW[c, n] (fp32, contiguous) = sum over r of X(r, c) G[r, n]: the weight
- * gradient from activations kept in 8 bits.  G is used in full (no rounding);
- * sums in 32 bits.  _size: the workspace in bytes. */
+ * gradient from activations kept in 8 bits.  G is used in full, X and G down to
+ * multiples of 2^-133; sums in 32 bits.  _size: the workspace in bytes. */
 int sd_pack_gradient_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes);
 int sd_pack_gradient(const sd_packed_t *X, const void *G, int32_t type, int64_t n, int64_t row_stride, float *dW,
                      void *workspace, size_t bytes, void *stream);

@@ -3,10 +3,11 @@
 // The sum runs over the rows, so both operands are needed with neighbouring
 // rows in one register: a thread reads the same columns of eight rows and
 // writes them as eight consecutive 16-bit values of one column to shared memory.
-// Codes become bf16 with their scale, which is exact (at most 4 significant
-// bits times a power of two).  G in bf16 is used as it is; f16 and f32 are cut
-// into two and three bf16 terms (8 significant bits each), which hold all of
-// the 11 and 24 bits, and v_mfma_f32_16x16x32_bf16 sums the products in 32 bits.
+// Codes become bf16 with their scale (at most 4 significant bits times a power of
+// two).  G in bf16 is used as it is; f16 and f32 are cut into two and three bf16
+// terms (8 significant bits each), which hold all of the 11 and 24 bits, and
+// v_mfma_f32_16x16x32_bf16 sums the products in 32 bits.  All of that is exact as
+// far as bf16 reaches, down to multiples of 2^-133.
 // Workgroups share a tile's rows; their sums go to the workspace and a second
 // kernel adds them in a fixed order.
 // 262144 x 128 codes with 64 columns of fp32 take 28 us and the join 4: 3.7 TB/s,

@@ -93,3 +93,31 @@ def test_error_before_the_rounding(rows, n, dtype):
     left = dense.product(X, W, bias, TYPES[dtype]).double().cpu().numpy()
     err = left - (want + bias.double().cpu().numpy())
     assert np.linalg.norm(err) <= 1e-6 * np.linalg.norm(np.broadcast_to(want, err.shape))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("power", [-100, -118, -126, -133, -140])
+def test_numbers_at_the_end_of_bf16(power, fmt, dtype):
+    """Tables of tiny numbers times large ones: a number of the table is off by at most
+    half of 2^-133, the least one of bf16, and by nothing where it is a multiple."""
+    g = np.random.default_rng(-power)
+    X, x64 = packed(g.standard_normal((40, 200)) * 2.0 ** power, fmt)
+    W, w64 = packed(g.standard_normal((30, 200)) * 2.0 ** 110)
+    held = np.round(x64 / 2.0 ** -133) * 2.0 ** -133  # to nearest, ties to even
+    if power >= (-110 if fmt == "e4m3" else -100):
+        assert np.array_equal(held, x64)
+    want, size = held @ w64.T, np.abs(held) @ np.abs(w64).T
+    got = dense.product(X, W, dtype=TYPES[dtype]).double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= 202 * 2.0 ** -24 * size + HALF_ULP[dtype] * 1.001 * np.abs(want))
+
+
+@pytest.mark.parametrize("power", [-100, -118, -126, -133])
+def test_gradients_of_tiny_numbers(power):
+    """G of fp32 is cut into terms of bf16: what is under 2^-133 is left out of a number."""
+    g = np.random.default_rng(-power)
+    X, x64 = packed(g.standard_normal((300, 20)) * 2.0 ** 100)
+    G = (g.standard_normal((300, 24)) * 2.0 ** power).astype(np.float32)
+    got = dense.weight_gradient(X, torch.from_numpy(G).cuda()).double().cpu().numpy()
+    want, size = x64.T @ G.astype(np.float64), np.abs(x64).T @ np.abs(G.astype(np.float64))
+    assert np.all(np.abs(got - want) <= (300 / 16 + 64) * 2.0 ** -24 * size + np.abs(x64).sum(0)[:, None] * 2.0 ** -133)
