@@ -12,13 +12,14 @@
 // and channel, one joins them per segment and group in 64 bits, one applies the
 // result, chunks in reverse so that what the first pass read last is still in
 // the Infinity Cache.  Bound by the bytes moved: x is read twice and written once.
-// 2400000 x 128 fp32, 8-bit copy kept: sums 206 us, apply 561 us (4.9 TB/s); backward
-// 287 us and 562 us.
+// 2400000 x 128 fp32, 8-bit copy kept: sums 208 us, apply 559 us (4.9 TB/s); backward
+// 289 us and 561 us.
 //
 // Short segments take one launch instead: a team of threads holds a segment's
 // rows in registers, adds them up in shared memory and applies the result.  100003
-// rows of 96 bf16 in 3001 segments take 33 us, bound by the 64-bit sums, the joins
-// between lanes and the activation; 37 rows of 64 fp32 take 5.5 us.
+// rows of 96 bf16 in 3001 segments take 36 us: three workgroups fit a compute unit,
+// so there are four rounds of some 9 us, each a chain of offsets, rows, two joins and
+// the stores, which few waves hide.  37 rows of 64 fp32 take 6 us.
 //
 // Every sum has a fixed order: results do not change from run to run.
 #include "dense.h"
@@ -29,7 +30,7 @@ using namespace dense;
 
 constexpr int kThreads = 256;
 constexpr int V = 4;         // channels per lane
-constexpr int kBatch = 4;    // rows of a lane in flight: eight waves per SIMD fit the registers
+constexpr int kBatch = 4;    // rows of a lane in flight: 4 (backward sums) to 8 waves per SIMD fit the registers
 
 // What every kernel needs of the call.
 struct Shape {
@@ -630,7 +631,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_grad(Shape p, X x, Dense<cons
 // ------------------------------------------------------ short segments -----
 constexpr int kHeld = 8;  // rows of a lane that stay in registers
 // Waves a SIMD: without the limit the compiler takes registers for two, and 100003 rows
-// of 96 bf16 in 3001 segments take 43 us instead of 34.
+// of 96 bf16 in 3001 segments take 43 us a call instead of 34.
 constexpr int kTeamWaves = 3;
 
 template <int N>
