@@ -14,6 +14,8 @@ namespace dense {
 
 typedef __bf16 bf16;
 typedef _Float16 f16;
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -121,6 +123,17 @@ __device__ inline void decode4(uint32_t w, float (&out)[4]) {
   out[1] = lo[1];
   out[2] = hi[0];
   out[3] = hi[1];
+}
+
+// Two of w's codes, the lower or the upper ones, times the scale s.
+template <int FMT>
+__device__ inline bf16x2 to_bf16(uint32_t w, float s, bool hi) {
+  if constexpr (FMT == SD_PACK_E4M3)
+    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
+              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
+  else
+    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true)
+              : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
 }
 
 // v of another lane: quad_perm and mirror forms of the data-parallel primitives.

@@ -19,9 +19,6 @@ namespace {
 
 using namespace dense;
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
 constexpr int kThreads = 256;
 constexpr int kRows = 64;   // rows of a step
 constexpr int kTileC = 128; // columns of X per tile: one block, so one scale a row
@@ -29,16 +26,6 @@ constexpr int kTileC = 128; // columns of X per tile: one block, so one scale a 
 template <typename T>
 constexpr int terms() {
   return sizeof(T) == 4 ? 3 : __is_same(T, f16) ? 2 : 1;
-}
-
-template <int FMT>
-__device__ inline bf16x2 to_bf16(uint32_t w, float s, bool hi) {
-  if constexpr (FMT == SD_PACK_E4M3)
-    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
-              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
-  else
-    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true)
-              : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
 }
 
 // v without its leading 8 significant bits (the upper half of its 32), which is

@@ -23,23 +23,11 @@ namespace {
 using namespace dense;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 struct Operand {
   const uint8_t *codes, *scales;
   int64_t ld, rows;
 };
-
-template <int FMT>
-__device__ inline bf16x2 to_bf16(uint32_t w, float s, bool hi) {
-  if constexpr (FMT == SD_PACK_E4M3)
-    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true)
-              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false);
-  else
-    return hi ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, true)
-              : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, s, false);
-}
 
 // 32 codes of one row in a block, and the block's scale byte.
 struct Frag {
@@ -236,7 +224,7 @@ __global__ __launch_bounds__(KW * 64) void k_product_rows(Operand X, Operand W,
 // the mixing is done on the memory side, since a wave's 64 lanes write 1 KiB in
 // order.  Scale bytes lie by lane, the tile's 16-row groups side by side, so one
 // read serves all of a lane's products.  Bound by the matrix units and the
-// conversions to bf16: 8192 cubed in 800 to 890 us, 1.3 PFLOP/s.
+// conversions to bf16: 8192 cubed in 760 to 890 us, 1.3 PFLOP/s.
 template <typename T, int XF, int WF, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(WM *WN * 64) void k_product_tile(Operand X, Operand W, const float *__restrict__ bias,
                                                               T *__restrict__ Y, int64_t stride, int32_t k16,
