@@ -576,6 +576,86 @@ int sd_group_norm_backward(const sd_norm_t *d, const void *dy, int64_t dy_stride
                            int64_t dx_stride, float *dweight, float *dbias, void *workspace, size_t bytes,
                            void *stream);
 
+/* ------------------------------------------------------- 4-bit tables --- */
+/* A rows x cols table in 4 bits.  Element (r, c) stands for
+ *   e2m1(half c % 2 of codes[r * ld + c / 2], the lower half first)
+ *     * 2^(scales[((c / 128) * rows + r) * 4 + c / 32 % 4] - 127).
+ * e2m1 holds 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 to 7) and their negatives (8 to
+ * 15).  A scale byte of 255 makes its whole block of 32 columns NaN.  Rows are
+ * `ld` bytes apart (a multiple of 16, at least 16 for every 32 columns begun);
+ * codes past cols in the last block of a row are zero.  The rules of the dense
+ * operators above hold for every call below. */
+typedef struct {
+  int64_t rows, cols, ld;
+  int64_t reserved; /* 0 */
+  uint8_t *codes;   /* [rows][ld], 16-byte aligned */
+  uint8_t *scales;  /* [ceil(cols / 128)][rows][4], 4-byte aligned */
+} sd_nibble_t;
+
+/* x (element (r, c) at r * row_stride + c * col_stride; any strides >= 0) into
+ * out's codes and scales; out gives the sizes.  For each row and block of 32
+ * columns the scale is the least power of two with (largest magnitude) <= 6 scale,
+ * 2^-127 at least (1 for a block of zeros); codes are x / scale to nearest, ties to
+ * even.  A block that holds a NaN or an infinity gets scale byte 255 and zero codes. */
+int sd_nibble_pack(const void *x, int32_t type, int64_t row_stride, int64_t col_stride, const sd_nibble_t *out,
+                   void *stream);
+/* The values, rounded once to y's type. */
+int sd_nibble_unpack(const sd_nibble_t *x, void *y, int32_t type, int64_t row_stride, void *stream);
+
+/* Y[m, n] = sum over k of X(m, k) W(n, k), + bias[n] if bias is not null; X and W
+ * have the same cols.  Sums in 32 bits, rounded once to Y's type.  With tables
+ * packed along the rows of a layer this gives its gradients too: dX from G and W^T,
+ * dW from X^T and G^T.  _size: the workspace in bytes. */
+int sd_nibble_product_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes);
+int sd_nibble_product(const sd_nibble_t *X, const sd_nibble_t *W, const float *bias, void *Y, int32_t type,
+                      int64_t row_stride, void *workspace, size_t bytes, void *stream);
+
+/* --------------------------------------------------- rows sorted by expert --- */
+/* k experts (or node types) for each of `rows` rows, as a list of entries (t, j),
+ * j < k, sorted by expert and among one expert's by t, then j.  Entry i < total =
+ * rows * k of the list belongs to expert e for offsets[e] <= i < offsets[e + 1];
+ * place[t * k + j] is the place of entry (t, j) in the list, or -1 where it has no
+ * expert; source[i] is the row t of the list's entry i, -1 from offsets[experts] on. */
+typedef struct {
+  int64_t rows;       /* rows * k below 2^31 */
+  int32_t k, experts; /* experts at most 4095 (SD_ERR_UNSUPPORTED) */
+  int32_t *offsets;   /* [experts + 1] */
+  int32_t *place;     /* [rows * k] */
+  int32_t *source;    /* [rows * k] */
+} sd_route_t;
+
+/* Fills out's arrays from chosen[t * k + j], 4- or 8-byte integers; numbers outside
+ * [0, experts) are no expert.  An expert may be chosen more than once by a row.
+ * _size: the workspace in bytes. */
+int sd_route_size(int64_t rows, int32_t k, int32_t experts, size_t *bytes);
+int sd_route(const void *chosen, int32_t index_bytes, const sd_route_t *out, void *workspace, size_t bytes,
+             void *stream);
+
+/* y[place[t, j]] = x[t]: x [rows][cols] to y [rows * k][cols] in the list's order;
+ * zeros from row offsets[experts] on. */
+int sd_dispatch(const sd_route_t *route, const void *x, int32_t type, int64_t cols, int64_t x_stride, void *y,
+                int64_t y_stride, void *stream);
+/* out[t] = sum over j of weights[t * k + j] y[place[t, j]] (weights null: 1), added
+ * in the order of j in 32 bits and rounded once; entries without an expert add
+ * nothing.  With null weights this is sd_dispatch's gradient. */
+int sd_combine(const sd_route_t *route, const void *y, int32_t type, int64_t cols, int64_t y_stride,
+               const float *weights, void *out, int64_t out_stride, void *stream);
+/* sd_combine's gradients from dout [rows][cols]: dy[place[t, j]] = weights dout[t],
+ * zeros from row offsets[experts] on; dweights[t * k + j] = sum over columns of
+ * dout[t] y[place[t, j]], 0 for entries without an expert.  dy or dweights may be
+ * null; y is read for dweights alone. */
+int sd_combine_backward(const sd_route_t *route, const void *dout, int32_t type, int64_t cols, int64_t dout_stride,
+                        const void *y, int64_t y_stride, const float *weights, void *dy, int64_t dy_stride,
+                        float *dweights, void *stream);
+
+/* The experts' product of 4-bit tables: row i of Y [rows * k][n] is a row of X
+ * through the weights of the list's entry i: Y[i, m] = sum over k of
+ * X(source[i], k) W(e * n + m, k) + bias[e * n + m] (bias may be null), e the
+ * entry's expert; zeros from row offsets[experts] on.  W holds experts * n rows.
+ * sorted = 1: X is in the list's order itself, rows * k of them. */
+int sd_expert_product(const sd_nibble_t *X, const sd_nibble_t *W, const sd_route_t *route, int32_t sorted,
+                      const float *bias, void *Y, int32_t type, int64_t row_stride, void *stream);
+
 /* Static strings; never NULL. */
 const char *sd_status_string(int status);
 /* The last HIP error text seen by this thread ("" if none). */

@@ -139,6 +139,14 @@ class sd_norm_t(ctypes.Structure):
                 ("weight", _P), ("bias", _P)]
 
 
+class sd_nibble_t(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("cols", _i64), ("ld", _i64), ("reserved", _i64), ("codes", _P), ("scales", _P)]
+
+
+class sd_route_t(ctypes.Structure):
+    _fields_ = [("rows", _i64), ("k", _i32), ("experts", _i32), ("offsets", _P), ("place", _P), ("source", _P)]
+
+
 class SparseDittoError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -185,8 +193,21 @@ def _load():
     lib.sd_group_norm.argtypes = [norm, _P, _i64, _P, _i64, packed, packed, _P, _P, _P, ctypes.c_size_t, _P]
     lib.sd_group_norm_backward.argtypes = [norm, _P, _i64, _P, _i64, packed, _P, _P, _P, _i64, _P, _P, _P,
                                            ctypes.c_size_t, _P]
+    nibble, route = ctypes.POINTER(sd_nibble_t), ctypes.POINTER(sd_route_t)
+    lib.sd_nibble_pack.argtypes = [_P, _i32, _i64, _i64, nibble, _P]
+    lib.sd_nibble_unpack.argtypes = [nibble, _P, _i32, _i64, _P]
+    lib.sd_nibble_product_size.argtypes = [_i64, _i64, _i64, size]
+    lib.sd_nibble_product.argtypes = [nibble, nibble, _P, _P, _i32, _i64, _P, ctypes.c_size_t, _P]
+    lib.sd_route_size.argtypes = [_i64, _i32, _i32, size]
+    lib.sd_route.argtypes = [_P, _i32, route, _P, ctypes.c_size_t, _P]
+    lib.sd_dispatch.argtypes = [route, _P, _i32, _i64, _i64, _P, _i64, _P]
+    lib.sd_combine.argtypes = [route, _P, _i32, _i64, _i64, _P, _P, _i64, _P]
+    lib.sd_combine_backward.argtypes = [route, _P, _i32, _i64, _i64, _P, _i64, _P, _P, _i64, _P, _P]
+    lib.sd_expert_product.argtypes = [nibble, nibble, route, _i32, _P, _P, _i32, _i64, _P]
     for f in ("sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
-              "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward"):
+              "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_unpack",
+              "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
+              "sd_combine_backward", "sd_expert_product"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_spmm", "sd_plan_info", "sd_plan_export_size",
               "sd_plan_export", "sd_plan_device", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load"):
@@ -198,7 +219,9 @@ _lib = _load()
 EXPORTED = ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_plan_device", "sd_spmm", "sd_spmm_merge_noalloc", "sd_plan_info", "sd_plan_export_size",
             "sd_plan_export", "sd_plan_destroy", "sd_plan_cache_clear", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load", "sd_release_memory", "sd_status_string", "sd_last_error",
             "sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
-            "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward")
+            "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_unpack",
+            "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
+            "sd_combine_backward", "sd_expert_product")
 
 
 def _check(status: int, where: str):
@@ -426,6 +449,64 @@ def sd_group_norm_backward(d: sd_norm_t, dy, dy_stride: int, x, x_stride: int, x
     _check(_lib.sd_group_norm_backward(d, _devptr(dy), dy_stride, _devptr(x), x_stride, x_packed, _devptr(mean),
                                        _devptr(rstd), _devptr(dx), dx_stride, _devptr(dweight), _devptr(dbias),
                                        _devptr(workspace), bytes, _stream(stream)), "sd_group_norm_backward")
+
+
+def sd_nibble_pack(x, type: int, row_stride: int, col_stride: int, out: sd_nibble_t, stream=None) -> None:
+    """Device table x (pointer or tensor) into the 4-bit codes and scales of `out`."""
+    _check(_lib.sd_nibble_pack(_devptr(x), type, row_stride, col_stride, out, _stream(stream)), "sd_nibble_pack")
+
+
+def sd_nibble_unpack(x: sd_nibble_t, y, type: int, row_stride: int, stream=None) -> None:
+    _check(_lib.sd_nibble_unpack(x, _devptr(y), type, row_stride, _stream(stream)), "sd_nibble_unpack")
+
+
+def sd_nibble_product_size(rows: int, cols: int, n: int) -> int:
+    size = ctypes.c_size_t()
+    _check(_lib.sd_nibble_product_size(rows, cols, n, size), "sd_nibble_product_size")
+    return size.value
+
+
+def sd_nibble_product(X: sd_nibble_t, W: sd_nibble_t, bias, Y, type: int, row_stride: int, workspace, bytes: int,
+                      stream=None) -> None:
+    """Y = X.W^T (+ bias) of two 4-bit tables."""
+    _check(_lib.sd_nibble_product(X, W, _devptr(bias), _devptr(Y), type, row_stride, _devptr(workspace), bytes,
+                                  _stream(stream)), "sd_nibble_product")
+
+
+def sd_route_size(rows: int, k: int, experts: int) -> int:
+    size = ctypes.c_size_t()
+    _check(_lib.sd_route_size(rows, k, experts, size), "sd_route_size")
+    return size.value
+
+
+def sd_route(chosen, index_bytes: int, out: sd_route_t, workspace, bytes: int, stream=None) -> None:
+    """Fills out's arrays from the experts chosen for each row."""
+    _check(_lib.sd_route(_devptr(chosen), index_bytes, out, _devptr(workspace), bytes, _stream(stream)), "sd_route")
+
+
+def sd_dispatch(route: sd_route_t, x, type: int, cols: int, x_stride: int, y, y_stride: int, stream=None) -> None:
+    _check(_lib.sd_dispatch(route, _devptr(x), type, cols, x_stride, _devptr(y), y_stride, _stream(stream)),
+           "sd_dispatch")
+
+
+def sd_combine(route: sd_route_t, y, type: int, cols: int, y_stride: int, weights, out, out_stride: int,
+               stream=None) -> None:
+    _check(_lib.sd_combine(route, _devptr(y), type, cols, y_stride, _devptr(weights), _devptr(out), out_stride,
+                           _stream(stream)), "sd_combine")
+
+
+def sd_combine_backward(route: sd_route_t, dout, type: int, cols: int, dout_stride: int, y, y_stride: int, weights,
+                        dy, dy_stride: int, dweights, stream=None) -> None:
+    _check(_lib.sd_combine_backward(route, _devptr(dout), type, cols, dout_stride, _devptr(y), y_stride,
+                                    _devptr(weights), _devptr(dy), dy_stride, _devptr(dweights), _stream(stream)),
+           "sd_combine_backward")
+
+
+def sd_expert_product(X: sd_nibble_t, W: sd_nibble_t, route: sd_route_t, sorted: int, bias, Y, type: int,
+                      row_stride: int, stream=None) -> None:
+    """Each entry's row of X through its expert's rows of W."""
+    _check(_lib.sd_expert_product(X, W, route, sorted, _devptr(bias), _devptr(Y), type, row_stride, _stream(stream)),
+           "sd_expert_product")
 
 
 def sd_plan_info(plan: Plan) -> dict:

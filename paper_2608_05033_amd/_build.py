@@ -16,7 +16,7 @@ ROOT = os.path.dirname(HERE)
 
 HOST_SOURCES = ["host_csr.cpp", "host_plan.cpp"]
 HIP_SOURCES = ["kernels.hip", "runtime.hip", "analyze.hip", "convert.hip", "noalloc.hip", "pool.hip", "pack.hip", "norm.hip", "product.hip",
-               "gradient.hip"]
+               "gradient.hip", "nibble.hip", "nibble_product.hip", "experts.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,0 +1,37 @@
+"""Backward passes through kernels, which have no derivatives of their own."""
+from __future__ import annotations
+
+import functools
+
+import torch
+
+
+class _FirstOnly(torch.autograd.Function):
+    """A gradient as it is; asking for its derivative is an error."""
+
+    @staticmethod
+    def forward(ctx, g, *anchors):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, dg):
+        raise RuntimeError("no second derivatives here: the gradients of these kernels are not recorded")
+
+
+def first_derivatives_only(backward):
+    """A backward pass through kernels: where a graph of it is asked for
+    (create_graph), its results lead to an error and not to a part that is missing.
+    They hang on the output gradient and on what was saved, as far as those require
+    gradients, so that a derivative with respect to any of them finds the error."""
+
+    @functools.wraps(backward)
+    def wrapped(ctx, dZ):
+        with torch.no_grad():
+            grads = backward(ctx, dZ)
+        if not torch.is_grad_enabled():
+            return grads
+        anchors = [v for v in (dZ, *ctx.saved_tensors) if v is not None and v.requires_grad]
+        anchors = anchors or [dZ.new_empty(0).requires_grad_()]
+        return tuple(g if g is None else _FirstOnly.apply(g, *anchors) for g in grads)
+
+    return wrapped

@@ -1,0 +1,225 @@
+// sd_nibble_pack / sd_nibble_unpack: dense tables to 4 bits and back.
+//
+// value(r, c) = e2m1(code(r, c)) * 2^(s(c / 32, r) - 127).  The scale of a row's
+// block of 32 columns is the least power of two that brings its largest magnitude
+// to at most 6, the format's largest number, so nothing is cut off and both
+// directions are exact up to the one rounding (nearest, ties to even).  The format
+// has no NaN and no infinity of its own: a block that holds one gets the scale
+// byte 255, which makes all of it NaN here and in the matrix units.
+#include "nibble.h"
+
+namespace {
+
+using namespace nibble;
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;  // row groups in flight per lane group
+
+// A group of 128 / V lanes takes one row's group of 128 columns: V neighbouring
+// columns per lane (16 bytes), the largest bits of each block over its 32 / V
+// lanes, V codes per lane back.  COLS: consecutive elements of a row lie together
+// (else any strides, each lane's elements read one by one).
+template <typename T, bool COLS>
+__global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ x, int64_t row_stride,
+                                                          int64_t col_stride, int64_t rows, int32_t cols, int32_t ng,
+                                                          uint8_t *__restrict__ codes, int64_t ld,
+                                                          uint8_t *__restrict__ scales) {
+  constexpr int V = 16 / sizeof(T), LANES = kGroup / V, GROUPS = kThreads / LANES, SHARE = kCols / V;
+  const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  const int64_t first = (int64_t)workgroup() * (GROUPS * kUnroll);
+  const int64_t r0 = first / ng;
+  const uint32_t g0 = (uint32_t)(first - r0 * ng);
+  float v[kUnroll][V];
+  int64_t row[kUnroll];
+  int32_t grp[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const uint32_t at = g0 + u * GROUPS + group;
+    row[u] = r0 + at / (uint32_t)ng;
+    grp[u] = at % (uint32_t)ng;
+    const int32_t c = grp[u] * kGroup + lane * V;
+    const int left = row[u] < rows ? cols - c : 0;
+    if constexpr (COLS) {
+      const T *p = x + row[u] * row_stride + c;
+      if (left >= V)
+        load_span(p, v[u]);
+      else
+        load_part(p, left, v[u]);
+    } else {
+      const T *p = x + row[u] * row_stride + c * col_stride;
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[u][i] = i < left ? (float)p[i * col_stride] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t bits = __float_as_uint(v[u][i]) & 0x7fffffffu;
+      most = most > bits ? most : bits;
+    }
+    const uint32_t s = scale_byte(group_max_bits(most, SHARE));
+    const float scale = scale_value(s);
+    uint32_t w = encode2<0>(0u, v[u][0], v[u][1], scale);
+    w = encode2<1>(w, v[u][2], v[u][3], scale);
+    if constexpr (V == 8) {
+      w = encode2<2>(w, v[u][4], v[u][5], scale);
+      w = encode2<3>(w, v[u][6], v[u][7], scale);
+    }
+    if (s == kNanScale) w = 0;
+    if (row[u] >= rows) continue;
+    const int32_t c = grp[u] * kGroup + lane * V;
+    if (c < ((cols + kCols - 1) & ~(kCols - 1))) {
+      uint8_t *p = codes + row[u] * ld + c / 2;
+      if constexpr (V == 4)
+        *reinterpret_cast<uint16_t *>(p) = (uint16_t)w;
+      else
+        *reinterpret_cast<uint32_t *>(p) = w;
+    }
+    if (lane % SHARE == 0) scales[((int64_t)grp[u] * rows + row[u]) * 4 + lane / SHARE] = (uint8_t)s;
+  }
+}
+
+// The same where consecutive rows lie closer than consecutive columns (a
+// transposed table): lanes along the rows, a whole block for each lane, the four
+// blocks of a group for the four waves.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__restrict__ x, int64_t row_stride,
+                                                                 int64_t col_stride, int64_t rows, int32_t cols,
+                                                                 int32_t ng, uint8_t *__restrict__ codes, int64_t ld,
+                                                                 uint8_t *__restrict__ scales) {
+  const int64_t strip = workgroup() / (uint32_t)ng;
+  const int32_t grp = workgroup() % (uint32_t)ng;
+  const int block = threadIdx.x >> 6;
+  const int64_t row = strip * 64 + (threadIdx.x & 63);
+  if (row >= rows) return;
+  const int32_t c = grp * kGroup + block * kCols;
+  const int left = cols - c;
+  float v[kCols];
+  const T *p = x + row * row_stride + c * col_stride;
+  if (left >= kCols) {
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) v[i] = (float)p[i * col_stride];
+  } else {
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) v[i] = i < left ? (float)p[i * col_stride] : 0.0f;
+  }
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < kCols; ++i) {
+    const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
+    most = most > bits ? most : bits;
+  }
+  const uint32_t s = scale_byte(most);
+  const float scale = scale_value(s);
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t q = encode2<0>(0u, v[8 * i], v[8 * i + 1], scale);
+    q = encode2<1>(q, v[8 * i + 2], v[8 * i + 3], scale);
+    q = encode2<2>(q, v[8 * i + 4], v[8 * i + 5], scale);
+    q = encode2<3>(q, v[8 * i + 6], v[8 * i + 7], scale);
+    w[i] = s == kNanScale ? 0 : q;
+  }
+  if (left > 0) *reinterpret_cast<u32x4 *>(codes + row * ld + c / 2) = w;
+  scales[((int64_t)grp * rows + row) * 4 + block] = (uint8_t)s;
+}
+
+// Lanes along a row, eight codes each.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__restrict__ codes, int64_t ld,
+                                                            const uint8_t *__restrict__ scales, int64_t rows,
+                                                            int32_t cols, int32_t octs, T *__restrict__ y,
+                                                            int64_t row_stride) {
+  const int64_t first = (int64_t)workgroup() * (kThreads * kUnroll);
+  const int64_t r0 = first / octs;
+  const uint32_t q0 = (uint32_t)(first - r0 * octs);
+  uint32_t w[kUnroll], s[kUnroll];
+  int64_t row[kUnroll];
+  int32_t col[kUnroll];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const uint32_t at = q0 + u * kThreads + threadIdx.x;
+    row[u] = r0 + at / (uint32_t)octs;
+    col[u] = (int32_t)(at % (uint32_t)octs) * 8;
+    w[u] = 0;
+    s[u] = 127;
+    if (row[u] < rows) {
+      w[u] = *reinterpret_cast<const uint32_t *>(codes + row[u] * ld + col[u] / 2);
+      s[u] = scales[((int64_t)(col[u] / kGroup) * rows + row[u]) * 4 + col[u] / kCols % 4];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    if (row[u] >= rows) continue;
+    const float scale = s[u] == kNanScale ? __uint_as_float(0x7fc00000u) : scale_value(s[u]);
+    float v[8];
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 0);
+    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 1);
+    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 2);
+    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 3);
+    v[0] = a[0] * scale, v[1] = a[1] * scale, v[2] = b[0] * scale, v[3] = b[1] * scale;
+    v[4] = c[0] * scale, v[5] = c[1] * scale, v[6] = d[0] * scale, v[7] = d[1] * scale;
+    T *p = y + row[u] * row_stride + col[u];
+    const int left = cols - col[u];
+    if (left >= 8)
+      store_span(p, v);
+    else
+      store_part(p, left, v);
+  }
+}
+
+template <typename T>
+int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nibble_t *out, hipStream_t s) {
+  const T *p = static_cast<const T *>(x);
+  const int64_t ng = groups_of(out->cols);
+  const bool across = col_stride != 1 && row_stride < col_stride;
+  constexpr int per_wg = kThreads / (kGroup * (int)sizeof(T) / 16) * kUnroll;
+  const int64_t wgs = across ? ceil_div(out->rows, 64) * ng : ceil_div(out->rows * ng, per_wg);
+  if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
+  auto *kernel = across            ? k_nibble_pack_across<T>
+                 : col_stride == 1 ? k_nibble_pack<T, true>
+                                   : k_nibble_pack<T, false>;
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, p, row_stride, col_stride, out->rows,
+                     (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales);
+  return launched();
+}
+
+template <typename T>
+int unpack_as(const sd_nibble_t *x, void *y, int64_t row_stride, hipStream_t s) {
+  const int64_t octs = ceil_div(x->cols, 8), wgs = ceil_div(x->rows * octs, kThreads * kUnroll);
+  if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
+  hipLaunchKernelGGL(k_nibble_unpack<T>, grid_of(wgs), dim3(kThreads), 0, s, x->codes, x->ld, x->scales, x->rows,
+                     (int32_t)x->cols, (int32_t)octs, static_cast<T *>(y), row_stride);
+  return launched();
+}
+
+}  // namespace
+
+extern "C" int sd_nibble_pack(const void *x, int32_t type, int64_t row_stride, int64_t col_stride,
+                              const sd_nibble_t *out, void *stream) {
+  int st = check_nibble(out);
+  if (st != SD_OK) return st;
+  if (!type_ok(type) || row_stride < 0 || col_stride < 0) return SD_ERR_INVALID_VALUE;
+  if (row_stride > (1ll << 40) || col_stride > (1ll << 31)) return SD_ERR_OVERFLOW;
+  if (out->rows == 0 || out->cols == 0) return SD_OK;
+  if (!x || !aligned_to(x, type_bytes(type))) return SD_ERR_INVALID_VALUE;
+  if ((st = have_device()) != SD_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return type == SD_TYPE_F32   ? pack_any<float>(x, row_stride, col_stride, out, s)
+         : type == SD_TYPE_F16 ? pack_any<f16>(x, row_stride, col_stride, out, s)
+                               : pack_any<bf16>(x, row_stride, col_stride, out, s);
+}
+
+extern "C" int sd_nibble_unpack(const sd_nibble_t *x, void *y, int32_t type, int64_t row_stride, void *stream) {
+  int st = check_nibble(x);
+  if (st != SD_OK) return st;
+  if ((st = check_table(y, type, x->rows, x->cols, row_stride)) != SD_OK) return st;
+  if (x->rows == 0 || x->cols == 0) return SD_OK;
+  if ((st = have_device()) != SD_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return type == SD_TYPE_F32   ? unpack_as<float>(x, y, row_stride, s)
+         : type == SD_TYPE_F16 ? unpack_as<f16>(x, y, row_stride, s)
+                               : unpack_as<bf16>(x, y, row_stride, s);
+}

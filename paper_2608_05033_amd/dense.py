@@ -5,6 +5,7 @@
     out = group_norm(A, groups, w, b, activation="relu", keep="e4m3", pack_y="e4m3", dense_y=False)
     dW = weight_gradient(X8, dZ)                     X^T.dZ from the 8-bit copy
     dA, dw, db = group_norm_backward(dH, out.x, out.mean, out.rstd, groups, w, b, activation="relu")
+    Z  = product4(pack4(X), pack4(W, transpose=True))    the same in 4 bits, a scale per row and 32 columns
 
 Arguments are checked here and in the library; every call runs on the current
 stream of its tensors' device, and results and workspaces are torch tensors of
@@ -18,7 +19,8 @@ import functools
 
 import torch
 
-from . import (ACTIVATIONS, PACK_FORMATS, SD_TYPE_BF16, SD_TYPE_F16, SD_TYPE_F32, _check, _lib, sd_norm_t, sd_packed_t)
+from . import (ACTIVATIONS, PACK_FORMATS, SD_TYPE_BF16, SD_TYPE_F16, SD_TYPE_F32, _check, _lib, sd_nibble_t, sd_norm_t,
+               sd_packed_t)
 
 BLOCK = 128  # columns that share a scale
 TYPES = {torch.float32: SD_TYPE_F32, torch.float16: SD_TYPE_F16, torch.bfloat16: SD_TYPE_BF16}
@@ -171,6 +173,95 @@ def weight_gradient(x: Packed, g) -> torch.Tensor:
                                  None if work is None else work.data_ptr(), size, _raw_stream(x.index)),
            "sd_pack_gradient")
     return dw
+
+
+class Packed4:
+    """A rows x cols table in 4 bits: codes uint8 [rows, ld], two in a byte, the
+    even column in the lower half (ld a multiple of 16, 16 bytes for every 32
+    columns begun, zeros past cols), and scales uint8 [ceil(cols / 128), rows, 4].
+    A code's value is e2m1(code) times 2^(scale - 127); 255 makes a block NaN."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "index", "c")
+
+    def __init__(self, codes, scales, cols: int):
+        index = codes.get_device()
+        if codes.dtype != _uint8 or scales.dtype != _uint8 or codes.dim() != 2 or index < 0 or \
+                index != scales.get_device():
+            raise ValueError("codes and scales must be uint8 tensors on one GPU")
+        rows, width = codes.shape
+        ld, step = codes.stride()
+        need = (cols + 31) // 32 * 16
+        if cols < 0 or width < need or width > 1 and step != 1:
+            raise ValueError(f"codes must hold {cols} columns, two in a byte and rounded up to 32, next to each other")
+        if scales.shape != ((cols + 127) // 128, rows, 4) or not scales.is_contiguous():
+            raise ValueError(f"scales must be contiguous [{-(-cols // 128)}, {rows}, 4], got {tuple(scales.shape)}")
+        self.codes, self.scales, self.rows, self.cols, self.index = codes, scales, rows, cols, index
+        self.c = sd_nibble_t(rows, cols, ld if rows > 1 and cols else need, 0, codes.data_ptr(), scales.data_ptr())
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def get_device(self) -> int:
+        return self.index
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, like):
+        """A new one on the device of the tensor `like`: one allocation for codes and scales."""
+        ld, groups = (cols + 31) // 32 * 16, (cols + 127) // 128
+        size = rows * ld
+        store = like.new_empty(size + groups * rows * 4, dtype=_uint8)
+        p, at = cls.__new__(cls), store.data_ptr()
+        p.codes = store.as_strided((rows, ld), (ld, 1))
+        p.scales = store.as_strided((groups, rows, 4), (rows * 4, 4, 1), size)
+        p.rows, p.cols, p.index = rows, cols, store.get_device()
+        p.c = sd_nibble_t(rows, cols, ld, 0, at, at + size)
+        return p
+
+
+@_on_its_device
+def pack4(x, transpose: bool = False) -> Packed4:
+    """x in 4 bits (of x^T with transpose=True: a weight [k, n] as product4's
+    second operand).  Any strides."""
+    if x.dim() != 2 or x.dtype not in TYPES or not x.is_cuda:
+        raise ValueError(f"x must be a float32, float16 or bfloat16 matrix on the GPU, got {x.dtype} "
+                         f"{tuple(x.shape)} on {x.device}")
+    (rows, cols), (down, right) = x.shape, x.stride()
+    if transpose:
+        rows, cols, down, right = cols, rows, right, down
+    out = Packed4.empty(rows, cols, x)
+    _check(_lib.sd_nibble_pack(x.data_ptr(), TYPES[x.dtype], down, 1 if cols == 1 else right, out.c,
+                               _raw_stream(x.get_device())), "sd_nibble_pack")
+    return out
+
+
+@_on_its_device
+def unpack4(x: Packed4, dtype=torch.float32) -> torch.Tensor:
+    if dtype not in TYPES:
+        raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
+    y = x.codes.new_empty((x.rows, x.cols), dtype=dtype)
+    _check(_lib.sd_nibble_unpack(x.c, y.data_ptr(), TYPES[dtype], x.cols, _raw_stream(x.index)), "sd_nibble_unpack")
+    return y
+
+
+@_on_its_device
+def product4(x: Packed4, w: Packed4, bias=None, dtype=torch.float32) -> torch.Tensor:
+    """x.w^T (+ bias), [x.rows, w.rows], summed in 32 bits and rounded once to dtype."""
+    if x.cols != w.cols or x.index != w.index:
+        raise ValueError(f"operands must have the same columns on one device, got {x.cols} on {x.device} and "
+                         f"{w.cols} on {w.device}")
+    if dtype not in TYPES:
+        raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
+    n = w.rows
+    bias = _vector(bias, n, x.index, "bias")
+    y = x.codes.new_empty((x.rows, n), dtype=dtype)
+    size = ctypes.c_size_t()
+    _check(_lib.sd_nibble_product_size(x.rows, x.cols, n, size), "sd_nibble_product_size")
+    work = y.new_empty(size.value, dtype=_uint8) if size.value else None
+    _check(_lib.sd_nibble_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n,
+                                  None if work is None else work.data_ptr(), size, _raw_stream(x.index)),
+           "sd_nibble_product")
+    return y
 
 
 class NormOut:

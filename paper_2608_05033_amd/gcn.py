@@ -12,17 +12,18 @@ backward pass needs of each layer (the features, the normalisation's input, the
 activation) is kept at one byte an element instead of four, through the operators
 of dense.py.  The aggregations stay in fp32.
 
+`transform4` is a layer's dense transform in 4 bits with its gradients.
+
 Each aggregation is `spmm(B, fwd, bwd)`: C = Â·B with plan `fwd`, and in the
 backward pass dB = Âᵀ·dC with the transpose plan `bwd` (A is not assumed
 symmetric).  Plans are built once per (graph, width) and reused every epoch.
 """
 from __future__ import annotations
 
-import functools
-
 import torch
 
 from . import Plan, dense, sd_plan_device, sd_plan_ex, sd_spmm
+from .autograd import first_derivatives_only
 
 
 class _SpMM(torch.autograd.Function):
@@ -110,34 +111,6 @@ class GCN2(torch.nn.Module):
         return self.agg(H1 @ self.W2)
 
 
-class _FirstOnly(torch.autograd.Function):
-    """A gradient as it is; asking for its derivative is an error."""
-
-    @staticmethod
-    def forward(ctx, g, anchor):
-        return g.view_as(g)
-
-    @staticmethod
-    def backward(ctx, dg):
-        raise RuntimeError("GCN2Packed has no second derivatives: its kernels' gradients are not recorded")
-
-
-def _first_derivatives_only(backward):
-    """A backward pass through kernels: where a graph of it is asked for
-    (create_graph), its results lead to an error and not to a part that is missing."""
-
-    @functools.wraps(backward)
-    def wrapped(ctx, dZ):
-        with torch.no_grad():
-            grads = backward(ctx, dZ)
-        if not torch.is_grad_enabled():
-            return grads
-        anchor = dZ.new_empty(0).requires_grad_()
-        return tuple(g if g is None else _FirstOnly.apply(g, anchor) for g in grads)
-
-    return wrapped
-
-
 class _PackedTransform(torch.autograd.Function):
     """X.W from X in 8 bits, packed here where it is a float tensor.  That one has a
     gradient too, as if the packing did not round: the output gradient, multiplied
@@ -155,7 +128,7 @@ class _PackedTransform(torch.autograd.Function):
         return dense.product(X8, dense.pack(W, X8.format, transpose=True))
 
     @staticmethod
-    @_first_derivatives_only
+    @first_derivatives_only
     def backward(ctx, dZ):
         dX, dW, dZ = None, None, dZ.contiguous()
         codes, scales, *rest = ctx.saved_tensors
@@ -165,6 +138,40 @@ class _PackedTransform(torch.autograd.Function):
         if ctx.needs_input_grad[1]:
             dW = dense.weight_gradient(X8, dZ)
         return dX, dW, None, None
+
+
+class _Transform4(torch.autograd.Function):
+    """X.W and both gradients as products of 4-bit tables, each packed along its own
+    sum.  What the backward pass needs of X is kept packed along the rows, at half a
+    byte an element."""
+
+    @staticmethod
+    def forward(ctx, X, W):
+        ctx.dtype = X.dtype
+        Xt = dense.pack4(X, transpose=True) if ctx.needs_input_grad[1] else None
+        ctx.save_for_backward(W, *(() if Xt is None else (Xt.codes, Xt.scales)))
+        return dense.product4(dense.pack4(X), dense.pack4(W, transpose=True))
+
+    @staticmethod
+    @first_derivatives_only
+    def backward(ctx, dZ):
+        W, *Xt = ctx.saved_tensors
+        dX = dW = None
+        if ctx.needs_input_grad[0]:
+            dX = dense.product4(dense.pack4(dZ), dense.pack4(W), dtype=ctx.dtype)
+        if ctx.needs_input_grad[1]:
+            dW = dense.product4(dense.Packed4(*Xt, dZ.shape[0]), dense.pack4(dZ, transpose=True), dtype=W.dtype)
+        return dX, dW
+
+
+def transform4(X: torch.Tensor, W: torch.Tensor) -> torch.Tensor:
+    """X.W in float32 on the matrix units' 4-bit form, with gradients computed in the
+    same way: X and W are rounded to 4 bits along the features, the output gradient
+    and W along the outputs for X's gradient, X and the output gradient along the rows
+    for W's, as if the rounding were the identity.  No second derivatives."""
+    if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[0]:
+        raise ValueError(f"X and W must be matrices that fit, got {tuple(X.shape)} and {tuple(W.shape)}")
+    return _Transform4.apply(X, W)
 
 
 class _NormTransform(torch.autograd.Function):
@@ -181,7 +188,7 @@ class _NormTransform(torch.autograd.Function):
         return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True))
 
     @staticmethod
-    @_first_derivatives_only
+    @first_derivatives_only
     def backward(ctx, dZ):
         dZ = dZ.contiguous()
         W, gamma, beta, *A8, codes, scales, mean, rstd = ctx.saved_tensors

@@ -1,0 +1,468 @@
+"""Rows sorted by expert, brought there and back, and the experts' products on
+the GPU against plain 64-bit forms, with their gradients."""
+import numpy as np
+import pytest
+
+import nibble_reference as ref
+from test_gpu_nibble import HALF_ULP, TYPES, check_product, of, random_table, table, to64
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover - CPU container
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2608_05033_amd as sd  # noqa: E402
+from paper_2608_05033_amd import dense, experts, gcn  # noqa: E402
+
+
+def choose(rows, k, n, seed, kind="mixed"):
+    """Chosen experts: all kinds of numbers, dropped entries and repeated ones among
+    them; one expert for all; none at all; in falling order."""
+    g = np.random.default_rng(seed)
+    c = g.integers(0, n, (rows, k))
+    if kind == "mixed":
+        c[g.random((rows, k)) < 0.1] = -1
+        c[g.random((rows, k)) < 0.02] = n
+    if kind == "one":
+        c[:] = n // 2
+    if kind == "none":
+        c[:] = -7
+    if kind == "falling":
+        c = np.sort(c, axis=None)[::-1].reshape(rows, k).copy()
+    return c
+
+
+def check_route(r, chosen, n, plain=ref.route):
+    for got, want in zip((r.offsets, r.place, r.source), plain(chosen, n)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+# ---------------------------------------------------------------- sorting ---
+@pytest.mark.parametrize("index", [np.int32, np.int64])
+@pytest.mark.parametrize("rows,k,n", [(1, 1, 1), (1, 8, 64), (37, 2, 16), (64, 1, 3), (65, 3, 7), (1000, 4, 60),
+                                      (50, 2, 4095), (1, 3, 959), (1, 3, 960), (2048, 4, 9)])
+def test_route(rows, k, n, index):
+    print(f"case route {rows}x{k} of {n} {index.__name__}", flush=True)
+    for kind in ("mixed", "whole", "one", "none", "falling"):
+        c = choose(rows, k, n, rows + n, kind).astype(index)
+        check_route(experts.route(torch.from_numpy(c).cuda(), n), c, n)
+
+
+@pytest.mark.parametrize("rows,k,n", [(8192, 1, 5), (8193, 1, 5), (30001, 2, 200), (262144, 2, 8), (70000, 8, 1023),
+                                      (100003, 1, 4095), (600000, 2, 1)])
+def test_route_many(rows, k, n):
+    print(f"case route {rows}x{k} of {n}", flush=True)
+    for kind in ("mixed", "one", "falling"):
+        c = choose(rows, k, n, rows, kind)
+        check_route(experts.route(torch.from_numpy(c).cuda(), n), c, n, ref.route_fast)
+
+
+def test_route_of_numbers_past_32_bits():
+    c = np.array([[1 << 32, 1], [-(1 << 40) + 1, 2], [(1 << 32) + 1, 0]])
+    check_route(experts.route(torch.from_numpy(c).cuda(), 3), c, 3)
+
+
+def test_route_of_no_rows():
+    r = experts.route(torch.zeros(0, 3, dtype=torch.int64, device="cuda"), 5)
+    assert not r.offsets.any() and r.offsets.numel() == 6 and r.place.shape == (0, 3) and r.source.numel() == 0
+    x = torch.zeros(0, 7, device="cuda")
+    assert experts.dispatch(x, r).shape == (0, 7)
+    assert experts.combine(x, r, torch.zeros(0, 3, device="cuda")).shape == (0, 7)
+    p, w = dense.pack4(x), dense.pack4(torch.zeros(10, 7, device="cuda"))
+    assert experts.product(p, w, r).shape == (0, 2)
+
+
+# ------------------------------------------------------- to experts and back ---
+CASES = [(1, 1, 1, 1), (1, 8, 64, 100), (37, 2, 16, 64), (50, 9, 12, 33), (65, 3, 7, 129), (300, 4, 60, 601),
+         (7, 2, 3, 3000), (500, 17, 5, 5)]
+
+
+def weights_of(rows, k, seed):
+    return np.random.default_rng(seed).random((rows, k)).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,k,n,cols", CASES)
+def test_dispatch_and_combine(rows, k, n, cols, dtype):
+    """dispatch copies bits.  combine: k products and additions, each off by half a
+    unit of what is summed so far, then one rounding to the type; its gradients by one
+    product and a sum over the columns."""
+    print(f"case exchange {rows}x{k} of {n}, {cols} {dtype}", flush=True)
+    c = choose(rows, k, n, cols)
+    r = experts.route(torch.from_numpy(c).cuda(), n)
+    _, place, source = ref.route(c, n)
+    g = np.random.default_rng(cols)
+    X, x = table(g.standard_normal((rows, cols)), dtype)
+    xs = np.where((source >= 0)[:, None], x[np.maximum(source, 0)], 0)
+    assert np.array_equal(to64(experts.dispatch(X, r)), xs)
+
+    Y, y = table(g.standard_normal((rows * k, cols)), dtype)
+    w = weights_of(rows, k, cols)
+    Wt = torch.from_numpy(w).cuda()
+    for weights, w64 in ((Wt, w.astype(np.float64)), (None, np.ones((rows, k)))):
+        want, size = ref.combine(y, place, w64)
+        bound = (k + 1) * 2.0 ** -24 * size + (HALF_ULP[dtype] * np.abs(want) + 2.0 ** -25 if dtype != "f32" else 0)
+        assert np.all(np.abs(to64(experts.combine(Y, r, weights)) - want) <= bound)
+
+        D, d = table(g.standard_normal((rows, cols)), dtype)
+        dy, dw, dw_size = ref.combine_backward(d, y, place, w64)
+        got_dy, got_dw = experts.combine_backward(D, Y, r, weights)
+        assert np.all(np.abs(to64(got_dy) - dy) <= (HALF_ULP[dtype] + 2.0 ** -24) * np.abs(dy) +
+                      (2.0 ** -25 if dtype == "f16" else 0))
+        assert np.all(np.abs(to64(got_dw) - dw) <= (cols + 8) * 2.0 ** -24 * dw_size)
+        assert experts.combine_backward(D, None, r, weights, need_dweights=False)[1] is None
+        only, = [v for v in experts.combine_backward(D, Y, r, weights, need_dy=False) if v is not None]
+        assert torch.equal(only, got_dw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides(dtype):
+    """Tables that are parts of wider ones, at any column."""
+    c = choose(90, 3, 7, 1)
+    r = experts.route(torch.from_numpy(c).cuda(), 7)
+    wide = torch.randn(270, 100, generator=torch.Generator().manual_seed(1)).to(TYPES[dtype]).cuda()
+    w = torch.from_numpy(weights_of(90, 3, 2)).cuda()
+    for part in (wide[:, 1:70], wide[:, 3:4], wide[:, 8:72]):
+        whole = part.contiguous()
+        assert torch.equal(experts.dispatch(part[:90], r), experts.dispatch(whole[:90].contiguous(), r))
+        assert torch.equal(experts.combine(part, r, w), experts.combine(whole, r, w))
+        for a, b in zip(experts.combine_backward(part[:90], part, r, w),
+                        experts.combine_backward(whole[:90].contiguous(), whole, r, w)):
+            assert torch.equal(a, b)
+
+
+def test_results_that_are_parts_of_wider_tables():
+    """The C calls write the columns they are given and no others."""
+    r = experts.route(torch.from_numpy(choose(40, 2, 5, 3)).cuda(), 5)
+    x = torch.randn(40, 19, generator=torch.Generator().manual_seed(4)).cuda()
+    y = torch.randn(80, 19, generator=torch.Generator().manual_seed(5)).cuda()
+    s = torch.cuda.current_stream()
+    for rows, call, want in (
+            (80, lambda out: sd.sd_dispatch(r.c, x, sd.SD_TYPE_F32, 19, 19, out, 24, s), experts.dispatch(x, r)),
+            (40, lambda out: sd.sd_combine(r.c, y, sd.SD_TYPE_F32, 19, 19, None, out, 24, s), experts.combine(y, r)),
+            (80, lambda out: sd.sd_combine_backward(r.c, x, sd.SD_TYPE_F32, 19, 19, None, 0, None, out, 24, None, s),
+             experts.dispatch(x, r))):
+        wide = torch.full((rows, 24), 7.0, device="cuda")
+        call(wide[:, 2:])
+        assert torch.equal(wide[:, 2:21], want)
+        assert (wide[:, :2] == 7).all() and (wide[:, 21:] == 7).all()
+
+
+def test_values_that_are_not_finite():
+    """Rows that nobody was sorted to are not read, a weight of 0 does not hide NaN."""
+    c = np.array([[0, 1], [-1, 0], [1, -1]])
+    r = experts.route(torch.from_numpy(c).cuda(), 2)
+    y = torch.ones(6, 5, device="cuda")
+    y[4:] = float("nan")  # behind the last entry
+    w = torch.full((3, 2), 0.5, device="cuda")
+    assert torch.isfinite(experts.combine(y, r, w)).all()
+    dy, dw = experts.combine_backward(torch.ones(3, 5, device="cuda"), y, r, w)
+    assert torch.isfinite(dw).all() and not dy[4:].any() and dw[1, 0] == 0 and dw[2, 1] == 0
+    y[int(r.place[0, 1])] = float("nan")
+    w[0, 1] = 0
+    out = experts.combine(y, r, w)
+    assert torch.isnan(out[0]).all() and torch.isfinite(out[1]).all()
+
+
+def test_rows_of_another_type_of_route():
+    """Places and sources that do not fit the table are left alone."""
+    offsets = torch.tensor([0, 9], dtype=torch.int32, device="cuda")
+    place = torch.tensor([[5], [1 << 30], [-3]], dtype=torch.int32, device="cuda")
+    source = torch.tensor([1 << 30, -9, 2], dtype=torch.int32, device="cuda")
+    r = experts.Route(offsets, place, source)
+    x = torch.ones(3, 4, device="cuda")
+    y = experts.dispatch(x, r)
+    assert not y[1].any()
+    assert not experts.combine(x, r).any()
+    dy, dw = experts.combine_backward(x, x, r)
+    assert not dw.any() and not dy[1].any()
+    w = dense.pack4(torch.ones(2, 4, device="cuda"))
+    assert experts.product(dense.pack4(x), w, r).shape == (3, 2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients(dtype):
+    """Through torch, against the formulas, and the weights' against differences."""
+    c = choose(60, 3, 9, 8)
+    r = experts.route(torch.from_numpy(c).cuda(), 9)
+    _, place, source = ref.route(c, 9)
+    g = np.random.default_rng(8)
+    X, x = table(g.standard_normal((60, 40)), dtype)
+    Y, y = table(g.standard_normal((180, 40)), dtype)
+    w = weights_of(60, 3, 8)
+    W = torch.from_numpy(w).cuda()
+    D, d = table(g.standard_normal((60, 40)), dtype)
+    X.requires_grad_(), Y.requires_grad_(), W.requires_grad_()
+    out = experts.combine(Y, r, W)
+    gy, gw = torch.autograd.grad(out, (Y, W), D)
+    dy, dw, size = ref.combine_backward(d, y, place, w.astype(np.float64))
+    assert np.all(np.abs(to64(gy) - dy) <= (HALF_ULP[dtype] + 2.0 ** -24) * np.abs(dy))
+    assert np.all(np.abs(to64(gw) - dw) <= 48 * 2.0 ** -24 * size)
+    DS, ds = table(g.standard_normal((180, 40)), dtype)
+    gx, = torch.autograd.grad(experts.dispatch(X, r), X, DS)
+    want, size = ref.combine(ds, place, np.ones((60, 3)))
+    assert np.all(np.abs(to64(gx) - want) <= 4 * 2.0 ** -24 * size + HALF_ULP[dtype] * np.abs(want))
+    # both are linear: the change of <D, out> along a direction is the direction's product with the gradient
+    if dtype == "f32":
+        h = g.standard_normal((60, 3)).astype(np.float32)
+        change = to64(experts.combine(Y, r, torch.from_numpy(h).cuda()))
+        assert abs((change * d).sum() - (to64(gw) * h).sum()) <= 1e-4
+        hy = g.standard_normal((180, 40)).astype(np.float32)
+        change = to64(experts.combine(torch.from_numpy(hy).cuda(), r, W.detach()))
+        assert abs((change * d).sum() - (to64(gy) * hy).sum()) <= 1e-4
+
+
+def test_gradients_of_broadcast_and_repeated_use():
+    r = experts.route(torch.from_numpy(choose(30, 2, 4, 9, "whole")).cuda(), 4)
+    X = torch.randn(30, 8, generator=torch.Generator().manual_seed(1)).cuda().requires_grad_()
+    W = torch.from_numpy(weights_of(30, 2, 9)).cuda().requires_grad_()
+    ys = experts.dispatch(X, r)
+    out = experts.combine(ys, r, W) + experts.combine(ys, r)
+    out.sum().backward()  # an expanded gradient
+    assert torch.allclose(X.grad, (W.detach().sum(1, keepdim=True) + 2).expand(30, 8), rtol=0, atol=1e-5)
+    # second derivatives: none through the weights, and those of the plain sums are right
+    gx, = torch.autograd.grad((experts.combine(experts.dispatch(X, r), r) ** 2).sum(), X, create_graph=True)
+    again, = torch.autograd.grad(gx.sum(), X)
+    assert torch.equal(again, torch.full_like(X, 8.0))
+    gy, = torch.autograd.grad((experts.combine(ys, r, W) ** 2).sum(), W, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(gy.sum(), W)
+    with torch.no_grad():
+        assert not experts.combine(experts.dispatch(X, r), r, W).requires_grad
+
+
+def test_what_the_gradients_keep_is_watched():
+    r = experts.route(torch.from_numpy(choose(10, 2, 4, 9)).cuda(), 4)
+    Y = torch.ones(20, 8, device="cuda").requires_grad_()
+    W = torch.ones(10, 2, device="cuda").requires_grad_()
+    out = experts.combine(Y, r, W)
+    with torch.no_grad():
+        W.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+# --------------------------------------------------------- experts' products ---
+def expert_values(X, W, c, n, bias, k):
+    """64-bit rows of X and what they are multiplied with, entry by entry."""
+    offsets, _, source = ref.route(c, n)
+    x, w = of(X), of(W).reshape(n, -1, X.cols)
+    want = []
+    for e in range(n):
+        rows = source[offsets[e]:offsets[e + 1]]
+        want.append((offsets[e], offsets[e + 1], x[rows], w[e], None if bias is None else bias[e]))
+    return offsets[n], want
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,k,n,cols,out", [(1, 1, 1, 1, 1), (1, 8, 64, 256, 100), (37, 2, 16, 64, 33),
+                                               (200, 3, 7, 129, 65), (300, 1, 100, 601, 20), (1000, 2, 3, 260, 300),
+                                               (2000, 2, 5, 1030, 520), (5, 2, 200, 96, 17)])
+def test_expert_product(rows, k, n, cols, out, dtype):
+    print(f"case experts {rows}x{k} of {n}, {cols} to {out} {dtype}", flush=True)
+    for kind in ("mixed", "one"):
+        c = choose(rows, k, n, cols, kind)
+        r = experts.route(torch.from_numpy(c).cuda(), n)
+        X, W = random_table(rows, cols, 1, 2), random_table(n * out, cols, 2, 2)
+        W = dense.Packed4(W.codes, (W.scales.to(torch.int32) - 6).to(torch.uint8), cols)
+        b = np.random.default_rng(n).standard_normal((n, out)).astype(np.float32)
+        B = torch.from_numpy(b).cuda()
+        # X in the order of the list, from the unsorted one's codes
+        at = r.source.clamp(min=0).long()
+        Xs = dense.Packed4(X.codes[at], X.scales[:, at].contiguous(), cols)
+        for bias in (None, b.astype(np.float64)):
+            y = experts.product(X, W, r, None if bias is None else B, TYPES[dtype])
+            last, parts = expert_values(X, W, c, n, bias, k)
+            for lo, hi, x, w, be in parts:
+                if lo < hi:
+                    check_product(y[lo:hi], x, w, be, dtype)
+            assert not y[last:].any()
+            assert torch.equal(y, experts.product(Xs, W, r, None if bias is None else B, TYPES[dtype], sorted=True))
+
+
+def test_expert_product_from_one_row_to_all():
+    """Every split of 70 rows over two experts, the empty ones among them."""
+    X, W = random_table(70, 64, 3, 1), random_table(2 * 24, 64, 4, 1)
+    x, w = of(X), of(W).reshape(2, 24, 64)
+    for first in range(71):
+        c = (np.arange(70) >= first).astype(np.int32)[:, None]
+        y = to64(experts.product(X, W, experts.route(torch.from_numpy(c).cuda(), 2)))
+        assert np.array_equal(y, np.concatenate([x[:first] @ w[0].T, x[first:] @ w[1].T]))
+
+
+def test_expert_product_without_columns():
+    c = choose(20, 2, 3, 1)
+    r = experts.route(torch.from_numpy(c).cuda(), 3)
+    p, w = dense.pack4(torch.zeros(20, 0, device="cuda")), dense.pack4(torch.zeros(15, 0, device="cuda"))
+    b = torch.arange(15, dtype=torch.float32, device="cuda").view(3, 5)
+    y, offsets = experts.product(p, w, r, b), r.offsets.tolist()
+    for e in range(3):
+        assert torch.equal(y[offsets[e]:offsets[e + 1]], b[e].expand(offsets[e + 1] - offsets[e], 5))
+    assert not y[offsets[3]:].any()
+
+
+def test_expert_product_results_stay_inside():
+    """A table of results within a wider one: nothing else is written."""
+    c = choose(50, 2, 4, 2)
+    r = experts.route(torch.from_numpy(c).cuda(), 4)
+    X, W = random_table(50, 96, 5, 1), random_table(4 * 21, 96, 6, 1)
+    want = experts.product(X, W, r)
+    wide = torch.full((102, 32), 7.0, device="cuda")
+    sd.sd_expert_product(X.c, W.c, r.c, 0, None, wide[1:, 4:], sd.SD_TYPE_F32, 32, torch.cuda.current_stream())
+    assert torch.equal(wide[1:101, 4:25], want)
+    assert (wide[0] == 7).all() and (wide[101] == 7).all() and (wide[:, :4] == 7).all() and (wide[:, 25:] == 7).all()
+
+
+def test_expert_product_with_offsets_that_fall():
+    """Offsets of another origin that do not ascend or pass the end: results are
+    whatever, but nothing outside is read or written."""
+    X, W = random_table(40, 64, 7, 1), random_table(3 * 8, 64, 8, 1)
+    place, source = torch.zeros(40, 1, dtype=torch.int32).cuda(), torch.full((40,), 1 << 29, dtype=torch.int32).cuda()
+    wide = torch.full((42, 8), 7.0, device="cuda")
+    for offsets in ([0, 30, 10, 40], [-5, 2, 1 << 30, -1], [0, 0, 0, 1 << 30], [40, 40, 40, 40], [1 << 30] * 4):
+        r = experts.Route(torch.tensor(offsets, dtype=torch.int32).cuda(), place, source)
+        sd.sd_expert_product(X.c, W.c, r.c, 0, None, wide[1:], sd.SD_TYPE_F32, 8, torch.cuda.current_stream())
+        assert (wide[0] == 7).all() and (wide[41] == 7).all()
+
+
+# ------------------------------------------------------------------ together ---
+def test_a_layer_of_experts():
+    """Aggregated features through each node's experts in 4 bits and back, beside the
+    same from 64-bit forms of the rounded tables."""
+    import gen
+
+    A = gen.random_rows(300, 300, np.full(300, 6, np.int32), seed=3)
+    plan = sd.sd_plan_ex(A, 72)
+    B = torch.randn(300, 72, generator=torch.Generator().manual_seed(1)).cuda()
+    C = torch.empty(300, 72, device="cuda")
+    sd.sd_spmm(plan, B, C, torch.cuda.current_stream())
+    scores = torch.randn(300, 6, generator=torch.Generator().manual_seed(2)).cuda()
+    top, chosen = torch.topk(scores, 2, dim=1)
+    weights = torch.softmax(top, 1)
+    Wf = (torch.randn(6, 40, 72, generator=torch.Generator().manual_seed(3)) * 72 ** -0.5).cuda()
+    r = experts.route(chosen, 6)
+    X, W = dense.pack4(C), dense.pack4(Wf.view(240, 72))
+    out = experts.combine(experts.product(X, W, r, dtype=torch.bfloat16), r, weights)
+    x, w, wt = of(X), of(W).reshape(6, 40, 72), to64(weights)
+    want = np.zeros((300, 40))
+    size = np.zeros((300, 40))
+    for t in range(300):
+        for j in range(2):
+            e = int(chosen[t, j])
+            want[t] += wt[t, j] * (w[e] @ x[t])
+            size[t] += wt[t, j] * (np.abs(w[e]) @ np.abs(x[t]))
+    # the product's sum and its rounding, two products and additions, one rounding more
+    bound = 2 * 2.0 ** -8 * size + 80 * 2.0 ** -23 * size
+    assert np.all(np.abs(to64(out) - want) <= bound)
+    plan.destroy()
+
+
+def test_a_training_step_of_experts():
+    """Rows to float experts and back, gradients of features, experts' weights and
+    routing weights, against the same in 64 bits by torch."""
+    g = torch.Generator().manual_seed(5)
+    x, w = torch.randn(80, 24, generator=g), torch.randn(5, 24, 16, generator=g)
+    c, wt = torch.from_numpy(choose(80, 2, 5, 5)), torch.rand(80, 2, generator=g)
+    d = torch.randn(80, 16, generator=g)
+    X, W, Wt = (v.cuda().requires_grad_() for v in (x, w, wt))
+    r = experts.route(c.cuda(), 5)
+    off = r.offsets.tolist()
+    xs = experts.dispatch(X, r)
+    ys = torch.cat([xs[off[e]:off[e + 1]] @ W[e] for e in range(5)] + [xs[off[5]:, :16]])
+    got = torch.autograd.grad(experts.combine(ys, r, Wt), (X, W, Wt), d.cuda())
+    x6, w6, t6 = (v.double().requires_grad_() for v in (x, w, wt))
+    out = torch.zeros(80, 16, dtype=torch.float64)
+    for j in range(2):
+        for e in range(5):
+            there = (c[:, j] == e).double()[:, None]
+            out = out + there * t6[:, j:j + 1] * (x6 @ w6[e])
+    want = torch.autograd.grad(out, (x6, w6, t6), d.double())
+    for a, b in zip(got, want):
+        # sums of at most 160 products of fp32 numbers of the size of these
+        assert np.all(np.abs(to64(a) - b.numpy()) <= 200 * 2.0 ** -24 * np.abs(b.numpy()).max() * 4)
+
+
+def test_captured_and_replayed():
+    """Sorting, dispatch, products and the way back with gradients in a graph,
+    replayed with other experts and eager work between."""
+    chosen = torch.from_numpy(choose(9000, 2, 12, 6)).cuda()
+    x = torch.randn(9000, 40, generator=torch.Generator().manual_seed(1)).cuda()
+    w = torch.from_numpy(weights_of(9000, 2, 6)).cuda()
+    W = dense.pack4(torch.randn(12 * 40, 40, generator=torch.Generator().manual_seed(2)).cuda())
+
+    def step():
+        r = experts.route(chosen, 12)
+        y = experts.product(dense.pack4(x), W, r)
+        a, b, c = x.detach().requires_grad_(), y.requires_grad_(), w.detach().requires_grad_()
+        out, there = experts.combine(b, r, c), experts.dispatch(a, r)
+        grads = torch.autograd.grad((out, there), (a, b, c), (x, y.detach()))
+        return (r.offsets, r.place, r.source, y.detach(), out.detach(), there.detach(), *grads)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for i in range(3):
+        chosen.copy_(torch.from_numpy(choose(9000, 2, 12, 20 + i)))
+        x.copy_(torch.randn(9000, 40, generator=torch.Generator().manual_seed(20 + i)))
+        want = step()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_another_stream():
+    chosen = torch.from_numpy(choose(20000, 2, 30, 7)).cuda()
+    x = torch.randn(20000, 16, generator=torch.Generator().manual_seed(1)).cuda()
+    want = experts.dispatch(x, experts.route(chosen, 30))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = experts.dispatch(x, experts.route(chosen, 30))
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(got, want)
+
+
+def test_offsets_past_32_bits():
+    """Sorted tables of more than 2^31 elements, and places far down."""
+    rows, cols = 1 << 20, 1100
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    c = torch.arange(rows * 2, device="cuda").view(rows, 2) % 3
+    r = experts.route(c, 3)
+    x = (torch.arange(rows, device="cuda") % 251).to(torch.bfloat16)[:, None].expand(rows, cols).contiguous()
+    xs = experts.dispatch(x, r)
+    for at in (0, 1, rows, 2 * rows - 1):
+        assert (xs[at] == x[int(r.source[at])]).all()
+    out = experts.combine(xs, r)
+    assert torch.equal(out[-5:], 2 * x[-5:]) and torch.equal(out[:5], 2 * x[:5])
+    dy, dw = experts.combine_backward(x, xs, r)
+    assert torch.equal(dy[-1], x[int(r.source[-1])])
+    want = (x[-3:, 0].double() ** 2 * cols)[:, None].expand(3, 2)
+    assert torch.allclose(dw[-3:].double(), want, rtol=1e-4, atol=0)
+
+
+def test_refusals_of_tensors():
+    r = experts.route(torch.zeros(4, 2, dtype=torch.int64, device="cuda"), 3)
+    x, y, w = torch.zeros(4, 8, device="cuda"), torch.zeros(8, 8, device="cuda"), torch.zeros(4, 2, device="cuda")
+    p, q = dense.pack4(x), dense.pack4(torch.zeros(15, 8, device="cuda"))
+    ints = torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    for call in (lambda: experts.dispatch(y, r), lambda: experts.dispatch(x.t(), r), lambda: experts.combine(x, r),
+                 lambda: experts.combine(y, r, w.double()), lambda: experts.combine(y, r, w.t()),
+                 lambda: experts.combine(y, r, w.cpu()), lambda: experts.combine_backward(y, y, r),
+                 lambda: experts.combine_backward(x, y.bfloat16(), r), lambda: experts.product(q, q, r),
+                 lambda: experts.product(p, dense.pack4(torch.zeros(16, 8, device="cuda")), r),
+                 lambda: experts.product(p, q, r, torch.zeros(5, device="cuda")),
+                 lambda: experts.product(p, q, r, sorted=True), lambda: experts.product(p, q, r, dtype=torch.int32),
+                 lambda: experts.route(ints.t(), 3), lambda: experts.route(ints.short(), 3),
+                 lambda: experts.route(ints[:, :0].contiguous(), 3), lambda: experts.Route(ints, ints, ints),
+                 lambda: experts.Route(r.offsets, ints, r.source[:7].contiguous())):
+        with pytest.raises(ValueError):
+            call()
+    for n in (0, -1, 4096):
+        with pytest.raises(sd.SparseDittoError):
+            experts.route(ints, n)

@@ -1,0 +1,396 @@
+"""4-bit tables on the GPU against plain 64-bit forms: packing bit for bit,
+products and a transform's gradients, at the sizes, strides and values where they
+can go wrong."""
+import numpy as np
+import pytest
+
+import nibble_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():  # pragma: no cover - CPU container
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2608_05033_amd as sd  # noqa: E402
+from paper_2608_05033_amd import dense, gcn  # noqa: E402
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+# half a unit in the last place of a rounding to the type, relative
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+def table(x, dtype):
+    """x rounded to dtype on the GPU, and the same numbers in 64 bits."""
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(torch.float64).to(TYPES[dtype])
+    return t.cuda(), t.to(torch.float64).numpy()
+
+
+def to64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def activations(rows, cols, seed):
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((rows, cols)) * np.exp(g.standard_normal((rows, 1)))
+    x[:, ::3] = np.maximum(x[:, ::3], 0)
+    return x
+
+
+def of(p):
+    return ref.values(p.codes.cpu().numpy(), p.scales.cpu().numpy(), p.cols)
+
+
+def check_packed(p, x64):
+    """Codes, signs of zeros, scales and padding bit for bit."""
+    scale, units = ref.encode(x64)
+    codes, scales = p.codes.cpu().numpy(), p.scales.cpu().numpy()
+    blocks = -(-p.cols // 32)
+    assert np.array_equal(ref.scale_bytes(scales, p.cols), scale)
+    got = ref.GRID[ref.halves(codes, p.cols)]
+    assert np.array_equal(got, units) and np.array_equal(np.signbit(got), np.signbit(units))
+    assert not ref.halves(codes, blocks * 32)[:, p.cols:].any()
+    assert (ref.scale_bytes(scales, scales.shape[0] * 128)[:, blocks:] == 127).all()
+
+
+# ---------------------------------------------------------------- packing ---
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 31), (5, 32), (7, 33), (64, 128), (33, 300), (65, 129), (130, 96),
+                                       (1030, 17)])
+def test_pack_bit_for_bit(rows, cols, dtype):
+    print(f"case pack4 {rows}x{cols} {dtype}", flush=True)
+    t, x = table(activations(rows, cols, rows * 1000 + cols), dtype)
+    p = dense.pack4(t)
+    check_packed(p, x)
+    check_packed(dense.pack4(t, transpose=True), np.ascontiguousarray(x.T))
+    for out in ("f32", "bf16", "f16"):
+        assert torch.equal(dense.unpack4(p, TYPES[out]).cpu(), torch.from_numpy(of(p)).to(torch.float32).to(TYPES[out]))
+
+
+def test_pack_edges_of_the_range():
+    """Ties, zeros of both signs, values at and past a power of two times 6, the ends
+    of the fp32 range, subnormal numbers, infinities and NaN; along rows and across."""
+    x = np.zeros((14, 70))
+    x[1, 3] = 6
+    x[2, 5] = np.nextafter(np.float32(6), np.float32(np.inf))
+    x[3, :16] = [6, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, -0.25, -0.75, -1.25, -1.75, -2.5, -3.5, -5, -0.0]
+    x[4, :32] = np.nextafter(np.float32(np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6] * 4)), np.float32(0))
+    x[5, :32] = np.nextafter(np.float32(np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 5.5] * 4)), np.float32(9))
+    x[6, :4] = [np.finfo(np.float32).max, -1.0, 1e38, 3e37]
+    x[7, :4] = [1e-38, -2e-38, 3e-39, 1e-44]
+    x[8, :3] = [2.0 ** -126, 2.0 ** -127, 2.0 ** -149]
+    x[9, 2] = 2.0 ** -149
+    x[10, 33], x[10, 1] = np.nan, 3.0
+    x[11, 65], x[11, 40] = -np.inf, 2.0
+    x[12, :] = np.nan
+    x[13, :] = np.ldexp(1.0, -np.arange(70) % 9)
+    x = x.astype(np.float32).astype(np.float64)
+    t = torch.from_numpy(x).float().cuda()
+    p = dense.pack4(t)
+    check_packed(p, x)
+    check_packed(dense.pack4(t.t().contiguous(), transpose=True), x)
+    nan = np.isnan(to64(dense.unpack4(p)))
+    want = np.zeros_like(nan)
+    want[10, 32:64], want[11, 64:], want[12] = True, True, True
+    assert np.array_equal(nan, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pack_strides(dtype):
+    """Strided, broadcast, shifted and misaligned tables."""
+    t, x = table(activations(150, 210, 5), dtype)
+    check_packed(dense.pack4(t[3:140, 1:202]), x[3:140, 1:202])
+    check_packed(dense.pack4(t[3:140, 1:202], transpose=True), np.ascontiguousarray(x[3:140, 1:202].T))
+    check_packed(dense.pack4(t[::2, ::3]), x[::2, ::3])
+    check_packed(dense.pack4(t[::2, ::3], transpose=True), np.ascontiguousarray(x[::2, ::3].T))
+    check_packed(dense.pack4(t[:1].expand(40, 210)), np.repeat(x[:1], 40, 0))
+    check_packed(dense.pack4(t[:, :1].expand(150, 70)), np.repeat(x[:, :1], 70, 1))
+    check_packed(dense.pack4(t[:, 5:6]), x[:, 5:6])
+    flat = torch.zeros(150 * 210 + 1, dtype=t.dtype, device="cuda")
+    flat[1:] = t.reshape(-1)
+    check_packed(dense.pack4(flat[1:].view(150, 210)), x)
+
+
+def test_unpack_every_code_and_scale():
+    codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1).cuda()  # 512 columns, every pair of codes
+    scales = torch.zeros(4, 256, 4, dtype=torch.uint8)
+    scales[:] = torch.arange(256, dtype=torch.uint8)[None, :, None]
+    p = dense.Packed4(codes, scales.cuda(), 512)
+    got, want = dense.unpack4(p).cpu(), torch.from_numpy(of(p)).to(torch.float32)
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    assert torch.equal(torch.nan_to_num(got, 1.0, 2.0, 3.0), torch.nan_to_num(want, 1.0, 2.0, 3.0))
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (0, 0)])
+def test_empty_tables(rows, cols):
+    p = dense.pack4(torch.zeros(rows, cols, device="cuda"))
+    assert tuple(dense.unpack4(p).shape) == (rows, cols)
+    w = dense.pack4(torch.zeros(3, cols, device="cuda"))
+    bias = torch.arange(3, dtype=torch.float32, device="cuda")
+    assert torch.equal(dense.product4(p, w, bias), bias.expand(rows, 3))
+    assert torch.equal(dense.product4(p, w, bias, torch.bfloat16), bias.expand(rows, 3).bfloat16())
+
+
+# --------------------------------------------------------------- products ---
+def random_table(rows, cols, seed, spread=6):
+    """Random codes and scales, as far as `cols` reaches."""
+    g = np.random.default_rng(seed)
+    codes = g.integers(0, 256, (rows, -(-cols // 32) * 16), dtype=np.uint8)
+    if cols % 32:
+        c = np.arange(codes.shape[1]) * 2
+        codes[:, c >= cols] = 0
+        if cols % 2:
+            codes[:, cols // 2] &= 15
+    groups = -(-cols // 128)
+    scales = (127 + g.integers(-spread, spread + 1, (groups, rows, 4))).astype(np.uint8)
+    return dense.Packed4(torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), cols)
+
+
+def check_product(y, x64, w64, bias, dtype):
+    """A block's products are summed exactly; each addition of a block's sum, of parts
+    of the sum over k (at most 64) and of the bias is cut or rounded to 24 bits, off by
+    at most 2^-23 of the magnitudes summed.  Then one rounding to the type."""
+    want = x64 @ w64.T + (0 if bias is None else bias)
+    size = np.abs(x64) @ np.abs(w64).T + (0 if bias is None else np.abs(bias))
+    bound = (-(-x64.shape[1] // 32) + 66) * 2.0 ** -23 * size
+    if dtype != "f32":
+        bound = bound + HALF_ULP[dtype] * np.abs(want) + 2.0 ** -25
+    err = np.abs(to64(y) - want)
+    assert np.all(err <= bound + 1e-37), float((err - bound).max())
+    if dtype == "f32" and want.size > 64:
+        assert np.linalg.norm(to64(y) - want) <= 2e-7 * np.linalg.norm(size)
+
+
+SIZES = [(1, 1, 1), (1, 128, 64), (1, 1000, 260), (2, 129, 5), (16, 384, 33), (17, 64, 16), (100, 601, 47),
+         (65, 16, 128), (300, 128, 130), (130, 2050, 70), (513, 257, 255), (700, 640, 1), (1, 4096, 512),
+         (40, 5000, 40)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,n", SIZES)
+def test_product(rows, cols, n, dtype):
+    print(f"case product4 {rows}x{cols}x{n} {dtype}", flush=True)
+    X, W = random_table(rows, cols, rows + cols, 3), random_table(n, cols, n + cols + 1, 3)
+    x, w = of(X), of(W)
+    w_scaled = w * 2.0 ** -8
+    W = dense.Packed4(W.codes, (W.scales.to(torch.int32) - 8).to(torch.uint8), cols)
+    check_product(dense.product4(X, W, dtype=TYPES[dtype]), x, w_scaled, None, dtype)
+    b = np.random.default_rng(n).standard_normal(n).astype(np.float32)
+    check_product(dense.product4(X, W, torch.from_numpy(b).cuda(), TYPES[dtype]), x, w_scaled,
+                  b.astype(np.float64), dtype)
+
+
+@pytest.mark.parametrize("rows,cols,n", [(1100, 400, 1030), (2600, 140, 520), (520, 2304, 2100), (4100, 33, 300)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_product_many_tiles(rows, cols, n, dtype):
+    print(f"case product4 {rows}x{cols}x{n} {dtype}", flush=True)
+    X, W = random_table(rows, cols, rows, 2), random_table(n, cols, n, 2)
+    check_product(dense.product4(X, W, dtype=TYPES[dtype]), of(X), of(W), None, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rows,cols,n", [(15001, 48, 47), (20000, 200, 64), (30011, 128, 128), (14003, 512, 100)])
+def test_product_long_and_narrow(rows, cols, n, dtype):
+    print(f"case product4 {rows}x{cols}x{n} {dtype}", flush=True)
+    X, W = random_table(rows, cols, rows, 2), random_table(n, cols, n, 2)
+    b = np.random.default_rng(n).standard_normal(n).astype(np.float32)
+    check_product(dense.product4(X, W, torch.from_numpy(b).cuda(), TYPES[dtype]), of(X), of(W),
+                  b.astype(np.float64), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,n", [(33, 40000, 47), (128, 100100, 64), (200, 30000, 260)])
+def test_product_long_sums(rows, cols, n, dtype):
+    """Few results of long sums, as a weight's gradient has them."""
+    print(f"case product4 {rows}x{cols}x{n} {dtype}", flush=True)
+    X, W = random_table(rows, cols, rows, 2), random_table(n, cols, n, 2)
+    b = np.random.default_rng(n).standard_normal(n).astype(np.float32)
+    check_product(dense.product4(X, W, torch.from_numpy(b).cuda(), TYPES[dtype]), of(X), of(W),
+                  b.astype(np.float64), dtype)
+
+
+@pytest.mark.parametrize("rows,cols,n", [(3, 500, 40), (150, 1000, 140), (600, 4096, 600)])
+def test_product_of_one_scale_is_exact(rows, cols, n):
+    """Sums of multiples of 1/4 below 2^22 fit 24 bits at every step."""
+    X, W = random_table(rows, cols, 1, 0), random_table(n, cols, 2, 0)
+    assert np.array_equal(to64(dense.product4(X, W)), of(X) @ of(W).T)
+
+
+def test_product_of_all_scales():
+    """Blocks whose scales differ by 2^80 and sums that cancel."""
+    X, W = random_table(100, 512, 3, 40), random_table(90, 512, 4, 40)
+    check_product(dense.product4(X, W), of(X), of(W), None, "f32")
+    x, w = random_table(64, 256, 5, 0), random_table(64, 256, 6, 0)
+    x.scales[0], w.scales[0] = 127 + 30, 127
+    x.codes[:, 32:64] = x.codes[:, :32]  # blocks 2 and 3 like 0 and 1 ...
+    w.codes[:, 32:64] = w.codes[:, :32] ^ 0x88  # ... times the negative
+    check_product(dense.product4(x, w), of(x), of(w), None, "f32")
+
+
+def test_product_at_the_ends_of_the_scales():
+    x, w = random_table(40, 200, 7, 0), random_table(30, 200, 8, 0)
+    want = of(x) @ of(w).T
+    for a, b in ((0, 254), (254, 0), (27, 227)):
+        x.scales[:], w.scales[:] = a, b
+        assert np.array_equal(to64(dense.product4(x, w)), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [4, 200, 700])
+def test_product_padding_and_strides(rows, dtype):
+    """Rows further apart than their codes need, other codes and scales of NaN
+    past the last block: they take no part."""
+    X, W = random_table(rows, 290, 9, 2), random_table(600, 290, 10, 2)
+    want = of(X), of(W)
+    out = []
+    for p in (X, W):
+        wide = torch.full((p.rows, 256), 0xFF, dtype=torch.uint8, device="cuda")
+        wide[:, :160] = p.codes
+        scales = p.scales.clone()
+        scales[2, :, 2:] = 255
+        out.append(dense.Packed4(wide, scales, 290))
+    check_product(dense.product4(*out, dtype=TYPES[dtype]), *want, None, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("rows,cols", [(3, 140), (150, 140), (600, 1100)])
+def test_product_keeps_nan_to_its_row(rows, cols, dtype):
+    g = np.random.default_rng(1)
+    x = g.standard_normal((rows, cols))
+    x[rows - 1, cols - 10] = np.inf
+    X = dense.pack4(torch.from_numpy(x).float().cuda())
+    W = dense.pack4(torch.from_numpy(g.standard_normal((270, cols))).float().cuda())
+    y = dense.product4(X, W, dtype=TYPES[dtype])
+    assert torch.isnan(y[rows - 1]).all() and torch.isfinite(y[:rows - 1]).all()
+
+
+def test_product_runs_on_the_current_stream_and_repeats():
+    X, W = random_table(64, 60000, 11, 2), random_table(80, 60000, 12, 2)
+    first = dense.product4(X, W)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        again = [dense.product4(X, W) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(first, y) for y in again)
+
+
+def test_captured_and_replayed():
+    """Packing, a product with a joined sum and unpacking in a graph, replayed with new
+    inputs and eager work between; two graphs whose workspaces are apart."""
+    x = torch.randn(300, 70, generator=torch.Generator().manual_seed(1)).cuda()
+    w = torch.randn(300, 90, generator=torch.Generator().manual_seed(2)).cuda()
+
+    def step():
+        a, b = dense.pack4(x, transpose=True), dense.pack4(w, transpose=True)
+        return dense.product4(a, b), dense.unpack4(a, torch.bfloat16)
+
+    step()
+    graphs = []
+    for _ in range(2):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out))
+    for i in range(3):
+        x.copy_(torch.randn(300, 70, generator=torch.Generator().manual_seed(10 + i)))
+        want = step()
+        for g, out in graphs:
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+# ---------------------------------------------------------------- gradients ---
+def rounded(x):
+    scale, units = ref.encode(x)
+    return units * np.repeat(np.ldexp(1.0, scale - 127), 32, axis=1)[:, :x.shape[1]]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,cols,n", [(1, 5, 3), (50, 33, 40), (700, 96, 130), (9000, 40, 24)])
+def test_transform_and_gradients(rows, cols, n, dtype):
+    """Z, dX and dW against products of what 64-bit forms round to 4 bits."""
+    t, x = table(activations(rows, cols, rows), dtype)
+    g = np.random.default_rng(n)
+    W, w = table(g.standard_normal((cols, n)) * cols ** -0.5, "f32")
+    dZ, dz = table(0.1 * g.standard_normal((rows, n)), "f32")
+    t.requires_grad_(), W.requires_grad_()
+    Z = gcn.transform4(t, W)
+    dX, dW = torch.autograd.grad(Z, (t, W), dZ)
+    assert dX.dtype == t.dtype and Z.dtype == dW.dtype == torch.float32
+    check_product(Z, rounded(x), rounded(w.T), None, "f32")
+    check_product(dX, rounded(dz), rounded(w), None, dtype)
+    check_product(dW, rounded(np.ascontiguousarray(x.T)), rounded(np.ascontiguousarray(dz.T)), None, "f32")
+
+
+def test_transform_gradients_are_differences():
+    """Inputs that 4 bits hold: the transform is then linear, and so are differences."""
+    g = torch.Generator().manual_seed(3)
+    grid = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+    def table_of(rows, cols):
+        v = grid[torch.randint(0, 8, (rows, cols), generator=g)] * (1 - 2.0 * torch.randint(0, 2, (rows, cols), generator=g))
+        v[:, ::16] = 6  # every block, along rows and across, has its largest
+        v[::16] = 6
+        return v
+
+    X, W, dX, dZ = table_of(64, 64), table_of(64, 64), table_of(64, 64), table_of(64, 64)
+    Xg = X.cuda().requires_grad_()
+    Wg = W.cuda().requires_grad_()
+    gx, gw = torch.autograd.grad(gcn.transform4(Xg, Wg), (Xg, Wg), dZ.cuda())
+    # <dZ, f(X + dX) - f(X)> = <gx, dX> for a linear f, all of it in whole quarters below 2^24
+    change = gcn.transform4(dX.cuda(), Wg.detach()).cpu().double()
+    assert float((dZ.double() * change).sum()) == float((gx.cpu().double() * dX.double()).sum())
+    change = gcn.transform4(Xg.detach(), dX.cuda()).cpu().double()
+    assert float((dZ.double() * change).sum()) == float((gw.cpu().double() * dX.double()).sum())
+
+
+def test_transform_only_what_is_asked_for():
+    X = torch.randn(40, 30, generator=torch.Generator().manual_seed(1)).cuda()
+    W = torch.randn(30, 20, generator=torch.Generator().manual_seed(2)).cuda().requires_grad_()
+    Z = gcn.transform4(X, W)
+    Z.sum().backward()  # an expanded output gradient
+    assert X.grad is None and W.grad.shape == W.shape
+    X.requires_grad_()
+    dX, = torch.autograd.grad(gcn.transform4(X, W.detach()).sum(), X)
+    assert torch.equal(dX, dense.product4(dense.pack4(torch.ones(40, 20, device="cuda")), dense.pack4(W.detach())))
+    gx, = torch.autograd.grad(gcn.transform4(X, W).sum(), X, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(gx.sum(), W)
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 bytes of codes: the last row alone is not zero."""
+    rows, cols = (1 << 27) + 3, 64
+    free, _ = torch.cuda.mem_get_info()
+    if free < 24 << 30:
+        pytest.skip("needs 24 GiB")
+    codes = torch.zeros(rows, 32, dtype=torch.uint8, device="cuda")
+    scales = torch.full((1, rows, 4), 127, dtype=torch.uint8, device="cuda")
+    codes[rows - 1] = 0x42  # 1 and 2 in turn
+    X = dense.Packed4(codes, scales, cols)
+    W = dense.pack4(torch.ones(4, cols, device="cuda"))
+    y = dense.product4(X, W)
+    assert torch.equal(y[-1], torch.full((4,), 32.0 * 3, device="cuda"))
+    assert not y[:-1].any()
+    v = dense.unpack4(X, torch.bfloat16)
+    assert torch.equal(v[-1].float(), torch.tensor([1.0, 2.0], device="cuda").repeat(32)) and not v[-5:-1].any()
+    again = dense.pack4(v)
+    assert torch.equal(dense.unpack4(again, torch.bfloat16)[-1], v[-1])
+
+
+def test_refusals_of_tensors():
+    x = torch.zeros(4, 40, device="cuda")
+    p, q = dense.pack4(x), dense.pack4(torch.zeros(4, 50, device="cuda"))
+    for call in (lambda: dense.product4(p, q), lambda: dense.product4(p, p, dtype=torch.float64),
+                 lambda: dense.product4(p, p, torch.zeros(5, device="cuda")), lambda: dense.unpack4(p, torch.int32),
+                 lambda: dense.Packed4(p.codes, p.scales, 70), lambda: dense.Packed4(p.codes, p.scales[:, :2], 40),
+                 lambda: dense.Packed4(p.codes, p.scales.cpu(), 40), lambda: dense.Packed4(p.codes.t(), p.scales, 4),
+                 lambda: gcn.transform4(x, torch.zeros(41, 3, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    shifted = torch.zeros(4 * 32 + 8, dtype=torch.uint8, device="cuda")[8:].view(4, 32)
+    with pytest.raises(sd.SparseDittoError):
+        dense.product4(dense.Packed4(shifted, p.scales, 40), p)
