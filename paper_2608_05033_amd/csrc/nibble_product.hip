@@ -12,12 +12,18 @@
 // block: sums of blocks of one scale are exact.  Measured over random codes, one
 // instruction is off by at most 2.1e-7 of the magnitudes summed, also where the
 // blocks' scales differ by 2^80 or the sum so far is 10^6 times the products.
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "nibble.h"
 #include "tiles.h"
 
 namespace {
 
 using namespace nibble;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 struct Operand {
   const uint8_t *codes, *scales;
@@ -144,16 +150,40 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
     const int64_t row = n0 + col_of<kWoven<T, NF>>(j, r);
     wrow[j] = w0 + (row < n ? row : n - 1);
   }
-  for (int32_t kg = wave; kg < ng; kg += KW) {
-    Frag x[MF], w[NF];
+  // Two neighbouring groups at a time, the whole line that holds them; the next two are on their way while
+  // these ones' products run.
+  struct Operands {
+    Frag x[2][MF], w[2][NF];
+  };
+  auto load = [&](int32_t pair, Operands &o) {
 #pragma unroll
-    for (int i = 0; i < MF; ++i) load_frag(X, xrow[i], kg, g, blocks, x[i]);
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int j = 0; j < NF; ++j) load_frag(W, wrow[j], kg, g, blocks, w[j]);
+      for (int i = 0; i < MF; ++i) load_frag(X, xrow[i], 2 * pair + h, g, blocks, o.x[h][i]);
 #pragma unroll
-    for (int i = 0; i < MF; ++i)
+      for (int j = 0; j < NF; ++j) load_frag(W, wrow[j], 2 * pair + h, g, blocks, o.w[h][j]);
+    }
+  };
+  auto multiply_all = [&](const Operands &o) {
 #pragma unroll
-      for (int j = 0; j < NF; ++j) acc[i][j] = multiply(w[j], x[i], acc[i][j]);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) acc[i][j] = multiply(o.w[h][j], o.x[h][i], acc[i][j]);
+  };
+  Operands a, b;
+  const int32_t pairs = (ng + 1) / 2;
+  int32_t pair = wave;
+  if (pair < pairs) load(pair, a);
+  while (pair < pairs) {
+    if (pair + KW < pairs) load(pair + KW, b);
+    multiply_all(a);
+    pair += KW;
+    if (pair >= pairs) break;
+    if (pair + KW < pairs) load(pair + KW, a);
+    multiply_all(b);
+    pair += KW;
   }
 #pragma unroll
   for (int i = 0; i < MF; ++i)
@@ -175,43 +205,481 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
   }
 }
 
+// s_waitcnt's operand: all of the wave's reads of shared memory are back, and all
+// but the last `left` of what it asked for from memory.
+__device__ constexpr int wait_until(int left) { return (left & 15) | (left >> 4) << 14 | 0x70; }
+
+// BM x BN tiles (rows of X by rows of W), operands through shared memory: WM x WN
+// waves, each (BM / WM) x (BN / WN) in products of 32 x 32 x 64, which run at 1.4 to
+// 1.8 times the rate of 16 x 16 x 128.
+//
+// Four buffers hold 128 k (a stage) each.  What is asked for goes from memory straight
+// to shared memory, up to four stages ahead: a stage takes about half of the time that
+// memory needs to answer.  A stage's two products per tile overlap with reads: while
+// the first runs, the second one's operands come from shared memory; then, behind the
+// one barrier of the stage, the next stage's first ones while the second runs.
+//
+// Rows of codes lie 64 bytes apart, their four blocks mixed with the row so that 16
+// rows read at one block touch all banks; the mixing is done on the memory side, since
+// a wave's 64 lanes write 1 KiB in order.  Lane (r, g) = (lane % 32, lane / 32) takes
+// blocks 2 g and 2 g + 1 of a row.  Scale words lie by lane, the tile's 32-row groups
+// side by side, and one read serves several products.
+//
+// A wave's results go through its share of the shared memory, 32 rows at a time, so
+// that whole lines are written.
+template <typename T, int BM, int BN, int BUFFERS, bool EXPERTS>
+__global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorted sorted,
+                                                             const float *__restrict__ bias, T *__restrict__ Y,
+                                                             int64_t stride, int64_t rows, int64_t n, int32_t blocks,
+                                                             int32_t stages, int32_t mt, int32_t nt,
+                                                             int32_t split_stages, int64_t split_stride) {
+  constexpr int THREADS = 256, WM = 2, WN = 2, MF = BM / WM / 32, NF = BN / WN / 32;
+  constexpr int ROWS = BM + BN, CHUNKS = ROWS * 8 / THREADS, SCALES = 2 * ROWS / THREADS;
+  constexpr int BUFFER = ROWS * 136, PITCH = NF * 32 + 4;  // PITCH: floats between a wave's rows of results
+  static_assert(ROWS % THREADS == 0 && BM % (THREADS / 8) == 0 && BM % 64 == 0, "one operand for a wave");
+  static_assert(2 * 32 * PITCH * 4 <= BUFFER && (BUFFERS == 2 || BUFFERS == 4), "two waves' results in a buffer");
+  // objects of their own and no array: reads of one then need not wait for what is on its way to another
+  __shared__ __align__(16) uint8_t buffer_a[BUFFER], buffer_b[BUFFER];
+  __shared__ __align__(16) uint8_t buffer_c[BUFFERS == 4 ? BUFFER : 16], buffer_d[BUFFERS == 4 ? BUFFER : 16];
+  const int t = threadIdx.x, lane = t & 63, r = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WN, wn = wave % WN;
+  const uint32_t tiles = (uint32_t)mt * (uint32_t)nt, split = workgroup() / tiles;
+  const int32_t first = split * split_stages, last = first + split_stages < stages ? first + split_stages : stages;
+  if (first >= last && split > 0) return;
+  Y += split * split_stride;
+  const uint32_t at = xcd_place(workgroup() - split * tiles, tiles);
+  // tiles in bands of 8 along m: neighbours in the list share X's and W's rows
+  const uint32_t band = at / (8u * nt), left = mt - band * 8u < 8u ? mt - band * 8u : 8u;
+  const uint32_t in_band = at - band * 8u * nt;
+  const uint32_t mtile = band * 8u + in_band % left;
+  const int64_t n0 = (int64_t)(in_band / left) * BN;
+  int64_t m0 = (int64_t)mtile * BM, m1 = rows, w0 = 0;
+  if constexpr (EXPERTS) {
+    int32_t expert;
+    if (!find_tile(sorted, mtile, BM, m0, m1, expert)) return;
+    if (expert < 0) {
+      clear_rows(Y, stride, m0, m1, n0, n0 + BN < n ? n0 + BN : n);
+      return;
+    }
+    w0 = expert * n;
+    if (bias) bias += w0;
+  }
+  const auto x_row = [&](int row) -> int64_t {  // X's row for one of the tile; past the last one, that
+    const int64_t m = m0 + row < m1 ? m0 + row : m1 - 1;
+    if constexpr (EXPERTS) {
+      if (sorted.source) {
+        const int64_t from = sorted.source[m];
+        return from < 0 ? 0 : from < X.rows ? from : X.rows - 1;
+      }
+    }
+    return m;
+  };
+  const auto w_row = [&](int row) -> int64_t { return w0 + (n0 + row < n ? n0 + row : n - 1); };
+
+  // Block i of thread t: row i * THREADS / 8 + t / 8 of the tile (X's rows first), place t % 8.
+  constexpr int XC = BM / (THREADS / 8);  // of them, X's
+  const int chunk = (t & 7) ^ ((t >> 4) & 7);
+  const int64_t xfirst = EXPERTS ? 0 : m0, wfirst = w0 + n0;
+  const uint8_t *xbase = X.codes + xfirst * X.ld, *wbase = W.codes + wfirst * W.ld;
+  uint32_t off[CHUNKS];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int row = (i < XC ? i : i - XC) * (THREADS / 8) + t / 8;
+    off[i] = i < XC ? (uint32_t)(x_row(row) - xfirst) * (uint32_t)X.ld
+                    : (uint32_t)(w_row(row) - wfirst) * (uint32_t)W.ld;
+  }
+  // Scale word i of thread t: place i * THREADS + t of [g][X's, then W's][wave row or column][r][product].
+  const uint8_t *ssrc[ROWS / THREADS];
+#pragma unroll
+  for (int i = 0; i < ROWS / THREADS; ++i) {
+    const bool of_x = i * THREADS + wave * 64 < BM;
+    const int u = i * THREADS + t - (of_x ? 0 : BM), f = of_x ? MF : NF;
+    const int row = (u / (32 * f) * f + u % f) * 32 + u / f % 32;
+    ssrc[i] = of_x ? X.scales + x_row(row) * 4 : W.scales + w_row(row) * 4;
+  }
+  // Part `part` of four of stage st; past the last stage: that one again, for nothing; past a row's last block
+  // or group of scales: that one again
+  auto fetch = [&](int32_t st, int part, uint8_t *buffer) {
+    st = st < last ? st : last - 1;
+    const uint32_t block = st * 8 + chunk < blocks ? st * 8 + chunk : blocks - 1;
+#pragma unroll
+    for (int i = part * (CHUNKS / 4); i < (part + 1) * (CHUNKS / 4); ++i)
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void *)((i < XC ? xbase : wbase) + (off[i] + block * 16)),
+          (__attribute__((address_space(3))) void *)(&buffer[(i * THREADS + wave * 64) * 16]), 16, 0, 0);
+#pragma unroll
+    for (int i = part * SCALES / 4; i < (part + 1) * SCALES / 4; ++i) {
+      const int at = i * THREADS + wave * 64;
+      const int64_t group = st * 2 + (at >= ROWS && st * 2 + 1 < (blocks + 3) / 4 ? 1 : 0);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void *)(ssrc[i % (ROWS / THREADS)] +
+                                                           group * ((at % ROWS < BM ? X.rows : W.rows) * 4)),
+          (__attribute__((address_space(3))) void *)(&buffer[ROWS * 128 + at * 4]), 4, 0, 0);
+    }
+  };
+
+  struct Operands {
+    i32x8 x[MF], w[NF];
+  };
+  struct Scales {
+    uint32_t x[MF], w[NF];
+  };
+  // Where a lane's block of its row lies: the mixing of a row is bits 1 to 3 of its number.
+  const int xlo = (wm * MF * 32 + r) * 128, wlo = (BM + wn * NF * 32 + r) * 128, mix = (r >> 1) & 7;
+  const int xs = ROWS * 128 + (g * ROWS + (wm * 32 + r) * MF) * 4;
+  const int ws = ROWS * 128 + (g * ROWS + BM + (wn * 32 + r) * NF) * 4;
+  auto load = [&](const uint8_t *buffer, int h, Operands &o) {
+    const int place = ((4 * g + h) ^ mix) * 16;
+#pragma unroll
+    for (int j = 0; j < NF; ++j) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(buffer + wlo + j * 32 * 128 + place);
+      o.w[j] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      const u32x4 v = *reinterpret_cast<const u32x4 *>(buffer + xlo + i * 32 * 128 + place);
+      o.x[i] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
+    }
+  };
+  // Blocks past the last, whose codes are another's, get the scale 2^-127 on both sides:
+  // what they add is under 2^-240.
+  auto load_scales = [&](const uint8_t *buffer, int32_t st, Scales &o) {
+    const int32_t have = st < last ? blocks - (st * 8 + g * 4) : 0;
+    const uint32_t mask = have >= 4 ? ~0u : have <= 0 ? 0u : (1u << (8 * have)) - 1;
+#pragma unroll
+    for (int i = 0; i < MF; ++i) o.x[i] = *reinterpret_cast<const uint32_t *>(buffer + xs + i * 4) & mask;
+#pragma unroll
+    for (int j = 0; j < NF; ++j) o.w[j] = *reinterpret_cast<const uint32_t *>(buffer + ws + j * 4) & mask;
+  };
+  f32x16 acc[MF][NF] = {};
+  auto multiply_all = [&](const Operands &o, const Scales &s, auto h) {
+    constexpr int H = decltype(h)::value;
+#pragma unroll
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(o.w[j], o.x[i], acc[i][j], 4, 4, H, (int)s.w[j], H,
+                                                                    (int)s.x[i]);
+  };
+  Operands a, b;
+  Scales s, s_next;
+  // The order within a fourth of a stage: a read of shared memory behind every product, or two and a request
+  // to memory.
+  auto weave = [&](auto requests) {
+    constexpr int R = decltype(requests)::value, READS = MF + NF, BOTH = READS > R ? READS : R;
+#pragma unroll
+    for (int i = 0; i < BOTH; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+      if (i < READS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // a read of shared memory
+      if (i < R) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);      // a request
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int ASKED = CHUNKS + SCALES, HALF = ASKED / 2;
+  auto stage = [&](int32_t st, uint8_t *buffer, const uint8_t *buffer_next, uint8_t *buffer_before) {
+    load(buffer, 1, b);
+    fetch(st + BUFFERS - 1, 2, buffer_before);
+    fetch(st + BUFFERS - 1, 3, buffer_before);
+    multiply_all(a, s, std::integral_constant<int, 0>());
+    weave(std::integral_constant<int, HALF>());
+    load(buffer, 2, a);
+    multiply_all(b, s, std::integral_constant<int, 1>());
+    weave(std::integral_constant<int, 0>());
+    load(buffer, 3, b);
+    multiply_all(a, s, std::integral_constant<int, 2>());
+    weave(std::integral_constant<int, 0>());
+    // This wave's part of the next stage is there; behind the barrier every wave's is, and nobody reads this
+    // stage's buffer any more.
+    __builtin_amdgcn_s_waitcnt(wait_until((BUFFERS - 2) * ASKED));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    load(buffer_next, 0, a);
+    load_scales(buffer_next, st + 1, s_next);
+    fetch(st + BUFFERS, 0, buffer);
+    fetch(st + BUFFERS, 1, buffer);
+    multiply_all(b, s, std::integral_constant<int, 3>());
+    weave(std::integral_constant<int, HALF>());
+    s = s_next;
+  };
+  if (first < last) {
+    auto fetch_half = [&](int32_t st, int half, uint8_t *buffer) {
+      fetch(st, 2 * half, buffer);
+      fetch(st, 2 * half + 1, buffer);
+    };
+    fetch_half(first, 0, buffer_a);
+    fetch_half(first, 1, buffer_a);
+    if constexpr (BUFFERS == 4) {
+      fetch_half(first + 1, 0, buffer_b);
+      fetch_half(first + 1, 1, buffer_b);
+      fetch_half(first + 2, 0, buffer_c);
+      fetch_half(first + 2, 1, buffer_c);
+      fetch_half(first + 3, 0, buffer_d);
+    } else {
+      fetch_half(first + 1, 0, buffer_b);
+    }
+    __builtin_amdgcn_s_waitcnt(wait_until((BUFFERS - 2) * ASKED + HALF));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(buffer_a, 0, a);
+    load_scales(buffer_a, first, s);
+    // Rounds of all buffers, then the rest: with no path on which a stage of a round is skipped the compiler
+    // sees which requests are still under way for which buffer, and waits for no others.
+    int32_t st = first;
+    if constexpr (BUFFERS == 2) {  // the last one may be of blocks past the last, which add nothing
+      for (; st < last; st += 2) {
+        stage(st, buffer_a, buffer_b, buffer_b);
+        stage(st + 1, buffer_b, buffer_a, buffer_a);
+      }
+    } else {
+      for (; st + 4 <= last; st += 4) {
+        stage(st, buffer_a, buffer_b, buffer_d);
+        stage(st + 1, buffer_b, buffer_c, buffer_a);
+        stage(st + 2, buffer_c, buffer_d, buffer_b);
+        stage(st + 3, buffer_d, buffer_a, buffer_c);
+      }
+      if (st < last) {
+        stage(st, buffer_a, buffer_b, buffer_d);
+        if (st + 1 < last) {
+          stage(st + 1, buffer_b, buffer_c, buffer_a);
+          if (st + 2 < last) stage(st + 2, buffer_c, buffer_d, buffer_b);
+        }
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(wait_until(0));  // nothing is on its way to shared memory any more, from no wave
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+
+  float *mine = reinterpret_cast<float *>(wave < 2 ? buffer_a : buffer_b) + wave % 2 * (32 * PITCH);
+  constexpr int V = 16 / sizeof(T), LANES = NF * 32 / V, STEP = 64 / LANES;  // columns of a lane, lanes of a row
+  const int vr = lane / LANES, vc = lane % LANES * V;
+  const int64_t c = n0 + wn * NF * 32 + vc;
+  const int there = n - c < V ? (int)(n - c) : V;
+  float add[V] = {};
+  if (bias) {
+#pragma unroll
+    for (int q = 0; q < V; ++q) add[q] = q < there ? bias[c + q] : 0.0f;
+  }
+  __builtin_amdgcn_s_waitcnt(wait_until(0));  // so that no read below waits for it, and with it for the writes under way
+  T *y = Y + (m0 + wm * MF * 32 + vr) * stride + c;
+  auto put = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(mine + r * PITCH + j * 32 + q * 8 + g * 4) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __builtin_amdgcn_wave_barrier();
+  };
+  auto get = [&](int row, float (&out)[V]) {
+#pragma unroll
+    for (int q = 0; q < V; q += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + row * PITCH + vc + q);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) out[q + p] = v[p] + add[q + p];
+    }
+  };
+  if (m0 + BM <= m1 && n0 + BN <= n) {  // a whole tile: no conditions between the reads and the writes
+#pragma unroll
+    for (int i = 0; i < MF; ++i) {
+      put(i);
+#pragma unroll
+      for (int k = 0; k < 32 / STEP; ++k) {
+        float out[V];
+        get(k * STEP + vr, out);
+        store_span(y + (i * 32 + k * STEP) * stride, out);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < MF; ++i) {
+    const int64_t m = m0 + (wm * MF + i) * 32;
+    put(i);
+    for (int k = 0; k < 32 / STEP; ++k) {
+      float out[V];
+      get(k * STEP + vr, out);
+      if (m + k * STEP + vr >= m1) continue;
+      if (there == V)
+        store_span(y + (i * 32 + k * STEP) * stride, out);
+      else
+        store_part(y + (i * 32 + k * STEP) * stride, there, out);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Y = the sum of the parts that workgroups of a split sum left + bias: TEAM threads for four columns, each
+// every TEAM-th part, then the threads' sums, all in one order.
+template <typename T, int TEAM>
+__global__ __launch_bounds__(256) void k_nibble_join(const float *__restrict__ parts, int32_t splits, int64_t rows,
+                                                     int64_t n, const float *__restrict__ bias, T *__restrict__ Y,
+                                                     int64_t stride) {
+  constexpr int QUADS = 256 / TEAM;
+  __shared__ f32x4 sums[TEAM][QUADS];
+  const int own = threadIdx.x % QUADS, team = threadIdx.x / QUADS;
+  const int64_t quads = (n + 3) / 4, at = (int64_t)workgroup() * QUADS + own, m = at / quads, c = at % quads * 4;
+  const int there = m >= rows ? 0 : n - c < 4 ? (int)(n - c) : 4;
+  const float *p = parts + (team * rows + m) * n + c;
+  float sum[4] = {};
+  if (there == 4) {
+#pragma unroll 4
+    for (int32_t i = team; i < splits; i += TEAM, p += TEAM * rows * n) {
+      float v[4];
+      load_span(p, v);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[q] += v[q];
+    }
+  } else {
+    for (int32_t i = team; i < splits; i += TEAM, p += TEAM * rows * n) {
+      float v[4];
+      load_part(p, there, v);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[q] += v[q];
+    }
+  }
+  if constexpr (TEAM > 1) {
+    sums[team][own] = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    __syncthreads();
+    if (team > 0) return;
+#pragma unroll
+    for (int i = 1; i < TEAM; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[q] += sums[i][own][q];
+  }
+  if (there == 0) return;
+  if (bias) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum[q] += q < there ? bias[c + q] : 0.0f;
+  }
+  if (there == 4)
+    store_span(Y + m * stride + c, sum);
+  else
+    store_part(Y + m * stride + c, there, sum);
+}
+
 struct Call {
   Operand x, w;
   Sorted sorted;
   const float *bias;
   int64_t stride, rows, n;
   int32_t blocks, ng;
+  float *parts;  // workspace of a split sum
 };
 
-// Tiles of bm rows: as many as there are, or for sorted rows at most as many as there can be.
-template <bool EXPERTS>
-int64_t row_tiles(const Call &c, int64_t bm) {
-  if (!EXPERTS) return ceil_div(c.rows, bm);
-  const int64_t parts = c.sorted.experts + 1 < c.rows ? c.sorted.experts + 1 : c.rows;  // that are not empty
-  return (c.rows - parts) / bm + parts;
+enum Form { kTile256, kTile128, kTile128Deep, kRows32, kRows32Short, kRows16, kRows16Short };
+struct Plan {
+  Form form;
+  int32_t splits, split_stages;
+};
+
+// Tiles of bm rows: as many as there are, or for rows sorted by expert at most as many as there can be.
+int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
+  if (experts == 0) return ceil_div(rows, bm);
+  const int64_t parts = experts + 1 < rows ? experts + 1 : rows;  // that are not empty
+  return (rows - parts) / bm + parts;
+}
+
+// Measured in us, 16-bit results, launches in a row (256 compute units; "s": 128 x 128 tiles with the sum in so
+// many parts, joined by a second launch):
+//   rows x columns x k      256x256   128x128  32x32  16x16   s4    s16   s64   s128
+//   8192 x 8192 x 8192          243       319
+//   4096 x 4096 x 4096           38        43
+//   2048 x 2048 x 2048           18       8.8
+//   1000 x 1000 x 1000           17       6.8   13.9   15.8
+//   256 x 4096 x 4096            25        11     24     37    20    26
+//   64 x 4096 x 4096             25        11    7.1     11    12    22
+//   512 x 512 x 4096             24        11    7.2     11    11    18
+//   1 x 4096 x 4096              23        10    5.2    3.7     9    12
+//   262144 x 47 x 64             65        29    167    100
+//   512 x 512 x 32768           147        55     39     72    21    19    43
+//   64 x 64 x 65536             273       103     71     37    33    15    11     11
+//   256 x 128 x 262144         1110       406    278    142   108    34    19     20
+// A stage of 256 k takes a lone 128 x 128 tile 0.5 us, and the parts go to memory and back at about
+// 2.5 TB/s: that gives the number of parts.
+Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) {
+  const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
+  const auto tiles = [&](int64_t bm, int64_t bn) { return row_tiles(rows, experts, bm) * ceil_div(n, bn); };
+  const auto whole = [&](Form f) { return Plan{f, 1, (int32_t)stages}; };
+  if (near) {
+    if (4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
+    const int64_t t = tiles(128, 128);
+    const bool wide = rows > 64 && n > 64 && t >= cus / 8, many = t >= cus / 2;
+    if (experts == 0 && !many && stages >= (wide ? 32 : 64)) {
+      const int64_t best = (int64_t)std::sqrt(0.5 * stages / ((double)rows * n * 8 / 2.5e6));
+      const int64_t splits = std::min(std::min(cus / t, stages / 4), best);
+      if (splits > 1) {
+        const int64_t each = ceil_div(stages, splits);
+        return Plan{kTile128Deep, (int32_t)ceil_div(stages, each), (int32_t)each};
+      }
+    }
+    // four buffers, and with them one workgroup a compute unit, where the sum is long and there are no more
+    // tiles: 2048 x 2048 x 8192 takes 23 us so and 28 with two
+    if (wide || many) return whole(t <= cus && stages >= 24 ? kTile128Deep : kTile128);
+  }
+  if (rows > 16 && n > 16 && tiles(32, 32) >= cus) return whole(stages > 4 ? kRows32 : kRows32Short);
+  return whole(stages > 4 ? kRows16 : kRows16Short);
+}
+size_t parts_bytes(const Plan &p, int64_t rows, int64_t n) {
+  return p.splits > 1 ? (size_t)p.splits * rows * n * 4 : 0;
 }
 
 template <typename T, int MF, int NF, int KW, bool EXPERTS>
 int rows_launch(const Call &c, T *y, hipStream_t s) {
   static_assert(MF <= KW, "a wave for each row group");
-  const int64_t nt = ceil_div(c.n, NF * 16), wgs = row_tiles<EXPERTS>(c, MF * 16) * nt;
+  const int64_t nt = ceil_div(c.n, NF * 16), wgs = row_tiles(c.rows, EXPERTS ? c.sorted.experts : 0, MF * 16) * nt;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   hipLaunchKernelGGL((k_nibble_rows<T, MF, NF, KW, EXPERTS>), grid_of(wgs), dim3(KW * 64), 0, s, c.x, c.w, c.sorted,
                      c.bias, y, c.stride, c.rows, c.n, c.blocks, c.ng, (int32_t)nt);
   return launched();
 }
 
+template <typename T, int BM, int BN, int BUFFERS, bool EXPERTS>
+int tile_launch(const Call &c, const Plan &p, T *y, hipStream_t s) {
+  const int64_t mt = row_tiles(c.rows, EXPERTS ? c.sorted.experts : 0, BM), nt = ceil_div(c.n, BN);
+  if (mt * nt > INT32_MAX / p.splits) return SD_ERR_OVERFLOW;
+  const bool parts = p.splits > 1;
+  hipLaunchKernelGGL((k_nibble_tile<T, BM, BN, BUFFERS, EXPERTS>), grid_of(mt * nt * p.splits), dim3(256), 0, s, c.x,
+                     c.w, c.sorted, parts ? nullptr : c.bias, y, parts ? c.n : c.stride, c.rows, c.n, c.blocks,
+                     (c.ng + 1) / 2, (int32_t)mt, (int32_t)nt, p.split_stages, c.rows * c.n);
+  return launched();
+}
+
 template <typename T, bool EXPERTS>
-int product_as(const Call &c, void *Y, hipStream_t s) {
-  return rows_launch<T, 2, 2, 4, EXPERTS>(c, static_cast<T *>(Y), s);
+int product_as(const Call &c, const Plan &p, void *Y, hipStream_t s) {
+  T *y = static_cast<T *>(Y);
+  if (p.splits > 1) {
+    int st = tile_launch<float, 128, 128, 4, false>(c, p, c.parts, s);
+    if (st != SD_OK) return st;
+    const int team = p.splits >= 16 ? 8 : 1;
+    const int64_t wgs = ceil_div(c.rows * ceil_div(c.n, 4), 256 / team);
+    if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
+    auto *kernel = team == 8 ? k_nibble_join<T, 8> : k_nibble_join<T, 1>;
+    hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(256), 0, s, c.parts, p.splits, c.rows, c.n, c.bias, y, c.stride);
+    return launched();
+  }
+  switch (p.form) {
+    case kTile256: return tile_launch<T, 256, 256, 2, EXPERTS>(c, p, y, s);
+    case kTile128: return tile_launch<T, 128, 128, 2, EXPERTS>(c, p, y, s);
+    case kTile128Deep: return tile_launch<T, 128, 128, 4, EXPERTS>(c, p, y, s);
+    case kRows32: return rows_launch<T, 2, 2, 8, EXPERTS>(c, y, s);
+    case kRows32Short: return rows_launch<T, 2, 2, 4, EXPERTS>(c, y, s);
+    case kRows16: return rows_launch<T, 1, 1, 8, EXPERTS>(c, y, s);
+    default: return rows_launch<T, 1, 1, 4, EXPERTS>(c, y, s);
+  }
 }
 template <bool EXPERTS>
-int product(const Call &c, void *Y, int32_t type, void *stream) {
+int product(const Call &c, const Plan &p, void *Y, int32_t type, void *stream) {
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  return type == SD_TYPE_F32   ? product_as<float, EXPERTS>(c, Y, s)
-         : type == SD_TYPE_F16 ? product_as<f16, EXPERTS>(c, Y, s)
-                               : product_as<bf16, EXPERTS>(c, Y, s);
+  return type == SD_TYPE_F32   ? product_as<float, EXPERTS>(c, p, Y, s)
+         : type == SD_TYPE_F16 ? product_as<f16, EXPERTS>(c, p, Y, s)
+                               : product_as<bf16, EXPERTS>(c, p, Y, s);
 }
+
+// The large tiles keep the distance of a tile's rows in 32 bits.
+bool near_rows(const sd_nibble_t *p) { return p->ld <= (1 << 23); }
 
 Operand operand(const sd_nibble_t *p) { return Operand{p->codes, p->scales, p->ld, p->rows}; }
 
@@ -220,7 +688,7 @@ Operand operand(const sd_nibble_t *p) { return Operand{p->codes, p->scales, p->l
 extern "C" int sd_nibble_product_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes) {
   if (!bytes || rows < 0 || cols < 0 || n < 0) return SD_ERR_INVALID_VALUE;
   if (rows > kMaxRows || n > kMaxRows || cols > kMaxRows - 1024) return SD_ERR_OVERFLOW;
-  *bytes = 0;
+  *bytes = rows == 0 || n == 0 ? 0 : parts_bytes(plan_of(rows, 0, n, cols, true), rows, n);
   return SD_OK;
 }
 
@@ -238,9 +706,10 @@ extern "C" int sd_nibble_product(const sd_nibble_t *X, const sd_nibble_t *W, con
   if (st != SD_OK) return st;
   if (X->rows == 0 || W->rows == 0) return SD_OK;
   if ((st = have_device()) != SD_OK) return st;
+  const Plan p = plan_of(X->rows, 0, W->rows, X->cols, near_rows(X) && near_rows(W));
   const Call c{operand(X), operand(W), Sorted{}, bias, row_stride, X->rows, W->rows, (int32_t)col_blocks(X->cols),
-               (int32_t)groups_of(X->cols)};
-  return product<false>(c, Y, type, stream);
+               (int32_t)groups_of(X->cols), static_cast<float *>(workspace)};
+  return product<false>(c, p, Y, type, stream);
 }
 
 extern "C" int sd_expert_product(const sd_nibble_t *X, const sd_nibble_t *W, const sd_route_t *route, int32_t sorted,
@@ -258,7 +727,10 @@ extern "C" int sd_expert_product(const sd_nibble_t *X, const sd_nibble_t *W, con
   if (bias && !aligned_to(bias, 4)) return SD_ERR_INVALID_VALUE;
   if (total == 0 || n == 0) return SD_OK;
   if ((st = have_device()) != SD_OK) return st;
+  // the large tiles take X's rows from anywhere and keep their distance from its first one in 32 bits
+  const bool near = near_rows(W) && X->rows <= (1ll << 32) / (X->ld > 0 ? X->ld : 1);
+  const Plan p = plan_of(total, route->experts, n, X->cols, near);
   const Call c{operand(X), operand(W), Sorted{route->offsets, sorted ? nullptr : route->source, route->experts, total},
-               bias, row_stride, total, n, (int32_t)col_blocks(X->cols), (int32_t)groups_of(X->cols)};
-  return product<true>(c, Y, type, stream);
+               bias, row_stride, total, n, (int32_t)col_blocks(X->cols), (int32_t)groups_of(X->cols), nullptr};
+  return product<true>(c, p, Y, type, stream);
 }
