@@ -195,6 +195,7 @@ def _load():
                                            ctypes.c_size_t, _P]
     nibble, route = ctypes.POINTER(sd_nibble_t), ctypes.POINTER(sd_route_t)
     lib.sd_nibble_pack.argtypes = [_P, _i32, _i64, _i64, nibble, _P]
+    lib.sd_nibble_pack_both.argtypes = [_P, _i32, _i64, _i64, nibble, nibble, _P]
     lib.sd_nibble_unpack.argtypes = [nibble, _P, _i32, _i64, _P]
     lib.sd_nibble_product_size.argtypes = [_i64, _i64, _i64, size]
     lib.sd_nibble_product.argtypes = [nibble, nibble, _P, _P, _i32, _i64, _P, ctypes.c_size_t, _P]
@@ -205,8 +206,8 @@ def _load():
     lib.sd_combine_backward.argtypes = [route, _P, _i32, _i64, _i64, _P, _i64, _P, _P, _i64, _P, _P]
     lib.sd_expert_product.argtypes = [nibble, nibble, route, _i32, _P, _P, _i32, _i64, _P]
     for f in ("sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
-              "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_unpack",
-              "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
+              "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_pack_both",
+              "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
               "sd_combine_backward", "sd_expert_product"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_spmm", "sd_plan_info", "sd_plan_export_size",
@@ -219,8 +220,8 @@ _lib = _load()
 EXPORTED = ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_plan_device", "sd_spmm", "sd_spmm_merge_noalloc", "sd_plan_info", "sd_plan_export_size",
             "sd_plan_export", "sd_plan_destroy", "sd_plan_cache_clear", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load", "sd_release_memory", "sd_status_string", "sd_last_error",
             "sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
-            "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_unpack",
-            "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
+            "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_pack_both",
+            "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
             "sd_combine_backward", "sd_expert_product")
 
 
@@ -454,6 +455,13 @@ def sd_group_norm_backward(d: sd_norm_t, dy, dy_stride: int, x, x_stride: int, x
 def sd_nibble_pack(x, type: int, row_stride: int, col_stride: int, out: sd_nibble_t, stream=None) -> None:
     """Device table x (pointer or tensor) into the 4-bit codes and scales of `out`."""
     _check(_lib.sd_nibble_pack(_devptr(x), type, row_stride, col_stride, out, _stream(stream)), "sd_nibble_pack")
+
+
+def sd_nibble_pack_both(x, type: int, row_stride: int, col_stride: int, out: sd_nibble_t, out_t: sd_nibble_t,
+                        stream=None) -> None:
+    """The table and its transpose from one reading."""
+    _check(_lib.sd_nibble_pack_both(_devptr(x), type, row_stride, col_stride, out, out_t, _stream(stream)),
+           "sd_nibble_pack_both")
 
 
 def sd_nibble_unpack(x: sd_nibble_t, y, type: int, row_stride: int, stream=None) -> None:

@@ -35,21 +35,35 @@ __device__ inline uint64_t same_kind(uint32_t kind, int bits, bool there) {
   return mask;
 }
 
+// Calls f(entry, whether there is one, its kind) for entries [begin, end), 64 at a time by one wave, the kinds of
+// eight such steps read ahead.
+template <typename F>
+__device__ inline void walk_run(const void *chosen, int wide, uint32_t experts, int64_t begin, int64_t end, F f) {
+  constexpr int AHEAD = 8;
+  const int lane = threadIdx.x & 63;
+  for (int64_t first = begin; first < end; first += 64 * AHEAD) {
+    const int64_t i = first + lane;
+    uint32_t kind[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) kind[u] = i + u * 64 < end ? kind_of(chosen, wide, i + u * 64, experts) : 0u;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (first + u * 64 < end) f(i + u * 64, i + u * 64 < end, kind[u]);
+  }
+}
 // Counts of each kind among entries [begin, end), by one wave.
 __device__ inline void count_run(const void *chosen, int wide, uint32_t experts, int64_t begin, int64_t end,
                                  uint32_t *counts) {
-  for (int64_t i = begin + (threadIdx.x & 63); i < end; i += 64)
-    atomicAdd(&counts[kind_of(chosen, wide, i, experts)], 1u);
+  walk_run(chosen, wide, experts, begin, end, [&](int64_t, bool there, uint32_t kind) {
+    if (there) atomicAdd(&counts[kind], 1u);
+  });
 }
 // Positions of entries [begin, end), by one wave: next[kind] is the position of
 // its next entry.
 __device__ inline void place_run(const void *chosen, int wide, uint32_t experts, int bits, int32_t k, int64_t begin,
                                  int64_t end, uint32_t *next, int32_t *place, int32_t *source) {
   const int lane = threadIdx.x & 63;
-  for (int64_t i0 = begin; i0 < end; i0 += 64) {
-    const int64_t i = i0 + lane;
-    const bool there = i < end;
-    const uint32_t kind = there ? kind_of(chosen, wide, i, experts) : 0u;
+  walk_run(chosen, wide, experts, begin, end, [&](int64_t i, bool there, uint32_t kind) {
     const uint64_t same = same_kind(kind, bits, there);
     if (there) {
       const int before = __popcll(same & ((1ull << lane) - 1));
@@ -58,10 +72,10 @@ __device__ inline void place_run(const void *chosen, int wide, uint32_t experts,
       if (before == 0) next[kind] = at + (uint32_t)__popcll(same);
       const bool kept = kind < experts;
       place[i] = kept ? (int32_t)at : -1;
-      source[at] = kept ? (int32_t)(i / k) : -1;
+      source[at] = kept ? (int32_t)((uint32_t)i / (uint32_t)k) : -1;
     }
     __builtin_amdgcn_wave_barrier();
-  }
+  });
 }
 
 // Sums of v over the threads before this one, of up to 1024; `sums` holds 16.
@@ -146,22 +160,24 @@ __global__ __launch_bounds__(256) void k_route_place(const void *__restrict__ ch
   extern __shared__ uint32_t place_lds[];  // [4][kinds]
   __shared__ uint32_t sums[4];
   const int kinds = experts + 1, wave = threadIdx.x >> 6;
-  // every kind's first position, 16 kinds a thread (4096 kinds at most)
-  uint32_t own = 0;
-  for (int i = 0; i < 16; ++i) {
-    const int kind = threadIdx.x * 16 + i;
-    if (kind < kinds) own += totals[kind];
-  }
-  uint32_t at = sum_before(own, sums);
-  for (int i = 0; i < 16; ++i) {
-    const int kind = threadIdx.x * 16 + i;
-    if (kind >= kinds) break;
-    if (blockIdx.x == 0) offsets[kind] = (int32_t)at;
-    for (int w = 0; w < 4; ++w) {
-      const int32_t r = blockIdx.x * 4 + w;
-      place_lds[w * kinds + kind] = at + (r < runs ? counts[(int64_t)kind * runs + r] : 0u);
+  // every kind's first position, 256 kinds at a time
+  uint32_t before = 0;
+  for (int first = 0; first < kinds; first += 256) {
+    const int kind = first + threadIdx.x;
+    const uint32_t own = kind < kinds ? totals[kind] : 0u;
+    const uint32_t *c = counts + (int64_t)kind * runs + blockIdx.x * 4;
+    uint32_t runs_before[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      runs_before[w] = kind < kinds && (int32_t)(blockIdx.x * 4) + w < runs ? c[w] : 0u;
+    const uint32_t at = before + sum_before(own, sums);
+    if (kind < kinds) {
+      if (blockIdx.x == 0) offsets[kind] = (int32_t)at;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) place_lds[w * kinds + kind] = at + runs_before[w];
     }
-    at += totals[kind];
+    before += sums[0] + sums[1] + sums[2] + sums[3];
+    __syncthreads();  // the sums are free again
   }
   __syncthreads();
   const int64_t begin = (int64_t)(blockIdx.x * 4 + wave) * run, end = begin + run < entries ? begin + run : entries;
@@ -180,83 +196,125 @@ int64_t run_of(int64_t entries) {
 bool few(int64_t entries, int32_t experts) { return entries <= kOneGroup && experts + 1 <= kKindsAlone; }
 
 // ------------------------------------------------------- rows to and back ---
-// A team of LANES lanes for each row t; 16 bytes of it a lane and step.
+// A team of LANES lanes for each row t; 16 bytes of it a lane and step.  Entries
+// are taken KB at a time, whose rows are read (or written) together; with k <= KB
+// their places are read once.  A row's last step begins V columns before its end
+// and does some columns twice, with the same results (WHOLE: rows have V columns).
 constexpr int kThreads = 256;
+
+// The team's row and place in it, and the places of entries (t, j0 ..), -1 for none.
+template <int LANES>
+struct Team {
+  int64_t t;
+  int lane;
+  __device__ Team() : t((int64_t)workgroup() * (kThreads / LANES) + threadIdx.x / LANES), lane(threadIdx.x % LANES) {}
+};
+template <int KB>
+struct Places {
+  int32_t at[KB];
+  __device__ void read(const int32_t *place, int64_t t, int32_t k, int32_t j0, int64_t total) {
+#pragma unroll
+    for (int u = 0; u < KB; ++u) {
+      const int32_t p = j0 + u < k ? place[t * k + j0 + u] : -1;
+      at[u] = p < total ? p : -1;
+    }
+  }
+};
+template <bool WHOLE, int V, typename T>
+__device__ inline void read_columns(const T *p, int left, float (&v)[V]) {
+  if constexpr (WHOLE)
+    load_span(p, v);
+  else
+    load_part(p, left, v);
+}
+template <bool WHOLE, int V, typename T>
+__device__ inline void write_columns(T *p, int left, const float (&v)[V]) {
+  if constexpr (WHOLE)
+    store_span(p, v);
+  else
+    store_part(p, left, v);
+}
 
 // y[place[t, j]] = x[t]; rows of y that no entry is sorted to (those behind the
 // last expert's) become zeros.
-template <typename T, int LANES>
+template <typename T, int LANES, int KB, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_dispatch(const T *__restrict__ x, int64_t x_stride, int64_t rows,
                                                        int32_t k, int32_t cols, const int32_t *__restrict__ place,
                                                        const int32_t *__restrict__ source, T *__restrict__ y,
                                                        int64_t y_stride) {
   constexpr int V = 16 / sizeof(T);
-  const int64_t t = (int64_t)workgroup() * (kThreads / LANES) + threadIdx.x / LANES;
+  const Team<LANES> team;
+  const int64_t t = team.t;
   if (t >= rows) return;
-  const int64_t total = rows * k;
-  const int32_t *p = place + t * k, *s = source + t * k;
-  for (int32_t c = threadIdx.x % LANES * V; c < cols; c += LANES * V) {
+  Places<KB> p;
+  uint32_t clear = 0;
+  auto read = [&](int32_t j0) {
+    p.read(place, t, k, j0, rows * k);
+    clear = 0;
+#pragma unroll
+    for (int u = 0; u < KB; ++u) clear |= (j0 + u < k && source[t * k + j0 + u] < 0 ? 1u : 0u) << u;
+  };
+  if (k <= KB) read(0);
+  for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
+    const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
     float v[V];
     const float none[V] = {};
-    const int left = cols - c;
-    if (left >= V)
-      load_span(x + t * x_stride + c, v);
-    else
-      load_part(x + t * x_stride + c, left, v);
-    for (int32_t j = 0; j < k; ++j) {
-      const int64_t to = p[j];
-      if (to >= 0 && to < total) {
-        if (left >= V)
-          store_span(y + to * y_stride + c, v);
-        else
-          store_part(y + to * y_stride + c, left, v);
-      }
-      if (s[j] < 0) {
-        if (left >= V)
-          store_span(y + (t * k + j) * y_stride + c, none);
-        else
-          store_part(y + (t * k + j) * y_stride + c, left, none);
+    read_columns<WHOLE>(x + t * x_stride + c, cols - c, v);
+    for (int32_t j0 = 0; j0 < k; j0 += KB) {
+      if (k > KB) read(j0);
+#pragma unroll
+      for (int u = 0; u < KB; ++u)
+        if (p.at[u] >= 0) write_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v);
+      if (clear) {
+#pragma unroll
+        for (int u = 0; u < KB; ++u)
+          if (clear >> u & 1) write_columns<WHOLE>(y + (t * k + j0 + u) * y_stride + c, cols - c, none);
       }
     }
   }
 }
 
 // out[t] = sum over j, in this order, of weights[t, j] y[place[t, j]].
-template <typename T, int LANES, bool WEIGHTS>
+template <typename T, int LANES, int KB, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, int64_t y_stride, int64_t rows,
                                                       int32_t k, int32_t cols, const int32_t *__restrict__ place,
                                                       const float *__restrict__ weights, T *__restrict__ out,
                                                       int64_t out_stride) {
   constexpr int V = 16 / sizeof(T);
-  const int64_t t = (int64_t)workgroup() * (kThreads / LANES) + threadIdx.x / LANES;
+  const Team<LANES> team;
+  const int64_t t = team.t;
   if (t >= rows) return;
-  const int64_t total = rows * k;
-  const int32_t *p = place + t * k;
-  for (int32_t c = threadIdx.x % LANES * V; c < cols; c += LANES * V) {
-    float sum[V] = {};
-    const int left = cols - c;
-    for (int32_t j = 0; j < k; ++j) {
-      const int64_t from = p[j];
-      if (from < 0 || from >= total) continue;
-      float v[V];
-      if (left >= V)
-        load_span(y + from * y_stride + c, v);
-      else
-        load_part(y + from * y_stride + c, left, v);
-      const float w = WEIGHTS ? weights[t * k + j] : 1.0f;
+  Places<KB> p;
+  float w[KB];
+  auto read = [&](int32_t j0) {
+    p.read(place, t, k, j0, rows * k);
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum[i] = WEIGHTS ? fmaf(w, v[i], sum[i]) : sum[i] + v[i];
+    for (int u = 0; u < KB; ++u) w[u] = weights && j0 + u < k ? weights[t * k + j0 + u] : 1.0f;
+  };
+  if (k <= KB) read(0);
+  for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
+    const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
+    float sum[V] = {};
+    for (int32_t j0 = 0; j0 < k; j0 += KB) {
+      if (k > KB) read(j0);
+      float v[KB][V];
+#pragma unroll
+      for (int u = 0; u < KB; ++u)
+        if (p.at[u] >= 0) read_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v[u]);
+#pragma unroll
+      for (int u = 0; u < KB; ++u)
+        if (p.at[u] >= 0) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum[i] = fmaf(w[u], v[u][i], sum[i]);
+        }
     }
-    if (left >= V)
-      store_span(out + t * out_stride + c, sum);
-    else
-      store_part(out + t * out_stride + c, left, sum);
+    write_columns<WHOLE>(out + t * out_stride + c, cols - c, sum);
   }
 }
 
 // dy[place[t, j]] = weights[t, j] dout[t], zeros in rows that no entry is sorted
 // to; dweights[t, j] = the dot product of dout[t] and y[place[t, j]].
-template <typename T, int LANES>
+template <typename T, int LANES, int KB, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restrict__ dout, int64_t dout_stride,
                                                                const T *__restrict__ y, int64_t y_stride, int64_t rows,
                                                                int32_t k, int32_t cols,
@@ -265,98 +323,119 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
                                                                const float *__restrict__ weights, T *__restrict__ dy,
                                                                int64_t dy_stride, float *__restrict__ dweights) {
   constexpr int V = 16 / sizeof(T);
-  const int64_t t = (int64_t)workgroup() * (kThreads / LANES) + threadIdx.x / LANES;
+  const Team<LANES> team;
+  const int64_t t = team.t;
   if (t >= rows) return;
-  const int lane = threadIdx.x % LANES;
-  const int64_t total = rows * k;
-  for (int32_t j = 0; j < k; ++j) {
-    const int64_t at = place[t * k + j];
-    const bool there = at >= 0 && at < total, clear = dy && source[t * k + j] < 0;
-    const float w = weights ? weights[t * k + j] : 1.0f;
-    float dot = 0.0f;
-    for (int32_t c = lane * V; c < cols; c += LANES * V) {
-      const int left = cols - c;
-      if (there) {
-        float d[V];
-        if (left >= V)
-          load_span(dout + t * dout_stride + c, d);
-        else
-          load_part(dout + t * dout_stride + c, left, d);
-        if (dweights) {
-          float v[V];
-          if (left >= V)
-            load_span(y + at * y_stride + c, v);
-          else
-            load_part(y + at * y_stride + c, left, v);
+  for (int32_t j0 = 0; j0 < k; j0 += KB) {
+    Places<KB> p;
+    p.read(place, t, k, j0, rows * k);
+    uint32_t clear = 0;
+    float w[KB], dot[KB] = {};
 #pragma unroll
-          for (int i = 0; i < V; ++i) dot = fmaf(d[i], v[i], dot);
-        }
-        if (dy) {
+    for (int u = 0; u < KB; ++u) {
+      w[u] = weights && j0 + u < k ? weights[t * k + j0 + u] : 1.0f;
+      clear |= (dy && j0 + u < k && source[t * k + j0 + u] < 0 ? 1u : 0u) << u;
+    }
+    for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
+      const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
+      float d[V], v[KB][V];
+      read_columns<WHOLE>(dout + t * dout_stride + c, cols - c, d);
+      if (dweights) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) d[i] *= w;
-          if (left >= V)
-            store_span(dy + at * dy_stride + c, d);
-          else
-            store_part(dy + at * dy_stride + c, left, d);
-        }
+        for (int u = 0; u < KB; ++u)
+          if (p.at[u] >= 0) read_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v[u]);
+#pragma unroll
+        for (int u = 0; u < KB; ++u)
+          if (p.at[u] >= 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i)  // columns that the step before has done count once
+              if (!WHOLE || c + i >= c0) dot[u] = fmaf(d[i], v[u][i], dot[u]);
+          }
       }
-      if (clear) {
-        const float none[V] = {};
-        if (left >= V)
-          store_span(dy + (t * k + j) * dy_stride + c, none);
-        else
-          store_part(dy + (t * k + j) * dy_stride + c, left, none);
+      if (dy) {
+#pragma unroll
+        for (int u = 0; u < KB; ++u)
+          if (p.at[u] >= 0) {
+            float o[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = w[u] * d[i];
+            write_columns<WHOLE>(dy + p.at[u] * dy_stride + c, cols - c, o);
+          }
+        if (clear) {
+          const float none[V] = {};
+#pragma unroll
+          for (int u = 0; u < KB; ++u)
+            if (clear >> u & 1) write_columns<WHOLE>(dy + (t * k + j0 + u) * dy_stride + c, cols - c, none);
+        }
       }
     }
     if (dweights) {
 #pragma unroll
-      for (int d = LANES / 2; d > 0; d /= 2) dot += __shfl_xor(dot, d);
-      if (lane == 0) dweights[t * k + j] = dot;
+      for (int u = 0; u < KB; ++u) {
+#pragma unroll
+        for (int s = LANES / 2; s > 0; s /= 2) dot[u] += __shfl_xor(dot[u], s);
+        if (team.lane == 0 && j0 + u < k) dweights[t * k + j0 + u] = dot[u];
+      }
     }
   }
 }
 
-// Calls f with the number of lanes for rows of `cols` elements: a power of two up to a wave.
+// Calls f(lanes, entries at a time, whether rows have 16 bytes) for rows of `cols`
+// elements: the most lanes of which four in five have work in all steps.
 template <typename T, typename F>
-int with_lanes(int64_t cols, const F &f) {
-  const int64_t steps = ceil_div(cols * (int64_t)sizeof(T), 16);
-  if (steps > 32) return f(std::integral_constant<int, 64>());
-  if (steps > 16) return f(std::integral_constant<int, 32>());
-  if (steps > 8) return f(std::integral_constant<int, 16>());
-  return f(std::integral_constant<int, 8>());
+int with_shape(int64_t cols, int32_t k, const F &f) {
+  constexpr int V = 16 / sizeof(T);
+  const int64_t steps = ceil_div(cols, V);
+  int lanes = 64;
+  while (lanes > 8 && 5 * steps < 4 * lanes * ceil_div(steps, lanes)) lanes /= 2;
+  if (steps <= 2) lanes = 2;
+  const auto entries = [&](auto l, auto whole) {
+    if (k == 1) return f(l, std::integral_constant<int, 1>(), whole);
+    if (k == 2) return f(l, std::integral_constant<int, 2>(), whole);
+    if (k <= 4) return f(l, std::integral_constant<int, 4>(), whole);
+    return f(l, std::integral_constant<int, 8>(), whole);
+  };
+  if (cols < V) return entries(std::integral_constant<int, 2>(), std::false_type());
+  switch (lanes) {
+    case 64: return entries(std::integral_constant<int, 64>(), std::true_type());
+    case 32: return entries(std::integral_constant<int, 32>(), std::true_type());
+    case 16: return entries(std::integral_constant<int, 16>(), std::true_type());
+    case 8: return entries(std::integral_constant<int, 8>(), std::true_type());
+    default: return entries(std::integral_constant<int, 2>(), std::true_type());
+  }
 }
 
 template <typename T>
 int dispatch_as(const sd_route_t *r, const void *x, int64_t cols, int64_t x_stride, void *y, int64_t y_stride,
                 hipStream_t s) {
-  return with_lanes<T>(cols, [&](auto lanes) {
+  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
-    hipLaunchKernelGGL((k_dispatch<T, L>), grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s,
-                       static_cast<const T *>(x), x_stride, r->rows, r->k, (int32_t)cols, r->place, r->source,
-                       static_cast<T *>(y), y_stride);
+    hipLaunchKernelGGL((k_dispatch<T, L, decltype(kb)::value, decltype(whole)::value>),
+                       grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(x),
+                       x_stride, r->rows, r->k, (int32_t)cols, r->place, r->source, static_cast<T *>(y), y_stride);
     return launched();
   });
 }
 template <typename T>
 int combine_as(const sd_route_t *r, const void *y, int64_t cols, int64_t y_stride, const float *weights, void *out,
                int64_t out_stride, hipStream_t s) {
-  return with_lanes<T>(cols, [&](auto lanes) {
+  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
-    auto *kernel = weights ? k_combine<T, L, true> : k_combine<T, L, false>;
-    hipLaunchKernelGGL(kernel, grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s,
-                       static_cast<const T *>(y), y_stride, r->rows, r->k, (int32_t)cols, r->place, weights,
-                       static_cast<T *>(out), out_stride);
+    hipLaunchKernelGGL((k_combine<T, L, decltype(kb)::value, decltype(whole)::value>),
+                       grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(y),
+                       y_stride, r->rows, r->k, (int32_t)cols, r->place, weights, static_cast<T *>(out), out_stride);
     return launched();
   });
 }
 template <typename T>
 int backward_as(const sd_route_t *r, const void *dout, int64_t cols, int64_t dout_stride, const void *y,
                 int64_t y_stride, const float *weights, void *dy, int64_t dy_stride, float *dweights, hipStream_t s) {
-  return with_lanes<T>(cols, [&](auto lanes) {
+  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
-    hipLaunchKernelGGL((k_combine_backward<T, L>), grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s,
-                       static_cast<const T *>(dout), dout_stride, static_cast<const T *>(y), y_stride, r->rows, r->k,
-                       (int32_t)cols, r->place, r->source, weights, static_cast<T *>(dy), dy_stride, dweights);
+    hipLaunchKernelGGL((k_combine_backward<T, L, decltype(kb)::value, decltype(whole)::value>),
+                       grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(dout),
+                       dout_stride, static_cast<const T *>(y), y_stride, r->rows, r->k, (int32_t)cols, r->place,
+                       r->source, weights, static_cast<T *>(dy), dy_stride, dweights);
     return launched();
   });
 }

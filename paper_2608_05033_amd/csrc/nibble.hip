@@ -126,6 +126,112 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__rest
   scales[((int64_t)grp * rows + row) * 4 + block] = (uint8_t)s;
 }
 
+// A table and its transpose from one reading, of consecutive elements in a row.
+// A workgroup takes 128 rows x 128 columns, a wave 32 of the rows: it packs them along
+// the columns as k_nibble_pack does, leaves them in shared memory and takes them
+// column by column, so that a lane has a block of the transpose.  The four waves'
+// blocks of a column leave together, 64 bytes of codes and a word of scales.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restrict__ x, int64_t row_stride,
+                                                               int64_t rows, int32_t cols, int32_t ng,
+                                                               uint8_t *__restrict__ codes, int64_t ld,
+                                                               uint8_t *__restrict__ scales,
+                                                               uint8_t *__restrict__ codes_t, int64_t ld_t,
+                                                               uint8_t *__restrict__ scales_t) {
+  constexpr int V = 16 / sizeof(T), LANES = kGroup / V, SHARE = kCols / V, AT_ONCE = 64 / LANES, STEPS = 32 / AT_ONCE;
+  // by whole words: an odd number of them between rows, so that neither way of reading meets itself
+  constexpr int PITCH = kGroup + 4 / (int)sizeof(T);
+  __shared__ __align__(16) T tile[4][32 * PITCH];
+  __shared__ __align__(16) u32x4 blocks[4][kGroup];
+  __shared__ uint8_t bytes[kGroup][4];
+  const int t = threadIdx.x, wave = t >> 6, l = t & 63, lane = l % LANES, down = l / LANES;
+  const int64_t strip = workgroup() / (uint32_t)ng, row0 = strip * 128 + wave * 32;
+  const int32_t grp = workgroup() % (uint32_t)ng;
+  if (strip * 128 >= rows) return;
+  const int32_t c = grp * kGroup + lane * V;
+  float v[STEPS][V];
+#pragma unroll
+  for (int u = 0; u < STEPS; ++u) {
+    const int64_t row = row0 + u * AT_ONCE + down;
+    const int left = row < rows ? cols - c : 0;
+    const T *p = x + row * row_stride + c;
+    if (left >= V)
+      load_span(p, v[u]);
+    else
+      load_part(p, left, v[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < STEPS; ++u) {
+    const int64_t row = row0 + u * AT_ONCE + down;
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const uint32_t bits = __float_as_uint(v[u][i]) & 0x7fffffffu;
+      most = most > bits ? most : bits;
+    }
+    const uint32_t s = scale_byte(group_max_bits(most, SHARE));
+    const float scale = scale_value(s);
+    uint32_t w = encode2<0>(0u, v[u][0], v[u][1], scale);
+    w = encode2<1>(w, v[u][2], v[u][3], scale);
+    if constexpr (V == 8) {
+      w = encode2<2>(w, v[u][4], v[u][5], scale);
+      w = encode2<3>(w, v[u][6], v[u][7], scale);
+    }
+    if (s == kNanScale) w = 0;
+    T *q = &tile[wave][(u * AT_ONCE + down) * PITCH + lane * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) q[i] = (T)v[u][i];
+    if (row < rows) {
+      if (c < ((cols + kCols - 1) & ~(kCols - 1))) {
+        uint8_t *o = codes + row * ld + c / 2;
+        if constexpr (V == 4)
+          *reinterpret_cast<uint16_t *>(o) = (uint16_t)w;
+        else
+          *reinterpret_cast<uint32_t *>(o) = w;
+      }
+      if (lane % SHARE == 0) scales[((int64_t)grp * rows + row) * 4 + lane / SHARE] = (uint8_t)s;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {  // column h * 64 + l of the wave's 32 rows
+    float d[kCols];
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) {
+      d[i] = (float)tile[wave][i * PITCH + h * 64 + l];
+      const uint32_t bits = __float_as_uint(d[i]) & 0x7fffffffu;
+      most = most > bits ? most : bits;
+    }
+    const uint32_t s = scale_byte(most);
+    const float scale = scale_value(s);
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t q = encode2<0>(0u, d[8 * i], d[8 * i + 1], scale);
+      q = encode2<1>(q, d[8 * i + 2], d[8 * i + 3], scale);
+      q = encode2<2>(q, d[8 * i + 4], d[8 * i + 5], scale);
+      q = encode2<3>(q, d[8 * i + 6], d[8 * i + 7], scale);
+      w[i] = s == kNanScale ? 0 : q;
+    }
+    blocks[wave][h * 64 + l] = w;
+    bytes[h * 64 + l][wave] = (uint8_t)s;
+  }
+  __syncthreads();
+  // blocks of 32 rows that there are; four threads a column
+  const int64_t have = (rows - strip * 128 + 31) / 32;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int column = h * 64 + t / 4, part = t & 3;
+    const int64_t col = (int64_t)grp * kGroup + column;
+    if (col < cols && part < have)
+      *reinterpret_cast<u32x4 *>(codes_t + col * ld_t + strip * 64 + part * 16) = blocks[part][column];
+  }
+  const int64_t col = (int64_t)grp * kGroup + t;
+  if (t < kGroup && col < cols)
+    *reinterpret_cast<uint32_t *>(scales_t + (strip * cols + col) * 4) = *reinterpret_cast<const uint32_t *>(bytes[t]);
+}
+
 // Lanes along a row, eight codes each.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__restrict__ codes, int64_t ld,
@@ -187,6 +293,16 @@ int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nib
 }
 
 template <typename T>
+int both_any(const void *x, int64_t row_stride, const sd_nibble_t *out, const sd_nibble_t *out_t, hipStream_t s) {
+  const int64_t ng = groups_of(out->cols), wgs = ceil_div(out->rows, 128) * ng;
+  if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
+  hipLaunchKernelGGL(k_nibble_pack_both<T>, grid_of(wgs), dim3(kThreads), 0, s, static_cast<const T *>(x), row_stride,
+                     out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, out_t->codes,
+                     out_t->ld, out_t->scales);
+  return launched();
+}
+
+template <typename T>
 int unpack_as(const sd_nibble_t *x, void *y, int64_t row_stride, hipStream_t s) {
   const int64_t octs = ceil_div(x->cols, 8), wgs = ceil_div(x->rows * octs, kThreads * kUnroll);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
@@ -210,6 +326,27 @@ extern "C" int sd_nibble_pack(const void *x, int32_t type, int64_t row_stride, i
   return type == SD_TYPE_F32   ? pack_any<float>(x, row_stride, col_stride, out, s)
          : type == SD_TYPE_F16 ? pack_any<f16>(x, row_stride, col_stride, out, s)
                                : pack_any<bf16>(x, row_stride, col_stride, out, s);
+}
+
+extern "C" int sd_nibble_pack_both(const void *x, int32_t type, int64_t row_stride, int64_t col_stride,
+                                   const sd_nibble_t *out, const sd_nibble_t *out_t, void *stream) {
+  int st = check_nibble(out);
+  if (st == SD_OK) st = check_nibble(out_t);
+  if (st == SD_OK && (out_t->rows != out->cols || out_t->cols != out->rows)) st = SD_ERR_INVALID_VALUE;
+  if (st != SD_OK) return st;
+  if (col_stride != 1) {  // one after the other
+    st = sd_nibble_pack(x, type, row_stride, col_stride, out, stream);
+    return st == SD_OK ? sd_nibble_pack(x, type, col_stride, row_stride, out_t, stream) : st;
+  }
+  if (!type_ok(type) || row_stride < 0) return SD_ERR_INVALID_VALUE;
+  if (row_stride > (1ll << 31)) return SD_ERR_OVERFLOW;
+  if (out->rows == 0 || out->cols == 0) return SD_OK;
+  if (!x || !aligned_to(x, type_bytes(type))) return SD_ERR_INVALID_VALUE;
+  if ((st = have_device()) != SD_OK) return st;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  return type == SD_TYPE_F32   ? both_any<float>(x, row_stride, out, out_t, s)
+         : type == SD_TYPE_F16 ? both_any<f16>(x, row_stride, out, out_t, s)
+                               : both_any<bf16>(x, row_stride, out, out_t, s);
 }
 
 extern "C" int sd_nibble_unpack(const sd_nibble_t *x, void *y, int32_t type, int64_t row_stride, void *stream) {

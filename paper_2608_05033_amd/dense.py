@@ -236,6 +236,19 @@ def pack4(x, transpose: bool = False) -> Packed4:
 
 
 @_on_its_device
+def pack4_both(x):
+    """(pack4(x), pack4(x, transpose=True)) from one reading of x."""
+    if x.dim() != 2 or x.dtype not in TYPES or not x.is_cuda:
+        raise ValueError(f"x must be a float32, float16 or bfloat16 matrix on the GPU, got {x.dtype} "
+                         f"{tuple(x.shape)} on {x.device}")
+    (rows, cols), (down, right) = x.shape, x.stride()
+    out, out_t = Packed4.empty(rows, cols, x), Packed4.empty(cols, rows, x)
+    _check(_lib.sd_nibble_pack_both(x.data_ptr(), TYPES[x.dtype], down if rows > 1 else cols, 1 if cols == 1 else right,
+                                    out.c, out_t.c, _raw_stream(x.get_device())), "sd_nibble_pack_both")
+    return out, out_t
+
+
+@_on_its_device
 def unpack4(x: Packed4, dtype=torch.float32) -> torch.Tensor:
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")

@@ -148,19 +148,25 @@ class _Transform4(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W):
         ctx.dtype = X.dtype
-        Xt = dense.pack4(X, transpose=True) if ctx.needs_input_grad[1] else None
+        X4, Xt = dense.pack4_both(X) if ctx.needs_input_grad[1] else (dense.pack4(X), None)
         ctx.save_for_backward(W, *(() if Xt is None else (Xt.codes, Xt.scales)))
-        return dense.product4(dense.pack4(X), dense.pack4(W, transpose=True))
+        return dense.product4(X4, dense.pack4(W, transpose=True))
 
     @staticmethod
     @first_derivatives_only
     def backward(ctx, dZ):
         W, *Xt = ctx.saved_tensors
         dX = dW = None
+        if all(ctx.needs_input_grad):
+            G, Gt = dense.pack4_both(dZ)
+        elif ctx.needs_input_grad[0]:
+            G = dense.pack4(dZ)
+        else:
+            Gt = dense.pack4(dZ, transpose=True)
         if ctx.needs_input_grad[0]:
-            dX = dense.product4(dense.pack4(dZ), dense.pack4(W), dtype=ctx.dtype)
+            dX = dense.product4(G, dense.pack4(W), dtype=ctx.dtype)
         if ctx.needs_input_grad[1]:
-            dW = dense.product4(dense.Packed4(*Xt, dZ.shape[0]), dense.pack4(dZ, transpose=True), dtype=W.dtype)
+            dW = dense.product4(dense.Packed4(*Xt, dZ.shape[0]), Gt, dtype=W.dtype)
         return dX, dW
 
 

@@ -111,6 +111,24 @@ def test_pack_strides(dtype):
     check_packed(dense.pack4(flat[1:].view(150, 210)), x)
 
 
+def same_table(a, b):
+    return torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 200), (200, 1), (31, 33), (128, 128), (129, 127), (300, 260),
+                                       (1000, 40), (33, 1030)])
+def test_pack_both(rows, cols, dtype):
+    """The same bits as one after the other: whole tables, parts of wider ones, any strides."""
+    t, x = table(activations(rows, cols, rows + cols), dtype)
+    t[rows // 2, cols // 2] = float("inf")
+    wide = torch.full((rows, cols + 9), 5.0, dtype=t.dtype, device="cuda")
+    wide[:, 3:cols + 3] = t
+    for v in (t, wide[:, 3:cols + 3], t.t().contiguous().t(), t[:, ::2], t[:1].expand(rows, cols)):
+        one, other = dense.pack4_both(v)
+        assert same_table(one, dense.pack4(v)) and same_table(other, dense.pack4(v, transpose=True))
+
+
 def test_unpack_every_code_and_scale():
     codes = torch.arange(256, dtype=torch.uint8).repeat(256, 1).cuda()  # 512 columns, every pair of codes
     scales = torch.zeros(4, 256, 4, dtype=torch.uint8)

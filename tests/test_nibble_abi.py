@@ -61,6 +61,8 @@ def test_tables_are_checked_everywhere(bad):
     status = sd.SD_ERR_OVERFLOW if bad in LONG_TABLE else sd.SD_ERR_INVALID_VALUE
     p, ok = table(**bad), table(rows=bad.get("rows", 4), cols=bad.get("cols", 40))
     refused(status, sd.sd_nibble_pack, P, F32, 40, 1, p)
+    refused(status, sd.sd_nibble_pack_both, P, F32, 40, 1, p, ok)
+    refused(status, sd.sd_nibble_pack_both, P, F32, 40, 1, ok, p)
     refused(status, sd.sd_nibble_unpack, p, P, F32, 40)
     refused(status, sd.sd_nibble_product, p, ok, None, P, F32, 1 << 20, P, BIG)
     refused(status, sd.sd_nibble_product, ok, p, None, P, F32, 1 << 20, P, BIG)
@@ -72,6 +74,11 @@ def test_packing_refusals():
     each(sd.SD_ERR_INVALID_VALUE, sd.sd_nibble_pack, [P, F32, 40, 1, table()],
          [(0, None), (0, P + 2), (1, 0), (1, 4), (2, -1), (3, -1), (4, None)])
     each(sd.SD_ERR_OVERFLOW, sd.sd_nibble_pack, [P, F32, 40, 1, table()], [(2, 1 << 41), (3, 1 << 32)])
+    good = [P, F32, 40, 1, table(), table(rows=40, cols=4)]
+    each(sd.SD_ERR_INVALID_VALUE, sd.sd_nibble_pack_both, good,
+         [(0, None), (0, P + 2), (1, 0), (2, -1), (3, -1), (4, None), (4, table(cols=41)), (5, None), (5, table()),
+          (5, table(rows=40, cols=4, codes=None))])
+    each(sd.SD_ERR_OVERFLOW, sd.sd_nibble_pack_both, good, [(2, 1 << 32), (3, 1 << 32)])
     each(sd.SD_ERR_INVALID_VALUE, sd.sd_nibble_unpack, [table(), P, F32, 40],
          [(0, None), (1, None), (1, P + 1), (2, 0), (3, 39)])
     refused(sd.SD_ERR_OVERFLOW, sd.sd_nibble_unpack, table(), P, F32, 1 << 31)
@@ -149,7 +156,8 @@ def test_tensor_functions_refuse_what_they_cannot_take():
     from paper_2608_05033_amd import dense, experts, gcn
 
     host, ints = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32)
-    for call in (lambda: dense.pack4(host), lambda: dense.pack4(host[0]), lambda: dense.pack4(host.double()),
+    for call in (lambda: dense.pack4(host), lambda: dense.pack4(host[0]), lambda: dense.pack4_both(host),
+                 lambda: dense.pack4(host.double()),
                  lambda: dense.Packed4(host, host, 8), lambda: dense.Packed4(ints.byte(), ints.byte(), 4),
                  lambda: experts.route(ints, 3), lambda: experts.route(host, 3), lambda: experts.route(ints[0], 3),
                  lambda: experts.Route(ints[0], ints, ints.view(-1)), lambda: gcn.transform4(host, host)):
