@@ -235,9 +235,9 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
                                                              int32_t split_stages, int64_t split_stride) {
   constexpr int THREADS = 256, WM = 2, WN = 2, MF = BM / WM / 32, NF = BN / WN / 32;
   constexpr int ROWS = BM + BN, CHUNKS = ROWS * 8 / THREADS, SCALES = 2 * ROWS / THREADS;
-  constexpr int BUFFER = ROWS * 136, PITCH = NF * 32 + 4;  // PITCH: floats between a wave's rows of results
+  constexpr int BUFFER = ROWS * 136, PITCH = NF * 32 + 16 / (int)sizeof(T);  // PITCH: between a wave's rows of results
   static_assert(ROWS % THREADS == 0 && BM % (THREADS / 8) == 0 && BM % 64 == 0, "one operand for a wave");
-  static_assert(2 * 32 * PITCH * 4 <= BUFFER && (BUFFERS == 2 || BUFFERS == 4), "two waves' results in a buffer");
+  static_assert(2 * 32 * PITCH * (int)sizeof(T) <= BUFFER && (BUFFERS == 2 || BUFFERS == 4), "two waves' results in a buffer");
   // objects of their own and no array: reads of one then need not wait for what is on its way to another
   __shared__ __align__(16) uint8_t buffer_a[BUFFER], buffer_b[BUFFER];
   __shared__ __align__(16) uint8_t buffer_c[BUFFERS == 4 ? BUFFER : 16], buffer_d[BUFFERS == 4 ? BUFFER : 16];
@@ -264,29 +264,27 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     w0 = expert * n;
     if (bias) bias += w0;
   }
-  const auto x_row = [&](int row) -> int64_t {  // X's row for one of the tile; past the last one, that
-    const int64_t m = m0 + row < m1 ? m0 + row : m1 - 1;
-    if constexpr (EXPERTS) {
-      if (sorted.source) {
-        const int64_t from = sorted.source[m];
-        return from < 0 ? 0 : from < X.rows ? from : X.rows - 1;
-      }
-    }
-    return m;
+  // X's and W's rows for one of the tile, counted from the first; past the last one, that
+  const int32_t xlast = (int32_t)(m1 - m0 < BM ? m1 - m0 : BM) - 1, wlast = (int32_t)(n - n0 < BN ? n - n0 : BN) - 1;
+  const bool gathered = EXPERTS && sorted.source;
+  const int64_t xfirst = gathered ? 0 : m0, wfirst = w0 + n0;
+  const auto x_row = [&](int row) -> uint32_t {
+    row = row < xlast ? row : xlast;
+    if (!gathered) return row;
+    const int32_t from = sorted.source[m0 + row];
+    return from < 0 ? 0 : from < X.rows ? from : X.rows - 1;
   };
-  const auto w_row = [&](int row) -> int64_t { return w0 + (n0 + row < n ? n0 + row : n - 1); };
+  const auto w_row = [&](int row) -> uint32_t { return row < wlast ? row : wlast; };
 
   // Block i of thread t: row i * THREADS / 8 + t / 8 of the tile (X's rows first), place t % 8.
   constexpr int XC = BM / (THREADS / 8);  // of them, X's
   const int chunk = (t & 7) ^ ((t >> 4) & 7);
-  const int64_t xfirst = EXPERTS ? 0 : m0, wfirst = w0 + n0;
   const uint8_t *xbase = X.codes + xfirst * X.ld, *wbase = W.codes + wfirst * W.ld;
   uint32_t off[CHUNKS];
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
     const int row = (i < XC ? i : i - XC) * (THREADS / 8) + t / 8;
-    off[i] = i < XC ? (uint32_t)(x_row(row) - xfirst) * (uint32_t)X.ld
-                    : (uint32_t)(w_row(row) - wfirst) * (uint32_t)W.ld;
+    off[i] = i < XC ? x_row(row) * (uint32_t)X.ld : w_row(row) * (uint32_t)W.ld;
   }
   // Scale word i of thread t: place i * THREADS + t of [g][X's, then W's][wave row or column][r][product].
   const uint8_t *ssrc[ROWS / THREADS];
@@ -295,7 +293,7 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     const bool of_x = i * THREADS + wave * 64 < BM;
     const int u = i * THREADS + t - (of_x ? 0 : BM), f = of_x ? MF : NF;
     const int row = (u / (32 * f) * f + u % f) * 32 + u / f % 32;
-    ssrc[i] = of_x ? X.scales + x_row(row) * 4 : W.scales + w_row(row) * 4;
+    ssrc[i] = of_x ? X.scales + (xfirst + x_row(row)) * 4 : W.scales + (wfirst + w_row(row)) * 4;
   }
   // Part `part` of four of stage st; past the last stage: that one again, for nothing; past a row's last block
   // or group of scales: that one again
@@ -451,46 +449,50 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 
-  float *mine = reinterpret_cast<float *>(wave < 2 ? buffer_a : buffer_b) + wave % 2 * (32 * PITCH);
+  if (bias) {
+#pragma unroll
+    for (int j = 0; j < NF; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const int64_t c = n0 + (wn * NF + j) * 32 + (q >> 2) * 8 + g * 4 + (q & 3);
+        const float v = bias[c < n ? c : n - 1];
+#pragma unroll
+        for (int i = 0; i < MF; ++i) acc[i][j][q] += v;
+        __builtin_amdgcn_sched_barrier(0);  // one at a time: the accumulators leave few registers
+      }
+  }
+  // Results in Y's type, 32 rows of the wave's columns: a lane leaves four neighbours of its row at a time and
+  // takes 16 bytes of a row for the memory.
+  T *mine = reinterpret_cast<T *>((wave < 2 ? buffer_a : buffer_b) + wave % 2 * (32 * PITCH * sizeof(T)));
   constexpr int V = 16 / sizeof(T), LANES = NF * 32 / V, STEP = 64 / LANES;  // columns of a lane, lanes of a row
   const int vr = lane / LANES, vc = lane % LANES * V;
   const int64_t c = n0 + wn * NF * 32 + vc;
   const int there = n - c < V ? (int)(n - c) : V;
-  float add[V] = {};
-  if (bias) {
-#pragma unroll
-    for (int q = 0; q < V; ++q) add[q] = q < there ? bias[c + q] : 0.0f;
-  }
-  __builtin_amdgcn_s_waitcnt(wait_until(0));  // so that no read below waits for it, and with it for the writes under way
   T *y = Y + (m0 + wm * MF * 32 + vr) * stride + c;
   auto put = [&](int i) {
 #pragma unroll
     for (int j = 0; j < NF; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4 *>(mine + r * PITCH + j * 32 + q * 8 + g * 4) =
-            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-    __builtin_amdgcn_wave_barrier();
-  };
-  auto get = [&](int row, float (&out)[V]) {
+      for (int q = 0; q < 4; ++q) {
+        const int at = j * 32 + q * 8 + g * 4;
+        Span<T, 4, 4 * sizeof(T)> o;
 #pragma unroll
-    for (int q = 0; q < V; q += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(mine + row * PITCH + vc + q);
-#pragma unroll
-      for (int p = 0; p < 4; ++p) out[q + p] = v[p] + add[q + p];
-    }
+        for (int p = 0; p < 4; ++p) o.v[p] = rounded<T>(acc[i][j][4 * q + p]);
+        *reinterpret_cast<Span<T, 4, 4 * sizeof(T)> *>(mine + r * PITCH + at) = o;
+      }
+    __builtin_amdgcn_sched_barrier(0);
   };
+  auto get = [&](int row) { return *reinterpret_cast<const Span<T, V, 16> *>(mine + row * PITCH + vc); };
   if (m0 + BM <= m1 && n0 + BN <= n) {  // a whole tile: no conditions between the reads and the writes
 #pragma unroll
     for (int i = 0; i < MF; ++i) {
       put(i);
 #pragma unroll
       for (int k = 0; k < 32 / STEP; ++k) {
-        float out[V];
-        get(k * STEP + vr, out);
-        store_span(y + (i * 32 + k * STEP) * stride, out);
+        const auto o = get(k * STEP + vr);
+        *reinterpret_cast<Span<T, V> *>(y + (i * 32 + k * STEP) * stride) = *reinterpret_cast<const Span<T, V> *>(&o);
       }
-      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
     }
     return;
   }
@@ -499,13 +501,16 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     const int64_t m = m0 + (wm * MF + i) * 32;
     put(i);
     for (int k = 0; k < 32 / STEP; ++k) {
-      float out[V];
-      get(k * STEP + vr, out);
       if (m + k * STEP + vr >= m1) continue;
-      if (there == V)
-        store_span(y + (i * 32 + k * STEP) * stride, out);
-      else
-        store_part(y + (i * 32 + k * STEP) * stride, there, out);
+      const auto o = get(k * STEP + vr);
+      T *to = y + (i * 32 + k * STEP) * stride;
+      if (there == V) {
+        *reinterpret_cast<Span<T, V> *>(to) = *reinterpret_cast<const Span<T, V> *>(&o);
+      } else {
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+          if (q < there) to[q] = o.v[q];
+      }
     }
     __builtin_amdgcn_wave_barrier();
   }
