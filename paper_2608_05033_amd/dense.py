@@ -181,7 +181,7 @@ class Packed4:
     columns begun, zeros past cols), and scales uint8 [ceil(cols / 128), rows, 4].
     A code's value is e2m1(code) times 2^(scale - 127); 255 makes a block NaN."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "index", "c")
+    __slots__ = ("_codes", "_scales", "_store", "rows", "cols", "index", "c")
 
     def __init__(self, codes, scales, cols: int):
         index = codes.get_device()
@@ -195,28 +195,44 @@ class Packed4:
             raise ValueError(f"codes must hold {cols} columns, two in a byte and rounded up to 32, next to each other")
         if scales.shape != ((cols + 127) // 128, rows, 4) or not scales.is_contiguous():
             raise ValueError(f"scales must be contiguous [{-(-cols // 128)}, {rows}, 4], got {tuple(scales.shape)}")
-        self.codes, self.scales, self.rows, self.cols, self.index = codes, scales, rows, cols, index
+        self._codes, self._scales, self._store, self.rows, self.cols, self.index = codes, scales, None, rows, cols, index
         self.c = sd_nibble_t(rows, cols, ld if rows > 1 and cols else need, 0, codes.data_ptr(), scales.data_ptr())
-
-    @property
-    def device(self):
-        return self.codes.device
-
-    def get_device(self) -> int:
-        return self.index
 
     @classmethod
     def empty(cls, rows: int, cols: int, like):
-        """A new one on the device of the tensor `like`: one allocation for codes and scales."""
-        ld, groups = (cols + 31) // 32 * 16, (cols + 127) // 128
+        """A new one on the device of the tensor `like`: one allocation for codes and
+        scales, which become tensors of their own when they are asked for."""
+        ld = (cols + 31) // 32 * 16
         size = rows * ld
-        store = like.new_empty(size + groups * rows * 4, dtype=_uint8)
+        store = like.new_empty(size + (cols + 127) // 128 * rows * 4, dtype=_uint8)
         p, at = cls.__new__(cls), store.data_ptr()
-        p.codes = store.as_strided((rows, ld), (ld, 1))
-        p.scales = store.as_strided((groups, rows, 4), (rows * 4, 4, 1), size)
-        p.rows, p.cols, p.index = rows, cols, store.get_device()
+        p._codes, p._scales, p._store, p.rows, p.cols, p.index = None, None, store, rows, cols, store.get_device()
         p.c = sd_nibble_t(rows, cols, ld, 0, at, at + size)
         return p
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            ld = self.c.ld
+            self._codes = self._store.as_strided((self.rows, ld), (ld, 1))
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            shape = (self.cols + 127) // 128, self.rows, 4
+            self._scales = self._store.as_strided(shape, (self.rows * 4, 4, 1), self.rows * self.c.ld)
+        return self._scales
+
+    def new_empty(self, *args, **kw):
+        return (self._codes if self._store is None else self._store).new_empty(*args, **kw)
+
+    @property
+    def device(self):
+        return (self._codes if self._store is None else self._store).device
+
+    def get_device(self) -> int:
+        return self.index
 
 
 @_on_its_device
@@ -252,9 +268,17 @@ def pack4_both(x):
 def unpack4(x: Packed4, dtype=torch.float32) -> torch.Tensor:
     if dtype not in TYPES:
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
-    y = x.codes.new_empty((x.rows, x.cols), dtype=dtype)
+    y = x.new_empty((x.rows, x.cols), dtype=dtype)
     _check(_lib.sd_nibble_unpack(x.c, y.data_ptr(), TYPES[dtype], x.cols, _raw_stream(x.index)), "sd_nibble_unpack")
     return y
+
+
+@functools.lru_cache(maxsize=4096)
+def _product4_size(rows, cols, n, index):
+    """The workspace in bytes on GPU `index`, which is the current one."""
+    size = ctypes.c_size_t()
+    _check(_lib.sd_nibble_product_size(rows, cols, n, size), "sd_nibble_product_size")
+    return size.value
 
 
 @_on_its_device
@@ -267,12 +291,10 @@ def product4(x: Packed4, w: Packed4, bias=None, dtype=torch.float32) -> torch.Te
         raise ValueError(f"dtype must be one of {list(TYPES)}, got {dtype}")
     n = w.rows
     bias = _vector(bias, n, x.index, "bias")
-    y = x.codes.new_empty((x.rows, n), dtype=dtype)
-    size = ctypes.c_size_t()
-    _check(_lib.sd_nibble_product_size(x.rows, x.cols, n, size), "sd_nibble_product_size")
-    work = y.new_empty(size.value, dtype=_uint8) if size.value else None
-    _check(_lib.sd_nibble_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n,
-                                  None if work is None else work.data_ptr(), size, _raw_stream(x.index)),
+    y = x.new_empty((x.rows, n), dtype=dtype)
+    size = _product4_size(x.rows, x.cols, n, x.index)
+    work = y.new_empty(size, dtype=_uint8).data_ptr() if size else None
+    _check(_lib.sd_nibble_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, work, size, _raw_stream(x.index)),
            "sd_nibble_product")
     return y
 

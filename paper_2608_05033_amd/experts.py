@@ -13,6 +13,7 @@ that stream.  `dispatch` and `combine` record gradients where torch does.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -31,7 +32,7 @@ class Route:
     without an expert) and source int32 [rows * k] (the row of the i-th entry, -1
     behind the last)."""
 
-    __slots__ = ("offsets", "place", "source", "rows", "k", "experts", "index", "c")
+    __slots__ = ("_offsets", "_place", "_source", "_store", "rows", "k", "experts", "index", "c")
 
     def __init__(self, offsets, place, source):
         index = offsets.get_device()
@@ -42,19 +43,54 @@ class Route:
         if k < 1 or offsets.numel() < 2 or source.numel() != rows * k:
             raise ValueError(f"offsets, place and source must be [experts + 1], [rows, k] and [rows * k], got "
                              f"{tuple(offsets.shape)}, {tuple(place.shape)} and {tuple(source.shape)}")
-        self._set(offsets, place, source, rows, k, offsets.numel() - 1, index)
+        self._offsets, self._place, self._source, self._store = offsets, place, source, None
+        self.rows, self.k, self.experts, self.index = rows, k, offsets.numel() - 1, index
+        self.c = sd_route_t(rows, k, self.experts, offsets.data_ptr(), place.data_ptr(), source.data_ptr())
 
-    def _set(self, offsets, place, source, rows, k, experts, index):
-        self.offsets, self.place, self.source = offsets, place, source
-        self.rows, self.k, self.experts, self.index = rows, k, experts, index
-        self.c = sd_route_t(rows, k, experts, offsets.data_ptr(), place.data_ptr(), source.data_ptr())
+    @classmethod
+    def empty(cls, rows: int, k: int, experts: int, like):
+        """A new one on the device of the tensor `like`: one allocation, whose parts
+        become tensors of their own when they are asked for."""
+        store = like.new_empty(experts + 1 + 2 * rows * k, dtype=_int32)
+        r, at = cls.__new__(cls), store.data_ptr()
+        r._offsets, r._place, r._source, r._store = None, None, None, store
+        r.rows, r.k, r.experts, r.index = rows, k, experts, store.get_device()
+        place = at + 4 * (experts + 1)
+        r.c = sd_route_t(rows, k, experts, at, place, place + 4 * rows * k)
+        return r
+
+    @property
+    def offsets(self):
+        if self._offsets is None:
+            self._offsets = self._store.as_strided((self.experts + 1,), (1,))
+        return self._offsets
+
+    @property
+    def place(self):
+        if self._place is None:
+            self._place = self._store.as_strided((self.rows, self.k), (self.k, 1), self.experts + 1)
+        return self._place
+
+    @property
+    def source(self):
+        if self._source is None:
+            entries = self.rows * self.k
+            self._source = self._store.as_strided((entries,), (1,), self.experts + 1 + entries)
+        return self._source
 
     @property
     def device(self):
-        return self.offsets.device
+        return (self._offsets if self._store is None else self._store).device
 
     def get_device(self) -> int:
         return self.index
+
+
+@functools.lru_cache(maxsize=4096)
+def _route_size(rows, k, experts):
+    size = ctypes.c_size_t()
+    _check(_lib.sd_route_size(rows, k, experts, size), "sd_route_size")
+    return size.value
 
 
 @_on_its_device
@@ -66,16 +102,11 @@ def route(chosen, experts: int) -> Route:
         raise ValueError(f"chosen must be a contiguous int32 or int64 [rows, k] on the GPU, got {chosen.dtype} "
                          f"{tuple(chosen.shape)} on {chosen.device}")
     rows, k = chosen.shape
-    size = ctypes.c_size_t()
-    _check(_lib.sd_route_size(rows, k, experts, size), "sd_route_size")
-    index, entries = chosen.get_device(), rows * k
-    store = chosen.new_empty(experts + 1 + 2 * entries, dtype=_int32)
-    r = Route.__new__(Route)
-    r._set(store.as_strided((experts + 1,), (1,)), store.as_strided((rows, k), (k, 1), experts + 1),
-           store.as_strided((entries,), (1,), experts + 1 + entries), rows, k, experts, index)
-    work = chosen.new_empty(size.value, dtype=_uint8) if size.value else None
-    _check(_lib.sd_route(chosen.data_ptr(), _INDEX_BYTES[chosen.dtype], r.c,
-                         None if work is None else work.data_ptr(), size, _raw_stream(index)), "sd_route")
+    size = _route_size(rows, k, experts)
+    r = Route.empty(rows, k, experts, chosen)
+    work = chosen.new_empty(size, dtype=_uint8).data_ptr() if size else None
+    _check(_lib.sd_route(chosen.data_ptr(), _INDEX_BYTES[chosen.dtype], r.c, work, size, _raw_stream(r.index)),
+           "sd_route")
     return r
 
 
@@ -211,7 +242,7 @@ def product(x: Packed4, w: Packed4, route: Route, bias=None, dtype=torch.float32
     if bias is not None and (bias.shape != (route.experts, n) or bias.dtype != _float32 or
                              bias.get_device() != x.index or not bias.is_contiguous()):
         raise ValueError(f"bias must be contiguous float32 [{route.experts}, {n}] on {x.device}")
-    y = x.codes.new_empty((total, n), dtype=dtype)
+    y = x.new_empty((total, n), dtype=dtype)
     _check(_lib.sd_expert_product(x.c, w.c, route.c, int(sorted), None if bias is None else bias.data_ptr(),
                                   y.data_ptr(), TYPES[dtype], n, _raw_stream(x.index)), "sd_expert_product")
     return y
