@@ -88,9 +88,12 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__restrict__ x, int64_t row_stride,
                                                                  int64_t col_stride, int64_t rows, int32_t cols,
                                                                  int32_t ng, uint8_t *__restrict__ codes, int64_t ld,
-                                                                 uint8_t *__restrict__ scales) {
-  const int64_t strip = workgroup() / (uint32_t)ng;
-  const int32_t grp = workgroup() % (uint32_t)ng;
+                                                                 uint8_t *__restrict__ scales, uint32_t wgs) {
+  if (workgroup() >= wgs) return;
+  // neighbouring groups of a row share lines, and run on one XCD
+  const uint32_t at = xcd_place(workgroup(), wgs);
+  const int64_t strip = at / (uint32_t)ng;
+  const int32_t grp = at % (uint32_t)ng;
   const int block = threadIdx.x >> 6;
   const int64_t row = strip * 64 + (threadIdx.x & 63);
   if (row >= rows) return;
@@ -137,7 +140,8 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
                                                                uint8_t *__restrict__ codes, int64_t ld,
                                                                uint8_t *__restrict__ scales,
                                                                uint8_t *__restrict__ codes_t, int64_t ld_t,
-                                                               uint8_t *__restrict__ scales_t) {
+                                                               uint8_t *__restrict__ scales_t, uint32_t strips,
+                                                               uint32_t wgs) {
   constexpr int V = 16 / sizeof(T), LANES = kGroup / V, SHARE = kCols / V, AT_ONCE = 64 / LANES, STEPS = 32 / AT_ONCE;
   // by whole words: an odd number of them between rows, so that neither way of reading meets itself
   constexpr int PITCH = kGroup + 4 / (int)sizeof(T);
@@ -145,9 +149,11 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
   __shared__ __align__(16) u32x4 blocks[4][kGroup];
   __shared__ uint8_t bytes[kGroup][4];
   const int t = threadIdx.x, wave = t >> 6, l = t & 63, lane = l % LANES, down = l / LANES;
-  const int64_t strip = workgroup() / (uint32_t)ng, row0 = strip * 128 + wave * 32;
-  const int32_t grp = workgroup() % (uint32_t)ng;
-  if (strip * 128 >= rows) return;
+  if (workgroup() >= wgs) return;
+  // neighbouring strips share lines of the transpose, and run on one XCD
+  const uint32_t at = xcd_place(workgroup(), wgs);
+  const int64_t strip = at % strips, row0 = strip * 128 + wave * 32;
+  const int32_t grp = at / strips;
   const int32_t c = grp * kGroup + lane * V;
   float v[STEPS][V];
 #pragma unroll
@@ -284,9 +290,12 @@ int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nib
   constexpr int per_wg = kThreads / (kGroup * (int)sizeof(T) / 16) * kUnroll;
   const int64_t wgs = across ? ceil_div(out->rows, 64) * ng : ceil_div(out->rows * ng, per_wg);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  auto *kernel = across            ? k_nibble_pack_across<T>
-                 : col_stride == 1 ? k_nibble_pack<T, true>
-                                   : k_nibble_pack<T, false>;
+  if (across) {
+    hipLaunchKernelGGL(k_nibble_pack_across<T>, grid_of(wgs), dim3(kThreads), 0, s, p, row_stride, col_stride,
+                       out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, (uint32_t)wgs);
+    return launched();
+  }
+  auto *kernel = col_stride == 1 ? k_nibble_pack<T, true> : k_nibble_pack<T, false>;
   hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, p, row_stride, col_stride, out->rows,
                      (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales);
   return launched();
@@ -298,7 +307,7 @@ int both_any(const void *x, int64_t row_stride, const sd_nibble_t *out, const sd
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   hipLaunchKernelGGL(k_nibble_pack_both<T>, grid_of(wgs), dim3(kThreads), 0, s, static_cast<const T *>(x), row_stride,
                      out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, out_t->codes,
-                     out_t->ld, out_t->scales);
+                     out_t->ld, out_t->scales, (uint32_t)(wgs / ng), (uint32_t)wgs);
   return launched();
 }
 
