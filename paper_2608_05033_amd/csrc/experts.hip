@@ -381,19 +381,23 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
 }
 
 // Calls f(lanes, entries at a time, whether rows have 16 bytes) for rows of `cols`
-// elements: the most lanes of which four in five have work in all steps.
-template <typename T, typename F>
+// elements: lanes for a whole row up to 32, then 64.  Measured in us (to the experts, back,
+// gradients):
+//   rows, entries of each, columns     8 lanes       16           32           64
+//   262144, 2, 128 fp32               82, 78, 136  75, 73, 125  76, 71, 119  104, 83, 146
+//   262144, 2, 129 fp32             165, 121, 246 116, 92, 197  93, 81, 157  116, 94, 171
+//   20011, 4, 601 bf16                32, 27, 63   27, 26, 55   24, 25, 47   23, 24, 49
+//   100000, 8, 64 bf16                21, 24, 56   24, 32, 97   37, 56, 187
+template <int MOST, typename T, typename F>
 int with_shape(int64_t cols, int32_t k, const F &f) {
   constexpr int V = 16 / sizeof(T);
   const int64_t steps = ceil_div(cols, V);
-  int lanes = 64;
-  while (lanes > 8 && 5 * steps < 4 * lanes * ceil_div(steps, lanes)) lanes /= 2;
-  if (steps <= 2) lanes = 2;
+  const int lanes = steps > 48 ? 64 : steps > 16 ? 32 : steps > 8 ? 16 : steps > 2 ? 8 : 2;
   const auto entries = [&](auto l, auto whole) {
     if (k == 1) return f(l, std::integral_constant<int, 1>(), whole);
     if (k == 2) return f(l, std::integral_constant<int, 2>(), whole);
-    if (k <= 4) return f(l, std::integral_constant<int, 4>(), whole);
-    return f(l, std::integral_constant<int, 8>(), whole);
+    if (k <= 4 || MOST == 4) return f(l, std::integral_constant<int, 4>(), whole);
+    return f(l, std::integral_constant<int, MOST>(), whole);
   };
   if (cols < V) return entries(std::integral_constant<int, 2>(), std::false_type());
   switch (lanes) {
@@ -408,7 +412,7 @@ int with_shape(int64_t cols, int32_t k, const F &f) {
 template <typename T>
 int dispatch_as(const sd_route_t *r, const void *x, int64_t cols, int64_t x_stride, void *y, int64_t y_stride,
                 hipStream_t s) {
-  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
     hipLaunchKernelGGL((k_dispatch<T, L, decltype(kb)::value, decltype(whole)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(x),
@@ -419,7 +423,7 @@ int dispatch_as(const sd_route_t *r, const void *x, int64_t cols, int64_t x_stri
 template <typename T>
 int combine_as(const sd_route_t *r, const void *y, int64_t cols, int64_t y_stride, const float *weights, void *out,
                int64_t out_stride, hipStream_t s) {
-  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
     hipLaunchKernelGGL((k_combine<T, L, decltype(kb)::value, decltype(whole)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(y),
@@ -430,7 +434,7 @@ int combine_as(const sd_route_t *r, const void *y, int64_t cols, int64_t y_strid
 template <typename T>
 int backward_as(const sd_route_t *r, const void *dout, int64_t cols, int64_t dout_stride, const void *y,
                 int64_t y_stride, const float *weights, void *dy, int64_t dy_stride, float *dweights, hipStream_t s) {
-  return with_shape<T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<4, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
     constexpr int L = decltype(lanes)::value;
     hipLaunchKernelGGL((k_combine_backward<T, L, decltype(kb)::value, decltype(whole)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(dout),
