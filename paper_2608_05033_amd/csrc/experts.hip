@@ -15,9 +15,9 @@ namespace {
 
 using namespace nibble;
 
-constexpr int64_t kMaxRuns = 1024;    // runs of entries that are counted apart
+constexpr int64_t kMaxRuns = 4096;    // runs of entries that are counted apart
 constexpr int64_t kRun = 512;         // entries of a run at least
-constexpr int64_t kOneGroup = 8192;   // entries that one workgroup sorts by itself
+constexpr int64_t kOneGroup = 8192;   // entries that one workgroup sorts by itself: 10 us; 16384 take 17, three launches 12
 constexpr int kWaves = 16;            // of it
 constexpr int kKindsAlone = 960;      // kinds whose counters for 16 waves and whose sums fit 64 KiB
 
@@ -144,12 +144,22 @@ __global__ __launch_bounds__(256) void k_route_count(const void *__restrict__ ch
 // and their sum.
 __global__ __launch_bounds__(1024) void k_route_sum(uint32_t *__restrict__ counts, int32_t runs,
                                                     uint32_t *__restrict__ totals) {
+  constexpr int EACH = kMaxRuns / 1024;
   __shared__ uint32_t sums[16];
   uint32_t *mine = counts + (int64_t)blockIdx.x * runs;
-  const uint32_t v = (int)threadIdx.x < runs ? mine[threadIdx.x] : 0u;
-  const uint32_t at = sum_before(v, sums);
-  if ((int)threadIdx.x < runs) mine[threadIdx.x] = at;
-  if (threadIdx.x == 1023) totals[blockIdx.x] = at + v;
+  const int first = threadIdx.x * EACH;
+  uint32_t v[EACH], own = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) v[i] = first + i < runs ? mine[first + i] : 0u;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) own += v[i];
+  uint32_t at = sum_before(own, sums);
+  if (threadIdx.x == 1023) totals[blockIdx.x] = at + own;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    if (first + i < runs) mine[first + i] = at;
+    at += v[i];
+  }
 }
 __global__ __launch_bounds__(256) void k_route_place(const void *__restrict__ chosen, int wide, int64_t entries,
                                                      int32_t k, int32_t experts, int bits,

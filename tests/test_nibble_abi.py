@@ -129,7 +129,7 @@ def test_route_refusals_and_workspace():
     assert need > 0
     for work, size in ((None, need), (P, need - 1), (P + 8, need)):
         refused(sd.SD_ERR_INVALID_VALUE, sd.sd_route, P, 4, route(rows=100000, experts=8), work, size)
-    assert sd.sd_route_size((1 << 31) - 1, 1, 4095) <= 32 << 20
+    assert sd.sd_route_size((1 << 31) - 1, 1, 4095) <= 65 << 20
 
 
 def test_exchange_refusals():
