@@ -59,6 +59,10 @@ class Route:
         r.c = sd_route_t(rows, k, experts, at, place, place + 4 * rows * k)
         return r
 
+    def kept(self):
+        """The tensors that hold it, for autograd to watch."""
+        return (self._offsets, self._place, self._source) if self._store is None else (self._store,)
+
     @property
     def offsets(self):
         if self._offsets is None:
@@ -170,15 +174,19 @@ def combine_backward(dout, y, route: Route, weights=None, need_dy: bool = True, 
     return dy, dweights
 
 
+# A route is kept whole, and its tensors as saved ones: one that was written to in
+# the meantime is found when they are asked for.
 class _Dispatch(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, route):
-        ctx.save_for_backward(route.offsets, route.place, route.source)
+        ctx.route = route
+        ctx.save_for_backward(*route.kept())
         return _dispatch(x, route)
 
     @staticmethod
     def backward(ctx, dy):
-        return combine(dy.contiguous(), Route(*ctx.saved_tensors)), None
+        ctx.saved_tensors
+        return combine(dy.contiguous(), ctx.route), None
 
 
 class _Sum(torch.autograd.Function):
@@ -186,28 +194,30 @@ class _Sum(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, y, route):
-        ctx.save_for_backward(route.offsets, route.place, route.source)
+        ctx.route = route
+        ctx.save_for_backward(*route.kept())
         return _combine(y, route, None)
 
     @staticmethod
     def backward(ctx, dout):
-        return dispatch(dout.contiguous(), Route(*ctx.saved_tensors)), None
+        ctx.saved_tensors
+        return dispatch(dout.contiguous(), ctx.route), None
 
 
 class _WeightedSum(torch.autograd.Function):
     @staticmethod
     def forward(ctx, y, weights, route):
-        ctx.save_for_backward(route.offsets, route.place, route.source,
-                              weights if ctx.needs_input_grad[0] else None, y if ctx.needs_input_grad[1] else None)
+        ctx.route = route
+        ctx.save_for_backward(weights if ctx.needs_input_grad[0] else None, y if ctx.needs_input_grad[1] else None,
+                              *route.kept())
         return _combine(y, route, weights)
 
     @staticmethod
     @first_derivatives_only
     def backward(ctx, dout):
-        offsets, place, source, weights, y = ctx.saved_tensors
+        weights, y = ctx.saved_tensors[:2]
         need_dy, need_dweights = ctx.needs_input_grad[:2]
-        return *combine_backward(dout.contiguous(), y, Route(offsets, place, source), weights, need_dy,
-                                 need_dweights), None
+        return *combine_backward(dout.contiguous(), y, ctx.route, weights, need_dy, need_dweights), None
 
 
 def dispatch(x: torch.Tensor, route: Route) -> torch.Tensor:

@@ -241,6 +241,12 @@ def test_what_the_gradients_keep_is_watched():
         W.mul_(2)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         out.sum().backward()
+    for r in (r, experts.Route(r.offsets.clone(), r.place.clone(), r.source.clone())):
+        for call in (lambda: experts.combine(Y, r, W), lambda: experts.combine(Y, r), lambda: experts.dispatch(W, r)):
+            out = call()
+            r.place.sub_(0)  # the same numbers, but written
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                out.sum().backward()
 
 
 # --------------------------------------------------------- experts' products ---
