@@ -26,10 +26,10 @@ def first_derivatives_only(backward):
 
     @functools.wraps(backward)
     def wrapped(ctx, dZ):
+        if not torch.is_grad_enabled():
+            return backward(ctx, dZ)
         with torch.no_grad():
             grads = backward(ctx, dZ)
-        if not torch.is_grad_enabled():
-            return grads
         anchors = [v for v in (dZ, *ctx.saved_tensors) if v is not None and v.requires_grad]
         anchors = anchors or [dZ.new_empty(0).requires_grad_()]
         return tuple(g if g is None else _FirstOnly.apply(g, *anchors) for g in grads)
