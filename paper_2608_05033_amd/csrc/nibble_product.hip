@@ -604,11 +604,24 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
 //   256 x 128 x 262144         1110       406    278    142   108    34    19     20
 // A stage of 256 k takes a lone 128 x 128 tile 0.5 us, and the parts go to memory and back at about
 // 2.5 TB/s: that gives the number of parts.
+//
+// Rows sorted by expert, us, launches in a row (rows of X, experts of each, experts, columns x k):
+//                              256x256   128x128  32x32  16x16
+//   4096, 2, 16, 4096 x 4096        113       119    634   1176
+//   1024, 2, 16, 4096 x 4096         66        49    175    307
+//   128, 8, 64, 1024 x 2048          39        24     29     32
+//   64, 8, 64, 1024 x 2048           40        23     27     23
+//   16, 8, 64, 1024 x 2048           38        23     24     18
 Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) {
   const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
-  const auto tiles = [&](int64_t bm, int64_t bn) { return row_tiles(rows, experts, bm) * ceil_div(n, bn); };
+  // of rows sorted by expert the tiles there will be: half a tile too many for each expert
+  const auto tiles = [&](int64_t bm, int64_t bn) {
+    return (experts == 0 ? ceil_div(rows, bm) : ceil_div(rows, bm) + std::min<int64_t>(experts / 2, rows)) *
+           ceil_div(n, bn);
+  };
   const auto whole = [&](Form f) { return Plan{f, 1, (int32_t)stages}; };
-  if (near) {
+  const bool few = experts > 0 && rows <= 8 * (int64_t)experts;  // of each expert
+  if (near && !few) {
     if (4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
     const int64_t t = tiles(128, 128);
     const bool wide = rows > 64 && n > 64 && t >= cus / 8, many = t >= cus / 2;
@@ -624,8 +637,12 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
     // tiles: 2048 x 2048 x 8192 takes 23 us so and 28 with two
     if (wide || many) return whole(t <= cus && stages >= 24 ? kTile128Deep : kTile128);
   }
-  if (rows > 16 && n > 16 && tiles(32, 32) >= cus) return whole(stages > 4 ? kRows32 : kRows32Short);
-  return whole(stages > 4 ? kRows16 : kRows16Short);
+  // Four waves share the sum where it is short or workgroups come in numbers, else eight: 1500 x 1500 x 1500
+  // takes 23 and 33 us in tiles of 16 x 16, 1 x 4096 x 4096 3.9 and 3.7.
+  const auto short_of = [&](int64_t t) { return stages <= 4 || t >= 2 * cus; };
+  if (rows > 16 && n > 16 && tiles(32, 32) >= cus && !few)
+    return whole(short_of(tiles(32, 32)) ? kRows32Short : kRows32);
+  return whole(short_of(tiles(16, 16)) ? kRows16Short : kRows16);
 }
 size_t parts_bytes(const Plan &p, int64_t rows, int64_t n) {
   return p.splits > 1 ? (size_t)p.splits * rows * n * 4 : 0;

@@ -379,6 +379,16 @@ def test_transform_only_what_is_asked_for():
         torch.autograd.grad(gx.sum(), W)
 
 
+@pytest.mark.parametrize("rows,cols,n", [(0, 5, 3), (4, 0, 3), (4, 5, 0)])
+def test_transform_of_nothing(rows, cols, n):
+    X = torch.ones(rows, cols, device="cuda", requires_grad=True)
+    W = torch.ones(cols, n, device="cuda", requires_grad=True)
+    Z = gcn.transform4(X, W)
+    dX, dW = torch.autograd.grad(Z, (X, W), torch.ones(rows, n, device="cuda"))
+    assert torch.equal(Z, torch.zeros(rows, n, device="cuda"))
+    assert torch.equal(dX, torch.zeros_like(X)) and torch.equal(dW, torch.zeros_like(W))
+
+
 def test_offsets_past_32_bits():
     """More than 2^32 bytes of codes: the last row alone is not zero."""
     rows, cols = (1 << 27) + 3, 64
