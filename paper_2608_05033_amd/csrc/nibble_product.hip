@@ -2,16 +2,20 @@
 // tables, and sd_expert_product: the same where each row of Y is one row of X
 // through the weights of the expert it was sorted to.
 //
-// A wave's 16 x 16 tile over 128 k: lane (r, g) = (lane % 16, lane / 16) holds a
-// whole block of row r of each side, its 32 codes in 16 bytes and its scale byte,
-// which is what v_mfma_scale_f32_16x16x128_f8f6f4 takes.  W is the first operand,
-// so a lane ends with four neighbouring n of one row m.
+// The matrix unit takes a block of a row from each lane: its 32 codes in 16 bytes
+// and its scale byte.  Few rows run products of 16 x 16 x 128 (16 rows, 4 blocks),
+// large tiles of 32 x 32 x 64 (32 rows, 2 blocks).  W is the first operand, so a lane
+// ends with runs of four neighbouring n of one row m.
 //
 // Products of e2m1 codes are multiples of 1/4 up to 36, so that the unit, which
 // drops what lies far under the largest product of a run, drops nothing within a
 // block: sums of blocks of one scale are exact.  Measured over random codes, one
 // instruction is off by at most 2.1e-7 of the magnitudes summed, also where the
 // blocks' scales differ by 2^80 or the sum so far is 10^6 times the products.
+//
+// With operands in registers the 32 x 32 form reaches 9.4 PFLOP/s on zeros and 6.7 on
+// random codes, where power lets the clock fall to 1.65 GHz; the 16 x 16 form 6.9 on
+// zeros.  6.7 is what the large products are held against.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -109,7 +113,11 @@ __device__ inline void clear_rows(T *Y, int64_t stride, int64_t m0, int64_t m1, 
 }
 
 // MF x NF tiles of 16 x 16 by one workgroup, operands straight from memory: KW
-// waves each take every KW-th group of 128 k and join their sums in shared memory.
+// waves each take every KW-th pair of groups of 128 k and join their sums in shared
+// memory.  Lane (r, g) = (lane % 16, lane / 16) takes block g of a group of row r.
+// Bound by the latency of the loads where there are few tiles: 1 x 4096 x 4096 takes
+// 3.7 us (2.4 TB/s of W), the launch itself 2; by W's bytes where there are many: 16
+// rows through 2 of 16 experts of 4096 x 4096 take 28, 5.1 TB/s.
 template <typename T, int MF, int NF, int KW, bool EXPERTS>
 __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, Sorted sorted,
                                                          const float *__restrict__ bias, T *__restrict__ Y,
@@ -210,23 +218,32 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
 __device__ constexpr int wait_until(int left) { return (left & 15) | (left >> 4) << 14 | 0x70; }
 
 // BM x BN tiles (rows of X by rows of W), operands through shared memory: WM x WN
-// waves, each (BM / WM) x (BN / WN) in products of 32 x 32 x 64, which run at 1.4 to
-// 1.8 times the rate of 16 x 16 x 128.
+// waves, each (BM / WM) x (BN / WN) in products of 32 x 32 x 64.
 //
-// Four buffers hold 128 k (a stage) each.  What is asked for goes from memory straight
-// to shared memory, up to four stages ahead: a stage takes about half of the time that
-// memory needs to answer.  A stage's two products per tile overlap with reads: while
-// the first runs, the second one's operands come from shared memory; then, behind the
-// one barrier of the stage, the next stage's first ones while the second runs.
+// A buffer holds 256 k (a stage), 128 bytes of every row: whole lines, which the caches
+// hand out at twice the rate of their halves (34 and 18 TB/s over the card).  What is
+// asked for goes from memory straight to shared memory; with two buffers a stage is
+// asked for as soon as the one before the last has been read, with four, where only
+// 128 rows a side leave room, two stages earlier.  A stage has four products per 32 x
+// 32 tile.  While one runs, the next one's operands come from shared memory; the
+// requests for the next stage are woven in between, one behind each product, since a
+// wave that asks for all at once waits until the last request is taken.  The one
+// barrier of a stage stands before its last product, whose operands are there already.
 //
-// Rows of codes lie 64 bytes apart, their four blocks mixed with the row so that 16
-// rows read at one block touch all banks; the mixing is done on the memory side, since
-// a wave's 64 lanes write 1 KiB in order.  Lane (r, g) = (lane % 32, lane / 32) takes
-// blocks 2 g and 2 g + 1 of a row.  Scale words lie by lane, the tile's 32-row groups
+// Rows of codes lie 128 bytes apart, their eight blocks mixed with the row so that 16
+// rows read at one block touch all banks (no conflicts counted); the mixing is done on
+// the memory side, since a wave's 64 lanes write 1 KiB in order.  Lane (r, g) = (lane %
+// 32, lane / 32) takes blocks 4 g .. 4 g + 3 of a row, so that one word holds all the
+// scale bytes it needs of the row; these words lie by lane, the tile's 32-row groups
 // side by side, and one read serves several products.
 //
-// A wave's results go through its share of the shared memory, 32 rows at a time, so
+// A wave's results go through shared memory in their own type, 32 rows at a time, so
 // that whole lines are written.
+//
+// Bound by the matrix units at the clock that power allows, and by what the requests
+// take from them: 8192 cubed to bf16 takes 245 to 285 us (box and warmth), 3.9 to 4.5
+// PFLOP/s, of which a tile's 32 stages take 60 (2850 cycles each at 1.5 to 1.65 GHz,
+// 2112 of them products), the way in 2.4 and the way out 4.  2048 cubed takes 8.8 us.
 template <typename T, int BM, int BN, int BUFFERS, bool EXPERTS>
 __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorted sorted,
                                                              const float *__restrict__ bias, T *__restrict__ Y,
@@ -517,7 +534,7 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
 }
 
 // Y = the sum of the parts that workgroups of a split sum left + bias: TEAM threads for four columns, each
-// every TEAM-th part, then the threads' sums, all in one order.
+// every TEAM-th part, then the threads' sums, all in one order.  64 parts of 256 x 128 take 4 us, 2.1 TB/s.
 template <typename T, int TEAM>
 __global__ __launch_bounds__(256) void k_nibble_join(const float *__restrict__ parts, int32_t splits, int64_t rows,
                                                      int64_t n, const float *__restrict__ bias, T *__restrict__ Y,

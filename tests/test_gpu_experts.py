@@ -149,6 +149,14 @@ def test_results_that_are_parts_of_wider_tables():
         assert (wide[:, :2] == 7).all() and (wide[:, 21:] == 7).all()
 
 
+def test_tables_of_no_columns():
+    r = experts.route(torch.from_numpy(choose(7, 3, 4, 1)).cuda(), 4)
+    x, y = torch.zeros(7, 0, device="cuda"), torch.zeros(21, 0, device="cuda")
+    assert experts.dispatch(x, r).shape == (21, 0) and experts.combine(y, r).shape == (7, 0)
+    dy, dw = experts.combine_backward(x, y, r)
+    assert dy.shape == (21, 0) and torch.equal(dw, torch.zeros(7, 3, device="cuda"))
+
+
 def test_values_that_are_not_finite():
     """Rows that nobody was sorted to are not read, a weight of 0 does not hide NaN."""
     c = np.array([[0, 1], [-1, 0], [1, -1]])

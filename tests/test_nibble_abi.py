@@ -79,6 +79,7 @@ def test_packing_refusals():
          [(0, None), (0, P + 2), (1, 0), (2, -1), (3, -1), (4, None), (4, table(cols=41)), (5, None), (5, table()),
           (5, table(rows=40, cols=4, codes=None))])
     each(sd.SD_ERR_OVERFLOW, sd.sd_nibble_pack_both, good, [(2, 1 << 32), (3, 1 << 32)])
+    refused(sd.SD_ERR_OVERFLOW, sd.sd_nibble_pack_both, P, F32, 1 << 32, 2, *good[4:])
     each(sd.SD_ERR_INVALID_VALUE, sd.sd_nibble_unpack, [table(), P, F32, 40],
          [(0, None), (1, None), (1, P + 1), (2, 0), (3, 39)])
     refused(sd.SD_ERR_OVERFLOW, sd.sd_nibble_unpack, table(), P, F32, 1 << 31)
