@@ -142,31 +142,35 @@ class _PackedTransform(torch.autograd.Function):
 
 class _Transform4(torch.autograd.Function):
     """X.W and both gradients as products of 4-bit tables, each packed along its own
-    sum.  What the backward pass needs of X is kept packed along the rows, at half a
-    byte an element."""
+    sum.  What the backward pass needs of X and W is kept packed along the other side,
+    at half a byte an element."""
 
     @staticmethod
     def forward(ctx, X, W):
-        ctx.dtype = X.dtype
-        X4, Xt = dense.pack4_both(X) if ctx.needs_input_grad[1] else (dense.pack4(X), None)
-        ctx.save_for_backward(W, *(() if Xt is None else (Xt.codes, Xt.scales)))
-        return dense.product4(X4, dense.pack4(W, transpose=True))
+        need_dX, need_dW = ctx.needs_input_grad
+        X4, Xt = dense.pack4_both(X) if need_dW else (dense.pack4(X), None)
+        W4, Wt = dense.pack4_both(W) if need_dX else (None, dense.pack4(W, transpose=True))
+        ctx.dtypes, ctx.sizes = (X.dtype, W.dtype), (X.shape[0], W.shape[1])
+        ctx.save_for_backward(W, *(() if W4 is None else (W4.codes, W4.scales)),
+                              *(() if Xt is None else (Xt.codes, Xt.scales)))
+        return dense.product4(X4, Wt)
 
     @staticmethod
     @first_derivatives_only
     def backward(ctx, dZ):
-        W, *Xt = ctx.saved_tensors
+        need_dX, need_dW = ctx.needs_input_grad
+        kept, (rows, n) = ctx.saved_tensors, ctx.sizes
         dX = dW = None
-        if all(ctx.needs_input_grad):
+        if need_dX and need_dW:
             G, Gt = dense.pack4_both(dZ)
-        elif ctx.needs_input_grad[0]:
+        elif need_dX:
             G = dense.pack4(dZ)
         else:
             Gt = dense.pack4(dZ, transpose=True)
-        if ctx.needs_input_grad[0]:
-            dX = dense.product4(G, dense.pack4(W), dtype=ctx.dtype)
-        if ctx.needs_input_grad[1]:
-            dW = dense.product4(dense.Packed4(*Xt, dZ.shape[0]), Gt, dtype=W.dtype)
+        if need_dX:
+            dX = dense.product4(G, dense.Packed4(*kept[1:3], n), dtype=ctx.dtypes[0])
+        if need_dW:
+            dW = dense.product4(dense.Packed4(*kept[-2:], rows), Gt, dtype=ctx.dtypes[1])
         return dX, dW
 
 
