@@ -293,9 +293,9 @@ def product4(x: Packed4, w: Packed4, bias=None, dtype=torch.float32) -> torch.Te
     bias = _vector(bias, n, x.index, "bias")
     y = x.new_empty((x.rows, n), dtype=dtype)
     size = _product4_size(x.rows, x.cols, n, x.index)
-    work = y.new_empty(size, dtype=_uint8).data_ptr() if size else None
-    _check(_lib.sd_nibble_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, work, size, _raw_stream(x.index)),
-           "sd_nibble_product")
+    work = y.new_empty(size, dtype=_uint8) if size else None  # lives until the call has been enqueued
+    _check(_lib.sd_nibble_product(x.c, w.c, bias, y.data_ptr(), TYPES[dtype], n, work.data_ptr() if size else None, size,
+                                  _raw_stream(x.index)), "sd_nibble_product")
     return y
 
 

@@ -108,9 +108,9 @@ def route(chosen, experts: int) -> Route:
     rows, k = chosen.shape
     size = _route_size(rows, k, experts)
     r = Route.empty(rows, k, experts, chosen)
-    work = chosen.new_empty(size, dtype=_uint8).data_ptr() if size else None
-    _check(_lib.sd_route(chosen.data_ptr(), _INDEX_BYTES[chosen.dtype], r.c, work, size, _raw_stream(r.index)),
-           "sd_route")
+    work = chosen.new_empty(size, dtype=_uint8) if size else None  # lives until the call has been enqueued
+    _check(_lib.sd_route(chosen.data_ptr(), _INDEX_BYTES[chosen.dtype], r.c, work.data_ptr() if size else None, size,
+                         _raw_stream(r.index)), "sd_route")
     return r
 
 

@@ -1,6 +1,8 @@
 """Every form of the 4-bit products at its edges: sizes that the choice of tiles,
 of buffers and of a split sum goes by, with the results' types, biases, rows of NaN
 and exact sums.  Sizes are made from the card's compute units."""
+import gc
+
 import numpy as np
 import pytest
 
@@ -123,6 +125,35 @@ def test_tables_far_apart_in_memory():
     assert np.array_equal(to64(experts.product(F, W, experts.route(c, 1))), want)
     assert np.array_equal(to64(experts.product(W, F, experts.route(torch.zeros(700, 1, dtype=torch.int32).cuda(), 1))),
                           want.T)
+
+
+@pytest.mark.parametrize("name,at", [("sd_nibble_product", 6), ("sd_route", 3)])
+def test_workspaces_live_until_the_call_is_enqueued(name, at, monkeypatch):
+    """Memory given back before could be another thread's by then."""
+    seen = []
+
+    class Watch:
+        def __init__(self, lib):
+            self.lib = lib
+
+        def __getattr__(self, what):
+            f = getattr(self.lib, what)
+            if what != name:
+                return f
+
+            def call(*args):
+                seen.append(any(t.data_ptr() == args[at] for t in gc.get_objects()
+                                if type(t) is torch.Tensor and t.dtype == torch.uint8 and t.is_cuda))
+                return f(*args)
+
+            return call
+
+    for module in (dense, experts):
+        monkeypatch.setattr(module, "_lib", Watch(module._lib))
+    X = random_table(64, 40000, 1, 2)
+    dense.product4(X, X)
+    experts.route(torch.zeros(30000, 2, dtype=torch.int32, device="cuda"), 3)
+    assert seen == [True]
 
 
 def test_streams_at_once():
