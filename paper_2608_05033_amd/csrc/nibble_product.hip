@@ -253,11 +253,12 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
   constexpr int THREADS = 256, WM = 2, WN = 2, MF = BM / WM / 32, NF = BN / WN / 32;
   constexpr int ROWS = BM + BN, CHUNKS = ROWS * 8 / THREADS, SCALES = 2 * ROWS / THREADS;
   constexpr int BUFFER = ROWS * 136, PITCH = NF * 32 + 16 / (int)sizeof(T);  // PITCH: between a wave's rows of results
-  static_assert(ROWS % THREADS == 0 && BM % (THREADS / 8) == 0 && BM % 64 == 0, "one operand for a wave");
-  static_assert(2 * 32 * PITCH * (int)sizeof(T) <= BUFFER && (BUFFERS == 2 || BUFFERS == 4), "two waves' results in a buffer");
+  static_assert(ROWS % THREADS == 0 && BM % (THREADS / 8) == 0 && BM % 64 == 0, "one operand for a wave's requests");
+  static_assert((BUFFERS == 1 ? 4 : 2) * 32 * PITCH * (int)sizeof(T) <= BUFFER, "the waves' results in the buffers");
   // objects of their own and no array: reads of one then need not wait for what is on its way to another
-  __shared__ __align__(16) uint8_t buffer_a[BUFFER], buffer_b[BUFFER];
+  __shared__ __align__(16) uint8_t buffer_a[BUFFER], buffer_b[BUFFERS > 1 ? BUFFER : 16];
   __shared__ __align__(16) uint8_t buffer_c[BUFFERS == 4 ? BUFFER : 16], buffer_d[BUFFERS == 4 ? BUFFER : 16];
+  __shared__ __align__(16) float shared_bias[BN];
   const int t = threadIdx.x, lane = t & 63, r = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wm = wave / WN, wn = wave % WN;
   const uint32_t tiles = (uint32_t)mt * (uint32_t)nt, split = workgroup() / tiles;
@@ -304,11 +305,11 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     off[i] = i < XC ? x_row(row) * (uint32_t)X.ld : w_row(row) * (uint32_t)W.ld;
   }
   // Scale word i of thread t: place i * THREADS + t of [g][X's, then W's][wave row or column][r][product].
-  const uint8_t *ssrc[ROWS / THREADS];
+  const uint8_t *ssrc[SCALES];
 #pragma unroll
-  for (int i = 0; i < ROWS / THREADS; ++i) {
-    const bool of_x = i * THREADS + wave * 64 < BM;
-    const int u = i * THREADS + t - (of_x ? 0 : BM), f = of_x ? MF : NF;
+  for (int i = 0; i < SCALES; ++i) {
+    const bool of_x = (i * THREADS + wave * 64) % ROWS < BM;
+    const int u = (i * THREADS + t) % ROWS - (of_x ? 0 : BM), f = of_x ? MF : NF;
     const int row = (u / (32 * f) * f + u % f) * 32 + u / f % 32;
     ssrc[i] = of_x ? X.scales + (xfirst + x_row(row)) * 4 : W.scales + (wfirst + w_row(row)) * 4;
   }
@@ -318,17 +319,16 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     st = st < last ? st : last - 1;
     const uint32_t block = st * 8 + chunk < blocks ? st * 8 + chunk : blocks - 1;
 #pragma unroll
-    for (int i = part * (CHUNKS / 4); i < (part + 1) * (CHUNKS / 4); ++i)
+    for (int i = part * CHUNKS / 4; i < (part + 1) * CHUNKS / 4; ++i)
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void *)((i < XC ? xbase : wbase) + (off[i] + block * 16)),
           (__attribute__((address_space(3))) void *)(&buffer[(i * THREADS + wave * 64) * 16]), 16, 0, 0);
 #pragma unroll
     for (int i = part * SCALES / 4; i < (part + 1) * SCALES / 4; ++i) {
-      const int at = i * THREADS + wave * 64;
+      const int at = i * THREADS + wave * 64, u = at % ROWS;
       const int64_t group = st * 2 + (at >= ROWS && st * 2 + 1 < (blocks + 3) / 4 ? 1 : 0);
       __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void *)(ssrc[i % (ROWS / THREADS)] +
-                                                           group * ((at % ROWS < BM ? X.rows : W.rows) * 4)),
+          (const __attribute__((address_space(1))) void *)(ssrc[i] + group * ((u < BM ? X.rows : W.rows) * 4)),
           (__attribute__((address_space(3))) void *)(&buffer[ROWS * 128 + at * 4]), 4, 0, 0);
     }
   };
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     weave(std::integral_constant<int, 0>());
     // This wave's part of the next stage is there; behind the barrier every wave's is, and nobody reads this
     // stage's buffer any more.
-    __builtin_amdgcn_s_waitcnt(wait_until((BUFFERS - 2) * ASKED));
+    __builtin_amdgcn_s_waitcnt(wait_until(BUFFERS > 2 ? (BUFFERS - 2) * ASKED : 0));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
@@ -417,7 +417,24 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     weave(std::integral_constant<int, HALF>());
     s = s_next;
   };
-  if (first < last) {
+  if constexpr (BUFFERS == 1) {  // other workgroups of the compute unit have work while this one waits
+    for (int32_t st = first; st < last; ++st) {
+#pragma unroll
+      for (int part = 0; part < 4; ++part) fetch(st, part, buffer_a);
+      __builtin_amdgcn_s_waitcnt(wait_until(0));
+      __syncthreads();
+      load_scales(buffer_a, st, s);
+      load(buffer_a, 0, a);
+      multiply_all(a, s, std::integral_constant<int, 0>());
+      load(buffer_a, 1, a);
+      multiply_all(a, s, std::integral_constant<int, 1>());
+      load(buffer_a, 2, a);
+      multiply_all(a, s, std::integral_constant<int, 2>());
+      load(buffer_a, 3, a);
+      multiply_all(a, s, std::integral_constant<int, 3>());
+      __syncthreads();
+    }
+  } else if (first < last) {
     auto fetch_half = [&](int32_t st, int half, uint8_t *buffer) {
       fetch(st, 2 * half, buffer);
       fetch(st, 2 * half + 1, buffer);
@@ -433,7 +450,7 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     } else {
       fetch_half(first + 1, 0, buffer_b);
     }
-    __builtin_amdgcn_s_waitcnt(wait_until((BUFFERS - 2) * ASKED + HALF));
+    __builtin_amdgcn_s_waitcnt(wait_until(BUFFERS > 2 ? (BUFFERS - 2) * ASKED + HALF : HALF));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     load(buffer_a, 0, a);
@@ -441,11 +458,17 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
     // Rounds of all buffers, then the rest: with no path on which a stage of a round is skipped the compiler
     // sees which requests are still under way for which buffer, and waits for no others.
     int32_t st = first;
-    if constexpr (BUFFERS == 2) {  // the last one may be of blocks past the last, which add nothing
+    if constexpr (MF * NF == 16) {  // no registers for a stage more: the last one may be of blocks past the last
       for (; st < last; st += 2) {
         stage(st, buffer_a, buffer_b, buffer_b);
         stage(st + 1, buffer_b, buffer_a, buffer_a);
       }
+    } else if constexpr (BUFFERS == 2) {
+      for (; st + 2 <= last; st += 2) {
+        stage(st, buffer_a, buffer_b, buffer_b);
+        stage(st + 1, buffer_b, buffer_a, buffer_a);
+      }
+      if (st < last) stage(st, buffer_a, buffer_b, buffer_b);
     } else {
       for (; st + 4 <= last; st += 4) {
         stage(st, buffer_a, buffer_b, buffer_d);
@@ -466,21 +489,25 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 
-  if (bias) {
+  if (bias) {  // by way of shared memory: every lane needs 16 of each 32 columns'
+    if (t < BN) shared_bias[t] = n0 + t < n ? bias[n0 + t] : 0.0f;
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < NF; ++j)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const int64_t c = n0 + (wn * NF + j) * 32 + (q >> 2) * 8 + g * 4 + (q & 3);
-        const float v = bias[c < n ? c : n - 1];
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(shared_bias + (wn * NF + j) * 32 + q * 8 + g * 4);
 #pragma unroll
-        for (int i = 0; i < MF; ++i) acc[i][j][q] += v;
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+          for (int p = 0; p < 4; ++p) acc[i][j][4 * q + p] += v[p];
         __builtin_amdgcn_sched_barrier(0);  // one at a time: the accumulators leave few registers
       }
   }
   // Results in Y's type, 32 rows of the wave's columns: a lane leaves four neighbours of its row at a time and
   // takes 16 bytes of a row for the memory.
-  T *mine = reinterpret_cast<T *>((wave < 2 ? buffer_a : buffer_b) + wave % 2 * (32 * PITCH * sizeof(T)));
+  T *mine = reinterpret_cast<T *>(BUFFERS == 1 ? buffer_a + wave * (32 * PITCH * sizeof(T))
+                                               : (wave < 2 ? buffer_a : buffer_b) + wave % 2 * (32 * PITCH * sizeof(T)));
   constexpr int V = 16 / sizeof(T), LANES = NF * 32 / V, STEP = 64 / LANES;  // columns of a lane, lanes of a row
   const int vr = lane / LANES, vc = lane % LANES * V;
   const int64_t c = n0 + wn * NF * 32 + vc;
@@ -591,7 +618,7 @@ struct Call {
   float *parts;  // workspace of a split sum
 };
 
-enum Form { kTile256, kTile128, kTile128Deep, kRows32, kRows32Short, kRows16, kRows16Short };
+enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows32Short, kRows16, kRows16Short };
 struct Plan {
   Form form;
   int32_t splits, split_stages;
@@ -604,18 +631,20 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
   return (rows - parts) / bm + parts;
 }
 
-// Measured in us, 16-bit results, launches in a row (256 compute units; "s": 128 x 128 tiles with the sum in so
-// many parts, joined by a second launch):
+// Measured in us, 16-bit results, launches in a row (256 compute units; 128 x 128 with the better number of
+// buffers; "s": such tiles with the sum in so many parts, joined by a second launch):
 //   rows x columns x k      256x256   128x128  32x32  16x16   s4    s16   s64   s128
-//   8192 x 8192 x 8192          243       319
-//   4096 x 4096 x 4096           38        43
-//   2048 x 2048 x 2048           18       8.8
-//   1000 x 1000 x 1000           17       6.8   13.9   15.8
-//   256 x 4096 x 4096            25        11     24     37    20    26
+//   8192 x 8192 x 8192          243       300   2234
+//   8192 x 8192 x 512            50        41    288    298
+//   4096 x 4096 x 4096           37        42    282    559
+//   2048 x 2048 x 2048           17       9.5     41     73
+//   1000 x 1000 x 1000           15       6.7    9.2     12
+//   256 x 4096 x 4096            23        10     20     37    20    26
 //   64 x 4096 x 4096             25        11    7.1     11    12    22
 //   512 x 512 x 4096             24        11    7.2     11    11    18
 //   1 x 4096 x 4096              23        10    5.2    3.7     9    12
-//   262144 x 47 x 64             65        29    167    100
+//   262144 x 128 x 128           59        19    120    106
+//   1000000 x 20 x 128          235        64    172    119
 //   512 x 512 x 32768           147        55     39     72    21    19    43
 //   64 x 64 x 65536             273       103     71     37    33    15    11     11
 //   256 x 128 x 262144         1110       406    278    142   108    34    19     20
@@ -624,11 +653,12 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
 //
 // Rows sorted by expert, us, launches in a row (rows of X, experts of each, experts, columns x k):
 //                              256x256   128x128  32x32  16x16
-//   4096, 2, 16, 4096 x 4096        113       119    634   1176
-//   1024, 2, 16, 4096 x 4096         66        49    175    307
-//   128, 8, 64, 1024 x 2048          39        24     29     32
-//   64, 8, 64, 1024 x 2048           40        23     27     23
-//   16, 8, 64, 1024 x 2048           38        23     24     18
+//   4096, 2, 16, 4096 x 4096        114       115    632   1180
+//   1024, 2, 16, 4096 x 4096         67        50    174    307
+//   64, 2, 16, 4096 x 4096           59        31     37     35
+//   16, 2, 16, 4096 x 4096           58        29     32     28
+//   64, 8, 64, 1024 x 2048           39        19     26     22
+//   16, 8, 64, 1024 x 2048           38        18     22     17
 Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) {
   const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
   // of rows sorted by expert the tiles there will be: half a tile too many for each expert
@@ -637,9 +667,9 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
            ceil_div(n, bn);
   };
   const auto whole = [&](Form f) { return Plan{f, 1, (int32_t)stages}; };
-  const bool few = experts > 0 && rows <= 8 * (int64_t)experts;  // of each expert
+  const bool few = experts > 0 && rows <= 3 * (int64_t)experts;  // of each expert
   if (near && !few) {
-    if (4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
+    if (stages >= 8 && 4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
     const int64_t t = tiles(128, 128);
     const bool wide = rows > 64 && n > 64 && t >= cus / 8, many = t >= cus / 2;
     if (experts == 0 && !many && stages >= (wide ? 32 : 64)) {
@@ -650,9 +680,12 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
         return Plan{kTile128Deep, (int32_t)ceil_div(stages, each), (int32_t)each};
       }
     }
-    // four buffers, and with them one workgroup a compute unit, where the sum is long and there are no more
-    // tiles: 2048 x 2048 x 8192 takes 23 us so and 28 with two
-    if (wide || many) return whole(t <= cus && stages >= 24 ? kTile128Deep : kTile128);
+    // Buffers for 128 x 128: one, and three workgroups a compute unit, where there are more tiles than units or
+    // the sum is short (3000 x 3000 x 3000 takes 27, 31 and 31 us with one, two and four, 533036 x 44 x 26 40,
+    // 54 and 105); four where the sum is long (2048 x 2048 x 8192 28 with two, 23 with four), else two (2048
+    // cubed 11.2, 9.5 and 9.7).
+    if (wide || many)
+      return whole(t > cus || stages <= 2 ? kTile128Short : stages >= 24 ? kTile128Deep : kTile128);
   }
   // Four waves share the sum where it is short or workgroups come in numbers, else eight: 1500 x 1500 x 1500
   // takes 23 and 33 us in tiles of 16 x 16, 1 x 4096 x 4096 3.9 and 3.7.
@@ -703,6 +736,7 @@ int product_as(const Call &c, const Plan &p, void *Y, hipStream_t s) {
     case kTile256: return tile_launch<T, 256, 256, 2, EXPERTS>(c, p, y, s);
     case kTile128: return tile_launch<T, 128, 128, 2, EXPERTS>(c, p, y, s);
     case kTile128Deep: return tile_launch<T, 128, 128, 4, EXPERTS>(c, p, y, s);
+    case kTile128Short: return tile_launch<T, 128, 128, 1, EXPERTS>(c, p, y, s);
     case kRows32: return rows_launch<T, 2, 2, 8, EXPERTS>(c, y, s);
     case kRows32Short: return rows_launch<T, 2, 2, 4, EXPERTS>(c, y, s);
     case kRows16: return rows_launch<T, 1, 1, 8, EXPERTS>(c, y, s);

@@ -22,9 +22,13 @@ SIDE = int((0.75 * CUS) ** 0.5) + 1  # SIDE * SIDE large tiles are enough for th
 
 # rows, columns, results: forms from the largest tiles to the smallest, odd and whole numbers of stages
 FORMS = {
-    "large": (256 * SIDE, 512, 256 * SIDE),
-    "large_odd": (256 * SIDE - 57, 130, 256 * SIDE - 13),
-    "large_three": (256 * SIDE - 1, 600, 256 * SIDE - 255 + 200),
+    "large": (256 * SIDE, 2048, 256 * SIDE),
+    "large_odd": (256 * SIDE - 57, 2100, 256 * SIDE - 13),
+    "large_ten": (256 * SIDE - 1, 2500, 256 * SIDE - 255 + 200),
+    "many": (256 * SIDE, 512, 256 * SIDE),
+    "many_odd": (256 * SIDE - 57, 130, 256 * SIDE - 13),
+    "many_three": (128 * CUS + 5, 600, 70),
+    "many_narrow": (64 * CUS + 65, 33, 5),
     "middle": (128 * 8 + 1, 1000, 128 * 8 - 3),
     "middle_one_stage": (128 * 9, 32, 128 * 9),
     "middle_deep": (128 * 11 - 7, 256 * 25 + 40, 128 * 12 - 60),
@@ -71,11 +75,14 @@ def test_forms_are_exact_and_keep_nan(form):
 
 
 EXPERTS = {
-    "large": (128 * SIDE, 2, 3, 520, 256 * SIDE - 9),
-    "large_one": (256 * SIDE, 1, 1, 300, 256 * SIDE),
+    "large": (128 * SIDE, 2, 3, 2060, 256 * SIDE - 9),
+    "large_one": (256 * SIDE, 1, 1, 2048, 256 * SIDE),
+    "many": (128 * SIDE, 2, 3, 520, 256 * SIDE - 9),
+    "many_short": (900, 2, 7, 200, 2000),
     "middle": (700, 2, 5, 257, 600),
     "middle_deep": (500, 1, 4, 256 * 24 + 1, 700),
     "few_of_each": (30, 4, 40, 700, 300),
+    "few_of_each_many": (40, 4, 60, 90, 1100),
     "thirty_two": (300, 1, 2, 1100, 130),
     "sixteen": (3, 2, 9, 900, 70),
 }
