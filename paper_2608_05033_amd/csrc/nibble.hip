@@ -15,16 +15,31 @@ using namespace nibble;
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;  // row groups in flight per lane group
 
-// A group of 128 / V lanes takes one row's group of 128 columns: V neighbouring
-// columns per lane (16 bytes), the largest bits of each block over its 32 / V
-// lanes, V codes per lane back.  COLS: consecutive elements of a row lie together
-// (else any strides, each lane's elements read one by one).
-template <typename T, bool COLS>
+// The first `left` of V elements; zero for the others, which are read too where the
+// next row lies behind them.
+template <typename T, int V>
+__device__ inline void load_end(const T *p, int left, bool next_row, float (&v)[V]) {
+  if (left >= V || (left > 0 && next_row)) {
+    load_span(p, v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i < left ? v[i] : 0.0f;
+  } else {
+    load_part(p, left, v);
+  }
+}
+
+// A group of WIDE / V lanes takes one row's group of 128 columns, of which there are
+// at most WIDE: V neighbouring columns per lane (16 bytes), the largest bits of each
+// block over its 32 / V lanes, V codes per lane back.  Bound by the bytes, four groups
+// in flight: 262144 x 128 fp32 take 23 us, 6.6 TB/s of bytes that the 256 MB Infinity
+// Cache partly serves.  COLS: consecutive elements of a row lie together (else any
+// strides, each lane's elements read one by one).
+template <typename T, int WIDE, bool COLS>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ x, int64_t row_stride,
                                                           int64_t col_stride, int64_t rows, int32_t cols, int32_t ng,
                                                           uint8_t *__restrict__ codes, int64_t ld,
                                                           uint8_t *__restrict__ scales) {
-  constexpr int V = 16 / sizeof(T), LANES = kGroup / V, GROUPS = kThreads / LANES, SHARE = kCols / V;
+  constexpr int V = 16 / sizeof(T), LANES = WIDE / V, GROUPS = kThreads / LANES, SHARE = kCols / V;
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   const int64_t first = (int64_t)workgroup() * (GROUPS * kUnroll);
   const int64_t r0 = first / ng;
@@ -40,11 +55,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ 
     const int32_t c = grp[u] * kGroup + lane * V;
     const int left = row[u] < rows ? cols - c : 0;
     if constexpr (COLS) {
-      const T *p = x + row[u] * row_stride + c;
-      if (left >= V)
-        load_span(p, v[u]);
-      else
-        load_part(p, left, v[u]);
+      load_end(x + row[u] * row_stride + c, left, row[u] + 1 < rows && row_stride >= V, v[u]);
     } else {
       const T *p = x + row[u] * row_stride + c * col_stride;
 #pragma unroll
@@ -77,7 +88,15 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ 
       else
         *reinterpret_cast<uint32_t *>(p) = w;
     }
-    if (lane % SHARE == 0) scales[((int64_t)grp[u] * rows + row[u]) * 4 + lane / SHARE] = (uint8_t)s;
+    if (lane % SHARE == 0) {
+      uint8_t *p = scales + ((int64_t)grp[u] * rows + row[u]) * 4;
+      if constexpr (WIDE == 32) {
+        *reinterpret_cast<uint32_t *>(p) = s | 0x7f7f7f00u;
+      } else {
+        p[lane / SHARE] = (uint8_t)s;
+        if constexpr (WIDE == 64) p[2 + lane / SHARE] = 127;
+      }
+    }
   }
 }
 
@@ -163,12 +182,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
 #pragma unroll
   for (int u = 0; u < STEPS; ++u) {
     const int64_t row = row0 + u * AT_ONCE + down;
-    const int left = row < rows ? cols - c : 0;
-    const T *p = x + row * row_stride + c;
-    if (left >= V)
-      load_span(p, v[u]);
-    else
-      load_part(p, left, v[u]);
+    load_end(x + row * row_stride + c, row < rows ? cols - c : 0, row + 1 < rows && row_stride >= V, v[u]);
   }
 #pragma unroll
   for (int u = 0; u < STEPS; ++u) {
@@ -243,8 +257,10 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
 }
 
 // Lanes along a row, eight codes each.  Bound by the bytes written: 262144 x 128 to
-// bf16 take 21 us, 4.1 TB/s.
-template <typename T>
+// bf16 take 21 us, 4.1 TB/s.  END 1: a row's last lane begins eight columns before its
+// end, so that all write whole spans; its codes lie in two words and may lie in two
+// blocks.  END 2: rows of fewer than eight columns.
+template <typename T, int END>
 __global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__restrict__ codes, int64_t ld,
                                                             const uint8_t *__restrict__ scales, int64_t rows,
                                                             int32_t cols, int32_t octs, T *__restrict__ y,
@@ -252,7 +268,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__res
   const int64_t first = (int64_t)workgroup() * (kThreads * kUnroll);
   const int64_t r0 = first / octs;
   const uint32_t q0 = (uint32_t)(first - r0 * octs);
-  uint32_t w[kUnroll], s[kUnroll];
+  uint32_t w[kUnroll], w1[kUnroll], s[kUnroll], s1[kUnroll];
   int64_t row[kUnroll];
   int32_t col[kUnroll];
 #pragma unroll
@@ -260,30 +276,52 @@ __global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__res
     const uint32_t at = q0 + u * kThreads + threadIdx.x;
     row[u] = r0 + at / (uint32_t)octs;
     col[u] = (int32_t)(at % (uint32_t)octs) * 8;
-    w[u] = 0;
-    s[u] = 127;
+    if (END == 1 && col[u] > cols - 8) col[u] = cols - 8;
+    w[u] = w1[u] = 0;
+    s[u] = s1[u] = 127;
     if (row[u] < rows) {
-      w[u] = *reinterpret_cast<const uint32_t *>(codes + row[u] * ld + col[u] / 2);
-      s[u] = scales[((int64_t)(col[u] / kGroup) * rows + row[u]) * 4 + col[u] / kCols % 4];
+      const uint8_t *p = codes + row[u] * ld;
+      const auto scale_at = [&](int32_t c) {
+        return (uint32_t)scales[((int64_t)(c / kGroup) * rows + row[u]) * 4 + c / kCols % 4];
+      };
+      w[u] = *reinterpret_cast<const uint32_t *>(p + col[u] / 8 * 4);
+      s[u] = scale_at(col[u]);
+      if constexpr (END == 1) {
+        w1[u] = *reinterpret_cast<const uint32_t *>(p + (col[u] + 7) / 8 * 4);
+        s1[u] = scale_at(col[u] + 7);
+      }
     }
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
     if (row[u] >= rows) continue;
-    const float scale = s[u] == kNanScale ? __uint_as_float(0x7fc00000u) : scale_value(s[u]);
+    const auto value_of = [](uint32_t b) {
+      return b == kNanScale ? __uint_as_float(0x7fc00000u) : scale_value(b);
+    };
+    const float scale = value_of(s[u]);
+    uint32_t codes8 = w[u];
+    if constexpr (END == 1)
+      codes8 = (uint32_t)((((uint64_t)w1[u] << 32) | w[u]) >> (4 * (col[u] & 7)));
     float v[8];
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 0);
-    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 1);
-    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 2);
-    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.0f, 3);
-    v[0] = a[0] * scale, v[1] = a[1] * scale, v[2] = b[0] * scale, v[3] = b[1] * scale;
-    v[4] = c[0] * scale, v[5] = c[1] * scale, v[6] = d[0] * scale, v[7] = d[1] * scale;
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes8, 1.0f, 0);
+    const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes8, 1.0f, 1);
+    const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes8, 1.0f, 2);
+    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes8, 1.0f, 3);
+    v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
+    if constexpr (END == 1) {
+      const float scale1 = value_of(s1[u]);
+      const int turn = kCols - (col[u] & (kCols - 1));  // the first of the next block
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= i < turn ? scale : scale1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= scale;
+    }
     T *p = y + row[u] * row_stride + col[u];
-    const int left = cols - col[u];
-    if (left >= 8)
-      store_span(p, v);
+    if constexpr (END == 2)
+      store_part(p, cols, v);
     else
-      store_part(p, left, v);
+      store_span(p, v);
   }
 }
 
@@ -292,7 +330,8 @@ int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nib
   const T *p = static_cast<const T *>(x);
   const int64_t ng = groups_of(out->cols);
   const bool across = col_stride != 1 && row_stride < col_stride;
-  constexpr int per_wg = kThreads / (kGroup * (int)sizeof(T) / 16) * kUnroll;
+  const int wide = out->cols <= 32 ? 32 : out->cols <= 64 ? 64 : 128;
+  const int64_t per_wg = kThreads / (wide * (int)sizeof(T) / 16) * kUnroll;
   const int64_t wgs = across ? ceil_div(out->rows, 64) * ng : ceil_div(out->rows * ng, per_wg);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
   if (across) {
@@ -300,7 +339,12 @@ int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nib
                        out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, (uint32_t)wgs);
     return launched();
   }
-  auto *kernel = col_stride == 1 ? k_nibble_pack<T, true> : k_nibble_pack<T, false>;
+  auto *kernel = col_stride != 1 ? (wide == 32   ? k_nibble_pack<T, 32, false>
+                                    : wide == 64 ? k_nibble_pack<T, 64, false>
+                                                 : k_nibble_pack<T, 128, false>)
+                                 : (wide == 32   ? k_nibble_pack<T, 32, true>
+                                    : wide == 64 ? k_nibble_pack<T, 64, true>
+                                                 : k_nibble_pack<T, 128, true>);
   hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, p, row_stride, col_stride, out->rows,
                      (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales);
   return launched();
@@ -320,7 +364,8 @@ template <typename T>
 int unpack_as(const sd_nibble_t *x, void *y, int64_t row_stride, hipStream_t s) {
   const int64_t octs = ceil_div(x->cols, 8), wgs = ceil_div(x->rows * octs, kThreads * kUnroll);
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL(k_nibble_unpack<T>, grid_of(wgs), dim3(kThreads), 0, s, x->codes, x->ld, x->scales, x->rows,
+  auto *kernel = x->cols % 8 == 0 ? k_nibble_unpack<T, 0> : x->cols > 8 ? k_nibble_unpack<T, 1> : k_nibble_unpack<T, 2>;
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, x->codes, x->ld, x->scales, x->rows,
                      (int32_t)x->cols, (int32_t)octs, static_cast<T *>(y), row_stride);
   return launched();
 }

@@ -67,6 +67,30 @@ def test_pack_bit_for_bit(rows, cols, dtype):
         assert torch.equal(dense.unpack4(p, TYPES[out]).cpu(), torch.from_numpy(of(p)).to(torch.float32).to(TYPES[out]))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(4100, 1), (1029, 2), (515, 7), (300, 8), (700, 9), (260, 16), (131, 34), (259, 39),
+                                       (65, 50), (140, 63), (70, 64), (40, 66), (33, 97), (50, 127), (20, 135)])
+def test_pack_narrow(rows, cols, dtype):
+    """Rows that end inside a lane's 16 bytes, in tables of their own, in parts of
+    wider ones whose other columns hold NaN, and rows that lie on top of each other."""
+    print(f"case narrow pack4 {rows}x{cols} {dtype}", flush=True)
+    t, x = table(activations(rows, cols, rows * 1000 + cols), dtype)
+    wide = torch.full((rows, cols + 3), float("nan"), dtype=t.dtype, device="cuda")
+    wide[:, 1:cols + 1] = t
+    for part in (t, wide[:, 1:cols + 1]):
+        p = dense.pack4(part)
+        check_packed(p, x)
+        for out in TYPES.values():
+            assert torch.equal(dense.unpack4(p, out).cpu(), torch.from_numpy(of(p)).to(torch.float32).to(out))
+        for p, want in zip(dense.pack4_both(part), (x, np.ascontiguousarray(x.T))):
+            check_packed(p, want)
+    flat = x.reshape(-1)
+    for step in (1, 3, 5):
+        if rows > 1 and (rows - 1) * step + cols <= flat.size:
+            over = t.as_strided((rows, cols), (step, 1))
+            check_packed(dense.pack4(over), flat[np.arange(rows)[:, None] * step + np.arange(cols)])
+
+
 def test_pack_edges_of_the_range():
     """Ties, zeros of both signs, values at and past a power of two times 6, the ends
     of the fp32 range, subnormal numbers, infinities and NaN; along rows and across."""
