@@ -218,8 +218,9 @@ bool few(int64_t entries, int32_t experts) { return entries <= kOneGroup && expe
 // ------------------------------------------------------- rows to and back ---
 // A team of LANES lanes for each row t; 16 bytes of it a lane and step.  Entries
 // are taken KB at a time, whose rows are read (or written) together; with k <= KB
-// their places are read once.  A row's last step begins V columns before its end
-// and does some columns twice, with the same results (WHOLE: rows have V columns).
+// their places are read once.  A step takes V columns, the 16 bytes or, of shorter
+// rows, the most that they have; a row's last step begins V columns before its end and
+// does some columns twice, with the same results.
 constexpr int kThreads = 256;
 
 // The team's row and place in it, and the places of entries (t, j0 ..), -1 for none.
@@ -240,30 +241,14 @@ struct Places {
     }
   }
 };
-template <bool WHOLE, int V, typename T>
-__device__ inline void read_columns(const T *p, int left, float (&v)[V]) {
-  if constexpr (WHOLE)
-    load_span(p, v);
-  else
-    load_part(p, left, v);
-}
-template <bool WHOLE, int V, typename T>
-__device__ inline void write_columns(T *p, int left, const float (&v)[V]) {
-  if constexpr (WHOLE)
-    store_span(p, v);
-  else
-    store_part(p, left, v);
-}
-
 // y[place[t, j]] = x[t]; rows of y that no entry is sorted to (those behind the
 // last expert's) become zeros.  Bound by the bytes, each row of x read once: 2^18 x
 // 128 fp32 to two experts each take 70 us, 5.8 TB/s with what the caches serve.
-template <typename T, int LANES, int KB, bool WHOLE>
+template <typename T, int LANES, int KB, int V>
 __global__ __launch_bounds__(kThreads) void k_dispatch(const T *__restrict__ x, int64_t x_stride, int64_t rows,
                                                        int32_t k, int32_t cols, const int32_t *__restrict__ place,
                                                        const int32_t *__restrict__ source, T *__restrict__ y,
                                                        int64_t y_stride) {
-  constexpr int V = 16 / sizeof(T);
   const Team<LANES> team;
   const int64_t t = team.t;
   if (t >= rows) return;
@@ -277,19 +262,19 @@ __global__ __launch_bounds__(kThreads) void k_dispatch(const T *__restrict__ x, 
   };
   if (k <= KB) read(0);
   for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
-    const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
+    const int32_t c = c0 > cols - V ? cols - V : c0;
     float v[V];
     const float none[V] = {};
-    read_columns<WHOLE>(x + t * x_stride + c, cols - c, v);
+    load_span(x + t * x_stride + c, v);
     for (int32_t j0 = 0; j0 < k; j0 += KB) {
       if (k > KB) read(j0);
 #pragma unroll
       for (int u = 0; u < KB; ++u)
-        if (p.at[u] >= 0) write_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v);
+        if (p.at[u] >= 0) store_span(y + p.at[u] * y_stride + c, v);
       if (clear) {
 #pragma unroll
         for (int u = 0; u < KB; ++u)
-          if (clear >> u & 1) write_columns<WHOLE>(y + (t * k + j0 + u) * y_stride + c, cols - c, none);
+          if (clear >> u & 1) store_span(y + (t * k + j0 + u) * y_stride + c, none);
       }
     }
   }
@@ -297,12 +282,11 @@ __global__ __launch_bounds__(kThreads) void k_dispatch(const T *__restrict__ x, 
 
 // out[t] = sum over j, in this order, of weights[t, j] y[place[t, j]].  Bound by the
 // bytes: 71 to 87 us at those sizes, 4.6 to 5.7 TB/s.
-template <typename T, int LANES, int KB, bool WHOLE>
+template <typename T, int LANES, int KB, int V>
 __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, int64_t y_stride, int64_t rows,
                                                       int32_t k, int32_t cols, const int32_t *__restrict__ place,
                                                       const float *__restrict__ weights, T *__restrict__ out,
                                                       int64_t out_stride) {
-  constexpr int V = 16 / sizeof(T);
   const Team<LANES> team;
   const int64_t t = team.t;
   if (t >= rows) return;
@@ -315,14 +299,14 @@ __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, i
   };
   if (k <= KB) read(0);
   for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
-    const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
+    const int32_t c = c0 > cols - V ? cols - V : c0;
     float sum[V] = {};
     for (int32_t j0 = 0; j0 < k; j0 += KB) {
       if (k > KB) read(j0);
       float v[KB][V];
 #pragma unroll
       for (int u = 0; u < KB; ++u)
-        if (p.at[u] >= 0) read_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v[u]);
+        if (p.at[u] >= 0) load_span(y + p.at[u] * y_stride + c, v[u]);
 #pragma unroll
       for (int u = 0; u < KB; ++u)
         if (p.at[u] >= 0) {
@@ -330,14 +314,14 @@ __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, i
           for (int i = 0; i < V; ++i) sum[i] = fmaf(w[u], v[u][i], sum[i]);
         }
     }
-    write_columns<WHOLE>(out + t * out_stride + c, cols - c, sum);
+    store_span(out + t * out_stride + c, sum);
   }
 }
 
 // dy[place[t, j]] = weights[t, j] dout[t], zeros in rows that no entry is sorted
 // to; dweights[t, j] = the dot product of dout[t] and y[place[t, j]].  One reading of
 // dout and y serves both: 120 us at those sizes, 5.6 TB/s.
-template <typename T, int LANES, int KB, bool WHOLE>
+template <typename T, int LANES, int KB, int V>
 __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restrict__ dout, int64_t dout_stride,
                                                                const T *__restrict__ y, int64_t y_stride, int64_t rows,
                                                                int32_t k, int32_t cols,
@@ -345,7 +329,6 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
                                                                const int32_t *__restrict__ source,
                                                                const float *__restrict__ weights, T *__restrict__ dy,
                                                                int64_t dy_stride, float *__restrict__ dweights) {
-  constexpr int V = 16 / sizeof(T);
   const Team<LANES> team;
   const int64_t t = team.t;
   if (t >= rows) return;
@@ -360,19 +343,19 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
       clear |= (dy && j0 + u < k && source[t * k + j0 + u] < 0 ? 1u : 0u) << u;
     }
     for (int32_t c0 = team.lane * V; c0 < cols; c0 += LANES * V) {
-      const int32_t c = WHOLE && c0 > cols - V ? cols - V : c0;
+      const int32_t c = c0 > cols - V ? cols - V : c0;
       float d[V], v[KB][V];
-      read_columns<WHOLE>(dout + t * dout_stride + c, cols - c, d);
+      load_span(dout + t * dout_stride + c, d);
       if (dweights) {
 #pragma unroll
         for (int u = 0; u < KB; ++u)
-          if (p.at[u] >= 0) read_columns<WHOLE>(y + p.at[u] * y_stride + c, cols - c, v[u]);
+          if (p.at[u] >= 0) load_span(y + p.at[u] * y_stride + c, v[u]);
 #pragma unroll
         for (int u = 0; u < KB; ++u)
           if (p.at[u] >= 0) {
 #pragma unroll
             for (int i = 0; i < V; ++i)  // columns that the step before has done count once
-              if (!WHOLE || c + i >= c0) dot[u] = fmaf(d[i], v[u][i], dot[u]);
+              if (c + i >= c0) dot[u] = fmaf(d[i], v[u][i], dot[u]);
           }
       }
       if (dy) {
@@ -382,13 +365,13 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
             float o[V];
 #pragma unroll
             for (int i = 0; i < V; ++i) o[i] = w[u] * d[i];
-            write_columns<WHOLE>(dy + p.at[u] * dy_stride + c, cols - c, o);
+            store_span(dy + p.at[u] * dy_stride + c, o);
           }
         if (clear) {
           const float none[V] = {};
 #pragma unroll
           for (int u = 0; u < KB; ++u)
-            if (clear >> u & 1) write_columns<WHOLE>(dy + (t * k + j0 + u) * dy_stride + c, cols - c, none);
+            if (clear >> u & 1) store_span(dy + (t * k + j0 + u) * dy_stride + c, none);
         }
       }
     }
@@ -403,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
   }
 }
 
-// Calls f(lanes, entries at a time, whether rows have 16 bytes) for rows of `cols`
+// Calls f(lanes, entries at a time, columns of a step) for rows of `cols`
 // elements: lanes for a whole row up to 32, then 64.  Measured in us (to the experts, back,
 // gradients):
 //   rows, entries of each, columns     8 lanes       16           32           64
@@ -415,29 +398,29 @@ template <int MOST, typename T, typename F>
 int with_shape(int64_t cols, int32_t k, const F &f) {
   constexpr int V = 16 / sizeof(T);
   const int64_t steps = ceil_div(cols, V);
-  const int lanes = steps > 48 ? 64 : steps > 16 ? 32 : steps > 8 ? 16 : steps > 2 ? 8 : 2;
-  const auto entries = [&](auto l, auto whole) {
-    if (k == 1) return f(l, std::integral_constant<int, 1>(), whole);
-    if (k == 2) return f(l, std::integral_constant<int, 2>(), whole);
-    if (k <= 4 || MOST == 4) return f(l, std::integral_constant<int, 4>(), whole);
-    return f(l, std::integral_constant<int, MOST>(), whole);
+  const auto entries = [&](auto l, auto v) {
+    if (k == 1) return f(l, std::integral_constant<int, 1>(), v);
+    if (k == 2) return f(l, std::integral_constant<int, 2>(), v);
+    if (k <= 4 || MOST == 4) return f(l, std::integral_constant<int, 4>(), v);
+    return f(l, std::integral_constant<int, MOST>(), v);
   };
-  if (cols < V) return entries(std::integral_constant<int, 2>(), std::false_type());
-  switch (lanes) {
-    case 64: return entries(std::integral_constant<int, 64>(), std::true_type());
-    case 32: return entries(std::integral_constant<int, 32>(), std::true_type());
-    case 16: return entries(std::integral_constant<int, 16>(), std::true_type());
-    case 8: return entries(std::integral_constant<int, 8>(), std::true_type());
-    default: return entries(std::integral_constant<int, 2>(), std::true_type());
-  }
+  constexpr std::integral_constant<int, V> whole{};
+  if (steps > 48) return entries(std::integral_constant<int, 64>(), whole);
+  if (steps > 16) return entries(std::integral_constant<int, 32>(), whole);
+  if (steps > 8) return entries(std::integral_constant<int, 16>(), whole);
+  if (steps > 2) return entries(std::integral_constant<int, 8>(), whole);
+  if (cols >= V) return entries(std::integral_constant<int, 2>(), whole);
+  if (V == 8 && cols >= 4) return entries(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+  if (cols >= 2) return entries(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
+  return entries(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
 }
 
 template <typename T>
 int dispatch_as(const sd_route_t *r, const void *x, int64_t cols, int64_t x_stride, void *y, int64_t y_stride,
                 hipStream_t s) {
-  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto v) {
     constexpr int L = decltype(lanes)::value;
-    hipLaunchKernelGGL((k_dispatch<T, L, decltype(kb)::value, decltype(whole)::value>),
+    hipLaunchKernelGGL((k_dispatch<T, L, decltype(kb)::value, decltype(v)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(x),
                        x_stride, r->rows, r->k, (int32_t)cols, r->place, r->source, static_cast<T *>(y), y_stride);
     return launched();
@@ -446,9 +429,9 @@ int dispatch_as(const sd_route_t *r, const void *x, int64_t cols, int64_t x_stri
 template <typename T>
 int combine_as(const sd_route_t *r, const void *y, int64_t cols, int64_t y_stride, const float *weights, void *out,
                int64_t out_stride, hipStream_t s) {
-  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<8, T>(cols, r->k, [&](auto lanes, auto kb, auto v) {
     constexpr int L = decltype(lanes)::value;
-    hipLaunchKernelGGL((k_combine<T, L, decltype(kb)::value, decltype(whole)::value>),
+    hipLaunchKernelGGL((k_combine<T, L, decltype(kb)::value, decltype(v)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(y),
                        y_stride, r->rows, r->k, (int32_t)cols, r->place, weights, static_cast<T *>(out), out_stride);
     return launched();
@@ -457,9 +440,9 @@ int combine_as(const sd_route_t *r, const void *y, int64_t cols, int64_t y_strid
 template <typename T>
 int backward_as(const sd_route_t *r, const void *dout, int64_t cols, int64_t dout_stride, const void *y,
                 int64_t y_stride, const float *weights, void *dy, int64_t dy_stride, float *dweights, hipStream_t s) {
-  return with_shape<4, T>(cols, r->k, [&](auto lanes, auto kb, auto whole) {
+  return with_shape<4, T>(cols, r->k, [&](auto lanes, auto kb, auto v) {
     constexpr int L = decltype(lanes)::value;
-    hipLaunchKernelGGL((k_combine_backward<T, L, decltype(kb)::value, decltype(whole)::value>),
+    hipLaunchKernelGGL((k_combine_backward<T, L, decltype(kb)::value, decltype(v)::value>),
                        grid_of(ceil_div(r->rows, kThreads / L)), dim3(kThreads), 0, s, static_cast<const T *>(dout),
                        dout_stride, static_cast<const T *>(y), y_stride, r->rows, r->k, (int32_t)cols, r->place,
                        r->source, weights, static_cast<T *>(dy), dy_stride, dweights);

@@ -75,7 +75,8 @@ def test_route_of_no_rows():
 
 # ------------------------------------------------------- to experts and back ---
 CASES = [(1, 1, 1, 1), (1, 8, 64, 100), (37, 2, 16, 64), (50, 9, 12, 33), (65, 3, 7, 129), (300, 4, 60, 601),
-         (7, 2, 3, 3000), (500, 17, 5, 5)]
+         (7, 2, 3, 3000), (500, 17, 5, 5), (900, 1, 3, 1), (400, 7, 20, 2), (90, 3, 5, 3), (270, 2, 4, 4), (131, 6, 9, 6),
+         (77, 2, 4, 7)]
 
 
 def weights_of(rows, k, seed):
