@@ -118,27 +118,29 @@ __device__ inline void clear_rows(T *Y, int64_t stride, int64_t m0, int64_t m1, 
 // Bound by the latency of the loads where there are few tiles: 1 x 4096 x 4096 takes
 // 3.7 us (2.4 TB/s of W), the launch itself 2; by W's bytes where there are many: 16
 // rows through 2 of 16 experts of 4096 x 4096 take 28, 5.1 TB/s.
-template <typename T, int MF, int NF, int KW, bool EXPERTS>
+// ALONG: the waves take a tile each, KW neighbouring ones, and the whole sum.
+template <typename T, int MF, int NF, int KW, bool EXPERTS, bool ALONG>
 __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, Sorted sorted,
                                                          const float *__restrict__ bias, T *__restrict__ Y,
                                                          int64_t stride, int64_t rows, int64_t n, int32_t blocks,
                                                          int32_t ng, int32_t nt) {
-  __shared__ f32x4 part[KW][MF * NF][64];
+  __shared__ f32x4 part[ALONG ? 1 : KW][MF * NF][64];
+  constexpr int WIDE = NF * 16 * (ALONG ? KW : 1);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
   int64_t m0 = (int64_t)(workgroup() / (uint32_t)nt) * (MF * 16), m1 = rows;
-  const int64_t n0 = (int64_t)(workgroup() % (uint32_t)nt) * (NF * 16);
+  const int64_t first = (int64_t)(workgroup() % (uint32_t)nt) * WIDE, n0 = first + (ALONG ? wave * NF * 16 : 0);
   int64_t w0 = 0;
   if constexpr (EXPERTS) {
     int32_t expert;
     if (!find_tile(sorted, workgroup() / (uint32_t)nt, MF * 16, m0, m1, expert)) return;
     if (expert < 0) {
-      clear_rows(Y, stride, m0, m1, n0, n0 + NF * 16 < n ? n0 + NF * 16 : n);
+      clear_rows(Y, stride, m0, m1, first, first + WIDE < n ? first + WIDE : n);
       return;
     }
     w0 = expert * n;
     if (bias) bias += w0;
   }
-  if (m0 >= m1) return;
+  if (m0 >= m1 || n0 >= n) return;
   f32x4 acc[MF][NF] = {};
   int64_t xrow[MF], wrow[NF];  // rows past the last read the last one
 #pragma unroll
@@ -181,22 +183,27 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
         for (int j = 0; j < NF; ++j) acc[i][j] = multiply(o.w[h][j], o.x[h][i], acc[i][j]);
   };
   Operands a, b;
+  constexpr int STEP = ALONG ? 1 : KW;
   const int32_t pairs = (ng + 1) / 2;
-  int32_t pair = wave;
+  int32_t pair = ALONG ? 0 : wave;
   if (pair < pairs) load(pair, a);
   while (pair < pairs) {
-    if (pair + KW < pairs) load(pair + KW, b);
+    if (pair + STEP < pairs) load(pair + STEP, b);
     multiply_all(a);
-    pair += KW;
+    pair += STEP;
     if (pair >= pairs) break;
-    if (pair + KW < pairs) load(pair + KW, a);
+    if (pair + STEP < pairs) load(pair + STEP, a);
     multiply_all(b);
-    pair += KW;
+    pair += STEP;
+  }
+  if constexpr (ALONG) {
+    store_tiles<MF, NF>(acc, m0, n0, m1, n, bias, Y, stride);
+    return;
   }
 #pragma unroll
   for (int i = 0; i < MF; ++i)
 #pragma unroll
-    for (int j = 0; j < NF; ++j) part[wave][i * NF + j][lane] = acc[i][j];
+    for (int j = 0; j < NF; ++j) part[ALONG ? 0 : wave][i * NF + j][lane] = acc[i][j];
   __syncthreads();
   // wave i adds up and writes row group i
 #pragma unroll
@@ -207,7 +214,7 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
     for (int j = 0; j < NF; ++j) {
       sum[0][j] = part[0][i * NF + j][lane];
 #pragma unroll
-      for (int t = 1; t < KW; ++t) sum[0][j] += part[t][i * NF + j][lane];
+      for (int t = 1; t < (ALONG ? 1 : KW); ++t) sum[0][j] += part[t][i * NF + j][lane];
     }
     store_tiles<1, NF>(sum, m0 + i * 16, n0, m1, n, bias, Y, stride);
   }
@@ -618,7 +625,7 @@ struct Call {
   float *parts;  // workspace of a split sum
 };
 
-enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows32Short, kRows16, kRows16Short };
+enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows32Short, kRows16, kRows16Short, kRows16Along };
 struct Plan {
   Form form;
   int32_t splits, split_stages;
@@ -667,11 +674,23 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
            ceil_div(n, bn);
   };
   const auto whole = [&](Form f) { return Plan{f, 1, (int32_t)stages}; };
-  const bool few = experts > 0 && rows <= 3 * (int64_t)experts;  // of each expert
+  // A wave for each 16 x 32 where the sum is short and what the waves read twice is little, us with it and
+  // without: 3000 x 300 x 100 3.8 and 6.1, 1000 x 1000 x 256 4.2 and 5.2, but 1500 x 1500 x 256 7.2 and 5.8;
+  // 16 x 131072 x 300 5.7 and 9.4.  So do rows of many experts, few of each, up to 8, where W is all there is to
+  // read: 16 rows to 8 of 64 experts, 1024 x 2048, 15.4 and 18.3 (128 rows 23 and 19; 2 rows, too few waves, 8.4
+  // and 5.9).
+  const int64_t waves = tiles(16, 32), thin = std::min(rows, n);
+  const bool few = experts > 0 && rows <= 8 * (int64_t)experts;
+  if (experts > 0 ? few && waves >= 5 * cus
+                  : stages <= 3 && waves >= 2 * cus && (thin <= 16 || waves * ceil_div(cols, 128) <= 30 * cus))
+    return whole(kRows16Along);
   if (near && !few) {
     if (stages >= 8 && 4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
     const int64_t t = tiles(128, 128);
-    const bool wide = rows > 64 && n > 64 && t >= cus / 8, many = t >= cus / 2;
+    // 256 x 2048 x 1000 takes 4.8 us in tiles of 32 x 32 and 5.4 of 128 x 128, 512 x 1024 x 4096 11.5 and 10.2;
+    // 20000 x 16 x 4096 13.8 of 16 x 16 and 16.4.
+    const bool wide = rows > 64 && n > 64 && t >= cus / 8 && (stages > 8 || tiles(32, 32) > 2 * cus);
+    const bool many = t >= cus / 2 && (experts > 0 || thin > 16 || t >= 2 * cus);
     if (experts == 0 && !many && stages >= (wide ? 32 : 64)) {
       const int64_t best = (int64_t)std::sqrt(0.5 * stages / ((double)rows * n * 8 / 2.5e6));
       const int64_t splits = std::min(std::min(cus / t, stages / 4), best);
@@ -688,23 +707,24 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
       return whole(t > cus || stages <= 2 ? kTile128Short : stages >= 24 ? kTile128Deep : kTile128);
   }
   // Four waves share the sum where it is short or workgroups come in numbers, else eight: 1500 x 1500 x 1500
-  // takes 23 and 33 us in tiles of 16 x 16, 1 x 4096 x 4096 3.9 and 3.7.
+  // takes 23 and 33 us in tiles of 16 x 16, 400 x 1000 x 1500 5.4 and 7.9 of 32 x 32, 1 x 4096 x 4096 3.9 and 3.7.
   const auto short_of = [&](int64_t t) { return stages <= 4 || t >= 2 * cus; };
   if (rows > 16 && n > 16 && tiles(32, 32) >= cus && !few)
-    return whole(short_of(tiles(32, 32)) ? kRows32Short : kRows32);
+    return whole(short_of(tiles(32, 32)) || tiles(32, 32) > cus ? kRows32Short : kRows32);
   return whole(short_of(tiles(16, 16)) ? kRows16Short : kRows16);
 }
 size_t parts_bytes(const Plan &p, int64_t rows, int64_t n) {
   return p.splits > 1 ? (size_t)p.splits * rows * n * 4 : 0;
 }
 
-template <typename T, int MF, int NF, int KW, bool EXPERTS>
+template <typename T, int MF, int NF, int KW, bool EXPERTS, bool ALONG = false>
 int rows_launch(const Call &c, T *y, hipStream_t s) {
   static_assert(MF <= KW, "a wave for each row group");
-  const int64_t nt = ceil_div(c.n, NF * 16), wgs = row_tiles(c.rows, EXPERTS ? c.sorted.experts : 0, MF * 16) * nt;
+  const int64_t nt = ceil_div(c.n, NF * 16 * (ALONG ? KW : 1));
+  const int64_t wgs = row_tiles(c.rows, EXPERTS ? c.sorted.experts : 0, MF * 16) * nt;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL((k_nibble_rows<T, MF, NF, KW, EXPERTS>), grid_of(wgs), dim3(KW * 64), 0, s, c.x, c.w, c.sorted,
-                     c.bias, y, c.stride, c.rows, c.n, c.blocks, c.ng, (int32_t)nt);
+  hipLaunchKernelGGL((k_nibble_rows<T, MF, NF, KW, EXPERTS, ALONG>), grid_of(wgs), dim3(KW * 64), 0, s, c.x, c.w,
+                     c.sorted, c.bias, y, c.stride, c.rows, c.n, c.blocks, c.ng, (int32_t)nt);
   return launched();
 }
 
@@ -740,7 +760,8 @@ int product_as(const Call &c, const Plan &p, void *Y, hipStream_t s) {
     case kRows32: return rows_launch<T, 2, 2, 8, EXPERTS>(c, y, s);
     case kRows32Short: return rows_launch<T, 2, 2, 4, EXPERTS>(c, y, s);
     case kRows16: return rows_launch<T, 1, 1, 8, EXPERTS>(c, y, s);
-    default: return rows_launch<T, 1, 1, 4, EXPERTS>(c, y, s);
+    case kRows16Short: return rows_launch<T, 1, 1, 4, EXPERTS>(c, y, s);
+    default: return rows_launch<T, 1, 2, 4, EXPERTS, true>(c, y, s);
   }
 }
 template <bool EXPERTS>

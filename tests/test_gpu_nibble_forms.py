@@ -39,6 +39,11 @@ FORMS = {
     "thirty_two_short": (33, 300, 32 * CUS + 1),
     "sixteen": (9, 3000, 333),
     "sixteen_short": (17, 1024, 16),
+    "sixteen_long": (16, 1100, 128 * CUS - 3),
+    "along": (1000, 700, 1000),
+    "along_one_group": (3001, 100, 301),
+    "along_thin": (9, 300, 64 * CUS + 17),
+    "along_thin_rows": (64 * CUS + 5, 513, 16),
 }
 
 
@@ -85,6 +90,8 @@ EXPERTS = {
     "few_of_each_many": (40, 4, 60, 90, 1100),
     "thirty_two": (300, 1, 2, 1100, 130),
     "sixteen": (3, 2, 9, 900, 70),
+    "along": (40, 3, 60, 1030, 1111),
+    "along_eight_of_each": (200, 2, 50, 40, 2048 + 31),
 }
 
 
