@@ -15,26 +15,52 @@ using namespace nibble;
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;  // row groups in flight per lane group
 
-// The first `left` of V elements; zero for the others, which are read too where the
-// next row lies behind them.
-template <typename T, int V>
-__device__ inline void load_end(const T *p, int left, bool next_row, float (&v)[V]) {
-  if (left >= V || (left > 0 && next_row)) {
-    load_span(p, v);
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = i < left ? v[i] : 0.0f;
-  } else {
-    load_part(p, left, v);
+// V elements of a row, of which `left` lie inside the table; all or none where rows are
+// EVEN, of whole spans.  Else a row's end is read with what lies behind it where the
+// next row does; the last row's element by element, and a table's of rows so close or
+// few that V elements from its first pass its end.  What is asked for (`ask`, of many
+// rows in a row) is converted and cut off (`take`) later: done at once, each row waited
+// for its own.
+template <typename T, bool EVEN>
+struct Ends {
+  static constexpr int V = 16 / sizeof(T);
+  const T *x;
+  int64_t row_stride, rows;
+  int32_t cols;
+  struct Some {
+    Span<T, V> span;
+    const T *p;
+    int left;
+    bool whole;
+  };
+  __device__ inline bool any_whole() const { return cols >= V || (rows > 1 && row_stride >= V); }
+  __device__ inline Some ask(int64_t row, int32_t c) const {
+    Some o;
+    o.p = x + row * row_stride + c;
+    o.left = row < rows ? cols - c : 0;
+    o.span = Span<T, V>{};
+    if constexpr (EVEN) {
+      if (o.left > 0) o.span = *reinterpret_cast<const Span<T, V> *>(o.p);
+      return o;
+    }
+    o.whole = o.left >= V || (o.left > 0 && row + 1 < rows && row_stride >= V);
+    if (any_whole()) o.span = *reinterpret_cast<const Span<T, V> *>(o.whole ? o.p : x);
+    return o;
   }
-}
+  __device__ inline void take(const Some &o, float (&v)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = EVEN || i < o.left ? (float)o.span.v[i] : 0.0f;
+    if (!EVEN && o.left > 0 && !o.whole) load_part(o.p, o.left, v);
+  }
+};
 
 // A group of WIDE / V lanes takes one row's group of 128 columns, of which there are
 // at most WIDE: V neighbouring columns per lane (16 bytes), the largest bits of each
 // block over its 32 / V lanes, V codes per lane back.  Bound by the bytes, four groups
 // in flight: 262144 x 128 fp32 take 23 us, 6.6 TB/s of bytes that the 256 MB Infinity
-// Cache partly serves.  COLS: consecutive elements of a row lie together (else any
+// Cache partly serves; 563394 x 127 bf16 35.  COLS: consecutive elements of a row lie together (else any
 // strides, each lane's elements read one by one).
-template <typename T, int WIDE, bool COLS>
+template <typename T, int WIDE, bool COLS, bool EVEN>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ x, int64_t row_stride,
                                                           int64_t col_stride, int64_t rows, int32_t cols, int32_t ng,
                                                           uint8_t *__restrict__ codes, int64_t ld,
@@ -44,6 +70,8 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ 
   const int64_t first = (int64_t)workgroup() * (GROUPS * kUnroll);
   const int64_t r0 = first / ng;
   const uint32_t g0 = (uint32_t)(first - r0 * ng);
+  const Ends<T, EVEN> ends{x, row_stride, rows, cols};
+  typename Ends<T, EVEN>::Some some[kUnroll];
   float v[kUnroll][V];
   int64_t row[kUnroll];
   int32_t grp[kUnroll];
@@ -53,10 +81,10 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ 
     row[u] = r0 + at / (uint32_t)ng;
     grp[u] = at % (uint32_t)ng;
     const int32_t c = grp[u] * kGroup + lane * V;
-    const int left = row[u] < rows ? cols - c : 0;
     if constexpr (COLS) {
-      load_end(x + row[u] * row_stride + c, left, row[u] + 1 < rows && row_stride >= V, v[u]);
+      some[u] = ends.ask(row[u], c);
     } else {
+      const int left = row[u] < rows ? cols - c : 0;
       const T *p = x + row[u] * row_stride + c * col_stride;
 #pragma unroll
       for (int i = 0; i < V; ++i) v[u][i] = i < left ? (float)p[i * col_stride] : 0.0f;
@@ -64,6 +92,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack(const T *__restrict__ 
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
+    if constexpr (COLS) ends.take(some[u], v[u]);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -157,7 +186,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__rest
 // blocks of a column leave together, 64 bytes of codes and a word of scales.  Bound by
 // the bytes, two workgroups a compute unit for fp32: 2^18 x 256 take 77 us, 4.4 TB/s,
 // where the two ways one after the other take 102.
-template <typename T>
+template <typename T, bool EVEN>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restrict__ x, int64_t row_stride,
                                                                int64_t rows, int32_t cols, int32_t ng,
                                                                uint8_t *__restrict__ codes, int64_t ld,
@@ -178,33 +207,33 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
   const int64_t strip = at % strips, row0 = strip * 128 + wave * 32;
   const int32_t grp = at / strips;
   const int32_t c = grp * kGroup + lane * V;
-  float v[STEPS][V];
+  const Ends<T, EVEN> ends{x, row_stride, rows, cols};
+  typename Ends<T, EVEN>::Some some[STEPS];
+#pragma unroll
+  for (int u = 0; u < STEPS; ++u) some[u] = ends.ask(row0 + u * AT_ONCE + down, c);
 #pragma unroll
   for (int u = 0; u < STEPS; ++u) {
     const int64_t row = row0 + u * AT_ONCE + down;
-    load_end(x + row * row_stride + c, row < rows ? cols - c : 0, row + 1 < rows && row_stride >= V, v[u]);
-  }
-#pragma unroll
-  for (int u = 0; u < STEPS; ++u) {
-    const int64_t row = row0 + u * AT_ONCE + down;
+    float v[V];
+    ends.take(some[u], v);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const uint32_t bits = __float_as_uint(v[u][i]) & 0x7fffffffu;
+      const uint32_t bits = __float_as_uint(v[i]) & 0x7fffffffu;
       most = most > bits ? most : bits;
     }
     const uint32_t s = scale_byte(group_max_bits(most, SHARE));
     const float scale = scale_value(s);
-    uint32_t w = encode2<0>(0u, v[u][0], v[u][1], scale);
-    w = encode2<1>(w, v[u][2], v[u][3], scale);
+    uint32_t w = encode2<0>(0u, v[0], v[1], scale);
+    w = encode2<1>(w, v[2], v[3], scale);
     if constexpr (V == 8) {
-      w = encode2<2>(w, v[u][4], v[u][5], scale);
-      w = encode2<3>(w, v[u][6], v[u][7], scale);
+      w = encode2<2>(w, v[4], v[5], scale);
+      w = encode2<3>(w, v[6], v[7], scale);
     }
     if (s == kNanScale) w = 0;
     T *q = &tile[wave][(u * AT_ONCE + down) * PITCH + lane * V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) q[i] = (T)v[u][i];
+    for (int i = 0; i < V; ++i) q[i] = (T)v[i];
     if (row < rows) {
       if (c < ((cols + kCols - 1) & ~(kCols - 1))) {
         uint8_t *o = codes + row * ld + c / 2;
@@ -325,6 +354,13 @@ __global__ __launch_bounds__(kThreads) void k_nibble_unpack(const uint8_t *__res
   }
 }
 
+template <typename T, bool COLS, bool EVEN>
+auto pack_kernel(int wide) {
+  return wide == 32   ? k_nibble_pack<T, 32, COLS, EVEN>
+         : wide == 64 ? k_nibble_pack<T, 64, COLS, EVEN>
+                      : k_nibble_pack<T, 128, COLS, EVEN>;
+}
+
 template <typename T>
 int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nibble_t *out, hipStream_t s) {
   const T *p = static_cast<const T *>(x);
@@ -339,12 +375,10 @@ int pack_any(const void *x, int64_t row_stride, int64_t col_stride, const sd_nib
                        out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, (uint32_t)wgs);
     return launched();
   }
-  auto *kernel = col_stride != 1 ? (wide == 32   ? k_nibble_pack<T, 32, false>
-                                    : wide == 64 ? k_nibble_pack<T, 64, false>
-                                                 : k_nibble_pack<T, 128, false>)
-                                 : (wide == 32   ? k_nibble_pack<T, 32, true>
-                                    : wide == 64 ? k_nibble_pack<T, 64, true>
-                                                 : k_nibble_pack<T, 128, true>);
+  const bool even = out->cols % (16 / sizeof(T)) == 0;
+  auto *kernel = col_stride != 1 ? pack_kernel<T, false, false>(wide)
+                 : even          ? pack_kernel<T, true, true>(wide)
+                                 : pack_kernel<T, true, false>(wide);
   hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, p, row_stride, col_stride, out->rows,
                      (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales);
   return launched();
@@ -354,9 +388,10 @@ template <typename T>
 int both_any(const void *x, int64_t row_stride, const sd_nibble_t *out, const sd_nibble_t *out_t, hipStream_t s) {
   const int64_t ng = groups_of(out->cols), wgs = ceil_div(out->rows, 128) * ng;
   if (wgs > INT32_MAX) return SD_ERR_OVERFLOW;
-  hipLaunchKernelGGL(k_nibble_pack_both<T>, grid_of(wgs), dim3(kThreads), 0, s, static_cast<const T *>(x), row_stride,
-                     out->rows, (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, out_t->codes,
-                     out_t->ld, out_t->scales, (uint32_t)(wgs / ng), (uint32_t)wgs);
+  auto *kernel = out->cols % (16 / sizeof(T)) == 0 ? k_nibble_pack_both<T, true> : k_nibble_pack_both<T, false>;
+  hipLaunchKernelGGL(kernel, grid_of(wgs), dim3(kThreads), 0, s, static_cast<const T *>(x), row_stride, out->rows,
+                     (int32_t)out->cols, (int32_t)ng, out->codes, out->ld, out->scales, out_t->codes, out_t->ld,
+                     out_t->scales, (uint32_t)(wgs / ng), (uint32_t)wgs);
   return launched();
 }
 
@@ -394,7 +429,9 @@ extern "C" int sd_nibble_pack_both(const void *x, int32_t type, int64_t row_stri
   if (st == SD_OK && (out_t->rows != out->cols || out_t->cols != out->rows)) st = SD_ERR_INVALID_VALUE;
   if (st != SD_OK) return st;
   if (row_stride > (1ll << 31)) return SD_ERR_OVERFLOW;
-  if (col_stride != 1) {  // one after the other
+  // One after the other where rows fill little of k_nibble_pack_both's 128 columns and the second launch does
+  // not count: 500000 x 50 fp32 take 43 us so and 67 at once, 1000000 x 64 bf16 54 and 54, 516016 x 75 62 and 47.
+  if (col_stride != 1 || (out->cols <= 64 && out->rows >= (1 << 17))) {
     st = sd_nibble_pack(x, type, row_stride, col_stride, out, stream);
     return st == SD_OK ? sd_nibble_pack(x, type, col_stride, row_stride, out_t, stream) : st;
   }

@@ -141,7 +141,7 @@ def same_table(a, b):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 200), (200, 1), (31, 33), (128, 128), (129, 127), (300, 260),
-                                       (1000, 40), (33, 1030)])
+                                       (1000, 40), (33, 1030), (140001, 33)])
 def test_pack_both(rows, cols, dtype):
     """The same bits as one after the other: whole tables, parts of wider ones, any strides."""
     t, x = table(activations(rows, cols, rows + cols), dtype)
