@@ -63,45 +63,67 @@ __device__ inline void load_frag(const Operand &p, int64_t row, int32_t kg, int 
   }
 }
 
-// Which rows the tile of rows `tile` (BM rows each, the experts' one after the
-// other, then the rows that have none) covers: [m0, m1) of Y, and its expert;
-// expert -1: zeros; false: there is no such tile.  For a whole wave.  Offsets are
-// taken as far as they ascend within Y.
-__device__ inline bool find_tile(const Sorted &s, uint32_t tile, int bm, int64_t &m0, int64_t &m1, int32_t &expert) {
+// Which rows a tile of rows (BM rows each, the experts' one after the other, then the
+// rows that have none) covers: [m0, m1) of Y, and its expert; expert -1: zeros; false:
+// there is no such tile.  The tile is tile_of(tiles that there are), which are counted
+// if COUNTED and given as 0 else.  For a whole wave, with the same results in all its
+// lanes, kept in scalar registers.  Offsets are taken as far as they ascend within Y.
+template <bool COUNTED, typename F>
+__device__ inline bool find_tile(const Sorted &s, int bm, const F &tile_of, int64_t &m0, int64_t &m1,
+                                 int32_t &expert) {
   const int lane = threadIdx.x & 63;
   const auto at = [&](int32_t e) {
-    const int64_t o = s.offsets[e];
-    return o < 0 ? 0 : o > s.total ? s.total : o;
+    const int32_t o = s.offsets[e];
+    return o < 0 ? 0 : o > s.total ? (int32_t)s.total : o;
   };
-  uint32_t before = 0;
-  for (int32_t e0 = 0; e0 <= s.experts; e0 += 64) {
-    const int32_t e = e0 + lane;
-    int64_t b = 0, end = 0;
+  // an expert's rows and tiles
+  int32_t b, end;
+  const auto own_of = [&](int32_t e) {
+    b = end = 0;
     if (e <= s.experts) {
       b = at(e);
-      end = e == s.experts ? s.total : at(e + 1);
+      end = e == s.experts ? (int32_t)s.total : at(e + 1);
     }
-    const uint32_t own = end > b ? (uint32_t)((end - b + bm - 1) / bm) : 0u;
-    uint32_t upto = own;
+    return end > b ? ((uint32_t)(end - b) + bm - 1) / (uint32_t)bm : 0u;
+  };
+  // 64 experts, one a lane: its tiles, those up to its last; the sum of all
+  uint32_t own, upto;
+  const auto scan = [&](int32_t e0) {
+    upto = own = own_of(e0 + lane);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       const uint32_t o = (uint32_t)__shfl_up((int)upto, d);
       if (lane >= d) upto += o;
     }
-    const uint32_t whole = before + (uint32_t)__shfl((int)upto, 63);
-    if (tile < whole) {
-      const bool mine = tile < before + upto && tile >= before + upto - own;
-      const int who = __ffsll((unsigned long long)__ballot(mine)) - 1;
-      const int64_t lo = __shfl((int)b, who), hi = __shfl((int)end, who);
-      const uint32_t first = before + (uint32_t)__shfl((int)(upto - own), who);
-      expert = e0 + who < s.experts ? e0 + who : -1;
-      m0 = lo + (int64_t)(tile - first) * bm;
-      m1 = m0 + bm < hi ? m0 + bm : hi;
-      return true;
-    }
-    before = whole;
+    return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  };
+  int32_t e0 = 0;
+  uint32_t before = 0, whole, all = 0;
+  if (COUNTED && s.experts >= 64) {
+    uint32_t some = 0;
+    for (int32_t e = lane; e <= s.experts; e += 64) some += own_of(e);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) some += (uint32_t)__shfl_xor((int)some, d);
+    all = (uint32_t)__builtin_amdgcn_readfirstlane((int)some);
   }
-  return false;
+  whole = scan(0);
+  if (COUNTED && s.experts < 64) all = whole;
+  const uint32_t tile = (uint32_t)__builtin_amdgcn_readfirstlane((int)tile_of(all));
+  while (tile >= before + whole) {
+    before += whole;
+    e0 += 64;
+    if (e0 > s.experts) return false;
+    whole = scan(e0);
+  }
+  const bool mine = tile < before + upto && tile >= before + upto - own;
+  const int who = __ffsll((unsigned long long)__ballot(mine)) - 1;
+  if (who < 0) return false;  // offsets that fall and rise until their sums pass 32 bits
+  const int32_t lo = __builtin_amdgcn_readlane(b, who), hi = __builtin_amdgcn_readlane(end, who);
+  const uint32_t first = before + (uint32_t)__builtin_amdgcn_readlane((int)(upto - own), who);
+  expert = e0 + who < s.experts ? e0 + who : -1;
+  m0 = lo + (int64_t)(tile - first) * bm;
+  m1 = m0 + bm < hi ? m0 + bm : hi;
+  return true;
 }
 
 // Zeros to rows [m0, m1) and columns [n0, n1) of Y, by the whole workgroup.
@@ -117,7 +139,7 @@ __device__ inline void clear_rows(T *Y, int64_t stride, int64_t m0, int64_t m1, 
 // memory.  Lane (r, g) = (lane % 16, lane / 16) takes block g of a group of row r.
 // Bound by the latency of the loads where there are few tiles: 1 x 4096 x 4096 takes
 // 3.7 us (2.4 TB/s of W), the launch itself 2; by W's bytes where there are many: 16
-// rows through 2 of 16 experts of 4096 x 4096 take 28, 5.1 TB/s.
+// rows through 8 of 64 experts of 1024 x 2048 take 15, 4.6 TB/s.
 // ALONG: the waves take a tile each, KW neighbouring ones, and the whole sum.
 template <typename T, int MF, int NF, int KW, bool EXPERTS, bool ALONG>
 __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, Sorted sorted,
@@ -132,7 +154,8 @@ __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, S
   int64_t w0 = 0;
   if constexpr (EXPERTS) {
     int32_t expert;
-    if (!find_tile(sorted, workgroup() / (uint32_t)nt, MF * 16, m0, m1, expert)) return;
+    const uint32_t tile = workgroup() / (uint32_t)nt;
+    if (!find_tile<false>(sorted, MF * 16, [=](uint32_t) { return tile; }, m0, m1, expert)) return;
     if (expert < 0) {
       clear_rows(Y, stride, m0, m1, first, first + WIDE < n ? first + WIDE : n);
       return;
@@ -272,22 +295,30 @@ __global__ __launch_bounds__(256) void k_nibble_tile(Operand X, Operand W, Sorte
   const int32_t first = split * split_stages, last = first + split_stages < stages ? first + split_stages : stages;
   if (first >= last && split > 0) return;
   Y += split * split_stride;
-  const uint32_t at = xcd_place(workgroup() - split * tiles, tiles);
-  // tiles in bands of 8 along m: neighbours in the list share X's and W's rows
-  const uint32_t band = at / (8u * nt), left = mt - band * 8u < 8u ? mt - band * 8u : 8u;
-  const uint32_t in_band = at - band * 8u * nt;
-  const uint32_t mtile = band * 8u + in_band % left;
-  const int64_t n0 = (int64_t)(in_band / left) * BN;
-  int64_t m0 = (int64_t)mtile * BM, m1 = rows, w0 = 0;
+  // The place of workgroup wg of `mtiles` rows of tiles, in bands of 8 along m: neighbours in the list share X's
+  // and W's rows
+  int64_t n0 = 0;
+  const auto place = [&](uint32_t wg, uint32_t mtiles) -> uint32_t {
+    if (wg >= mtiles * (uint32_t)nt) return ~0u;
+    const uint32_t at = xcd_place(wg, mtiles * (uint32_t)nt), band = at / (8u * nt);
+    const uint32_t left = mtiles - band * 8u < 8u ? mtiles - band * 8u : 8u, in_band = at - band * 8u * nt;
+    n0 = (int64_t)(in_band / left) * BN;
+    return band * 8u + in_band % left;
+  };
+  int64_t m0, m1 = rows, w0 = 0;
   if constexpr (EXPERTS) {
+    // The tiles that there are, and not those that there could be, go to all XCDs alike: 1024 rows to 2 of 16
+    // experts, 4096 x 4096, take 39 us, not 56.
     int32_t expert;
-    if (!find_tile(sorted, mtile, BM, m0, m1, expert)) return;
+    if (!find_tile<true>(sorted, BM, [&](uint32_t all) { return place(workgroup(), all); }, m0, m1, expert)) return;
     if (expert < 0) {
       clear_rows(Y, stride, m0, m1, n0, n0 + BN < n ? n0 + BN : n);
       return;
     }
     w0 = expert * n;
     if (bias) bias += w0;
+  } else {
+    m0 = (int64_t)place(workgroup() - split * tiles, mt) * BM;
   }
   // X's and W's rows for one of the tile, counted from the first; past the last one, that
   const int32_t xlast = (int32_t)(m1 - m0 < BM ? m1 - m0 : BM) - 1, wlast = (int32_t)(n - n0 < BN ? n - n0 : BN) - 1;
@@ -658,33 +689,34 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
 // A stage of 256 k takes a lone 128 x 128 tile 0.5 us, and the parts go to memory and back at about
 // 2.5 TB/s: that gives the number of parts.
 //
-// Rows sorted by expert, us, launches in a row (rows of X, experts of each, experts, columns x k):
+// Rows sorted by expert, us, launches in a row (rows of X, experts of each, experts, columns x k; 16 x 16 with
+// the best of sums shared by the waves or not):
 //                              256x256   128x128  32x32  16x16
-//   4096, 2, 16, 4096 x 4096        114       115    632   1180
-//   1024, 2, 16, 4096 x 4096         67        50    174    307
-//   64, 2, 16, 4096 x 4096           59        31     37     35
-//   16, 2, 16, 4096 x 4096           58        29     32     28
-//   64, 8, 64, 1024 x 2048           39        19     26     22
-//   16, 8, 64, 1024 x 2048           38        18     22     17
+//   4096, 2, 16, 4096 x 4096        106       104    634    869
+//   1024, 2, 16, 4096 x 4096         40        39    173    230
+//   64, 2, 16, 4096 x 4096           33        25     38     28
+//   16, 2, 16, 4096 x 4096           32        22     32     26
+//   64, 8, 64, 1024 x 2048           23        17     26     17
+//   16, 8, 64, 1024 x 2048           22        16     24     15
+//   1, 8, 64, 1024 x 2048            17         9    5.3    4.4
 Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) {
   const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
   // of rows sorted by expert the tiles there will be: half a tile too many for each expert
   const auto tiles = [&](int64_t bm, int64_t bn) {
-    return (experts == 0 ? ceil_div(rows, bm) : ceil_div(rows, bm) + std::min<int64_t>(experts / 2, rows)) *
-           ceil_div(n, bn);
+    const int64_t mt = ceil_div(rows, bm);
+    return (experts == 0 ? mt : std::min<int64_t>(mt + experts / 2, rows)) * ceil_div(n, bn);
   };
   const auto whole = [&](Form f) { return Plan{f, 1, (int32_t)stages}; };
   // A wave for each 16 x 32 where the sum is short and what the waves read twice is little, us with it and
   // without: 3000 x 300 x 100 3.8 and 6.1, 1000 x 1000 x 256 4.2 and 5.2, but 1500 x 1500 x 256 7.2 and 5.8;
-  // 16 x 131072 x 300 5.7 and 9.4.  So do rows of many experts, few of each, up to 8, where W is all there is to
-  // read: 16 rows to 8 of 64 experts, 1024 x 2048, 15.4 and 18.3 (128 rows 23 and 19; 2 rows, too few waves, 8.4
-  // and 5.9).
+  // 16 x 131072 x 300 5.7 and 9.4.  Of rows sorted by expert, where each has few of them: 2000 to 100 experts,
+  // 1000 x 100, 7.3 and 11.9; 600 to 64, 1024 x 512, 6.2 and 7.8, x 768 10.1 and 8.7.
   const int64_t waves = tiles(16, 32), thin = std::min(rows, n);
-  const bool few = experts > 0 && rows <= 8 * (int64_t)experts;
-  if (experts > 0 ? few && waves >= 5 * cus
+  const bool spread = 2 * waves >= 9 * cus, few = rows <= 8 * (int64_t)experts;  // few rows of each expert
+  if (experts > 0 ? spread && (rows * stages <= 24 * (int64_t)experts || (few && stages <= 8))
                   : stages <= 3 && waves >= 2 * cus && (thin <= 16 || waves * ceil_div(cols, 128) <= 30 * cus))
     return whole(kRows16Along);
-  if (near && !few) {
+  if (near && (!few || spread)) {
     if (stages >= 8 && 4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
     const int64_t t = tiles(128, 128);
     // 256 x 2048 x 1000 takes 4.8 us in tiles of 32 x 32 and 5.4 of 128 x 128, 512 x 1024 x 4096 11.5 and 10.2;
@@ -702,9 +734,12 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
     // Buffers for 128 x 128: one, and three workgroups a compute unit, where there are more tiles than units or
     // the sum is short (3000 x 3000 x 3000 takes 27, 31 and 31 us with one, two and four, 533036 x 44 x 26 40,
     // 54 and 105); four where the sum is long (2048 x 2048 x 8192 28 with two, 23 with four), else two (2048
-    // cubed 11.2, 9.5 and 9.7).
-    if (wide || many)
-      return whole(t > cus || stages <= 2 ? kTile128Short : stages >= 24 ? kTile128Deep : kTile128);
+    // cubed 11.2, 9.5 and 9.7).  Of rows sorted by expert the tiles are fewer than thought: 16 rows to 4 of 16
+    // experts, 4096 x 8192, 34.6 with two, 40.3 with one.
+    if (wide || many || few) {
+      const bool one = stages <= 2 || (experts > 0 && stages >= 16 ? t > 2 * cus : t > cus);
+      return whole(one ? kTile128Short : stages >= 24 && t <= cus ? kTile128Deep : kTile128);
+    }
   }
   // Four waves share the sum where it is short or workgroups come in numbers, else eight: 1500 x 1500 x 1500
   // takes 23 and 33 us in tiles of 16 x 16, 400 x 1000 x 1500 5.4 and 7.9 of 32 x 32, 1 x 4096 x 4096 3.9 and 3.7.

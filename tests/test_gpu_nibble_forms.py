@@ -91,6 +91,8 @@ EXPERTS = {
     "thirty_two": (300, 1, 2, 1100, 130),
     "sixteen": (3, 2, 9, 900, 70),
     "along": (40, 3, 60, 1030, 1111),
+    "few_long": (30, 2, 11, 256 * 17 + 3, 128 * CUS // 6 + 77),
+    "many_kinds": (700, 3, 200, 700, 500),
     "along_eight_of_each": (200, 2, 50, 40, 2048 + 31),
 }
 
