@@ -599,8 +599,8 @@ typedef struct {
  * even.  A block that holds a NaN or an infinity gets scale byte 255 and zero codes. */
 int sd_nibble_pack(const void *x, int32_t type, int64_t row_stride, int64_t col_stride, const sd_nibble_t *out,
                    void *stream);
-/* x and its transpose (out_t of out->cols x out->rows) from one reading where
- * col_stride is 1, the same bits as two calls. */
+/* x and its transpose (out_t of out->cols x out->rows), from one reading where
+ * that is faster, the same bits as two calls. */
 int sd_nibble_pack_both(const void *x, int32_t type, int64_t row_stride, int64_t col_stride, const sd_nibble_t *out,
                         const sd_nibble_t *out_t, void *stream);
 /* The values, rounded once to y's type. */

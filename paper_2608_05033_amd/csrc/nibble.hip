@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__rest
 // the columns as k_nibble_pack does, leaves them in shared memory and takes them
 // column by column, so that a lane has a block of the transpose.  The four waves'
 // blocks of a column leave together, 64 bytes of codes and a word of scales.  Bound by
-// the bytes, two workgroups a compute unit for fp32: 2^18 x 256 take 77 us, 4.4 TB/s,
+// the bytes, two workgroups a compute unit for fp32: 2^18 x 256 take 75 us, 4.5 TB/s,
 // where the two ways one after the other take 102.
 template <typename T, bool EVEN>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restrict__ x, int64_t row_stride,
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
 }
 
 // Lanes along a row, eight codes each.  Bound by the bytes written: 262144 x 128 to
-// bf16 take 21 us, 4.1 TB/s.  END 1: a row's last lane begins eight columns before its
+// bf16 take 14 us, 6 TB/s of bytes that the caches partly serve.  END 1: a row's last lane begins eight columns before its
 // end, so that all write whole spans; its codes lie in two words and may lie in two
 // blocks.  END 2: rows of fewer than eight columns.
 template <typename T, int END>

@@ -253,7 +253,7 @@ def pack4(x, transpose: bool = False) -> Packed4:
 
 @_on_its_device
 def pack4_both(x):
-    """(pack4(x), pack4(x, transpose=True)) from one reading of x."""
+    """(pack4(x), pack4(x, transpose=True)), from one reading of x where that is faster."""
     if x.dim() != 2 or x.dtype not in TYPES or not x.is_cuda:
         raise ValueError(f"x must be a float32, float16 or bfloat16 matrix on the GPU, got {x.dtype} "
                          f"{tuple(x.shape)} on {x.device}")
