@@ -8,7 +8,9 @@
 
 Arguments are checked here and in the library; every call runs on the current
 stream of its tensors' device, and results and workspaces are torch tensors of
-that stream.  `dispatch` and `combine` record gradients where torch does.
+that stream.  `dispatch` and `combine` record gradients where torch does; a step that
+is captured into a graph takes leaves of its own (x.detach().requires_grad_()), since
+torch ties a leaf to the stream that it was first used on.
 """
 from __future__ import annotations
 

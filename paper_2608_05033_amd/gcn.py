@@ -178,7 +178,8 @@ def transform4(X: torch.Tensor, W: torch.Tensor) -> torch.Tensor:
     """X.W in float32 on the matrix units' 4-bit form, with gradients computed in the
     same way: X and W are rounded to 4 bits along the features, the output gradient
     and W along the outputs for X's gradient, X and the output gradient along the rows
-    for W's, as if the rounding were the identity.  No second derivatives."""
+    for W's, as if the rounding were the identity.  No second derivatives.  A step that is
+    captured into a graph takes leaves of its own (X.detach().requires_grad_())."""
     if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[0]:
         raise ValueError(f"X and W must be matrices that fit, got {tuple(X.shape)} and {tuple(W.shape)}")
     return _Transform4.apply(X, W)

@@ -344,6 +344,33 @@ def test_captured_and_replayed():
             assert all(torch.equal(a, b) for a, b in zip(out, want))
 
 
+def test_a_training_step_captured_and_replayed():
+    """A transform and both gradients, the weight's a sum split over workgroups, with
+    an eager step's graph alive beside it."""
+    g = torch.Generator().manual_seed(1)
+    X, W, dZ = (torch.randn(*size, generator=g).cuda() for size in ((20000, 40), (40, 24), (20000, 24)))
+
+    def step():
+        a, b = X.detach().requires_grad_(), W.detach().requires_grad_()
+        Z = gcn.transform4(a, b)
+        return Z, *torch.autograd.grad(Z, (a, b), dZ, retain_graph=True)
+
+    eager = step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(3):
+        for t in (X, W, dZ):
+            t.copy_(torch.randn(*t.shape, generator=torch.Generator().manual_seed(10 + i)))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+        assert not torch.equal(eager[0], want[0])
+
+
 # ---------------------------------------------------------------- gradients ---
 def rounded(x):
     scale, units = ref.encode(x)
