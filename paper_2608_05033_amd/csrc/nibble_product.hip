@@ -273,7 +273,8 @@ __device__ constexpr int wait_until(int left) { return (left & 15) | (left >> 4)
 // Bound by the matrix units at the clock that power allows, and by what the requests
 // take from them: 8192 cubed to bf16 takes 245 to 285 us (box and warmth), 3.9 to 4.5
 // PFLOP/s, of which a tile's 32 stages take 60 (2850 cycles each at 1.5 to 1.65 GHz,
-// 2112 of them products), the way in 2.4 and the way out 4.  2048 cubed takes 8.8 us.
+// 2112 of them products), the way in 2.4 and the way out 4.  2048 cubed takes 9.7 us.
+// With one buffer four workgroups share a compute unit and cover each other's waits.
 template <typename T, int BM, int BN, int BUFFERS, bool EXPERTS>
 __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Operand X, Operand W, Sorted sorted,
                                                              const float *__restrict__ bias, T *__restrict__ Y,
@@ -713,7 +714,7 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
 //   64, 8, 64, 1024 x 2048           23        17     26     17
 //   16, 8, 64, 1024 x 2048           22        16     24     15
 //   1, 8, 64, 1024 x 2048            17         9    5.3    4.4
-Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) {
+Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, int32_t type, bool near) {
   const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
   // of rows sorted by expert the tiles there will be: half a tile too many for each expert
   const auto tiles = [&](int64_t bm, int64_t bn) {
@@ -731,7 +732,14 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
                   : stages <= 3 && waves >= 2 * cus && (thin <= 16 || waves * ceil_div(cols, 128) <= 30 * cus))
     return whole(kRows16Along);
   if (near && (!few || spread)) {
-    if (stages >= 8 && 4 * tiles(256, 256) >= 3 * cus && 32 * tiles(256, 256) <= 9 * tiles(128, 128)) return whole(kTile256);
+    // Large tiles, us with them and with one buffer of 128 x 128: 4096 x 4096 x 2048 25.3 and 26.7 to bf16, 30.5 and
+    // 30.6 to fp32, 8192 x 8192 x 2048 118 and 102 to fp32, 4096 cubed 44 and 49.  Of rows sorted by expert, whose
+    // tiles begin with two more loads, where they are many: 16384 rows to 2 of 16, 4096 x 4096, 355 and 367, 8192 to
+    // 2 of 8 183 and 178, 4096 to 2 of 16 112 and 103.  Not where they cover much more than there is.
+    const int64_t large = tiles(256, 256);
+    if (stages >= (type == SD_TYPE_F32 ? 12 : 8) && 4 * large >= 3 * cus && 32 * large <= 9 * tiles(128, 128) &&
+        (experts == 0 || large * stages >= 80 * cus))
+      return whole(kTile256);
     const int64_t t = tiles(128, 128);
     // 256 x 2048 x 1000 takes 4.8 us in tiles of 32 x 32 and 5.4 of 128 x 128, 512 x 1024 x 4096 11.5 and 10.2;
     // 20000 x 16 x 4096 13.8 of 16 x 16 and 16.4.
@@ -745,9 +753,9 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, bool near) 
         return Plan{kTile128Deep, (int32_t)ceil_div(stages, each), (int32_t)each};
       }
     }
-    // Buffers for 128 x 128: one, and three workgroups a compute unit, where there are more tiles than units or
-    // the sum is short (3000 x 3000 x 3000 takes 27, 31 and 31 us with one, two and four, 533036 x 44 x 26 40,
-    // 54 and 105); four where the sum is long (2048 x 2048 x 8192 28 with two, 23 with four), else two (2048
+    // Buffers for 128 x 128: one, and four workgroups a compute unit, where there are more tiles than units or
+    // the sum is short (3000 x 3000 x 3000 takes 29, 32 and 35 us with one, two and four, 533036 x 44 x 26 33,
+    // 47 and 86); four where the sum is long (2048 x 2048 x 8192 28 with two, 23 with four), else two (2048
     // cubed 11.2, 9.5 and 9.7).  Of rows sorted by expert the tiles are fewer than thought: 16 rows to 4 of 16
     // experts, 4096 x 8192, 34.6 with two, 40.3 with one.
     if (wide || many || few) {
@@ -831,7 +839,8 @@ Operand operand(const sd_nibble_t *p) { return Operand{p->codes, p->scales, p->l
 extern "C" int sd_nibble_product_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes) {
   if (!bytes || rows < 0 || cols < 0 || n < 0) return SD_ERR_INVALID_VALUE;
   if (rows > kMaxRows || n > kMaxRows || cols > kMaxRows - 1024) return SD_ERR_OVERFLOW;
-  *bytes = rows == 0 || n == 0 ? 0 : parts_bytes(plan_of(rows, 0, n, cols, true), rows, n);
+  // results of any type: it has no say in how a sum is split
+  *bytes = rows == 0 || n == 0 ? 0 : parts_bytes(plan_of(rows, 0, n, cols, SD_TYPE_BF16, true), rows, n);
   return SD_OK;
 }
 
@@ -849,7 +858,7 @@ extern "C" int sd_nibble_product(const sd_nibble_t *X, const sd_nibble_t *W, con
   if (st != SD_OK) return st;
   if (X->rows == 0 || W->rows == 0) return SD_OK;
   if ((st = have_device()) != SD_OK) return st;
-  const Plan p = plan_of(X->rows, 0, W->rows, X->cols, near_rows(X) && near_rows(W));
+  const Plan p = plan_of(X->rows, 0, W->rows, X->cols, type, near_rows(X) && near_rows(W));
   const Call c{operand(X), operand(W), Sorted{}, bias, row_stride, X->rows, W->rows, (int32_t)col_blocks(X->cols),
                (int32_t)groups_of(X->cols), static_cast<float *>(workspace)};
   return product<false>(c, p, Y, type, stream);
@@ -872,7 +881,7 @@ extern "C" int sd_expert_product(const sd_nibble_t *X, const sd_nibble_t *W, con
   if ((st = have_device()) != SD_OK) return st;
   // the large tiles take X's rows from anywhere and keep their distance from its first one in 32 bits
   const bool near = near_rows(W) && X->rows <= (1ll << 32) / (X->ld > 0 ? X->ld : 1);
-  const Plan p = plan_of(total, route->experts, n, X->cols, near);
+  const Plan p = plan_of(total, route->experts, n, X->cols, type, near);
   const Call c{operand(X), operand(W), Sorted{route->offsets, sorted ? nullptr : route->source, route->experts, total},
                bias, row_stride, total, n, (int32_t)col_blocks(X->cols), (int32_t)groups_of(X->cols), nullptr};
   return product<true>(c, p, Y, type, stream);

@@ -19,12 +19,14 @@ from paper_2608_05033_amd import dense, experts  # noqa: E402
 
 CUS = torch.cuda.get_device_properties(0).multi_processor_count
 SIDE = int((0.75 * CUS) ** 0.5) + 1  # SIDE * SIDE large tiles are enough for the card
+MANY = int((2 * CUS) ** 0.5) + 1  # MANY * MANY of 40 stages are, of rows sorted by expert
 
 # rows, columns, results: forms from the largest tiles to the smallest, odd and whole numbers of stages
 FORMS = {
     "large": (256 * SIDE, 2048, 256 * SIDE),
     "large_odd": (256 * SIDE - 57, 2100, 256 * SIDE - 13),
     "large_ten": (256 * SIDE - 1, 2500, 256 * SIDE - 255 + 200),
+    "large_long": (256 * SIDE - 57, 256 * 12 + 70, 256 * SIDE - 13),
     "many": (256 * SIDE, 512, 256 * SIDE),
     "many_odd": (256 * SIDE - 57, 130, 256 * SIDE - 13),
     "many_three": (128 * CUS + 5, 600, 70),
@@ -82,6 +84,8 @@ def test_forms_are_exact_and_keep_nan(form):
 EXPERTS = {
     "large": (128 * SIDE, 2, 3, 2060, 256 * SIDE - 9),
     "large_one": (256 * SIDE, 1, 1, 2048, 256 * SIDE),
+    "large_many": (128 * MANY - 5, 2, 2, 256 * 40 - 180, 256 * MANY - 9),
+    "large_many_one": (256 * MANY, 1, 1, 256 * 40, 256 * MANY),
     "many": (128 * SIDE, 2, 3, 520, 256 * SIDE - 9),
     "many_short": (900, 2, 7, 200, 2000),
     "middle": (700, 2, 5, 257, 600),
