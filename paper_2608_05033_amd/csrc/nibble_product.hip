@@ -671,7 +671,7 @@ struct Call {
   float *parts;  // workspace of a split sum
 };
 
-enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows32Short, kRows16, kRows16Short, kRows16Along };
+enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows16, kRows16Short, kRows16Along };
 struct Plan {
   Form form;
   int32_t splits, split_stages;
@@ -763,12 +763,11 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, int32_t typ
       return whole(one ? kTile128Short : stages >= 24 && t <= cus ? kTile128Deep : kTile128);
     }
   }
-  // Four waves share the sum where it is short or workgroups come in numbers, else eight: 1500 x 1500 x 1500
-  // takes 23 and 33 us in tiles of 16 x 16, 400 x 1000 x 1500 5.4 and 7.9 of 32 x 32, 1 x 4096 x 4096 3.9 and 3.7.
-  const auto short_of = [&](int64_t t) { return stages <= 4 || t >= 2 * cus; };
-  if (rows > 16 && n > 16 && tiles(32, 32) >= cus && !few)
-    return whole(short_of(tiles(32, 32)) || tiles(32, 32) > cus ? kRows32Short : kRows32);
-  return whole(short_of(tiles(16, 16)) ? kRows16Short : kRows16);
+  if (rows > 16 && n > 16 && tiles(32, 32) >= cus && !few) return whole(kRows32);
+  // Four waves share the sum where it is short or workgroups come in numbers, as for 32 x 32 always (512 x 512 x
+  // 4096 7.1 us, with eight 7.2, 400 x 1000 x 1500 5.4 and 7.9), else eight: 1500 x 1500 x 1500 takes 23 and 33 us
+  // in tiles of 16 x 16, 1 x 4096 x 4096 3.9 and 3.7.
+  return whole(stages <= 4 || tiles(16, 16) >= 2 * cus ? kRows16Short : kRows16);
 }
 size_t parts_bytes(const Plan &p, int64_t rows, int64_t n) {
   return p.splits > 1 ? (size_t)p.splits * rows * n * 4 : 0;
@@ -814,8 +813,7 @@ int product_as(const Call &c, const Plan &p, void *Y, hipStream_t s) {
     case kTile128: return tile_launch<T, 128, 128, 2, EXPERTS>(c, p, y, s);
     case kTile128Deep: return tile_launch<T, 128, 128, 4, EXPERTS>(c, p, y, s);
     case kTile128Short: return tile_launch<T, 128, 128, 1, EXPERTS>(c, p, y, s);
-    case kRows32: return rows_launch<T, 2, 2, 8, EXPERTS>(c, y, s);
-    case kRows32Short: return rows_launch<T, 2, 2, 4, EXPERTS>(c, y, s);
+    case kRows32: return rows_launch<T, 2, 2, 4, EXPERTS>(c, y, s);
     case kRows16: return rows_launch<T, 1, 1, 8, EXPERTS>(c, y, s);
     case kRows16Short: return rows_launch<T, 1, 1, 4, EXPERTS>(c, y, s);
     default: return rows_launch<T, 1, 2, 4, EXPERTS, true>(c, y, s);
