@@ -19,18 +19,20 @@ class _FirstOnly(torch.autograd.Function):
 
 
 def first_derivatives_only(backward):
-    """A backward pass through kernels: where a graph of it is asked for
-    (create_graph), its results lead to an error and not to a part that is missing.
-    They hang on the output gradient and on what was saved, as far as those require
-    gradients, so that a derivative with respect to any of them finds the error."""
+    """A backward pass through kernels, backward(ctx, saved tensors, dZ): where a graph
+    of it is asked for (create_graph), its results lead to an error and not to a part
+    that is missing.  They hang on the output gradient and on what was saved, as far as
+    those require gradients, so that a derivative with respect to any of them finds the
+    error.  What was saved is asked for once: a checkpoint computes it anew for that."""
 
     @functools.wraps(backward)
     def wrapped(ctx, dZ):
+        kept = ctx.saved_tensors
         if not torch.is_grad_enabled():
-            return backward(ctx, dZ)
+            return backward(ctx, kept, dZ)
         with torch.no_grad():
-            grads = backward(ctx, dZ)
-        anchors = [v for v in (dZ, *ctx.saved_tensors) if v is not None and v.requires_grad]
+            grads = backward(ctx, kept, dZ)
+        anchors = [v for v in (dZ, *kept) if v is not None and v.requires_grad]
         anchors = anchors or [dZ.new_empty(0).requires_grad_()]
         return tuple(g if g is None else _FirstOnly.apply(g, *anchors) for g in grads)
 

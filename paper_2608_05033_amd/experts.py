@@ -216,8 +216,8 @@ class _WeightedSum(torch.autograd.Function):
 
     @staticmethod
     @first_derivatives_only
-    def backward(ctx, dout):
-        weights, y = ctx.saved_tensors[:2]
+    def backward(ctx, kept, dout):
+        weights, y = kept[:2]
         need_dy, need_dweights = ctx.needs_input_grad[:2]
         return *combine_backward(dout.contiguous(), y, ctx.route, weights, need_dy, need_dweights), None
 

@@ -129,9 +129,9 @@ class _PackedTransform(torch.autograd.Function):
 
     @staticmethod
     @first_derivatives_only
-    def backward(ctx, dZ):
+    def backward(ctx, kept, dZ):
         dX, dW, dZ = None, None, dZ.contiguous()
-        codes, scales, *rest = ctx.saved_tensors
+        codes, scales, *rest = kept
         X8 = dense.Packed(codes, scales, *ctx.of_table)
         if ctx.needs_input_grad[0]:
             dX = dense.product(dense.pack(dZ, ctx.grad_fmt), dense.pack(rest[0], X8.format), dtype=ctx.dtype)
@@ -157,9 +157,9 @@ class _Transform4(torch.autograd.Function):
 
     @staticmethod
     @first_derivatives_only
-    def backward(ctx, dZ):
+    def backward(ctx, kept, dZ):
         need_dX, need_dW = ctx.needs_input_grad
-        kept, (rows, n) = ctx.saved_tensors, ctx.sizes
+        rows, n = ctx.sizes
         dX = dW = None
         if need_dX and need_dW:
             G, Gt = dense.pack4_both(dZ)
@@ -200,9 +200,9 @@ class _NormTransform(torch.autograd.Function):
 
     @staticmethod
     @first_derivatives_only
-    def backward(ctx, dZ):
+    def backward(ctx, kept, dZ):
         dZ = dZ.contiguous()
-        W, gamma, beta, *A8, codes, scales, mean, rstd = ctx.saved_tensors
+        W, gamma, beta, *A8, codes, scales, mean, rstd = kept
         A8, H8 = dense.Packed(*A8, *ctx.of_table), dense.Packed(codes, scales, *ctx.of_table)
         groups, eps, activation = ctx.args
         dA = dgamma = dbeta = dW = None
