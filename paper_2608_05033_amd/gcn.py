@@ -23,7 +23,7 @@ from __future__ import annotations
 import torch
 
 from . import Plan, dense, sd_plan_device, sd_plan_ex, sd_spmm
-from .autograd import first_derivatives_only
+from .autograd import anchor, first_derivatives_only
 
 
 class _SpMM(torch.autograd.Function):
@@ -124,8 +124,9 @@ class _PackedTransform(torch.autograd.Function):
         if ctx.needs_input_grad[0]:
             ctx.dtype, ctx.grad_fmt = X.dtype, grad_fmt
             kept.append(W)
+        kept.append(anchor(W))
         ctx.save_for_backward(*kept)
-        return dense.product(X8, dense.pack(W, X8.format, transpose=True))
+        return dense.product(X8, dense.pack(W, X8.format, transpose=True)), kept[-1]
 
     @staticmethod
     @first_derivatives_only
@@ -151,9 +152,10 @@ class _Transform4(torch.autograd.Function):
         X4, Xt = dense.pack4_both(X) if need_dW else (dense.pack4(X), None)
         W4, Wt = dense.pack4_both(W) if need_dX else (None, dense.pack4(W, transpose=True))
         ctx.dtypes, ctx.sizes = (X.dtype, W.dtype), (X.shape[0], W.shape[1])
-        ctx.save_for_backward(W, *(() if W4 is None else (W4.codes, W4.scales)),
-                              *(() if Xt is None else (Xt.codes, Xt.scales)))
-        return dense.product4(X4, Wt)
+        all_inputs = anchor(W)
+        ctx.save_for_backward(*(() if W4 is None else (W4.codes, W4.scales)),
+                              *(() if Xt is None else (Xt.codes, Xt.scales)), all_inputs)
+        return dense.product4(X4, Wt), all_inputs
 
     @staticmethod
     @first_derivatives_only
@@ -168,9 +170,9 @@ class _Transform4(torch.autograd.Function):
         else:
             Gt = dense.pack4(dZ, transpose=True)
         if need_dX:
-            dX = dense.product4(G, dense.Packed4(*kept[1:3], n), dtype=ctx.dtypes[0])
+            dX = dense.product4(G, dense.Packed4(*kept[:2], n), dtype=ctx.dtypes[0])
         if need_dW:
-            dW = dense.product4(dense.Packed4(*kept[-2:], rows), Gt, dtype=ctx.dtypes[1])
+            dW = dense.product4(dense.Packed4(*kept[-3:-1], rows), Gt, dtype=ctx.dtypes[1])
         return dX, dW
 
 
@@ -182,7 +184,7 @@ def transform4(X: torch.Tensor, W: torch.Tensor) -> torch.Tensor:
     captured into a graph takes leaves of its own (X.detach().requires_grad_())."""
     if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[0]:
         raise ValueError(f"X and W must be matrices that fit, got {tuple(X.shape)} and {tuple(W.shape)}")
-    return _Transform4.apply(X, W)
+    return _Transform4.apply(X, W)[0]
 
 
 class _NormTransform(torch.autograd.Function):
@@ -194,15 +196,16 @@ class _NormTransform(torch.autograd.Function):
     def forward(ctx, A, gamma, beta, W, groups, eps, activation, fmt, grad_fmt):
         out = dense.group_norm(A, groups, gamma, beta, eps, activation, keep=fmt, pack_y=fmt, dense_y=False)
         ctx.of_table, ctx.args, ctx.grad_fmt = (out.x.cols, fmt), (groups, eps, activation), grad_fmt
+        all_inputs = anchor(W)
         ctx.save_for_backward(W, gamma, beta, out.x.codes, out.x.scales, out.y_packed.codes, out.y_packed.scales,
-                              out.mean, out.rstd)
-        return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True))
+                              out.mean, out.rstd, all_inputs)
+        return dense.product(out.y_packed, dense.pack(W, fmt, transpose=True)), all_inputs
 
     @staticmethod
     @first_derivatives_only
     def backward(ctx, kept, dZ):
         dZ = dZ.contiguous()
-        W, gamma, beta, *A8, codes, scales, mean, rstd = kept
+        W, gamma, beta, *A8, codes, scales, mean, rstd, _ = kept
         A8, H8 = dense.Packed(*A8, *ctx.of_table), dense.Packed(codes, scales, *ctx.of_table)
         groups, eps, activation = ctx.args
         dA = dgamma = dbeta = dW = None
@@ -235,9 +238,9 @@ class GCN2Packed(torch.nn.Module):
         self.format, self.grad_format = format, grad_format
 
     def forward(self, X) -> torch.Tensor:
-        A1 = self.agg(_PackedTransform.apply(X, self.W1, self.format, self.grad_format))
+        A1 = self.agg(_PackedTransform.apply(X, self.W1, self.format, self.grad_format)[0])
         Z2 = _NormTransform.apply(A1, self.gamma, self.beta, self.W2, self.groups, self.eps, self.activation,
-                                  self.format, self.grad_format)
+                                  self.format, self.grad_format)[0]
         return self.agg(Z2)
 
 

@@ -175,3 +175,51 @@ def test_rows_to_experts_and_back(order, around, create):
     got = torch.autograd.grad(around(step, x, w).sum(), (x, w), create_graph=create)
     for a, b in zip(got, torch.autograd.grad(summed(sorted_rows(x, order), order, w).sum(), (x, w))):
         assert torch.allclose(a, b, rtol=0, atol=1e-5)
+
+
+# ----------------------------------------------------------- second derivatives ---
+@pytest.mark.parametrize("unused", [False, True])
+@pytest.mark.parametrize("of", ["X", "W"])
+def test_second_derivatives_are_never_left_out(layer, of, unused):
+    """The weights' gradient depends on X and that of X on the weights.  X and W come
+    from tensors that other parts of the sum depend on too: without an error a gradient
+    that lacks this part would come back."""
+    call, _ = layer
+    a, b = numbers(5, 4, seed=1), numbers(4, 3, seed=2)
+    X, W = torch.sin(a), torch.cos(b)
+    Z = call(X, W)
+    g, = torch.autograd.grad(Z.sum(), W if of == "X" else X, create_graph=True)
+    assert g.requires_grad
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(Z.sum() + g.square().sum(), a if of == "X" else b, allow_unused=unused)
+
+
+def test_second_derivatives_by_the_output_gradient(layer):
+    call, _ = layer
+    X, W, dZ = numbers(5, 4, seed=1), numbers(4, 3, seed=2), numbers(5, 3, seed=3)
+    for v in (X, W):
+        g, = torch.autograd.grad(call(X, W), v, dZ, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(g.sum() + dZ.sum(), dZ)
+
+
+@pytest.mark.parametrize("of", ["y", "weights"])
+def test_second_derivatives_of_weighted_sums(order, of):
+    a, b = numbers(6, 4, seed=1), numbers(3, 2, seed=2)
+    y, w = torch.sin(a), torch.cos(b)
+    out = experts.combine(y, order, w)
+    g, = torch.autograd.grad(out.sum(), w if of == "y" else y, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        torch.autograd.grad(out.sum() + g.square().sum(), a if of == "y" else b)
+
+
+def test_nothing_is_kept_for_second_derivatives(layer):
+    """What a gradient hangs on is of no size."""
+    call, _ = layer
+    X, W = numbers(5, 4, seed=1), numbers(4, 3, seed=2)
+    seen = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (seen.append(t), t)[1], lambda t: t):
+        Z = call(X, W)
+    assert not any(t.untyped_storage().data_ptr() in (X.untyped_storage().data_ptr(), Z.untyped_storage().data_ptr())
+                   for t in seen)
+    torch.autograd.grad(Z.sum(), (X, W))
