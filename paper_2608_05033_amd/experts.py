@@ -24,6 +24,8 @@ from .autograd import first_derivatives_only
 from .dense import TYPES, Packed4, _float32, _on_its_device, _raw_stream, _table, _uint8
 
 _int32 = torch.int32
+_forward = torch.autograd.forward_ad
+_tracing = torch._C._get_tracing_state
 _INDEX_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
@@ -222,16 +224,26 @@ class _WeightedSum(torch.autograd.Function):
         return *combine_backward(dout.contiguous(), y, ctx.route, weights, need_dy, need_dweights), None
 
 
+def _watched():
+    """Whether torch may be following tensors by other ways than gradients: inside a
+    level of forward derivatives, which it refuses here, or in a trace.  Asked for in
+    0.2 us, a tensor for its tangent in 0.4."""
+    return getattr(_forward, "_current_level", 0) >= 0 or _tracing() is not None
+
+
 def dispatch(x: torch.Tensor, route: Route) -> torch.Tensor:
     """x's rows in the order of the route, [rows * k, cols]; zeros behind the last entry."""
-    return _Dispatch.apply(x, route) if x.requires_grad and torch.is_grad_enabled() else _dispatch(x, route)
+    if x.requires_grad and torch.is_grad_enabled() or _watched():
+        return _Dispatch.apply(x, route)
+    return _dispatch(x, route)
 
 
 def combine(y: torch.Tensor, route: Route, weights=None) -> torch.Tensor:
     """out[t] = the sum over j of weights[t, j] times the row of y that entry (t, j) is
     sorted to (weights None: 1), [rows, cols] in y's type, summed in 32 bits.  Gradients
     for y and for weights, which are float32 [rows, k]; with weights no second ones."""
-    if torch.is_grad_enabled() and (y.requires_grad or weights is not None and weights.requires_grad):
+    if torch.is_grad_enabled() and (y.requires_grad or weights is not None and weights.requires_grad) or \
+            _watched():
         return _Sum.apply(y, route) if weights is None else _WeightedSum.apply(y, weights, route)
     return _combine(y, route, weights)
 

@@ -153,13 +153,24 @@ def summed_backward(dout, y, r, weights=None, need_dy=True, need_dweights=True):
 
 @pytest.fixture
 def order(monkeypatch):
-    """The stand-ins work on detached numbers, as the library's calls do."""
+    """The stand-ins work on memory, as the library's calls do: torch sees an empty
+    result of theirs and not how it is filled."""
     def raw(call):
-        return lambda *args: call(*(v.detach() if isinstance(v, torch.Tensor) else v for v in args))
+        def on_memory(first, *args):
+            values = [torch.from_numpy(v.detach().numpy()) if isinstance(v, torch.Tensor) else v
+                      for v in (first, *args)]
+            result = call(*values)
+            out = first.detach().new_empty(result.shape)
+            out.numpy()[:] = result.numpy()
+            return out
+        return on_memory
+
+    def raw_backward(*args):
+        return summed_backward(*(v.detach() if isinstance(v, torch.Tensor) else v for v in args))
 
     monkeypatch.setattr(experts, "_dispatch", raw(sorted_rows))
     monkeypatch.setattr(experts, "_combine", raw(summed))
-    monkeypatch.setattr(experts, "combine_backward", raw(summed_backward))
+    monkeypatch.setattr(experts, "combine_backward", raw_backward)
     return Order()
 
 
@@ -223,3 +234,37 @@ def test_nothing_is_kept_for_second_derivatives(layer):
     assert not any(t.untyped_storage().data_ptr() in (X.untyped_storage().data_ptr(), Z.untyped_storage().data_ptr())
                    for t in seen)
     torch.autograd.grad(Z.sum(), (X, W))
+
+
+# ------------------------------------------------------------------ forward mode ---
+def test_forward_derivatives_are_refused(order, layer):
+    """A tangent is never left out: torch names the function that has no rule for it."""
+    import torch.autograd.forward_ad as forward
+
+    x, y, w = torch.ones(3, 4), torch.ones(6, 4), torch.ones(3, 2)
+    with forward.dual_level():
+        dual = {v: forward.make_dual(v, torch.ones_like(v)) for v in (x, y, w)}
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad):
+                for f in (lambda: experts.dispatch(dual[x], order), lambda: experts.combine(dual[y], order),
+                          lambda: experts.combine(dual[y], order, w), lambda: experts.combine(y, order, dual[w]),
+                          lambda: experts.combine(dual[y], order, dual[w]),
+                          lambda: layer[0](dual[x], torch.ones(4, 3))):
+                    with pytest.raises(NotImplementedError, match="forward mode"):
+                        f()
+        # tensors without a tangent are as they were
+        assert torch.equal(experts.dispatch(x, order), sorted_rows(x, order))
+        assert torch.equal(experts.combine(y, order, w), summed(y, order, w))
+
+
+def test_traced_calls_are_recorded(order):
+    """A trace holds the call, and not the memory that its result had when it was traced."""
+    def step(x, w):
+        return experts.combine(experts.dispatch(x, order), order, w)
+
+    traced = torch.jit.trace(step, (torch.ones(3, 4), torch.ones(3, 2)), check_trace=False)
+    x, w = numbers(3, 4, seed=1).detach(), numbers(3, 2, seed=2).detach()
+    assert torch.equal(traced(x, w), step(x, w))
+    plain = torch.jit.trace(lambda x: experts.combine(experts.dispatch(x, order), order), torch.ones(3, 4),
+                            check_trace=False)
+    assert torch.equal(plain(x), experts.combine(experts.dispatch(x, order), order))

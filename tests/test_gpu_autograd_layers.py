@@ -1,5 +1,6 @@
 """What autograd makes of the layers' functions with the kernels under them: second
-derivatives by way of other tensors, checkpoints, weights changed under way."""
+derivatives by way of other tensors, checkpoints, weights changed under way, forward
+derivatives, traces."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -10,7 +11,7 @@ if not torch.cuda.is_available():  # pragma: no cover - CPU container
 
 from torch.utils.checkpoint import checkpoint  # noqa: E402
 
-from paper_2608_05033_amd import gcn  # noqa: E402
+from paper_2608_05033_amd import experts, gcn  # noqa: E402
 
 
 def numbers(*shape, seed):
@@ -60,3 +61,30 @@ def test_weights_changed_between_the_passes():
     with torch.no_grad():
         W.mul_(3)
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(Z.sum(), (X, W)), want))
+
+
+def test_forward_derivatives_are_refused():
+    import torch.autograd.forward_ad as forward
+
+    r = experts.route(torch.tensor([[0, 1], [1, 2], [2, -1]], device="cuda"), 3)
+    x, y, w = (torch.ones(*size, device="cuda") for size in ((3, 8), (6, 8), (3, 2)))
+    want = experts.dispatch(x, r), experts.combine(y, r, w)
+    with forward.dual_level():
+        dual = {v: forward.make_dual(v, torch.ones_like(v)) for v in (x, y, w)}
+        for f in (lambda: experts.dispatch(dual[x], r), lambda: experts.combine(dual[y], r),
+                  lambda: experts.combine(dual[y], r, w), lambda: experts.combine(y, r, dual[w]),
+                  lambda: gcn.transform4(dual[x], torch.ones(8, 4, device="cuda"))):
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                f()
+        assert torch.equal(experts.dispatch(x, r), want[0]) and torch.equal(experts.combine(y, r, w), want[1])
+
+
+def test_traced_calls_are_recorded():
+    r = experts.route(torch.tensor([[0, 1], [1, 2], [2, -1]], device="cuda"), 3)
+
+    def step(x, w):
+        return experts.combine(experts.dispatch(x, r), r, w), experts.combine(experts.dispatch(x, r), r)
+
+    x, w = numbers(3, 8, seed=1).detach(), numbers(3, 2, seed=2).detach()
+    traced = torch.jit.trace(step, (torch.ones_like(x), torch.ones_like(w)), check_trace=False)
+    assert all(torch.equal(a, b) for a, b in zip(traced(x, w), step(x, w)))
