@@ -144,11 +144,12 @@ class _PackedTransform(torch.autograd.Function):
 class _Transform4(torch.autograd.Function):
     """X.W and both gradients as products of 4-bit tables, each packed along its own
     sum.  What the backward pass needs of X and W is kept packed along the other side,
-    at half a byte an element."""
+    at half a byte an element.  grad: whether there will be one (torch asks for no
+    gradients within forward, and names the inputs that require one all the same)."""
 
     @staticmethod
-    def forward(ctx, X, W):
-        need_dX, need_dW = ctx.needs_input_grad
+    def forward(ctx, X, W, grad):
+        need_dX, need_dW = (grad and need for need in ctx.needs_input_grad[:2])
         X4, Xt = dense.pack4_both(X) if need_dW else (dense.pack4(X), None)
         W4, Wt = dense.pack4_both(W) if need_dX else (None, dense.pack4(W, transpose=True))
         ctx.dtypes, ctx.sizes = (X.dtype, W.dtype), (X.shape[0], W.shape[1])
@@ -160,7 +161,7 @@ class _Transform4(torch.autograd.Function):
     @staticmethod
     @first_derivatives_only
     def backward(ctx, kept, dZ):
-        need_dX, need_dW = ctx.needs_input_grad
+        need_dX, need_dW = ctx.needs_input_grad[:2]
         rows, n = ctx.sizes
         dX = dW = None
         if need_dX and need_dW:
@@ -173,7 +174,7 @@ class _Transform4(torch.autograd.Function):
             dX = dense.product4(G, dense.Packed4(*kept[:2], n), dtype=ctx.dtypes[0])
         if need_dW:
             dW = dense.product4(dense.Packed4(*kept[-3:-1], rows), Gt, dtype=ctx.dtypes[1])
-        return dX, dW
+        return dX, dW, None
 
 
 def transform4(X: torch.Tensor, W: torch.Tensor) -> torch.Tensor:
@@ -184,7 +185,7 @@ def transform4(X: torch.Tensor, W: torch.Tensor) -> torch.Tensor:
     captured into a graph takes leaves of its own (X.detach().requires_grad_())."""
     if X.dim() != 2 or W.dim() != 2 or X.shape[1] != W.shape[0]:
         raise ValueError(f"X and W must be matrices that fit, got {tuple(X.shape)} and {tuple(W.shape)}")
-    return _Transform4.apply(X, W)[0]
+    return _Transform4.apply(X, W, torch.is_grad_enabled())[0]
 
 
 class _NormTransform(torch.autograd.Function):

@@ -268,3 +268,24 @@ def test_traced_calls_are_recorded(order):
     plain = torch.jit.trace(lambda x: experts.combine(experts.dispatch(x, order), order), torch.ones(3, 4),
                             check_trace=False)
     assert torch.equal(plain(x), experts.combine(experts.dispatch(x, order), order))
+
+
+# ------------------------------------------------------- only what is asked for ---
+@pytest.mark.parametrize("need_X,need_W,grad,forward,backward", [
+    (True, True, True, ["pack4_both", "pack4_both", "product4"], ["pack4_both", "product4", "product4"]),
+    (True, False, True, ["pack4", "pack4_both", "product4"], ["pack4", "product4"]),
+    (False, True, True, ["pack4_both", "pack4_transposed", "product4"], ["pack4_transposed", "product4"]),
+    (False, False, True, ["pack4", "pack4_transposed", "product4"], None),
+    (True, True, False, ["pack4", "pack4_transposed", "product4"], None)])
+def test_transform4_packs_what_is_needed(dense, need_X, need_W, grad, forward, backward):
+    """X both ways only where the weights have a gradient, and nothing for a backward
+    pass that gradients switched off will not run."""
+    X, W = numbers(5, 4, seed=1).requires_grad_(need_X), numbers(4, 3, seed=2).requires_grad_(need_W)
+    with torch.set_grad_enabled(grad):
+        Z = gcn.transform4(X, W)
+    assert dense.calls == forward
+    assert torch.equal(Z.detach(), (X @ W).detach()) and Z.requires_grad == (backward is not None)
+    if backward is not None:
+        dense.calls = []
+        Z.sum().backward()
+        assert dense.calls == backward

@@ -88,3 +88,13 @@ def test_traced_calls_are_recorded():
     x, w = numbers(3, 8, seed=1).detach(), numbers(3, 2, seed=2).detach()
     traced = torch.jit.trace(step, (torch.ones_like(x), torch.ones_like(w)), check_trace=False)
     assert all(torch.equal(a, b) for a, b in zip(traced(x, w), step(x, w)))
+
+
+def test_transform4_without_gradients(monkeypatch):
+    """Nothing is packed for a backward pass; the result has the same bits."""
+    X, W = numbers(500, 40, seed=1), numbers(40, 24, seed=2)
+    want = gcn.transform4(X, W).detach()
+    monkeypatch.setattr(gcn.dense, "pack4_both", None)
+    with torch.no_grad():
+        assert torch.equal(gcn.transform4(X, W), want)
+    assert torch.equal(gcn.transform4(X.detach(), W.detach()), want)
