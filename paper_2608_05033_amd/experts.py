@@ -47,6 +47,7 @@ class Route:
         if k < 1 or offsets.numel() < 2 or source.numel() != rows * k:
             raise ValueError(f"offsets, place and source must be [experts + 1], [rows, k] and [rows * k], got "
                              f"{tuple(offsets.shape)}, {tuple(place.shape)} and {tuple(source.shape)}")
+        _fits(k, offsets.numel() - 1)
         self._offsets, self._place, self._source, self._store = offsets, place, source, None
         self.rows, self.k, self.experts, self.index = rows, k, offsets.numel() - 1, index
         self.c = sd_route_t(rows, k, self.experts, offsets.data_ptr(), place.data_ptr(), source.data_ptr())
@@ -94,8 +95,15 @@ class Route:
         return self.index
 
 
+def _fits(k, experts):
+    """Both are 32 bits wide in the library, and ctypes would cut off what is above."""
+    if not (k < 1 << 31 and -(1 << 31) <= experts < 1 << 31):
+        raise ValueError(f"the experts of a row and all experts must be fewer than 2^31, got {k} and {experts}")
+
+
 @functools.lru_cache(maxsize=4096)
 def _route_size(rows, k, experts):
+    _fits(k, experts)
     size = ctypes.c_size_t()
     _check(_lib.sd_route_size(rows, k, experts, size), "sd_route_size")
     return size.value
