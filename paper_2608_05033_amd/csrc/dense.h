@@ -175,6 +175,15 @@ __device__ inline uint32_t largest_finite(const float (&v)[N], int count, int wi
   return __float_as_uint(most);
 }
 
+// What a wave's lanes wrote to shared memory before is there for all of them after it, and what they read
+// before has been read: the unit takes a wave's accesses in order, so this is no instruction, only the order
+// that the compiler keeps to.
+__device__ inline void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Workgroup b of n as a place in a list of which each of the eight XCDs takes a
 // contiguous run: workgroups go to the XCDs in turn, and neighbours in the list
 // then share an L2.

@@ -71,13 +71,13 @@ __device__ inline void place_kinds(const Kinds &kinds, uint32_t experts, int bit
     if (there) {
       const int before = __popcll(same & ((1ull << lane) - 1));
       const uint32_t at = next[kind] + (uint32_t)before;
-      __builtin_amdgcn_wave_barrier();  // every lane has read before one writes
+      wave_order();  // every lane has read before one writes
       if (before == 0) next[kind] = at + (uint32_t)__popcll(same);
       const bool kept = kind < experts;
       place[i] = kept ? (int32_t)at : -1;
       source[at] = kept ? (int32_t)((uint32_t)i / (uint32_t)k) : -1;
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_order();  // and it has been written before one reads again
   }
 }
 

@@ -245,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
       if (lane % SHARE == 0) scales[((int64_t)grp * rows + row) * 4 + lane / SHARE] = (uint8_t)s;
     }
   }
-  __builtin_amdgcn_wave_barrier();
+  wave_order();  // the lanes' rows, before others read them
 #pragma unroll
   for (int h = 0; h < 2; ++h) {  // column h * 64 + l of the wave's 32 rows
     float d[kCols];

@@ -577,6 +577,7 @@ __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Opera
         }
         *reinterpret_cast<Span<T, 4, 4 * sizeof(T)> *>(mine + r * PITCH + at) = o;
       }
+    wave_order();  // before other lanes take them
     __builtin_amdgcn_sched_barrier(0);
   };
   auto get = [&](int row) { return *reinterpret_cast<const Span<T, V, 16> *>(mine + row * PITCH + vc); };
@@ -589,6 +590,7 @@ __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Opera
         const auto o = get(k * STEP + vr);
         *reinterpret_cast<Span<T, V> *>(y + (i * 32 + k * STEP) * stride) = *reinterpret_cast<const Span<T, V> *>(&o);
       }
+      wave_order();  // they have been taken before the next ones come
       __builtin_amdgcn_sched_barrier(0);
     }
     return;
@@ -609,7 +611,7 @@ __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Opera
           if (q < there) to[q] = o.v[q];
       }
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_order();
   }
 }
 
