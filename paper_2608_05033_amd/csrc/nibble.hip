@@ -199,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restri
   constexpr int PITCH = kGroup + 4 / (int)sizeof(T);
   __shared__ __align__(16) T tile[4][32 * PITCH];
   __shared__ __align__(16) u32x4 blocks[4][kGroup];
-  __shared__ uint8_t bytes[kGroup][4];
+  __shared__ __align__(4) uint8_t bytes[kGroup][4];  // read as words
   const int t = threadIdx.x, wave = t >> 6, l = t & 63, lane = l % LANES, down = l / LANES;
   if (workgroup() >= wgs) return;
   // neighbouring strips share lines of the transpose, and run on one XCD

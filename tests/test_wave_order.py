@@ -20,3 +20,16 @@ def test_wave_barriers_stand_behind_fences():
                 if not re.match(r'__builtin_amdgcn_fence\(__ATOMIC_\w+, "wavefront"\);', lines[i - 1]):
                     bare.append(f"{os.path.basename(path)}:{i + 1}")
     assert barriers > 0 and bare == []
+
+
+def test_bytes_in_shared_memory_are_aligned():
+    """They are read as words and more, which a byte's own alignment does not allow."""
+    found, bare = 0, []
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.hip"))):
+        with open(path) as f:
+            for number, line in enumerate(f, 1):
+                if re.search(r"__shared__[^;]*\buint8_t\b", line):
+                    found += 1
+                    if "__align__" not in line:
+                        bare.append(f"{os.path.basename(path)}:{number}")
+    assert found > 0 and bare == []
