@@ -614,6 +614,27 @@ int sd_nibble_product_size(int64_t rows, int64_t cols, int64_t n, size_t *bytes)
 int sd_nibble_product(const sd_nibble_t *X, const sd_nibble_t *W, const float *bias, void *Y, int32_t type,
                       int64_t row_stride, void *workspace, size_t bytes, void *stream);
 
+/* The kernel that a product runs as: tiles of 256 x 256 or 128 x 128 through shared
+ * memory, the latter with two, four or one buffer; tiles of 32 x 32 and 16 x 16 whose
+ * sum waves share (16 x 16: eight or four waves); a wave for each 16 x 32. */
+typedef enum {
+  SD_NIBBLE_TILE_256 = 0,
+  SD_NIBBLE_TILE_128 = 1,
+  SD_NIBBLE_TILE_128_DEEP = 2,
+  SD_NIBBLE_TILE_128_SHORT = 3,
+  SD_NIBBLE_ROWS_32 = 4,
+  SD_NIBBLE_ROWS_16 = 5,
+  SD_NIBBLE_ROWS_16_SHORT = 6,
+  SD_NIBBLE_ROWS_16_ALONG = 7
+} sd_nibble_form_t;
+/* Which form sd_nibble_product (experts 0) or sd_expert_product (rows: entries of the
+ * list) takes on the current device for these sizes and results' type, and the parts
+ * that the sum is split into (1: none), of tables whose rows lie one behind the other.
+ * Results do not depend on it but for the order of sums, and a later version may choose
+ * anew.  Host-only; 256 compute units where there is no device. */
+int sd_nibble_product_form(int64_t rows, int64_t cols, int64_t n, int32_t experts, int32_t type, int32_t *form,
+                           int32_t *parts);
+
 /* --------------------------------------------------- rows sorted by expert --- */
 /* k experts (or node types) for each of `rows` rows, as a list of entries (t, j),
  * j < k, sorted by expert and among one expert's by t, then j.  Entry i < total =

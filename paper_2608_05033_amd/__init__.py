@@ -125,6 +125,8 @@ SD_TYPE_F32, SD_TYPE_F16, SD_TYPE_BF16 = 1, 2, 3
 SD_PACK_E4M3, SD_PACK_E5M2 = 1, 2
 PACK_FORMATS = {"e4m3": SD_PACK_E4M3, "e5m2": SD_PACK_E5M2}
 SD_ACT_NONE, SD_ACT_RELU, SD_ACT_SILU, SD_ACT_GELU = 0, 1, 2, 3
+NIBBLE_FORMS = ("tile_256", "tile_128", "tile_128_deep", "tile_128_short", "rows_32", "rows_16", "rows_16_short",
+                "rows_16_along")
 ACTIVATIONS = {"none": SD_ACT_NONE, "relu": SD_ACT_RELU, "silu": SD_ACT_SILU, "gelu": SD_ACT_GELU}
 
 
@@ -199,6 +201,7 @@ def _load():
     lib.sd_nibble_unpack.argtypes = [nibble, _P, _i32, _i64, _P]
     lib.sd_nibble_product_size.argtypes = [_i64, _i64, _i64, size]
     lib.sd_nibble_product.argtypes = [nibble, nibble, _P, _P, _i32, _i64, _P, ctypes.c_size_t, _P]
+    lib.sd_nibble_product_form.argtypes = [_i64, _i64, _i64, _i32, _i32, ctypes.POINTER(_i32), ctypes.POINTER(_i32)]
     lib.sd_route_size.argtypes = [_i64, _i32, _i32, size]
     lib.sd_route.argtypes = [_P, _i32, route, _P, ctypes.c_size_t, _P]
     lib.sd_dispatch.argtypes = [route, _P, _i32, _i64, _i64, _P, _i64, _P]
@@ -207,8 +210,8 @@ def _load():
     lib.sd_expert_product.argtypes = [nibble, nibble, route, _i32, _P, _P, _i32, _i64, _P]
     for f in ("sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
               "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_pack_both",
-              "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
-              "sd_combine_backward", "sd_expert_product"):
+              "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_nibble_product_form", "sd_route_size",
+              "sd_route", "sd_dispatch", "sd_combine", "sd_combine_backward", "sd_expert_product"):
         getattr(lib, f).restype = ctypes.c_int
     for f in ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_spmm", "sd_plan_info", "sd_plan_export_size",
               "sd_plan_export", "sd_plan_device", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load"):
@@ -221,8 +224,8 @@ EXPORTED = ("sd_analyze", "sd_analyze_device", "sd_plan", "sd_plan_ex", "sd_plan
             "sd_plan_export", "sd_plan_destroy", "sd_plan_cache_clear", "sd_plan_cache_size", "sd_plan_cache_save", "sd_plan_cache_load", "sd_release_memory", "sd_status_string", "sd_last_error",
             "sd_pack", "sd_unpack", "sd_pack_product", "sd_pack_gradient_size", "sd_pack_gradient",
             "sd_group_norm_size", "sd_group_norm", "sd_group_norm_backward", "sd_nibble_pack", "sd_nibble_pack_both",
-            "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_route_size", "sd_route", "sd_dispatch", "sd_combine",
-            "sd_combine_backward", "sd_expert_product")
+            "sd_nibble_unpack", "sd_nibble_product_size", "sd_nibble_product", "sd_nibble_product_form", "sd_route_size",
+            "sd_route", "sd_dispatch", "sd_combine", "sd_combine_backward", "sd_expert_product")
 
 
 def _check(status: int, where: str):
@@ -479,6 +482,13 @@ def sd_nibble_product(X: sd_nibble_t, W: sd_nibble_t, bias, Y, type: int, row_st
     """Y = X.W^T (+ bias) of two 4-bit tables."""
     _check(_lib.sd_nibble_product(X, W, _devptr(bias), _devptr(Y), type, row_stride, _devptr(workspace), bytes,
                                   _stream(stream)), "sd_nibble_product")
+
+
+def sd_nibble_product_form(rows: int, cols: int, n: int, experts: int, type: int) -> tuple[str, int]:
+    """(one of NIBBLE_FORMS, parts of a split sum) of a 4-bit product on the current device."""
+    form, parts = _i32(), _i32()
+    _check(_lib.sd_nibble_product_form(rows, cols, n, experts, type, form, parts), "sd_nibble_product_form")
+    return NIBBLE_FORMS[form.value], parts.value
 
 
 def sd_route_size(rows: int, k: int, experts: int) -> int:

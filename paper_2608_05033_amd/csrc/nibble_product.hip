@@ -673,7 +673,16 @@ struct Call {
   float *parts;  // workspace of a split sum
 };
 
-enum Form { kTile256, kTile128, kTile128Deep, kTile128Short, kRows32, kRows16, kRows16Short, kRows16Along };
+enum Form {
+  kTile256 = SD_NIBBLE_TILE_256,
+  kTile128 = SD_NIBBLE_TILE_128,
+  kTile128Deep = SD_NIBBLE_TILE_128_DEEP,
+  kTile128Short = SD_NIBBLE_TILE_128_SHORT,
+  kRows32 = SD_NIBBLE_ROWS_32,
+  kRows16 = SD_NIBBLE_ROWS_16,
+  kRows16Short = SD_NIBBLE_ROWS_16_SHORT,
+  kRows16Along = SD_NIBBLE_ROWS_16_ALONG
+};
 struct Plan {
   Form form;
   int32_t splits, split_stages;
@@ -831,6 +840,8 @@ int product(const Call &c, const Plan &p, void *Y, int32_t type, void *stream) {
 
 // The large tiles keep the distance of a tile's rows in 32 bits.
 bool near_rows(const sd_nibble_t *p) { return p->ld <= (1 << 23); }
+// Of rows sorted by expert, X's from anywhere, and so their distance from its first one.
+bool near_entries(int64_t ld, int64_t rows) { return rows <= (1ll << 32) / (ld > 0 ? ld : 1); }
 
 Operand operand(const sd_nibble_t *p) { return Operand{p->codes, p->scales, p->ld, p->rows}; }
 
@@ -841,6 +852,19 @@ extern "C" int sd_nibble_product_size(int64_t rows, int64_t cols, int64_t n, siz
   if (rows > kMaxRows || n > kMaxRows || cols > kMaxRows - 1024) return SD_ERR_OVERFLOW;
   // results of any type: it has no say in how a sum is split
   *bytes = rows == 0 || n == 0 ? 0 : parts_bytes(plan_of(rows, 0, n, cols, SD_TYPE_BF16, true), rows, n);
+  return SD_OK;
+}
+
+extern "C" int sd_nibble_product_form(int64_t rows, int64_t cols, int64_t n, int32_t experts, int32_t type,
+                                      int32_t *form, int32_t *parts) {
+  if (!form || !parts || rows < 1 || cols < 0 || n < 1 || experts < 0 || !type_ok(type)) return SD_ERR_INVALID_VALUE;
+  if (rows > kMaxRows || n > kMaxRows || cols > kMaxRows - 1024) return SD_ERR_OVERFLOW;
+  if (experts > kMaxExperts) return SD_ERR_UNSUPPORTED;
+  const int64_t ld = col_blocks(cols) * 16;
+  const bool near = ld <= (1 << 23) && (experts == 0 || near_entries(ld, rows));
+  const Plan p = plan_of(rows, experts, n, cols, type, near);
+  *form = p.form;
+  *parts = p.splits;
   return SD_OK;
 }
 
@@ -879,8 +903,7 @@ extern "C" int sd_expert_product(const sd_nibble_t *X, const sd_nibble_t *W, con
   if (bias && !aligned_to(bias, 4)) return SD_ERR_INVALID_VALUE;
   if (total == 0 || n == 0) return SD_OK;
   if ((st = have_device()) != SD_OK) return st;
-  // the large tiles take X's rows from anywhere and keep their distance from its first one in 32 bits
-  const bool near = near_rows(W) && X->rows <= (1ll << 32) / (X->ld > 0 ? X->ld : 1);
+  const bool near = near_rows(W) && near_entries(X->ld, X->rows);
   const Plan p = plan_of(total, route->experts, n, X->cols, type, near);
   const Call c{operand(X), operand(W), Sorted{route->offsets, sorted ? nullptr : route->source, route->experts, total},
                bias, row_stride, total, n, (int32_t)col_blocks(X->cols), (int32_t)groups_of(X->cols), nullptr};
