@@ -181,7 +181,7 @@ class Packed4:
     columns begun, zeros past cols), and scales uint8 [ceil(cols / 128), rows, 4].
     A code's value is e2m1(code) times 2^(scale - 127); 255 makes a block NaN."""
 
-    __slots__ = ("_codes", "_scales", "_store", "rows", "cols", "index", "c")
+    __slots__ = ("_codes", "_scales", "store", "rows", "cols", "index", "c")
 
     def __init__(self, codes, scales, cols: int):
         index = codes.get_device()
@@ -195,41 +195,54 @@ class Packed4:
             raise ValueError(f"codes must hold {cols} columns, two in a byte and rounded up to 32, next to each other")
         if scales.shape != ((cols + 127) // 128, rows, 4) or not scales.is_contiguous():
             raise ValueError(f"scales must be contiguous [{-(-cols // 128)}, {rows}, 4], got {tuple(scales.shape)}")
-        self._codes, self._scales, self._store, self.rows, self.cols, self.index = codes, scales, None, rows, cols, index
+        self._codes, self._scales, self.store, self.rows, self.cols, self.index = codes, scales, None, rows, cols, index
         self.c = sd_nibble_t(rows, cols, ld if rows > 1 and cols else need, 0, codes.data_ptr(), scales.data_ptr())
 
     @classmethod
     def empty(cls, rows: int, cols: int, like):
         """A new one on the device of the tensor `like`: one allocation for codes and
         scales, which become tensors of their own when they are asked for."""
+        size = rows * ((cols + 31) // 32 * 16)
+        return cls._laid_out(like.new_empty(size + (cols + 127) // 128 * rows * 4, dtype=_uint8), rows, cols)
+
+    @classmethod
+    def of(cls, store, rows: int, cols: int):
+        """The one whose codes and, behind them, scales are `store`, the `store` of
+        another of this size (or a copy of it)."""
+        size = rows * ((cols + 31) // 32 * 16) + (cols + 127) // 128 * rows * 4
+        if store.dtype != _uint8 or not store.is_cuda or store.shape != (size,) or not store.is_contiguous():
+            raise ValueError(f"store must be {size} uint8 in a row on the GPU, got {store.dtype} {tuple(store.shape)} "
+                             f"on {store.device}")
+        return cls._laid_out(store, rows, cols)
+
+    @classmethod
+    def _laid_out(cls, store, rows, cols):
         ld = (cols + 31) // 32 * 16
-        size = rows * ld
-        store = like.new_empty(size + (cols + 127) // 128 * rows * 4, dtype=_uint8)
         p, at = cls.__new__(cls), store.data_ptr()
-        p._codes, p._scales, p._store, p.rows, p.cols, p.index = None, None, store, rows, cols, store.get_device()
-        p.c = sd_nibble_t(rows, cols, ld, 0, at, at + size)
+        p._codes, p._scales, p.store, p.rows, p.cols, p.index = None, None, store, rows, cols, store.get_device()
+        p.c = sd_nibble_t(rows, cols, ld, 0, at, at + rows * ld)
         return p
 
     @property
     def codes(self):
         if self._codes is None:
             ld = self.c.ld
-            self._codes = self._store.as_strided((self.rows, ld), (ld, 1))
+            self._codes = self.store.as_strided((self.rows, ld), (ld, 1))
         return self._codes
 
     @property
     def scales(self):
         if self._scales is None:
             shape = (self.cols + 127) // 128, self.rows, 4
-            self._scales = self._store.as_strided(shape, (self.rows * 4, 4, 1), self.rows * self.c.ld)
+            self._scales = self.store.as_strided(shape, (self.rows * 4, 4, 1), self.rows * self.c.ld)
         return self._scales
 
     def new_empty(self, *args, **kw):
-        return (self._codes if self._store is None else self._store).new_empty(*args, **kw)
+        return (self._codes if self.store is None else self.store).new_empty(*args, **kw)
 
     @property
     def device(self):
-        return (self._codes if self._store is None else self._store).device
+        return (self._codes if self.store is None else self.store).device
 
     def get_device(self) -> int:
         return self.index

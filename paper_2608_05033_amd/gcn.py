@@ -121,12 +121,12 @@ class _PackedTransform(torch.autograd.Function):
         X8 = X if isinstance(X, dense.Packed) else dense.pack(X, fmt)
         ctx.of_table = X8.cols, X8.format
         kept = [X8.codes, X8.scales]
+        all_inputs = None
         if ctx.needs_input_grad[0]:
-            ctx.dtype, ctx.grad_fmt = X.dtype, grad_fmt
-            kept.append(W)
-        kept.append(anchor(W))
+            ctx.dtype, ctx.grad_fmt, all_inputs = X.dtype, grad_fmt, anchor(W)
+            kept += W, all_inputs
         ctx.save_for_backward(*kept)
-        return dense.product(X8, dense.pack(W, X8.format, transpose=True)), kept[-1]
+        return dense.product(X8, dense.pack(W, X8.format, transpose=True)), all_inputs
 
     @staticmethod
     @first_derivatives_only
@@ -152,17 +152,17 @@ class _Transform4(torch.autograd.Function):
         need_dX, need_dW = (grad and need for need in ctx.needs_input_grad[:2])
         X4, Xt = dense.pack4_both(X) if need_dW else (dense.pack4(X), None)
         W4, Wt = dense.pack4_both(W) if need_dX else (None, dense.pack4(W, transpose=True))
-        ctx.dtypes, ctx.sizes = (X.dtype, W.dtype), (X.shape[0], W.shape[1])
-        all_inputs = anchor(W)
-        ctx.save_for_backward(*(() if W4 is None else (W4.codes, W4.scales)),
-                              *(() if Xt is None else (Xt.codes, Xt.scales)), all_inputs)
+        ctx.dtypes, ctx.sizes = (X.dtype, W.dtype), (X.shape[0], *W.shape)
+        all_inputs = anchor(W) if need_dX and need_dW else None  # each one's gradient depends on the other
+        ctx.save_for_backward(W4 and W4.store, Xt and Xt.store, all_inputs)
         return dense.product4(X4, Wt), all_inputs
 
     @staticmethod
     @first_derivatives_only
     def backward(ctx, kept, dZ):
         need_dX, need_dW = ctx.needs_input_grad[:2]
-        rows, n = ctx.sizes
+        W4, Xt, _ = kept
+        rows, cols, n = ctx.sizes
         dX = dW = None
         if need_dX and need_dW:
             G, Gt = dense.pack4_both(dZ)
@@ -171,9 +171,9 @@ class _Transform4(torch.autograd.Function):
         else:
             Gt = dense.pack4(dZ, transpose=True)
         if need_dX:
-            dX = dense.product4(G, dense.Packed4(*kept[:2], n), dtype=ctx.dtypes[0])
+            dX = dense.product4(G, dense.Packed4.of(W4, cols, n), dtype=ctx.dtypes[0])
         if need_dW:
-            dW = dense.product4(dense.Packed4(*kept[-3:-1], rows), Gt, dtype=ctx.dtypes[1])
+            dW = dense.product4(dense.Packed4.of(Xt, cols, rows), Gt, dtype=ctx.dtypes[1])
         return dX, dW, None
 
 

@@ -15,6 +15,12 @@ class Table:
 
     def __init__(self, codes, scales, cols, format="e4m3"):
         self.codes, self.scales, self.rows, self.cols, self.format = codes, scales, codes.shape[0], cols, format
+        self.store = codes
+
+    @classmethod
+    def of(cls, store, rows, cols):
+        assert store.shape == (rows, cols)
+        return cls(store, None, cols)
 
 
 class Dense:

@@ -98,3 +98,18 @@ def test_transform4_without_gradients(monkeypatch):
     with torch.no_grad():
         assert torch.equal(gcn.transform4(X, W), want)
     assert torch.equal(gcn.transform4(X.detach(), W.detach()), want)
+
+
+def test_kept_tables_go_through_autograds_hooks():
+    """Packed copies moved to the host between the passes give the same gradients; ones
+    that stay there, or come back as something else, are refused."""
+    X, W = numbers(50, 40, seed=1), numbers(40, 24, seed=2)
+    want = torch.autograd.grad(gcn.transform4(X, W).sum(), (X, W))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (t.device, t.cpu()), lambda kept: kept[1].to(kept[0])):
+        Z = gcn.transform4(X, W)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(Z.sum(), (X, W)), want))
+    for back in (lambda t: t, lambda t: t.cuda()[:-16], lambda t: t.cuda().float()):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t.cpu(), back):
+            Z = gcn.transform4(X, W)
+        with pytest.raises(ValueError, match="store"):
+            torch.autograd.grad(Z.sum(), (X, W))
