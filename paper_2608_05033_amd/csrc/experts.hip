@@ -6,9 +6,10 @@
 // last.  A wave counts a run of neighbouring entries 64 at a time; lanes of equal
 // kind find each other with one ballot for each bit of the kind, and a lane's rank
 // among them is the number of such lanes before it.  Nothing depends on the order
-// in which waves run.  Up to 8192 entries take one launch (74 entries 3.7 us, 8192
-// 10), more three (2^19 entries of 8 experts 13 us, 2^22 33): latency of launches and
-// loads, the entries' bytes would take 2 and 13.
+// in which waves run.  Up to 8192 entries take one launch (74 entries 3.8 us, 8192
+// 10), more three (calls in a row: 2^19 entries of 8 experts 13 us, 2^22 33; as the
+// first of a pass, with entries from memory, 2^15 to 2^19 take 17 to 20): latency of
+// launches and loads, the entries' bytes would take 2 and 13.
 #include <type_traits>
 
 #include "nibble.h"
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(kThreads) void k_dispatch(const T *__restrict__ x, 
 }
 
 // out[t] = sum over j, in this order, of weights[t, j] y[place[t, j]].  Bound by the
-// bytes: 71 to 87 us at those sizes, 4.6 to 5.7 TB/s.
+// bytes: 83 us at those sizes (74 to 92), 4.9 TB/s.
 template <typename T, int LANES, int KB, int V>
 __global__ __launch_bounds__(kThreads) void k_combine(const T *__restrict__ y, int64_t y_stride, int64_t rows,
                                                       int32_t k, int32_t cols, const int32_t *__restrict__ place,
@@ -388,7 +389,8 @@ __global__ __launch_bounds__(kThreads) void k_combine_backward(const T *__restri
 
 // Calls f(lanes, entries at a time, columns of a step) for rows of `cols`
 // elements: lanes for a whole row up to 32, then 64.  Measured in us (to the experts, back,
-// gradients):
+// gradients), calls in a row, whose rows the caches hold in part (with rows from memory
+// 20011, 4, 601 bf16 take 32, 38 and 60):
 //   rows, entries of each, columns     8 lanes       16           32           64
 //   262144, 2, 128 fp32               82, 78, 136  75, 73, 125  76, 71, 119  104, 83, 146
 //   262144, 2, 129 fp32             165, 121, 246 116, 92, 197  93, 81, 157  116, 94, 171

@@ -57,7 +57,7 @@ struct Ends {
 // A group of WIDE / V lanes takes one row's group of 128 columns, of which there are
 // at most WIDE: V neighbouring columns per lane (16 bytes), the largest bits of each
 // block over its 32 / V lanes, V codes per lane back.  Bound by the bytes, four groups
-// in flight: 262144 x 128 fp32 take 23 us, 6.6 TB/s of bytes that the 256 MB Infinity
+// in flight: 262144 x 128 fp32 take 24 us, 6.3 TB/s of bytes that the 256 MB Infinity
 // Cache partly serves; 563394 x 127 bf16 35.  COLS: consecutive elements of a row lie together (else any
 // strides, each lane's elements read one by one).
 template <typename T, int WIDE, bool COLS, bool EVEN>
@@ -184,8 +184,9 @@ __global__ __launch_bounds__(kThreads) void k_nibble_pack_across(const T *__rest
 // the columns as k_nibble_pack does, leaves them in shared memory and takes them
 // column by column, so that a lane has a block of the transpose.  The four waves'
 // blocks of a column leave together, 64 bytes of codes and a word of scales.  Bound by
-// the bytes, two workgroups a compute unit for fp32: 2^18 x 256 take 75 us, 4.5 TB/s,
-// where the two ways one after the other take 102.
+// the bytes, two workgroups a compute unit for fp32: 2^18 x 256 take 71 us with calls in
+// a row, 4.8 TB/s, where the two ways one after the other take 102; in a training step,
+// behind other tables, 85.
 template <typename T, bool EVEN>
 __global__ __launch_bounds__(kThreads) void k_nibble_pack_both(const T *__restrict__ x, int64_t row_stride,
                                                                int64_t rows, int32_t cols, int32_t ng,

@@ -138,8 +138,9 @@ __device__ inline void clear_rows(T *Y, int64_t stride, int64_t m0, int64_t m1, 
 // waves each take every KW-th pair of groups of 128 k and join their sums in shared
 // memory.  Lane (r, g) = (lane % 16, lane / 16) takes block g of a group of row r.
 // Bound by the latency of the loads where there are few tiles: 1 x 4096 x 4096 takes
-// 3.7 us (2.4 TB/s of W), the launch itself 2; by W's bytes where there are many: 16
-// rows through 8 of 64 experts of 1024 x 2048 take 15, 4.6 TB/s.
+// 3.7 us with calls in a row (2.4 TB/s of W) and 4.4 with W from memory, the launch
+// itself 2; by W's bytes where there are many: 16 rows through 8 of 64 experts of 1024 x
+// 2048 take 15, 4.6 TB/s.
 // ALONG: the waves take a tile each, KW neighbouring ones, and the whole sum.
 template <typename T, int MF, int NF, int KW, bool EXPERTS, bool ALONG>
 __global__ __launch_bounds__(KW * 64) void k_nibble_rows(Operand X, Operand W, Sorted sorted,
@@ -271,10 +272,14 @@ __device__ constexpr int wait_until(int left) { return (left & 15) | (left >> 4)
 // that whole lines are written.
 //
 // Bound by the matrix units at the clock that power allows, and by what the requests
-// take from them: 8192 cubed to bf16 takes 245 to 285 us (box and warmth), 3.9 to 4.5
-// PFLOP/s, of which a tile's 32 stages take 60 (2850 cycles each at 1.5 to 1.65 GHz,
-// 2112 of them products), the way in 2.4 and the way out 4.  2048 cubed takes 9.7 us.
+// take from them: 8192 cubed to bf16 takes 250 us and up to 320 as the clock falls, 4.4
+// to 3.4 PFLOP/s, of which a tile's 32 stages take 60 (2850 cycles each at 1.5 to 1.65
+// GHz, 2112 of them products), the way in 2.4 and the way out 4.  2048 cubed takes 9.4.
 // With one buffer four workgroups share a compute unit and cover each other's waits.
+//
+// 256 x 256 tiles use all 512 registers of a lane, and of 16-bit results 16, of fp32
+// ones 8 more lie in scratch (68 and 36 bytes a lane), used outside of the sum's loop
+// alone.
 template <typename T, int BM, int BN, int BUFFERS, bool EXPERTS>
 __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Operand X, Operand W, Sorted sorted,
                                                              const float *__restrict__ bias, T *__restrict__ Y,
@@ -529,8 +534,9 @@ __global__ __launch_bounds__(256, BUFFERS == 1 ? 3 : 1) void k_nibble_tile(Opera
   asm volatile("" ::: "memory");
 
   // The bias, by way of shared memory: every lane needs 16 of each 32 columns'.  Added (zeros without one) where the
-  // results leave, so that the accumulators stay in one place: 8192 x 8192 x 2048 to fp32 takes 116 us, not 138.
-  // The large tiles of 16-bit results, which leave more registers, add it here: 8192 cubed without one 242 and 247.
+  // results leave, so that the accumulators stay in one place: 8192 x 8192 x 2048 to fp32 in 256 x 256 tiles takes
+  // 113 us with one, and took 138.  Large tiles of 16-bit results add it here: 8192 cubed without a bias takes 242 us
+  // so and 247 with it added late, and 260 with one.
   constexpr bool LATE = MF * NF != 16 || sizeof(T) == 4;
   f32x4 add[NF][4] = {};
   if (bias) {
@@ -698,32 +704,33 @@ int64_t row_tiles(int64_t rows, int32_t experts, int64_t bm) {
 // Measured in us, 16-bit results, launches in a row (256 compute units; 128 x 128 with the better number of
 // buffers; "s": such tiles with the sum in so many parts, joined by a second launch):
 //   rows x columns x k      256x256   128x128  32x32  16x16   s4    s16   s64   s128
-//   8192 x 8192 x 8192          243       300   2234
-//   8192 x 8192 x 512            50        41    288    298
-//   4096 x 4096 x 4096           37        42    282    559
-//   2048 x 2048 x 2048           17       9.5     41     73
-//   1000 x 1000 x 1000           15       6.7    9.2     12
-//   256 x 4096 x 4096            23        10     20     37    20    26
-//   64 x 4096 x 4096             25        11    7.1     11    12    22
-//   512 x 512 x 4096             24        11    7.2     11    11    18
-//   1 x 4096 x 4096              23        10    5.2    3.7     9    12
-//   262144 x 128 x 128           59        19    120    106
-//   1000000 x 20 x 128          235        64    172    119
-//   512 x 512 x 32768           147        55     39     72    21    19    43
-//   64 x 64 x 65536             273       103     71     37    33    15    11     11
-//   256 x 128 x 262144         1110       406    278    142   108    34    19     20
+//   8192 x 8192 x 8192          251       301   2234
+//   8192 x 8192 x 512            50        36    273    304
+//   4096 x 4096 x 4096           40        44    282    559
+//   2048 x 2048 x 2048           17       9.4     41     73
+//   1000 x 1000 x 1000           15       7.0    9.1     12
+//   256 x 4096 x 4096            23        11     21     37    20    36
+//   64 x 4096 x 4096             24        11    7.1     11    12    22
+//   512 x 512 x 4096             23        10    7.2     11    11    18
+//   1 x 4096 x 4096              23        10    5.7    3.8     9    13
+//   262144 x 128 x 128           52        17    111    103
+//   1000000 x 20 x 128          214        54    164    115
+//   512 x 512 x 32768           144        55     40     72    22    20    43
+//   64 x 64 x 65536             266       103     71     37    33    15    11     11
+//   256 x 128 x 262144         1094       405    278    141   108    34    19     21
 // A stage of 256 k takes a lone 128 x 128 tile 0.5 us, and the parts go to memory and back at about
-// 2.5 TB/s: that gives the number of parts.
+// 2.5 TB/s: that gives the number of parts.  So it is for operands that the caches hold; 256 x 128 x 262144 in a
+// training step, whose operands come from memory, takes 69 parts 24 + 4 us, on 138 of the compute units.
 //
 // Rows sorted by expert, us, launches in a row (rows of X, experts of each, experts, columns x k; 16 x 16 with
 // the best of sums shared by the waves or not):
 //                              256x256   128x128  32x32  16x16
-//   4096, 2, 16, 4096 x 4096        106       104    634    869
-//   1024, 2, 16, 4096 x 4096         40        39    173    230
-//   64, 2, 16, 4096 x 4096           33        25     38     28
-//   16, 2, 16, 4096 x 4096           32        22     32     26
-//   64, 8, 64, 1024 x 2048           23        17     26     17
-//   16, 8, 64, 1024 x 2048           22        16     24     15
+//   4096, 2, 16, 4096 x 4096        111       104    632    870
+//   1024, 2, 16, 4096 x 4096         44        39    172    228
+//   64, 2, 16, 4096 x 4096           35        26     38     28
+//   16, 2, 16, 4096 x 4096           35        25     36     27
+//   64, 8, 64, 1024 x 2048           26        17     27     17
+//   16, 8, 64, 1024 x 2048           21        15     23     15
 //   1, 8, 64, 1024 x 2048            17         9    5.3    4.4
 Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, int32_t type, bool near) {
   const int64_t cus = cu_count(), stages = ceil_div(cols, 256);
@@ -743,10 +750,10 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, int32_t typ
                   : stages <= 3 && waves >= 2 * cus && (thin <= 16 || waves * ceil_div(cols, 128) <= 30 * cus))
     return whole(kRows16Along);
   if (near && (!few || spread)) {
-    // Large tiles, us with them and with one buffer of 128 x 128: 4096 x 4096 x 2048 25.3 and 26.7 to bf16, 30.5 and
-    // 30.6 to fp32, 8192 x 8192 x 2048 118 and 102 to fp32, 4096 cubed 44 and 49.  Of rows sorted by expert, whose
-    // tiles begin with two more loads, where they are many: 16384 rows to 2 of 16, 4096 x 4096, 355 and 367, 8192 to
-    // 2 of 8 183 and 178, 4096 to 2 of 16 112 and 103.  Not where they cover much more than there is.
+    // Large tiles, us with them and with one buffer of 128 x 128: 4096 x 4096 x 2048 25.5 and 26.2 to bf16, 30.6 and
+    // 30.6 to fp32, 8192 x 8192 x 2048 111 and 100 to fp32, 4096 cubed 44 and 49.  Of rows sorted by expert, whose
+    // tiles begin with two more loads, where they are many: 16384 rows to 2 of 16, 4096 x 4096, 364 and 368, 8192 to
+    // 2 of 8 179 and 178, 4096 to 2 of 16 111 and 104.  Not where they cover much more than there is.
     const int64_t large = tiles(256, 256);
     if (stages >= (type == SD_TYPE_F32 ? 12 : 8) && 4 * large >= 3 * cus && 32 * large <= 9 * tiles(128, 128) &&
         (experts == 0 || large * stages >= 80 * cus))
@@ -765,10 +772,10 @@ Plan plan_of(int64_t rows, int32_t experts, int64_t n, int64_t cols, int32_t typ
       }
     }
     // Buffers for 128 x 128: one, and four workgroups a compute unit, where there are more tiles than units or
-    // the sum is short (3000 x 3000 x 3000 takes 29, 32 and 35 us with one, two and four, 533036 x 44 x 26 33,
-    // 47 and 86); four where the sum is long (2048 x 2048 x 8192 28 with two, 23 with four), else two (2048
-    // cubed 11.2, 9.5 and 9.7).  Of rows sorted by expert the tiles are fewer than thought: 16 rows to 4 of 16
-    // experts, 4096 x 8192, 34.6 with two, 40.3 with one.
+    // the sum is short (3000 x 3000 x 3000 takes 30, 33 and 35 us with one, two and four, 533036 x 44 x 26 33,
+    // 47 and 86); four where the sum is long (2048 x 2048 x 8192 29 with two, 25 with four), else two (2048
+    // cubed 11.5, 9.4 and 9.9).  Of rows sorted by expert the tiles are fewer than thought: 16 rows to 4 of 16
+    // experts, 4096 x 8192, 44 with two, 53 with one.
     if (wide || many || few) {
       const bool one = stages <= 2 || (experts > 0 && stages >= 16 ? t > 2 * cus : t > cus);
       return whole(one ? kTile128Short : stages >= 24 && t <= cus ? kTile128Deep : kTile128);
