@@ -10,7 +10,9 @@ Arguments are checked here and in the library; every call runs on the current
 stream of its tensors' device, and results and workspaces are torch tensors of
 that stream.  `dispatch` and `combine` record gradients where torch does; a step that
 is captured into a graph takes leaves of its own (x.detach().requires_grad_()), since
-torch ties a leaf to the stream that it was first used on.
+torch ties a leaf to the stream that it was first used on.  Forward derivatives are
+refused.  A trace (torch.jit.trace) holds `dispatch` and `combine` with the route that
+they were given; `route` and `product` are not for one.
 """
 from __future__ import annotations
 
